@@ -282,6 +282,117 @@ int mdbf_msvid(const float* Z_dev, int rows, int cols, int64_t ld, int l, int it
                int8_t* S_dev, float* A_dev, float* Q_dev, float* sigma_dev, void* workspace_dev,
                size_t workspace_bytes, void* stream);
 
+/* ---- attention block of a serving step ---------------------------------------------------------
+ * What stands between the q, k, v projections and the output projection of a decoder layer: the new tokens' places
+ * in a cache in pages (mdbf_kv_slots), norm and rotation of queries and keys (mdbf_qk_norm_rope), keys and values into
+ * the cache (the same launch, or mdbf_kv_append) and attention over it (mdbf_kv_attention).
+ *
+ * The cache of one layer is a pool of pages of page_size tokens.  A page holds for each kv head in turn
+ *     key codes    page_size x head_dim / 2 bytes      value codes   the same
+ *     key scales   page_size x head_dim / 32 bytes     value scales  the same
+ * (token-major; mdbf_kv_page_bytes in all).  Codes are 4-bit floating point numbers e2m1 (0, 0.5, 1, 1.5, 2, 3, 4, 6 and
+ * their negatives), the even channel in the low half of a byte; a scale byte b per 32 channels stands for 2^(b - 127),
+ * and 255 for NaN throughout the block.  The smallest scale is taken that leaves the block's largest magnitude at most 7 units
+ * (it may round to 6: least error at 4 bits, 11 % of a normally distributed block's norm); values round to the nearest number, ties to
+ * the even code.  A block with a NaN or an infinity in it becomes NaN.  dtype bounds the scales, to 2^-23 .. 2^13 (MDBF_F16) or
+ * 2^-125 .. 2^125 (MDBF_BF16), so that every stored value is a number of that type: larger magnitudes saturate.
+ * 4.25 bits a channel.  A token's place is its slot, page * page_size + offset.
+ *
+ * Requests are described in device memory (integer arrays need the alignment of their elements only, so that they may be
+ * parts of larger ones): block tables (requests x table_width int32, row stride table_ld; entry i is the page of the
+ * request's tokens i * page_size ...), cu (requests + 1 int32: the first row of each request among the step's
+ * new tokens) and lengths (tokens of each request with the new ones). */
+typedef struct {
+  int32_t pages;       /* pages of the pool */
+  int32_t kv_heads;
+  int32_t head_dim;    /* 64, 128 or 256 */
+  int32_t page_size;   /* tokens per page: 16, 32, 64, 128 or 256 */
+  int32_t dtype;       /* MDBF_F16 or MDBF_BF16 */
+} mdbf_kv_t;
+
+/* Bytes of one page; the pool is `pages` of them, one after the other (host only). */
+int mdbf_kv_page_bytes(const mdbf_kv_t* kv, size_t* bytes_out);
+
+/* Block tables and slot map of a step from request lengths.  Request r has cached[r] tokens and gets fresh[r] new ones
+ * (0 is fine); the pages that it needs beyond its first ceil(cached / page_size) are taken from the free list in the order of requests,
+ * free[taken], free[taken + 1], ..., and entered in its table.  Writes
+ *   lengths (requests)    cached + fresh                 cu (requests + 1)   prefix sums of fresh
+ *   slots, positions (T)  of every new token, requests one after the other; -1 in the entries behind the last
+ *   taken_out             taken plus the pages used      status              0, or the sum of MDBF_KV_* below
+ * If status is not 0 the step is refused as a whole: tables stay as they are, taken_out = taken, lengths = cached (0 where that is negative),
+ * cu is 0, slots and positions are -1 throughout, so that launches behind it do nothing.  taken_out may be taken.
+ * One launch, two for long steps. */
+#define MDBF_KV_BAD_LENGTH 1   /* a negative count, or a length beyond 2^31 - 1 */
+#define MDBF_KV_BAD_WIDTH 2    /* a request needs more pages than its table's row has room for */
+#define MDBF_KV_BAD_TOKENS 4   /* more new tokens than T */
+#define MDBF_KV_NO_PAGES 8     /* more pages needed than the free list holds */
+int mdbf_kv_slots(int requests, int page_size, const int32_t* cached_dev, const int32_t* fresh_dev, int32_t* table_dev,
+                  int64_t table_ld, int table_width, const int32_t* free_dev, int free_count, const int32_t* taken_dev,
+                  int T, int32_t* lengths_dev, int32_t* cu_dev, int64_t* slots_dev, int32_t* positions_dev,
+                  int32_t* taken_out_dev, int32_t* status_dev, void* stream);
+
+/* Writes the keys and values of T tokens to their slots.  k_dev, v_dev: T rows of kv_heads x head_dim, row strides ldk,
+ * ldv >= kv_heads * head_dim, elements of x_dtype.  A slot outside the pool (-1: padding) is skipped; no two tokens of a call may
+ * have the same one. */
+int mdbf_kv_append(const mdbf_kv_t* kv, void* cache_dev, size_t cache_bytes, const void* k_dev, int64_t ldk,
+                   const void* v_dev, int64_t ldv, int x_dtype, const int64_t* slots_dev, int T, void* stream);
+
+/* The values that T slots hold, as rows like mdbf_kv_append's (elements of y_dtype; rounded only if it is the other of
+ * the two 16-bit types).  A slot outside the pool reads as zeros. */
+int mdbf_kv_read(const mdbf_kv_t* kv, const void* cache_dev, size_t cache_bytes, const int64_t* slots_dev, int T,
+                 void* k_dev, int64_t ldk, void* v_dev, int64_t ldv, int y_dtype, void* stream);
+
+#define MDBF_ROPE_INTERLEAVED 1u   /* rotated pairs are channels (2 i, 2 i + 1) instead of (i, i + rot_dim / 2) */
+typedef struct {
+  int32_t q_heads, kv_heads, head_dim;   /* head_dim 64, 128 or 256 */
+  int32_t rot_dim;                       /* channels that are rotated, the first ones: a multiple of 16 up to head_dim; 0: none */
+  int32_t rope_rows;                     /* positions that the table covers */
+  int32_t x_dtype, y_dtype;              /* of q, k, v as they come; of q_out, k_out */
+  uint32_t flags;
+  float eps;
+} mdbf_rope_t;
+
+/* For every head of q and k: x / sqrt(mean(x^2) + eps) * weight (left out where the weight is null), then the rotation by the
+ * token's position, (a, b) -> (a cos - b sin, b cos + a sin), in fp32 and rounded once.
+ *   q_dev, k_dev     T rows of q_heads resp. kv_heads x head_dim, row strides ldq, ldk (any, at least the row)
+ *   q_weight_dev, k_weight_dev   head_dim fp32, or null
+ *   rope_dev         rope_rows x rot_dim fp32: a position's rot_dim / 2 cosines, then its sines
+ *   positions_dev    T int32.  Negative (padding): the token's rows become zeros and nothing is cached.  At or beyond rope_rows: the rotated
+ *                    channels become NaN
+ *   q_out_dev        row stride ldqo; k_out_dev likewise, or null if only the cache is wanted
+ * Outputs may be the inputs themselves where strides and types agree.
+ * With kv (else null, like the arguments behind it) the same launch writes k, rounded to y_dtype, and v_dev (T rows
+ * of kv_heads x head_dim, of x_dtype) to the cache slots: the bytes are those of mdbf_kv_append on k_out and v. */
+int mdbf_qk_norm_rope(const mdbf_rope_t* desc, const void* q_dev, int64_t ldq, const void* k_dev, int64_t ldk,
+                      const float* q_weight_dev, const float* k_weight_dev, const float* rope_dev,
+                      const int32_t* positions_dev, int T, void* q_out_dev, int64_t ldqo, void* k_out_dev, int64_t ldko,
+                      const mdbf_kv_t* kv, void* cache_dev, size_t cache_bytes, const void* v_dev, int64_t ldv,
+                      const int64_t* slots_dev, void* stream);
+
+#define MDBF_ATTN_CAUSAL 1u   /* a token sees the ones up to its own position (the new tokens are the request's last);
+                                 without it all of the request */
+typedef struct {
+  int32_t q_heads;      /* a multiple of kv_heads: query head h reads kv head h / (q_heads / kv_heads) */
+  uint32_t flags;
+  int32_t window;       /* > 0 (causal only): a token sees the last `window` tokens up to itself; 0: all */
+  int32_t max_fresh;    /* most new tokens of a request, and ... */
+  int32_t max_length;   /* ... the longest request: launch sizes go by them.  Larger ones in cu and lengths are served as well, slowly */
+  float scale;          /* of the scores, usually head_dim^-1/2 */
+} mdbf_attn_t;
+
+/* out[t, h] = sum_j softmax_j(scale q[t, h] . k_j) v_j over the tokens j of t's request that it sees, whose keys and values
+ * come from the cache (the new tokens' own too: append first).  q_dev, out_dev: T rows of q_heads x head_dim of the cache's
+ * dtype, row strides ldq, ldo.  Rows behind the last request's are left as they are; a token that sees nothing gets zeros.
+ * What a token does not see has no influence on its row, whatever the bytes there are; a page number outside the pool reads as NaN.
+ * Lengths are cut to what the table's row covers, fresh counts to T.  Scores, running maxima and sums are fp32; products are of the
+ * cache's dtype, whose only rounding is that of the softmax's numerators.  Repeated calls return the same bits.
+ * The workspace (host arithmetic only) holds partial results where a long cache is split among workgroups; it may be null if 0 bytes are needed. */
+int mdbf_kv_attention_workspace_bytes(const mdbf_kv_t* kv, const mdbf_attn_t* attn, int requests, int T, size_t* bytes_out);
+int mdbf_kv_attention(const mdbf_kv_t* kv, const mdbf_attn_t* attn, const void* cache_dev, size_t cache_bytes,
+                      const int32_t* table_dev, int64_t table_ld, int table_width, const int32_t* cu_dev,
+                      const int32_t* lengths_dev, int requests, const void* q_dev, int64_t ldq, int T, void* out_dev,
+                      int64_t ldo, void* workspace_dev, size_t workspace_bytes, void* stream);
+
 /* ---- misc ----------------------------------------------------------------------------- */
 const char* mdbf_strerror(int status);
 const char* mdbf_last_hip_error(void);   /* text of the last failed HIP call on this thread, or "" */

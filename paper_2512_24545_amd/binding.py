@@ -18,6 +18,9 @@ MDBF_FLAG_PRECISE = 1
 MDBF_FLAG_BLOCK_SCALED = 2
 MDBF_FLAG_ACCUMULATE = 4
 MDBF_FLAG_FP16_STAGED = 8
+MDBF_KV_BAD_LENGTH, MDBF_KV_BAD_WIDTH, MDBF_KV_BAD_TOKENS, MDBF_KV_NO_PAGES = 1, 2, 4, 8
+MDBF_ROPE_INTERLEAVED = 1
+MDBF_ATTN_CAUSAL = 1
 DTYPE_CODE = {"f16": MDBF_F16, "bf16": MDBF_BF16, "f32": MDBF_F32}
 
 STATUS = {0: "MDBF_OK", -1: "MDBF_EINVAL", -2: "MDBF_EALIGN", -3: "MDBF_EDTYPE", -4: "MDBF_EWORKSPACE",
@@ -28,6 +31,8 @@ EXPORTS = [
     "mdbf_stream_read", "mdbf_workspace_bytes", "mdbf_forward", "mdbf_forward_static", "mdbf_batch_plan_bytes", "mdbf_batch_plan_build",
     "mdbf_forward_batch", "mdbf_forward_batch_part", "mdbf_batch_plan_kernel", "mdbf_batch_plan_launches", "mdbf_strerror", "mdbf_last_hip_error", "mdbf_version",
     "mdbf_msvid_block", "mdbf_msvid_workspace_bytes", "mdbf_msvid",
+    "mdbf_kv_page_bytes", "mdbf_kv_slots", "mdbf_kv_append", "mdbf_kv_read", "mdbf_qk_norm_rope",
+    "mdbf_kv_attention_workspace_bytes", "mdbf_kv_attention",
 ]
 
 
@@ -54,6 +59,22 @@ class Layer(C.Structure):
     _fields_ = [("desc", Desc), ("SA_packed_dev", C.c_void_p), ("SB_packed_dev", C.c_void_p), ("env", Env),
                 ("X_dev", C.c_void_p), ("ldx", C.c_int64), ("Y_dev", C.c_void_p), ("ldy", C.c_int64),
                 ("T", C.c_int32)]
+
+
+class KvDesc(C.Structure):
+    _fields_ = [("pages", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("page_size", C.c_int32),
+                ("dtype", C.c_int32)]
+
+
+class RopeDesc(C.Structure):
+    _fields_ = [("q_heads", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("rot_dim", C.c_int32),
+                ("rope_rows", C.c_int32), ("x_dtype", C.c_int32), ("y_dtype", C.c_int32), ("flags", C.c_uint32),
+                ("eps", C.c_float)]
+
+
+class AttnDesc(C.Structure):
+    _fields_ = [("q_heads", C.c_int32), ("flags", C.c_uint32), ("window", C.c_int32), ("max_fresh", C.c_int32),
+                ("max_length", C.c_int32), ("scale", C.c_float)]
 
 
 _lib = None
@@ -93,6 +114,16 @@ def lib():
     L.mdbf_msvid_workspace_bytes.argtypes = [C.c_int, C.c_int, C.c_int, C.POINTER(C.c_size_t)]
     L.mdbf_msvid.argtypes = [C.c_void_p, C.c_int, C.c_int, C.c_int64, C.c_int, C.c_int, C.c_void_p, C.c_void_p,
                              C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+    vp, i64, sz = C.c_void_p, C.c_int64, C.c_size_t
+    L.mdbf_kv_page_bytes.argtypes = [C.POINTER(KvDesc), C.POINTER(sz)]
+    L.mdbf_kv_slots.argtypes = [C.c_int, C.c_int, vp, vp, vp, i64, C.c_int, vp, C.c_int, vp, C.c_int, vp, vp, vp, vp, vp, vp, vp]
+    L.mdbf_kv_append.argtypes = [C.POINTER(KvDesc), vp, sz, vp, i64, vp, i64, C.c_int, vp, C.c_int, vp]
+    L.mdbf_kv_read.argtypes = [C.POINTER(KvDesc), vp, sz, vp, C.c_int, vp, i64, vp, i64, C.c_int, vp]
+    L.mdbf_qk_norm_rope.argtypes = [C.POINTER(RopeDesc), vp, i64, vp, i64, vp, vp, vp, vp, C.c_int, vp, i64, vp, i64,
+                                    C.POINTER(KvDesc), vp, sz, vp, i64, vp, vp]
+    L.mdbf_kv_attention_workspace_bytes.argtypes = [C.POINTER(KvDesc), C.POINTER(AttnDesc), C.c_int, C.c_int, C.POINTER(sz)]
+    L.mdbf_kv_attention.argtypes = [C.POINTER(KvDesc), C.POINTER(AttnDesc), vp, sz, vp, i64, C.c_int, vp, vp, C.c_int, vp, i64,
+                                    C.c_int, vp, i64, vp, sz, vp]
     L.mdbf_strerror.restype = C.c_char_p
     L.mdbf_strerror.argtypes = [C.c_int]
     L.mdbf_last_hip_error.restype = C.c_char_p
@@ -365,3 +396,166 @@ def mdbf_msvid(Z, l, X0, iters=8, stream=None, workspace=None):
                             Q.data_ptr(), sigma.data_ptr(), workspace.data_ptr(), workspace.numel(),
                             _stream_ptr(stream)), "mdbf_msvid")
     return S, A, Q, sigma
+
+
+# ---- attention block of a serving step ---------------------------------------------------------
+class KVCache:
+    """Pool of pages of one layer's 4-bit cache (layout and format: include/mdbf.h).  buffer: a uint8 CUDA tensor of at
+    least pages * page_bytes (a pool that the program has); without one, zeros are allocated."""
+
+    def __init__(self, pages, kv_heads, head_dim, page_size=64, dtype="bf16", device="cuda:0", buffer=None):
+        self.pages, self.kv_heads, self.head_dim, self.page_size, self.dtype = pages, kv_heads, head_dim, page_size, dtype
+        self.desc = KvDesc(pages, kv_heads, head_dim, page_size, DTYPE_CODE[dtype])
+        out = C.c_size_t(0)
+        _check(lib().mdbf_kv_page_bytes(self.desc, C.byref(out)), "mdbf_kv_page_bytes")
+        self.page_bytes = out.value
+        if buffer is None:
+            torch = _torch()
+            buffer = torch.zeros(pages * self.page_bytes, dtype=torch.uint8, device=device)
+        self.buffer = buffer
+        assert buffer.is_cuda and buffer.is_contiguous() and buffer.element_size() == 1
+        self.args = (buffer.data_ptr(), buffer.numel())
+
+
+class KVSlots:
+    """What mdbf_kv_slots writes: lengths, cu, slots, positions, taken, status.  Made once for `requests` and `tokens`, it can be
+    handed to every step's call."""
+
+    def __init__(self, requests, tokens, device="cuda:0"):
+        torch = _torch()
+        e = lambda n, t=torch.int32: torch.empty(n, dtype=t, device=device)
+        self.lengths, self.cu, self.positions, self.taken, self.status = e(requests), e(requests + 1), e(tokens), e(1), e(1)
+        self.slots = e(tokens, torch.int64)
+
+
+def _int_tensor(t, n=None, bits=32):
+    torch = _torch()
+    return t.is_cuda and t.dtype == (torch.int32 if bits == 32 else torch.int64) and t.is_contiguous() and (n is None or t.numel() == n)
+
+
+def mdbf_kv_slots(cached, fresh, table, free_pages, taken, page_size, tokens, out=None, stream=None):
+    """Block tables and slot map of a step: int32 CUDA tensors cached, fresh (requests), table (requests x width, updated in
+    place), free_pages, taken (one entry).  tokens: room for the step's new tokens.  Returns a KVSlots (`out` if given;
+    out.taken may be `taken`).  Nothing is read back: out.status is on the device."""
+    n = cached.numel()
+    assert _int_tensor(cached) and _int_tensor(fresh, n) and _int_tensor(free_pages) and _int_tensor(taken, 1)
+    assert table.is_cuda and table.dtype == cached.dtype and table.dim() == 2 and table.shape[0] == n and table.stride(1) == 1
+    o = KVSlots(n, tokens, cached.device) if out is None else out
+    if out is not None:
+        assert _int_tensor(o.lengths, n) and _int_tensor(o.cu, n + 1) and _int_tensor(o.positions, tokens)
+        assert _int_tensor(o.slots, tokens, 64) and _int_tensor(o.taken, 1) and _int_tensor(o.status, 1)
+    status = (_lib or lib()).mdbf_kv_slots(n, page_size, cached.data_ptr(), fresh.data_ptr(), table.data_ptr(), table.stride(0), table.shape[1],
+                                           free_pages.data_ptr(), free_pages.numel(), taken.data_ptr(), tokens, o.lengths.data_ptr(),
+                                           o.cu.data_ptr(), o.slots.data_ptr(), o.positions.data_ptr(), o.taken.data_ptr(),
+                                           o.status.data_ptr(), _stream_ptr(stream))
+    if status:
+        _check(status, "mdbf_kv_slots")
+    return o
+
+
+def _heads(x, d=None):
+    """Rows of heads (T, heads, d), the heads of a row side by side: its row stride."""
+    T, H, D = x.shape
+    s = x.stride()
+    assert x.is_cuda and s[2] == 1 and (s[1] == D or H == 1) and (d is None or D == d), "rows of heads side by side are needed"
+    return s[0] if T > 1 else max(s[0], H * D)
+
+
+def mdbf_kv_append(cache, k, v, slots, stream=None):
+    """Writes the rows of k and v (T, kv_heads, head_dim; f16/bf16/f32) to the cache's slots (int64; outside of the pool: skipped)."""
+    T = k.shape[0]
+    assert k.shape == v.shape == (T, cache.kv_heads, cache.head_dim) and k.dtype == v.dtype and _int_tensor(slots, T, 64)
+    status = (_lib or lib()).mdbf_kv_append(cache.desc, *cache.args, k.data_ptr(), _heads(k), v.data_ptr(), _heads(v),
+                                            DTYPE_CODE[_dtype_name(k)], slots.data_ptr(), T, _stream_ptr(stream))
+    if status:
+        _check(status, "mdbf_kv_append")
+
+
+def mdbf_kv_read(cache, slots, out=None, stream=None):
+    """The keys and values that the slots hold: two tensors (T, kv_heads, head_dim), `out` or new ones of the cache's dtype."""
+    T = slots.numel()
+    shape = (T, cache.kv_heads, cache.head_dim)
+    if out is None:
+        torch = _torch()
+        out = tuple(torch.empty(shape, dtype=_torch_dtype(cache.dtype), device=slots.device) for _ in range(2))
+    k, v = out
+    assert k.shape == v.shape == shape and k.dtype == v.dtype and _int_tensor(slots, T, 64)
+    status = (_lib or lib()).mdbf_kv_read(cache.desc, *cache.args, slots.data_ptr(), T, k.data_ptr(), _heads(k), v.data_ptr(), _heads(v),
+                                          DTYPE_CODE[_dtype_name(k)], _stream_ptr(stream))
+    if status:
+        _check(status, "mdbf_kv_read")
+    return k, v
+
+
+def mdbf_qk_norm_rope(q, k, rope, positions, q_weight=None, k_weight=None, eps=1e-6, interleaved=False, y_dtype=None, q_out=None,
+                      k_out=None, cache=None, v=None, slots=None, stream=None):
+    """Norm (where a weight is given) and rotation of every head of q (T, q_heads, d) and k (T, kv_heads, d).  rope: fp32 (rows, rot_dim), cosines
+    then sines of a position, or None; positions: int32 (T).  Returns (q_out, k_out), new tensors of y_dtype (that of q) unless given.
+    With a cache, the same launch writes k and v to its slots; k_out is then None unless it was given."""
+    torch = _torch()
+    T, Hq, d = q.shape
+    Hkv = k.shape[1]
+    assert k.shape == (T, Hkv, d) and k.dtype == q.dtype
+    name = _DTYPE_NAME[q.dtype]
+    if q_out is None:
+        q_out = torch.empty((T, Hq, d), dtype=_TORCH_DTYPE[y_dtype or name], device=q.device)
+    if k_out is None and cache is None:
+        k_out = torch.empty((T, Hkv, d), dtype=q_out.dtype, device=q.device)
+    assert q_out.shape == q.shape and (k_out is None or (k_out.shape == k.shape and k_out.dtype == q_out.dtype))
+    for w in (q_weight, k_weight):
+        assert w is None or (w.is_cuda and w.dtype == torch.float32 and w.is_contiguous() and w.numel() == d), "norm weights are head_dim fp32"
+    rows = rot = 0
+    if rope is not None:
+        rows, rot = rope.shape
+        assert rope.is_cuda and rope.dtype == torch.float32 and rope.is_contiguous() and _int_tensor(positions, T)
+    desc = RopeDesc(Hq, Hkv, d, rot, rows, DTYPE_CODE[name], DTYPE_CODE[_DTYPE_NAME[q_out.dtype]],
+                    MDBF_ROPE_INTERLEAVED if interleaved else 0, eps)
+    ptr = lambda t: None if t is None else t.data_ptr()
+    kv = (None, None, 0, None, 0, None)
+    if cache is not None:
+        assert v.shape == k.shape and v.dtype == k.dtype and _int_tensor(slots, T, 64)
+        kv = (cache.desc, *cache.args, v.data_ptr(), _heads(v), slots.data_ptr())
+    status = (_lib or lib()).mdbf_qk_norm_rope(desc, q.data_ptr(), _heads(q), k.data_ptr(), _heads(k), ptr(q_weight), ptr(k_weight), ptr(rope),
+                                               ptr(positions) if rot else None, T, q_out.data_ptr(), _heads(q_out), ptr(k_out),
+                                               0 if k_out is None else _heads(k_out), *kv, _stream_ptr(stream))
+    if status:
+        _check(status, "mdbf_qk_norm_rope")
+    return q_out, k_out
+
+
+def _attn_desc(cache, q_heads, max_fresh, max_length, causal, window, scale):
+    return AttnDesc(q_heads, MDBF_ATTN_CAUSAL if causal else 0, window, max_fresh, max_length,
+                    cache.head_dim ** -0.5 if scale is None else scale)
+
+
+def mdbf_kv_attention_workspace(cache, q_heads, requests, tokens, max_fresh, max_length, causal=True, window=0):
+    """The workspace (uint8 CUDA tensor, or None where none is needed) of mdbf_kv_attention calls of these sizes."""
+    out = C.c_size_t(0)
+    d = _attn_desc(cache, q_heads, max_fresh, max_length, causal, window, 1.0)
+    _check(lib().mdbf_kv_attention_workspace_bytes(cache.desc, d, requests, tokens, C.byref(out)), "mdbf_kv_attention_workspace_bytes")
+    torch = _torch()
+    return torch.empty(out.value, dtype=torch.uint8, device=cache.buffer.device) if out.value else None
+
+
+def mdbf_kv_attention(cache, q, table, cu, lengths, max_fresh, max_length, scale=None, causal=True, window=0, out=None, workspace=None,
+                      stream=None):
+    """Attention of the new tokens' queries q (T, q_heads, d; the cache's dtype) over the cache.  table (requests x width), cu (requests + 1)
+    and lengths (requests) are int32 CUDA tensors as mdbf_kv_slots leaves them; max_fresh, max_length: bounds of the
+    new tokens and the length of a request (launch sizes).  Returns out (T, q_heads, d)."""
+    T, Hq, d = q.shape
+    n = lengths.numel()
+    assert d == cache.head_dim and _dtype_name(q) == cache.dtype and _int_tensor(lengths) and _int_tensor(cu, n + 1)
+    assert table.is_cuda and table.dtype == lengths.dtype and table.dim() == 2 and table.shape[0] == n and table.stride(1) == 1
+    if out is None:
+        out = _torch().empty((T, Hq, d), dtype=q.dtype, device=q.device)
+    assert out.shape == q.shape and out.dtype == q.dtype
+    if workspace is None:
+        workspace = mdbf_kv_attention_workspace(cache, Hq, n, T, max_fresh, max_length, causal, window)
+    desc = _attn_desc(cache, Hq, max_fresh, max_length, causal, window, scale)
+    status = (_lib or lib()).mdbf_kv_attention(cache.desc, desc, *cache.args, table.data_ptr(), table.stride(0), table.shape[1], cu.data_ptr(),
+                                               lengths.data_ptr(), n, q.data_ptr(), _heads(q), T, out.data_ptr(), _heads(out),
+                                               None if workspace is None else workspace.data_ptr(),
+                                               0 if workspace is None else workspace.numel(), _stream_ptr(stream))
+    if status:
+        _check(status, "mdbf_kv_attention")
+    return out

@@ -12,15 +12,15 @@
 
 using namespace mdbf;
 
-namespace {
+static thread_local char g_hip_err[256] = "";
 
-thread_local char g_hip_err[256] = "";
-
-int hip_fail(int e) {
+int mdbf::hip_fail(int e) {
   if (e == 0) return MDBF_OK;
   snprintf(g_hip_err, sizeof(g_hip_err), "%s", hipGetErrorString((hipError_t)e));
   return MDBF_EHIP;
 }
+
+namespace {
 
 bool valid_dtype(int d) { return d == MDBF_F16 || d == MDBF_BF16 || d == MDBF_F32; }
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }

@@ -141,6 +141,9 @@ inline int kernel_setup(KernelSetup& k, F&& fn) {
   return k.err[dev];
 }
 
+// MDBF_OK for 0, else MDBF_EHIP, the error's text kept for mdbf_last_hip_error
+int hip_fail(int e);
+
 // launchers (defined in the kernel translation units); return hipError_t as int
 int launch_pack(const int8_t* signs, int rows, int cols, int64_t ld, uint32_t* packed, hipStream_t s);
 int launch_unpack(const uint32_t* packed, int rows, int cols, int8_t* signs, int64_t ld, hipStream_t s);
