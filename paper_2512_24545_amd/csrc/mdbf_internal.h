@@ -12,6 +12,8 @@
 // a wait for an LDS read would wait for every global load in flight as well.
 #define MDBF_GLOBAL __attribute__((address_space(1)))
 #define MDBF_LDS __attribute__((address_space(3)))
+// memory that no launch writes while this one runs: wave-uniform reads go through the scalar cache
+#define MDBF_CONST __attribute__((address_space(4)))
 
 namespace mdbf {
 

@@ -26,7 +26,8 @@ struct AttnArgs {
   const void* q;
   void* out;
   int64_t table_ld, ldq, ldo;
-  int32_t table_width, T, pages, kv_heads, group, page_shift, causal, window, row_tiles;
+  float* part;
+  int32_t table_width, T, pages, kv_heads, group, head_dim, page_shift, causal, window, row_tiles, splits, chunk, join_rows;
   float scale;                 // of the scores, times log2(e)
   uint8_t wide_q, wide_o;
 };
@@ -72,7 +73,7 @@ __device__ __forceinline__ Request request_of(const AttnArgs& a, int b) {
   Request r;
   r.start = min(max(a.cu[b], 0), a.T);
   r.fresh = (int)min(max((int64_t)a.cu[b + 1] - r.start, (int64_t)0), (int64_t)(a.T - r.start));
-  r.len = (int)min((int64_t)max(a.lengths[b], 0), min((int64_t)a.table_width << a.page_shift, (int64_t)0x7fffff00));
+  r.len = (int)min((int64_t)max(a.lengths[b], 0), min((int64_t)a.table_width << a.page_shift, (int64_t)0x7ffffe00));
   return r;
 }
 // the tokens lo <= j < hi that new token i sees
@@ -85,43 +86,145 @@ __device__ __forceinline__ Sees sees(const AttnArgs& a, const Request& r, int i)
   return {a.window ? max(pos - a.window + 1, 0) : 0, max(pos + 1, 0)};
 }
 
+// channels c0 .. c0 + N - 1 of a finished row: its sums over the sum of its numerators; zeros if it sees nothing
+template <int DT, int N>
+__device__ __forceinline__ void store_row(const AttnArgs& a, const Request& rq, int head, int64_t R, int c0, const float (&o)[N], float sum) {
+  const int i = (int)(R / a.group), g = (int)(R % a.group);
+  const Sees s = sees(a, rq, i);
+  const float inv = 1.0f / sum;
+  uint32_t w[N / 2];
+#pragma unroll
+  for (int c = 0; c < N / 2; ++c) w[c] = s.hi > s.lo ? round2<DT>(o[2 * c] * inv, o[2 * c + 1] * inv) : 0u;
+  MDBF_GLOBAL uint16_t* to = (MDBF_GLOBAL uint16_t*)a.out + (int64_t)(rq.start + i) * a.ldo + (int64_t)(head * a.group + g) * a.head_dim + c0;
+  if (a.wide_o) {
+#pragma unroll
+    for (int c = 0; c < N / 4; ++c) ((MDBF_GLOBAL U32x2*)to)[c] = U32x2{w[2 * c], w[2 * c + 1]};
+  } else {
+#pragma unroll
+    for (int c = 0; c < N / 2; ++c) {
+      to[2 * c] = (uint16_t)w[c];
+      to[2 * c + 1] = (uint16_t)(w[c] >> 16);
+    }
+  }
+}
+
 constexpr int kTile = 32;        // tokens per step of a wave
 constexpr int kWaves = 4;
+constexpr int kRows = 16;        // query rows of a workgroup
 
-// One kv head, 16 query rows; the tokens' tiles are dealt out to the four waves, which meet at the end.
+// The tokens that the rows of a tile of query rows see, and their part of each workgroup: `chunk` tokens from the first one's
+// tile on, the rest of them for the last workgroup.
+struct Span {
+  int lo, hi;              // what any row sees
+  int all_lo, all_hi;      // what all rows see
+  int from;                // where the first part begins
+  int parts;
+};
+__device__ __forceinline__ Span span_of(const AttnArgs& a, const Request& rq, int64_t tile, int64_t rows, int splits) {
+  const Sees s0 = sees(a, rq, (int)(tile * kRows / a.group)), s1 = sees(a, rq, (int)(min(tile * kRows + kRows - 1, rows - 1) / a.group));
+  Span s = {s0.lo, s1.hi, s1.lo, s0.hi, s0.lo & ~(kTile - 1), 1};
+  if (splits > 1 && s.hi > s.from) s.parts = (int)min((int64_t)splits, ((int64_t)s.hi - s.from + a.chunk - 1) / a.chunk);
+  return s;
+}
+
+// where the results of one part of a tile of rows go: kRows x D sums, then kRows maxima and kRows sums of numerators
+template <int D>
+__device__ __forceinline__ int64_t part_floats() { return kRows * (D + 2); }
+
+// One wave's tile of tokens: codes and scales of its keys and values as loaded.
+template <int D>
+struct Codes {
+  static constexpr int KW = D / 32;                  // dwords of codes per lane and 16 keys = matrix steps over the channels
+  static constexpr int KS = D <= 128 ? 1 : D / 128;  // scales among them
+  static constexpr int VU = D / 64;                  // 16-byte units of values per lane
+  static constexpr int VH = D == 64 ? 1 : VU / 2;    // of them in each half
+  uint32_t kc[2][KW], ks[2][KS];
+  U32x4 vc[VU];
+  uint32_t vs[VU];
+  // the half of a unit, and its place there: 16 tokens x D / 32 blocks
+  __device__ static __forceinline__ int half(int n, int lane) { return D == 64 ? lane >> 5 : n / VH; }
+  __device__ static __forceinline__ int unit(int n, int lane) { return D == 64 ? lane & 31 : (n % VH) * 64 + lane; }
+
+  // `page`: of the two halves' tokens, which begin at tok
+  __device__ __forceinline__ void load(const AttnArgs& a, int head, int64_t head_bytes, int tok, const int (&page)[2], int lane) {
+    const int P = 1 << a.page_shift, r = lane & 15, h = lane >> 4;
+    const MDBF_GLOBAL uint8_t* base[2];
+    bool there[2];
+    int off[2];
+#pragma unroll
+    for (int f = 0; f < 2; ++f) {
+      there[f] = (uint32_t)page[f] < (uint32_t)a.pages;
+      base[f] = (const MDBF_GLOBAL uint8_t*)a.cache + ((int64_t)(there[f] ? page[f] : 0) * a.kv_heads + head) * head_bytes;
+      off[f] = (tok + 16 * f) & (P - 1);
+      const MDBF_GLOBAL uint8_t* kp = base[f] + off[f] * (D / 2);
+      const uint32_t at = r * (D / 2) + h * (D / 8);
+      if (KW == 2) {
+        const U32x2 v = __builtin_nontemporal_load((const MDBF_GLOBAL U32x2*)(kp + at));
+        kc[f][0] = v[0], kc[f][1] = v[1];
+      } else {
+#pragma unroll
+        for (int s = 0; s < KW; s += 4) {
+          const U32x4 v = __builtin_nontemporal_load((const MDBF_GLOBAL U32x4*)(kp + at + 4 * s));
+#pragma unroll
+          for (int w = 0; w < 4; ++w) kc[f][(s + w) % KW] = v[w];
+        }
+      }
+      const MDBF_GLOBAL uint8_t* sp = base[f] + P * D + off[f] * (D / 32);
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        const uint32_t b = sp[(uint32_t)(r * (D / 32) + (D == 64 ? h >> 1 : h * KS + s))];
+        ks[f][s] = there[f] ? b : kKvNanScale;
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < VU; ++n) {
+      const int f = half(n, lane);
+      const uint32_t u = unit(n, lane);
+      const MDBF_GLOBAL uint8_t* at = f ? base[1] : base[0];
+      const int o = f ? off[1] : off[0];
+      vc[n] = __builtin_nontemporal_load((const MDBF_GLOBAL U32x4*)(at + (P + o) * (D / 2) + u * 16));
+      const uint32_t b = at[P * (D + D / 32) + o * (D / 32) + u];
+      vs[n] = (f ? there[1] : there[0]) ? b : kKvNanScale;
+    }
+  }
+};
+
+// One kv head, 16 query rows, one part of their tokens; the part's tiles are dealt out to the four waves, which meet at
+// the end.  A tile's loads are issued before the products of the one before it, and its page numbers a tile earlier still.
 template <int D, int DT>
-__global__ __launch_bounds__(64 * kWaves) void attn_few_kernel(AttnArgs a) {
-  constexpr int KW = D / 32;                  // dwords of codes per lane and key tile = matrix steps over the channels
-  constexpr int KS = D <= 128 ? 1 : D / 128;  // scales among them
-  constexpr int VU = D / 64;                  // 16-byte units of values per lane and tile
+__global__ __launch_bounds__(64 * kWaves, D == 64 ? 4 : D == 128 ? 3 : 2) void attn_few_kernel(AttnArgs a) {
+  using Tile = Codes<D>;
+  constexpr int KW = Tile::KW, KS = Tile::KS, VU = Tile::VU;
   constexpr int VROW = D * 2 + 32;            // bytes of a token's values in LDS
   constexpr int CT = D / 16;                  // channel tiles
   constexpr int OROW = D + 4;                 // floats of a row of results in LDS
-  static_assert(kTile * VROW >= 16 * OROW * 4, "the results fit the values' place");
+  static_assert(kTile * VROW >= kRows * OROW * 4, "the results fit the values' place");
   __shared__ __attribute__((aligned(16))) unsigned char lds[kWaves][kTile * VROW];
-  __shared__ float stat[kWaves][2][16];
+  __shared__ float stat[kWaves][2][kRows];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, h = lane >> 4;
   uint32_t idx = blockIdx.x;
+  const int part = idx % a.splits;
+  idx /= a.splits;
   const int rt0 = idx % a.row_tiles;
   idx /= a.row_tiles;
   const int head = idx % a.kv_heads, b = idx / a.kv_heads;
   const Request rq = request_of(a, b);
   const int64_t rows = (int64_t)rq.fresh * a.group;
-  const int P = 1 << a.page_shift;
-  const int64_t head_bytes = kv_head_bytes(P, D);
-  const MDBF_GLOBAL int32_t* table = (const MDBF_GLOBAL int32_t*)a.table + b * a.table_ld;
-  const MDBF_GLOBAL uint8_t* cache = (const MDBF_GLOBAL uint8_t*)a.cache;
+  const int64_t head_bytes = kv_head_bytes(1 << a.page_shift, D);
+  const MDBF_CONST int32_t* table = (const MDBF_CONST int32_t*)a.table + b * a.table_ld;
   unsigned char* vals = lds[wave];
 
-  for (int64_t rt = rt0; rt * 16 < rows; rt += a.row_tiles) {
-    const int64_t R = rt * 16 + r;
+  // (tiles of rows beyond those that the launch was sized for are not split)
+  for (int64_t rt = rt0; rt * kRows < rows; rt += a.row_tiles) {
+    const Span sp = span_of(a, rq, rt, rows, rt == rt0 ? a.splits : 1);
+    if (part >= sp.parts) continue;
+    const int64_t R = rt * kRows + r;
     const bool valid = R < rows;
     const int i = valid ? (int)(R / a.group) : 0, g = valid ? (int)(R % a.group) : 0;
     Sees me = sees(a, rq, i);
     if (!valid) me.hi = me.lo = 0;
-    // of the first and the last row: what any row sees, and what all rows see
-    const Sees s0 = sees(a, rq, (int)(rt * 16 / a.group)), s1 = sees(a, rq, (int)(min(rt * 16 + 15, rows - 1) / a.group));
-    const int tmin = s0.lo, tmax = s1.hi, all_lo = s1.lo, all_hi = s0.hi;
+    const int64_t first = sp.from + (int64_t)part * a.chunk;
+    const int tmin = max(sp.lo, (int)first), tmax = part == sp.parts - 1 ? sp.hi : (int)(first + a.chunk);
 
     U32x4 qf[KW];
     const int64_t q_at = (int64_t)(rq.start + i) * a.ldq + (int64_t)(head * a.group + g) * D + h * (D / 4);
@@ -144,49 +247,23 @@ __global__ __launch_bounds__(64 * kWaves) void attn_few_kernel(AttnArgs a) {
 #pragma unroll
     for (int c = 0; c < CT; ++c) acc[c] = F32x4{0, 0, 0, 0};
 
-    for (int t0 = (tmin & ~(kTile - 1)) + wave * kTile; t0 < tmax; t0 += kWaves * kTile) {
-      // the tile's two halves of 16 tokens lie in one page each; pages behind the last are not looked up
-      uint32_t kc[2][KW], ks[2][KS];
-      U32x4 vc[VU];
-      uint32_t vs[VU];
-      int64_t base[2];
-      int off[2];
-      bool there[2];
+    // page numbers of a tile's halves; behind the last token's none is looked up
+    auto pages_of = [&](int t, int (&page)[2]) __attribute__((always_inline)) {
 #pragma unroll
-      for (int f = 0; f < 2; ++f) {
-        const int tok = t0 + 16 * f;
-        const int page = table[min(tok, rq.len - 1) >> a.page_shift];
-        there[f] = (uint32_t)page < (uint32_t)a.pages;
-        base[f] = ((int64_t)(there[f] ? page : 0) * a.kv_heads + head) * head_bytes;
-        off[f] = tok & (P - 1);
-        const MDBF_GLOBAL uint32_t* kp = (const MDBF_GLOBAL uint32_t*)(cache + base[f] + (int64_t)(off[f] + r) * (D / 2) + h * (D / 8));
-#pragma unroll
-        for (int s = 0; s < KW; ++s) kc[f][s] = kp[s];
-        const MDBF_GLOBAL uint8_t* sp = cache + base[f] + (int64_t)P * D + (off[f] + r) * (D / 32);
-#pragma unroll
-        for (int s = 0; s < KS; ++s) ks[f][s] = there[f] ? sp[D == 64 ? h >> 1 : h * KS + s] : kKvNanScale;
-      }
-#pragma unroll
-      for (int n = 0; n < VU; ++n) {
-        const int f = D == 64 ? lane >> 5 : n / (VU / 2 ? VU / 2 : 1);
-        const int unit = D == 64 ? lane & 31 : (n % (VU / 2 ? VU / 2 : 1)) * 64 + lane;
-        const int64_t at = (f ? base[1] : base[0]);
-        const int o = f ? off[1] : off[0];
-        vc[n] = *(const MDBF_GLOBAL U32x4*)(cache + at + (int64_t)P * (D / 2) + o * (D / 2) + unit * 16);
-        vs[n] = (f ? there[1] : there[0]) ? cache[at + (int64_t)P * (D + D / 32) + o * (D / 32) + unit] : kKvNanScale;
-      }
-
+      for (int f = 0; f < 2; ++f) page[f] = table[min(t + 16 * f, rq.len - 1) >> a.page_shift];
+    };
+    auto work = [&](Tile& x, int t0) __attribute__((always_inline)) {
       // scores: a lane holds those of its row with tokens 4 h + 0 .. 3 of each half
       float z[2][4];
 #pragma unroll
       for (int f = 0; f < 2; ++f) {
         F32x4 s4 = {0, 0, 0, 0};
 #pragma unroll
-        for (int s = 0; s < KW; ++s) s4 = mma16<DT>(numbers<DT>(kc[f][s], unit_of(ks[f][KS == 1 ? 0 : s / 4])), qf[s], s4);
+        for (int s = 0; s < KW; ++s) s4 = mma16<DT>(numbers<DT>(x.kc[f][s], unit_of(x.ks[f][KS == 1 ? 0 : s / 4])), qf[s], s4);
 #pragma unroll
         for (int j = 0; j < 4; ++j) z[f][j] = s4[j] * a.scale;
       }
-      const bool inside = t0 >= all_lo && t0 + kTile <= all_hi;     // every row sees every token
+      const bool inside = t0 >= sp.all_lo && t0 + kTile <= sp.all_hi;     // every row sees every token
       if (!inside) {
 #pragma unroll
         for (int f = 0; f < 2; ++f)
@@ -221,32 +298,29 @@ __global__ __launch_bounds__(64 * kWaves) void attn_few_kernel(AttnArgs a) {
       // zero weight would bring it to all rows
 #pragma unroll
       for (int n = 0; n < VU; ++n) {
-        const int f = D == 64 ? lane >> 5 : n / (VU / 2 ? VU / 2 : 1);
-        const int unit = D == 64 ? lane & 31 : (n % (VU / 2 ? VU / 2 : 1)) * 64 + lane;
-        const int row = 16 * f + unit / (D / 32), tok = t0 + row;
-        if (!inside && (tok < tmin || tok >= tmax)) {
-          vc[n] = U32x4{0, 0, 0, 0};
-          vs[n] = 127;
+        const int unit = Tile::unit(n, lane), row = 16 * Tile::half(n, lane) + unit / (D / 32), tok = t0 + row;
+        if (!inside && (tok < sp.lo || tok >= sp.hi)) {
+          x.vc[n] = U32x4{0, 0, 0, 0};
+          x.vs[n] = 127;
         }
-        uint64_t bad = __ballot(vs[n] == kKvNanScale);
+        uint64_t bad = __ballot(x.vs[n] == kKvNanScale);
         if (bad) {
-          if (vs[n] == kKvNanScale) {
-            vc[n] = U32x4{0, 0, 0, 0};
-            vs[n] = 127;
+          if (x.vs[n] == kKvNanScale) {
+            x.vc[n] = U32x4{0, 0, 0, 0};
+            x.vs[n] = 127;
           }
           for (; bad; bad &= bad - 1) {
-            const int from = __builtin_ctzll(bad);
-            const int bu = D == 64 ? from & 31 : (n % (VU / 2 ? VU / 2 : 1)) * 64 + from, bf = D == 64 ? from >> 5 : f;
-            const int bt = t0 + 16 * bf + bu / (D / 32), bg = bu % (D / 32);
+            const int from = __builtin_ctzll(bad), bu = Tile::unit(n, from);
+            const int bt = t0 + 16 * Tile::half(n, from) + bu / (D / 32), bg = bu % (D / 32);
 #pragma unroll
             for (int c = 0; c < CT; ++c)
               if (c / 2 == bg && bt >= me.lo && bt < me.hi) acc[c] = F32x4{NAN, NAN, NAN, NAN};
           }
         }
-        const float unit_f = unit_of(vs[n]);
+        const float unit_f = unit_of(x.vs[n]);
         unsigned char* to = vals + row * VROW + (unit % (D / 32)) * 64;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) *reinterpret_cast<U32x4*>(to + w * 16) = numbers<DT>(vc[n][w], unit_f);
+        for (int w = 0; w < 4; ++w) *reinterpret_cast<U32x4*>(to + w * 16) = numbers<DT>(x.vc[n][w], unit_f);
       }
       wave_lds_order();
       // a lane's channel of tokens 4 h + 0 .. 3 of each half: the order of the scores' registers
@@ -258,6 +332,28 @@ __global__ __launch_bounds__(64 * kWaves) void attn_few_kernel(AttnArgs a) {
         acc[c] = mma16<DT>(U32x4{v0[0], v0[1], v1[0], v1[1]}, pf, acc[c]);
       }
       wave_lds_order();
+    };
+
+    constexpr int kStep = kWaves * kTile;
+    int t0 = (tmin & ~(kTile - 1)) + wave * kTile;
+    if (t0 < tmax) {
+      Tile x, y;
+      int page[2];
+      pages_of(t0, page);
+      x.load(a, head, head_bytes, t0, page, lane);
+      pages_of(t0 + kStep, page);
+      for (;;) {
+        if (t0 + kStep < tmax) y.load(a, head, head_bytes, t0 + kStep, page, lane);
+        pages_of(t0 + 2 * kStep, page);
+        work(x, t0);
+        t0 += kStep;
+        if (t0 >= tmax) break;
+        if (t0 + kStep < tmax) x.load(a, head, head_bytes, t0 + kStep, page, lane);
+        pages_of(t0 + 2 * kStep, page);
+        work(y, t0);
+        t0 += kStep;
+        if (t0 >= tmax) break;
+      }
     }
 
     // the waves meet
@@ -272,42 +368,91 @@ __global__ __launch_bounds__(64 * kWaves) void attn_few_kernel(AttnArgs a) {
     __syncthreads();
     {
       constexpr int N = D / 16;      // channels per thread
-      const int row = threadIdx.x >> 4, part = threadIdx.x & 15;
-      const int64_t Ro = rt * 16 + row;
+      const int row = threadIdx.x >> 4, piece = threadIdx.x & 15;
+      const int64_t Ro = rt * kRows + row;
       if (Ro < rows) {
-        const int io = (int)(Ro / a.group), go = (int)(Ro % a.group);
-        const Sees so = sees(a, rq, io);
         float top = stat[0][0][row];
 #pragma unroll
         for (int w = 1; w < kWaves; ++w) top = fmaxf(top, stat[w][0][row]);
-        if (top == -INFINITY) top = 0.0f;
+        const float use = top == -INFINITY ? 0.0f : top;
         float sum = 0, o[N];
 #pragma unroll
         for (int c = 0; c < N; ++c) o[c] = 0;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
-          const float f = __builtin_amdgcn_exp2f(stat[w][0][row] - top);
+          const float f = __builtin_amdgcn_exp2f(stat[w][0][row] - use);
           sum += f * stat[w][1][row];
-          const float* from = reinterpret_cast<const float*>(lds[w]) + row * OROW + part * N;
+          const float* from = reinterpret_cast<const float*>(lds[w]) + row * OROW + piece * N;
 #pragma unroll
           for (int c = 0; c < N; ++c) o[c] += f * from[c];
         }
-        const float inv = 1.0f / sum;
-        uint32_t w2[N / 2];
-#pragma unroll
-        for (int c = 0; c < N / 2; ++c) w2[c] = so.hi > so.lo ? round2<DT>(o[2 * c] * inv, o[2 * c + 1] * inv) : 0u;
-        MDBF_GLOBAL uint16_t* to = (MDBF_GLOBAL uint16_t*)a.out + (int64_t)(rq.start + io) * a.ldo + (int64_t)(head * a.group + go) * D + part * N;
-        if (a.wide_o) {
-#pragma unroll
-          for (int c = 0; c < N / 4; ++c) ((MDBF_GLOBAL U32x2*)to)[c] = U32x2{w2[2 * c], w2[2 * c + 1]};
-        } else {
-#pragma unroll
-          for (int c = 0; c < N / 2; ++c) {
-            to[2 * c] = (uint16_t)w2[c];
-            to[2 * c + 1] = (uint16_t)(w2[c] >> 16);
+        if (sp.parts > 1) {
+          MDBF_GLOBAL float* to = (MDBF_GLOBAL float*)a.part + (int64_t)blockIdx.x * part_floats<D>();
+          if (piece == 0) {
+            to[kRows * D + row] = top;
+            to[kRows * (D + 1) + row] = sum;
           }
+#pragma unroll
+          for (int c = 0; c < N / 4; ++c)
+            ((MDBF_GLOBAL F32x4*)(to + row * D + piece * N))[c] = F32x4{o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]};
+        } else {
+          store_row<DT, N>(a, rq, head, Ro, piece * N, o, sum);
         }
       }
+    }
+    __syncthreads();
+  }
+}
+
+// Joins the parts of a query row: a workgroup per row that the launch was sized for, D / 4 lanes side by side on its channels;
+// the groups of lanes take the parts in turn and meet in LDS, in one order.
+template <int D, int DT>
+__global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
+  constexpr int L = D / 4, GROUPS = 256 / L;
+  uint32_t idx = blockIdx.x;
+  const int row0 = idx % a.join_rows;
+  idx /= a.join_rows;
+  const uint32_t tile = idx;               // of the launch before
+  const int rt = idx % a.row_tiles;
+  idx /= a.row_tiles;
+  const int head = idx % a.kv_heads, b = idx / a.kv_heads;
+  const Request rq = request_of(a, b);
+  const int64_t rows = (int64_t)rq.fresh * a.group;
+  if ((int64_t)rt * kRows + row0 >= rows) return;
+  const Span sp = span_of(a, rq, rt, rows, a.splits);
+  if (sp.parts <= 1) return;
+  const MDBF_GLOBAL float* from = (const MDBF_GLOBAL float*)a.part + (int64_t)tile * a.splits * part_floats<D>();
+  __shared__ float stat[4];
+  __shared__ F32x4 sums[GROUPS][L + 1];
+  const int tid = threadIdx.x, l = tid % L, grp = tid / L;
+
+  for (int row = row0; row < kRows && (int64_t)rt * kRows + row < rows; row += a.join_rows) {
+    float top = -INFINITY;
+    for (int p = tid; p < sp.parts; p += 256) top = fmaxf(top, from[p * part_floats<D>() + kRows * D + row]);
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
+    if ((tid & 63) == 0) stat[tid >> 6] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(stat[0], stat[1]), fmaxf(stat[2], stat[3]));
+    const float use = top == -INFINITY ? 0.0f : top;
+    F32x4 o = {0, 0, 0, 0};
+    float sum = 0;
+    for (int p = grp; p < sp.parts; p += GROUPS) {
+      const MDBF_GLOBAL float* q = from + p * part_floats<D>();
+      const float f = __builtin_amdgcn_exp2f(q[kRows * D + row] - use);
+      sum += f * q[kRows * (D + 1) + row];
+      o += f * *(const MDBF_GLOBAL F32x4*)(q + row * D + l * 4);
+    }
+    sums[grp][l] = o;
+    if (l == 0) sums[grp][L][0] = sum;
+    __syncthreads();
+    if (grp == 0) {
+      for (int w = 1; w < GROUPS; ++w) {
+        o += sums[w][l];
+        sum += sums[w][L][0];
+      }
+      const float v[4] = {o[0], o[1], o[2], o[3]};
+      store_row<DT, 4>(a, rq, head, (int64_t)rt * kRows + row, l * 4, v, sum);
     }
     __syncthreads();
   }
@@ -324,11 +469,43 @@ static int check_attn(const mdbf_kv_t* kv, const mdbf_attn_t* at, int requests, 
   return MDBF_OK;
 }
 
+// How a call is cut up: tiles of query rows per request and kv head, and parts of the tokens of each.
+struct AttnGeom {
+  int64_t tiles;           // over all requests and kv heads
+  int row_tiles, splits, chunk;
+  size_t part_bytes;
+};
+// A part is one workgroup's: enough of them to fill the device several times over, so that requests of unequal length even
+// out, but none shorter than kLeastChunk tokens, two steps of its waves.
+constexpr int kLeastChunk = 256, kPartsWanted = 2048, kMostSplits = 1024;
+static AttnGeom attn_geom(const mdbf_kv_t& kv, const mdbf_attn_t& at, int requests, int T) {
+  AttnGeom g;
+  const int64_t group = at.q_heads / kv.kv_heads, most = std::min(at.max_fresh, T);
+  g.row_tiles = (int)std::min<int64_t>((most * group + kRows - 1) / kRows, 1 << 16);
+  g.tiles = (int64_t)requests * kv.kv_heads * g.row_tiles;
+  int64_t span = at.max_length;
+  if (at.window) span = std::min<int64_t>(span, (int64_t)at.window + kRows + kTile);
+  const int64_t splits = std::max<int64_t>(1, std::min<int64_t>({kPartsWanted / g.tiles, span / kLeastChunk, kMostSplits}));
+  const int64_t step = kWaves * kTile;
+  g.chunk = (int)(((span + splits - 1) / splits + step - 1) / step * step);
+  g.splits = (int)((span + g.chunk - 1) / g.chunk);
+  g.part_bytes = g.splits > 1 ? (size_t)g.tiles * g.splits * kRows * (kv.head_dim + 2) * 4 : 0;
+  return g;
+}
+
+template <int D, int DT>
+static int launch_few(const AttnArgs& a, const AttnGeom& g, hipStream_t s) {
+  attn_few_kernel<D, DT><<<(unsigned)(g.tiles * g.splits), 64 * kWaves, 0, s>>>(a);
+  int e = (int)hipGetLastError();
+  if (e == 0 && g.splits > 1) {
+    attn_join_kernel<D, DT><<<(unsigned)(g.tiles * a.join_rows), 256, 0, s>>>(a);
+    e = (int)hipGetLastError();
+  }
+  return e;
+}
 template <int DT>
-static void launch_few(int d, unsigned grid, const AttnArgs& a, hipStream_t s) {
-  if (d == 64) attn_few_kernel<64, DT><<<grid, 64 * kWaves, 0, s>>>(a);
-  else if (d == 128) attn_few_kernel<128, DT><<<grid, 64 * kWaves, 0, s>>>(a);
-  else attn_few_kernel<256, DT><<<grid, 64 * kWaves, 0, s>>>(a);
+static int launch_attn(int d, const AttnArgs& a, const AttnGeom& g, hipStream_t s) {
+  return d == 64 ? launch_few<64, DT>(a, g, s) : d == 128 ? launch_few<128, DT>(a, g, s) : launch_few<256, DT>(a, g, s);
 }
 
 }  // namespace mdbf
@@ -341,7 +518,7 @@ int mdbf_kv_attention_workspace_bytes(const mdbf_kv_t* kv, const mdbf_attn_t* at
   if (!bytes_out) return MDBF_EINVAL;
   int st = check_attn(kv, attn, requests, T);
   if (st) return st;
-  *bytes_out = 0;
+  *bytes_out = attn_geom(*kv, *attn, requests, T).part_bytes;
   return MDBF_OK;
 }
 
@@ -360,21 +537,21 @@ int mdbf_kv_attention(const mdbf_kv_t* kv, const mdbf_attn_t* attn, const void* 
     if (!kv_aligned(p, 16)) return MDBF_EALIGN;
   for (const void* p : ints)
     if (!kv_aligned(p, 4)) return MDBF_EALIGN;
-  (void)workspace_bytes;
+  const AttnGeom geom = attn_geom(*kv, *attn, requests, T);
+  if (geom.part_bytes && !workspace_dev) return MDBF_EINVAL;
+  if (workspace_bytes < geom.part_bytes) return MDBF_EWORKSPACE;
+  if (geom.tiles * std::max(geom.splits, kRows) > 0x7fffffff) return MDBF_EUNSUPPORTED;
   AttnArgs a = {};
   a.cache = (const uint8_t*)cache_dev, a.table = table_dev, a.cu = cu_dev, a.lengths = lengths_dev, a.q = q_dev, a.out = out_dev;
   a.table_ld = table_ld, a.ldq = ldq, a.ldo = ldo, a.table_width = table_width, a.T = T, a.pages = kv->pages;
-  a.kv_heads = kv->kv_heads, a.group = attn->q_heads / kv->kv_heads, a.page_shift = kv_page_shift(kv->page_size);
-  a.causal = attn->flags & MDBF_ATTN_CAUSAL, a.window = attn->window;
+  a.kv_heads = kv->kv_heads, a.group = attn->q_heads / kv->kv_heads, a.head_dim = kv->head_dim;
+  a.page_shift = kv_page_shift(kv->page_size), a.causal = attn->flags & MDBF_ATTN_CAUSAL, a.window = attn->window;
+  a.row_tiles = geom.row_tiles, a.splits = geom.splits, a.chunk = geom.chunk, a.part = (float*)workspace_dev;
+  a.join_rows = (int)std::min<int64_t>((int64_t)std::min(attn->max_fresh, T) * a.group, kRows);
   a.scale = (float)(attn->scale * 1.4426950408889634);
   a.wide_q = ldq % 8 == 0, a.wide_o = ldo % 4 == 0;
-  const int64_t most = std::min<int64_t>(attn->max_fresh, T);
-  a.row_tiles = (int32_t)std::min<int64_t>((most * a.group + 15) / 16, 1 << 16);
-  const int64_t grid = (int64_t)requests * a.kv_heads * a.row_tiles;
-  if (grid > 0x7fffffff) return MDBF_EUNSUPPORTED;
-  if (kv->dtype == MDBF_F16) launch_few<MDBF_F16>(kv->head_dim, (unsigned)grid, a, (hipStream_t)stream);
-  else launch_few<MDBF_BF16>(kv->head_dim, (unsigned)grid, a, (hipStream_t)stream);
-  return hip_fail((int)hipGetLastError());
+  return hip_fail(kv->dtype == MDBF_F16 ? launch_attn<MDBF_F16>(kv->head_dim, a, geom, (hipStream_t)stream)
+                                        : launch_attn<MDBF_BF16>(kv->head_dim, a, geom, (hipStream_t)stream));
 }
 
 }  // extern "C"
