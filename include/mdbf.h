@@ -377,7 +377,7 @@ typedef struct {
   int32_t window;       /* > 0 (causal only): a token sees the last `window` tokens up to itself; 0: all */
   int32_t max_fresh;    /* most new tokens of a request, and ... */
   int32_t max_length;   /* ... the longest request: launch sizes go by them.  Larger ones in cu and lengths are served as well, slowly */
-  float scale;          /* of the scores, usually head_dim^-1/2 */
+  float scale;          /* of the scores, usually head_dim^-1/2; not 0 */
 } mdbf_attn_t;
 
 /* out[t, h] = sum_j softmax_j(scale q[t, h] . k_j) v_j over the tokens j of t's request that it sees, whose keys and values

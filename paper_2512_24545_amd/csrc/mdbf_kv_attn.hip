@@ -28,7 +28,8 @@ struct AttnArgs {
   int64_t table_ld, ldq, ldo;
   float* part;
   int32_t table_width, T, pages, kv_heads, group, head_dim, page_shift, causal, window, row_tiles, splits, chunk, join_rows;
-  float scale;                 // of the scores, times log2(e)
+  float scale;                 // of the scores, times log2(e); its sign is the queries' (flip: 0x80008000)
+  uint32_t flip;
   uint8_t wide_q, wide_o;
 };
 
@@ -111,6 +112,7 @@ __device__ __forceinline__ void store_row(const AttnArgs& a, const Request& rq, 
 constexpr int kTile = 32;        // tokens per step of a wave
 constexpr int kWaves = 4;
 constexpr int kRows = 16;        // query rows of a workgroup
+constexpr float kSlack = 8;      // powers of two by which a score may exceed the running reference
 
 // The tokens that the rows of a tile of query rows see, and their part of each workgroup: `chunk` tokens from the first one's
 // tile on, the rest of them for the last workgroup.
@@ -131,8 +133,11 @@ __device__ __forceinline__ Span span_of(const AttnArgs& a, const Request& rq, in
 template <int D>
 __device__ __forceinline__ int64_t part_floats() { return kRows * (D + 2); }
 
-// One wave's tile of tokens: codes and scales of its keys and values as loaded.
-template <int D>
+constexpr int kNonTemporal = 2;  // of the buffer loads: the cache is read once
+
+// One wave's tile of tokens: codes and scales of its keys and values as loaded.  It lies in one page (ONE), or its halves of 16
+// tokens lie in one each (pages of 16 tokens).
+template <int D, bool ONE>
 struct Codes {
   static constexpr int KW = D / 32;                  // dwords of codes per lane and 16 keys = matrix steps over the channels
   static constexpr int KS = D <= 128 ? 1 : D / 128;  // scales among them
@@ -145,57 +150,92 @@ struct Codes {
   __device__ static __forceinline__ int half(int n, int lane) { return D == 64 ? lane >> 5 : n / VH; }
   __device__ static __forceinline__ int unit(int n, int lane) { return D == 64 ? lane & 31 : (n % VH) * 64 + lane; }
 
-  // `page`: of the two halves' tokens, which begin at tok
+  bool there[2];             // whether the halves' pages are pages of the pool
+
+  // `page`: of the two halves' tokens, which begin at tok.  Nothing here looks at what the loads bring: they are in flight while
+  // the tile before is worked on.  (Buffer loads: a page's part for the head is the buffer, a lane's place in a tile the offset.)
   __device__ __forceinline__ void load(const AttnArgs& a, int head, int64_t head_bytes, int tok, const int (&page)[2], int lane) {
     const int P = 1 << a.page_shift, r = lane & 15, h = lane >> 4;
-    const MDBF_GLOBAL uint8_t* base[2];
-    bool there[2];
+    const uint8_t* base[2];
+    __amdgpu_buffer_rsrc_t buf[2];
     int off[2];
 #pragma unroll
     for (int f = 0; f < 2; ++f) {
+      if (ONE && f) {
+        there[1] = there[0], buf[1] = buf[0], off[1] = off[0] + 16;
+        continue;
+      }
       there[f] = (uint32_t)page[f] < (uint32_t)a.pages;
-      base[f] = (const MDBF_GLOBAL uint8_t*)a.cache + ((int64_t)(there[f] ? page[f] : 0) * a.kv_heads + head) * head_bytes;
+      base[f] = a.cache + ((int64_t)(there[f] ? page[f] : 0) * a.kv_heads + head) * head_bytes;
+      buf[f] = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base[f]), 0, (int)head_bytes, 0x00027000);
       off[f] = (tok + 16 * f) & (P - 1);
-      const MDBF_GLOBAL uint8_t* kp = base[f] + off[f] * (D / 2);
-      const uint32_t at = r * (D / 2) + h * (D / 8);
+    }
+#pragma unroll
+    for (int f = 0; f < 2; ++f) {
+      const int at = r * (D / 2) + h * (D / 8);
       if (KW == 2) {
-        const U32x2 v = __builtin_nontemporal_load((const MDBF_GLOBAL U32x2*)(kp + at));
+        const U32x2 v = __builtin_amdgcn_raw_buffer_load_b64(buf[f], at, off[f] * (D / 2), kNonTemporal);
         kc[f][0] = v[0], kc[f][1] = v[1];
       } else {
 #pragma unroll
         for (int s = 0; s < KW; s += 4) {
-          const U32x4 v = __builtin_nontemporal_load((const MDBF_GLOBAL U32x4*)(kp + at + 4 * s));
+          const U32x4 v = __builtin_amdgcn_raw_buffer_load_b128(buf[f], at + 4 * s, off[f] * (D / 2), kNonTemporal);
 #pragma unroll
           for (int w = 0; w < 4; ++w) kc[f][(s + w) % KW] = v[w];
         }
       }
-      const MDBF_GLOBAL uint8_t* sp = base[f] + P * D + off[f] * (D / 32);
 #pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        const uint32_t b = sp[(uint32_t)(r * (D / 32) + (D == 64 ? h >> 1 : h * KS + s))];
-        ks[f][s] = there[f] ? b : kKvNanScale;
-      }
+      for (int s = 0; s < KS; ++s)
+        ks[f][s] = __builtin_amdgcn_raw_buffer_load_b8(buf[f], r * (D / 32) + (D == 64 ? h >> 1 : h * KS + s), P * D + off[f] * (D / 32), 0);
     }
 #pragma unroll
     for (int n = 0; n < VU; ++n) {
-      const int f = half(n, lane);
-      const uint32_t u = unit(n, lane);
-      const MDBF_GLOBAL uint8_t* at = f ? base[1] : base[0];
-      const int o = f ? off[1] : off[0];
-      vc[n] = __builtin_nontemporal_load((const MDBF_GLOBAL U32x4*)(at + (P + o) * (D / 2) + u * 16));
-      const uint32_t b = at[P * (D + D / 32) + o * (D / 32) + u];
-      vs[n] = (f ? there[1] : there[0]) ? b : kKvNanScale;
+      if (!ONE && D == 64) {      // the halves of one load in different pages
+        const MDBF_GLOBAL uint8_t* at = (const MDBF_GLOBAL uint8_t*)(lane < 32 ? base[0] : base[1]);
+        const uint32_t o = lane < 32 ? off[0] : off[1], u = lane & 31;
+        vc[n] = __builtin_nontemporal_load((const MDBF_GLOBAL U32x4*)(at + (P + o) * (D / 2) + u * 16));
+        vs[n] = at[P * (D + D / 32) + o * (D / 32) + u];
+      } else {
+        const int f = ONE ? 0 : n / VH, u = (ONE ? n : n % VH) * 64 + lane;
+        vc[n] = __builtin_amdgcn_raw_buffer_load_b128(buf[f], u * 16, (P + off[f]) * (D / 2), kNonTemporal);
+        vs[n] = __builtin_amdgcn_raw_buffer_load_b8(buf[f], u, P * (D + D / 32) + off[f] * (D / 32), 0);
+      }
     }
+  }
+  // a page that is none reads as NaN
+  __device__ __forceinline__ void check(int lane) {
+    if (there[0] && there[1]) return;
+#pragma unroll
+    for (int f = 0; f < 2; ++f)
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+        if (!there[f]) ks[f][s] = kKvNanScale;
+#pragma unroll
+    for (int n = 0; n < VU; ++n)
+      if (!(half(n, lane) ? there[1] : there[0])) vs[n] = kKvNanScale;
   }
 };
 
+// max over the four lanes that hold a query row, and their sum
+__device__ __forceinline__ float row_max(float x) {
+  const auto a = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+  const uint32_t a0 = a[0], a1 = a[1];
+  x = fmaxf(__builtin_bit_cast(float, a0), __builtin_bit_cast(float, a1));
+  const auto b = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+  const uint32_t b0 = b[0], b1 = b[1];
+  return fmaxf(__builtin_bit_cast(float, b0), __builtin_bit_cast(float, b1));
+}
+
 // One kv head, 16 query rows, one part of their tokens; the part's tiles are dealt out to the four waves, which meet at
 // the end.  A tile's loads are issued before the products of the one before it, and its page numbers a tile earlier still.
-template <int D, int DT>
+template <int D, int DT, bool ONE>
 __global__ __launch_bounds__(64 * kWaves, D == 64 ? 4 : D == 128 ? 3 : 2) void attn_few_kernel(AttnArgs a) {
-  using Tile = Codes<D>;
+  using Tile = Codes<D, ONE>;
   constexpr int KW = Tile::KW, KS = Tile::KS, VU = Tile::VU;
-  constexpr int VROW = D * 2 + 32;            // bytes of a token's values in LDS
+  // A token's values in LDS: 64 bytes per block, 16 more after each (D = 64) or every second one, rows an odd multiple of 32
+  // bytes apart: neither the writes nor the transposing reads meet on a bank.
+  constexpr int VROW = D == 64 ? 160 : D == 128 ? 288 : 608;
+  auto block_at = [](int g) { return g * 64 + (D == 64 ? g : g >> 1) * 16; };
   constexpr int CT = D / 16;                  // channel tiles
   constexpr int OROW = D + 4;                 // floats of a row of results in LDS
   static_assert(kTile * VROW >= kRows * OROW * 4, "the results fit the values' place");
@@ -239,10 +279,12 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 4 : D == 128 ? 3 : 2) void a
 #pragma unroll
           for (int j = 0; j < 4; ++j) qf[s][j] = (uint32_t)p[2 * j] | ((uint32_t)p[2 * j + 1] << 16);
         }
+        qf[s] ^= a.flip;
       }
     }
 
     float m = -INFINITY, l = 0;
+    uint32_t nan_blocks = 0;       // blocks of channels in which the row sees a NaN
     F32x4 acc[CT];
 #pragma unroll
     for (int c = 0; c < CT; ++c) acc[c] = F32x4{0, 0, 0, 0};
@@ -250,18 +292,17 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 4 : D == 128 ? 3 : 2) void a
     // page numbers of a tile's halves; behind the last token's none is looked up
     auto pages_of = [&](int t, int (&page)[2]) __attribute__((always_inline)) {
 #pragma unroll
-      for (int f = 0; f < 2; ++f) page[f] = table[min(t + 16 * f, rq.len - 1) >> a.page_shift];
+      for (int f = 0; f < (ONE ? 1 : 2); ++f) page[f] = table[min(t + 16 * f, rq.len - 1) >> a.page_shift];
     };
     auto work = [&](Tile& x, int t0) __attribute__((always_inline)) {
-      // scores: a lane holds those of its row with tokens 4 h + 0 .. 3 of each half
-      float z[2][4];
+      x.check(lane);
+      // scores (without their factor): a lane holds those of its row with tokens 4 h + 0 .. 3 of each half
+      F32x4 z[2];
 #pragma unroll
       for (int f = 0; f < 2; ++f) {
-        F32x4 s4 = {0, 0, 0, 0};
+        z[f] = F32x4{0, 0, 0, 0};
 #pragma unroll
-        for (int s = 0; s < KW; ++s) s4 = mma16<DT>(numbers<DT>(x.kc[f][s], unit_of(x.ks[f][KS == 1 ? 0 : s / 4])), qf[s], s4);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) z[f][j] = s4[j] * a.scale;
+        for (int s = 0; s < KW; ++s) z[f] = mma16<DT>(numbers<DT>(x.kc[f][s], unit_of(x.ks[f][KS == 1 ? 0 : s / 4])), qf[s], z[f]);
       }
       const bool inside = t0 >= sp.all_lo && t0 + kTile <= sp.all_hi;     // every row sees every token
       if (!inside) {
@@ -273,25 +314,23 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 4 : D == 128 ? 3 : 2) void a
             if (tok < me.lo || tok >= me.hi) z[f][j] = -INFINITY;
           }
       }
-      float top = fmaxf(fmaxf(fmaxf(z[0][0], z[0][1]), fmaxf(z[0][2], z[0][3])), fmaxf(fmaxf(z[1][0], z[1][1]), fmaxf(z[1][2], z[1][3])));
-      top = fmaxf(top, __shfl_xor(top, 16));
-      top = fmaxf(top, __shfl_xor(top, 32));
-      const float mn = fmaxf(m, top), use = mn == -INFINITY ? 0.0f : mn;
-      const float alpha = __builtin_amdgcn_exp2f(m - use);
-      m = mn;
-      float p[2][4], sum = 0;
-#pragma unroll
-      for (int f = 0; f < 2; ++f)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          p[f][j] = __builtin_amdgcn_exp2f(z[f][j] - use);
-          sum += p[f][j];
-        }
-      l = l * alpha + sum;
-      if (__any(alpha != 1.0f)) {
+      // The reference m follows the maximum only where that has grown by more than kSlack (numerators stay below 2^kSlack, in
+      // reach of fp16): most tiles exchange nothing between lanes and rescale nothing.
+      const float top = fmaxf(fmaxf(fmaxf(z[0][0], z[0][1]), fmaxf(z[0][2], z[0][3])), fmaxf(fmaxf(z[1][0], z[1][1]), fmaxf(z[1][2], z[1][3]))) * a.scale;
+      if (__any(top > m + kSlack)) {
+        const float mn = fmaxf(m, row_max(top)), alpha = __builtin_amdgcn_exp2f(m - (mn == -INFINITY ? 0.0f : mn));
+        m = mn;
+        l *= alpha;
 #pragma unroll
         for (int c = 0; c < CT; ++c) acc[c] *= alpha;
       }
+      const float use = m == -INFINITY ? 0.0f : m;
+      F32x4 p[2];
+#pragma unroll
+      for (int f = 0; f < 2; ++f)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) p[f][j] = __builtin_amdgcn_exp2f(z[f][j] * a.scale - use);
+      l += ((p[0][0] + p[0][1]) + (p[0][2] + p[0][3])) + ((p[1][0] + p[1][1]) + (p[1][2] + p[1][3]));
       const U32x4 pf = {round2<DT>(p[0][0], p[0][1]), round2<DT>(p[0][2], p[0][3]), round2<DT>(p[1][0], p[1][1]), round2<DT>(p[1][2], p[1][3])};
 
       // values that no row sees are zeros; NaN among the others goes to the rows that see it, not through the product, where a
@@ -312,13 +351,11 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 4 : D == 128 ? 3 : 2) void a
           for (; bad; bad &= bad - 1) {
             const int from = __builtin_ctzll(bad), bu = Tile::unit(n, from);
             const int bt = t0 + 16 * Tile::half(n, from) + bu / (D / 32), bg = bu % (D / 32);
-#pragma unroll
-            for (int c = 0; c < CT; ++c)
-              if (c / 2 == bg && bt >= me.lo && bt < me.hi) acc[c] = F32x4{NAN, NAN, NAN, NAN};
+            if (bt >= me.lo && bt < me.hi) nan_blocks |= 1u << bg;
           }
         }
         const float unit_f = unit_of(x.vs[n]);
-        unsigned char* to = vals + row * VROW + (unit % (D / 32)) * 64;
+        unsigned char* to = vals + row * VROW + block_at(unit % (D / 32));
 #pragma unroll
         for (int w = 0; w < 4; ++w) *reinterpret_cast<U32x4*>(to + w * 16) = numbers<DT>(x.vc[n][w], unit_f);
       }
@@ -326,7 +363,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 4 : D == 128 ? 3 : 2) void a
       // a lane's channel of tokens 4 h + 0 .. 3 of each half: the order of the scores' registers
 #pragma unroll
       for (int c = 0; c < CT; ++c) {
-        const unsigned char* from = vals + (4 * h + (r >> 2)) * VROW + c * 32 + (r & 3) * 8;
+        const unsigned char* from = vals + (4 * h + (r >> 2)) * VROW + block_at(c / 2) + (c & 1) * 32 + (r & 3) * 8;
         const U32x2 v0 = __builtin_bit_cast(U32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((MDBF_LDS S16x4*)from));
         const U32x2 v1 = __builtin_bit_cast(U32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((MDBF_LDS S16x4*)(from + 16 * VROW)));
         acc[c] = mma16<DT>(U32x4{v0[0], v0[1], v1[0], v1[1]}, pf, acc[c]);
@@ -355,6 +392,10 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 4 : D == 128 ? 3 : 2) void a
         if (t0 >= tmax) break;
       }
     }
+
+#pragma unroll
+    for (int c = 0; c < CT; ++c)
+      if (nan_blocks >> (c / 2) & 1) acc[c] = F32x4{NAN, NAN, NAN, NAN};
 
     // the waves meet
     l += __shfl_xor(l, 16);
@@ -404,12 +445,16 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 4 : D == 128 ? 3 : 2) void a
   }
 }
 
-// Joins the parts of a query row: a workgroup per row that the launch was sized for, D / 4 lanes side by side on its channels;
-// the groups of lanes take the parts in turn and meet in LDS, in one order.
-template <int D, int DT>
+// Joins the parts of a query row: a workgroup per row that the launch was sized for and CH of its channels, CH / 4 lanes side by
+// side on them; the groups of lanes take the parts in turn and meet in LDS, in one order.  A chain of two trips to memory at
+// most: the first parts' sums are requested before the weights are known.
+constexpr int kMostSplits = 1024;
+template <int D, int DT, int CH>
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
-  constexpr int L = D / 4, GROUPS = 256 / L;
+  constexpr int L = CH / 4, GROUPS = 256 / L, AHEAD = 8;
   uint32_t idx = blockIdx.x;
+  const int c0 = idx % (D / CH) * CH;
+  idx /= D / CH;
   const int row0 = idx % a.join_rows;
   idx /= a.join_rows;
   const uint32_t tile = idx;               // of the launch before
@@ -422,37 +467,58 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
   const Span sp = span_of(a, rq, rt, rows, a.splits);
   if (sp.parts <= 1) return;
   const MDBF_GLOBAL float* from = (const MDBF_GLOBAL float*)a.part + (int64_t)tile * a.splits * part_floats<D>();
-  __shared__ float stat[4];
-  __shared__ F32x4 sums[GROUPS][L + 1];
+  __shared__ float weight[kMostSplits], stat[4], total[4];
+  __shared__ F32x4 sums[GROUPS][L];
   const int tid = threadIdx.x, l = tid % L, grp = tid / L;
 
   for (int row = row0; row < kRows && (int64_t)rt * kRows + row < rows; row += a.join_rows) {
-    float top = -INFINITY;
-    for (int p = tid; p < sp.parts; p += 256) top = fmaxf(top, from[p * part_floats<D>() + kRows * D + row]);
+    const MDBF_GLOBAL float* mine = from + row * D + c0 + l * 4;
+    F32x4 ahead[AHEAD];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k)
+      if (grp + k * GROUPS < sp.parts) ahead[k] = *(const MDBF_GLOBAL F32x4*)(mine + (grp + k * GROUPS) * part_floats<D>());
+    float top = -INFINITY, tops[kMostSplits / 256], parts_sum[kMostSplits / 256];
+#pragma unroll
+    for (int k = 0; k < kMostSplits / 256; ++k) {
+      const int p = tid + k * 256;
+      tops[k] = -INFINITY, parts_sum[k] = 0;
+      if (p < sp.parts) {
+        tops[k] = from[p * part_floats<D>() + kRows * D + row];
+        parts_sum[k] = from[p * part_floats<D>() + kRows * (D + 1) + row];
+        top = fmaxf(top, tops[k]);
+      }
+    }
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
     if ((tid & 63) == 0) stat[tid >> 6] = top;
     __syncthreads();
     top = fmaxf(fmaxf(stat[0], stat[1]), fmaxf(stat[2], stat[3]));
     const float use = top == -INFINITY ? 0.0f : top;
-    F32x4 o = {0, 0, 0, 0};
     float sum = 0;
-    for (int p = grp; p < sp.parts; p += GROUPS) {
-      const MDBF_GLOBAL float* q = from + p * part_floats<D>();
-      const float f = __builtin_amdgcn_exp2f(q[kRows * D + row] - use);
-      sum += f * q[kRows * (D + 1) + row];
-      o += f * *(const MDBF_GLOBAL F32x4*)(q + row * D + l * 4);
-    }
+#pragma unroll
+    for (int k = 0; k < kMostSplits / 256; ++k)
+      if (tid + k * 256 < sp.parts) {
+        const float f = __builtin_amdgcn_exp2f(tops[k] - use);
+        weight[tid + k * 256] = f;
+        sum += f * parts_sum[k];
+      }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
+    if ((tid & 63) == 0) total[tid >> 6] = sum;
+    __syncthreads();
+    sum = (total[0] + total[1]) + (total[2] + total[3]);
+    F32x4 o = {0, 0, 0, 0};
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k)
+      if (grp + k * GROUPS < sp.parts) o += weight[grp + k * GROUPS] * ahead[k];
+    for (int p = grp + AHEAD * GROUPS; p < sp.parts; p += GROUPS) o += weight[p] * *(const MDBF_GLOBAL F32x4*)(mine + p * part_floats<D>());
     sums[grp][l] = o;
-    if (l == 0) sums[grp][L][0] = sum;
     __syncthreads();
     if (grp == 0) {
-      for (int w = 1; w < GROUPS; ++w) {
-        o += sums[w][l];
-        sum += sums[w][L][0];
-      }
+#pragma unroll
+      for (int w = 1; w < GROUPS; ++w) o += sums[w][l];
       const float v[4] = {o[0], o[1], o[2], o[3]};
-      store_row<DT, 4>(a, rq, head, (int64_t)rt * kRows + row, l * 4, v, sum);
+      store_row<DT, 4>(a, rq, head, (int64_t)rt * kRows + row, c0 + l * 4, v, sum);
     }
     __syncthreads();
   }
@@ -462,7 +528,7 @@ static int check_attn(const mdbf_kv_t* kv, const mdbf_attn_t* at, int requests, 
   int st = check_kv(kv);
   if (st) return st;
   if (!at || requests < 1 || T < 1) return MDBF_EINVAL;
-  if (at->q_heads <= 0 || at->q_heads % kv->kv_heads || at->window < 0 || at->max_fresh < 1 || at->max_length < 1 || !isfinite(at->scale))
+  if (at->q_heads <= 0 || at->q_heads % kv->kv_heads || at->window < 0 || at->max_fresh < 1 || at->max_length < 1 || !isfinite(at->scale) || at->scale == 0.0f)
     return MDBF_EINVAL;
   if (at->window && !(at->flags & MDBF_ATTN_CAUSAL)) return MDBF_EINVAL;
   if ((at->flags & ~MDBF_ATTN_CAUSAL) || at->q_heads > (1 << 16)) return MDBF_EUNSUPPORTED;
@@ -477,7 +543,7 @@ struct AttnGeom {
 };
 // A part is one workgroup's: enough of them to fill the device several times over, so that requests of unequal length even
 // out, but none shorter than kLeastChunk tokens, two steps of its waves.
-constexpr int kLeastChunk = 256, kPartsWanted = 2048, kMostSplits = 1024;
+constexpr int kLeastChunk = 256, kPartsWanted = 2048;
 static AttnGeom attn_geom(const mdbf_kv_t& kv, const mdbf_attn_t& at, int requests, int T) {
   AttnGeom g;
   const int64_t group = at.q_heads / kv.kv_heads, most = std::min(at.max_fresh, T);
@@ -495,10 +561,13 @@ static AttnGeom attn_geom(const mdbf_kv_t& kv, const mdbf_attn_t& at, int reques
 
 template <int D, int DT>
 static int launch_few(const AttnArgs& a, const AttnGeom& g, hipStream_t s) {
-  attn_few_kernel<D, DT><<<(unsigned)(g.tiles * g.splits), 64 * kWaves, 0, s>>>(a);
+  if (a.page_shift == 4) attn_few_kernel<D, DT, false><<<(unsigned)(g.tiles * g.splits), 64 * kWaves, 0, s>>>(a);
+  else attn_few_kernel<D, DT, true><<<(unsigned)(g.tiles * g.splits), 64 * kWaves, 0, s>>>(a);
   int e = (int)hipGetLastError();
   if (e == 0 && g.splits > 1) {
-    attn_join_kernel<D, DT><<<(unsigned)(g.tiles * a.join_rows), 256, 0, s>>>(a);
+    // few parts: all channels in one workgroup
+    if (g.splits > 16) attn_join_kernel<D, DT, 32><<<(unsigned)(g.tiles * a.join_rows * (D / 32)), 256, 0, s>>>(a);
+    else attn_join_kernel<D, DT, D><<<(unsigned)(g.tiles * a.join_rows), 256, 0, s>>>(a);
     e = (int)hipGetLastError();
   }
   return e;
@@ -540,7 +609,7 @@ int mdbf_kv_attention(const mdbf_kv_t* kv, const mdbf_attn_t* attn, const void* 
   const AttnGeom geom = attn_geom(*kv, *attn, requests, T);
   if (geom.part_bytes && !workspace_dev) return MDBF_EINVAL;
   if (workspace_bytes < geom.part_bytes) return MDBF_EWORKSPACE;
-  if (geom.tiles * std::max(geom.splits, kRows) > 0x7fffffff) return MDBF_EUNSUPPORTED;
+  if (geom.tiles * std::max(geom.splits, kRows * 8) > 0x7fffffff) return MDBF_EUNSUPPORTED;
   AttnArgs a = {};
   a.cache = (const uint8_t*)cache_dev, a.table = table_dev, a.cu = cu_dev, a.lengths = lengths_dev, a.q = q_dev, a.out = out_dev;
   a.table_ld = table_ld, a.ldq = ldq, a.ldo = ldo, a.table_width = table_width, a.T = T, a.pages = kv->pages;
@@ -548,7 +617,7 @@ int mdbf_kv_attention(const mdbf_kv_t* kv, const mdbf_attn_t* attn, const void* 
   a.page_shift = kv_page_shift(kv->page_size), a.causal = attn->flags & MDBF_ATTN_CAUSAL, a.window = attn->window;
   a.row_tiles = geom.row_tiles, a.splits = geom.splits, a.chunk = geom.chunk, a.part = (float*)workspace_dev;
   a.join_rows = (int)std::min<int64_t>((int64_t)std::min(attn->max_fresh, T) * a.group, kRows);
-  a.scale = (float)(attn->scale * 1.4426950408889634);
+  a.scale = (float)(fabs((double)attn->scale) * 1.4426950408889634), a.flip = attn->scale < 0 ? 0x80008000u : 0u;
   a.wide_q = ldq % 8 == 0, a.wide_o = ldo % 4 == 0;
   return hip_fail(kv->dtype == MDBF_F16 ? launch_attn<MDBF_F16>(kv->head_dim, a, geom, (hipStream_t)stream)
                                         : launch_attn<MDBF_BF16>(kv->head_dim, a, geom, (hipStream_t)stream));

@@ -475,6 +475,11 @@ def test_large_scores(gpu, dt, fresh, lengths):
     Step(gpu, lengths, fresh, 4, 2, 128, 16, dt).check(scale=3.0)
 
 
+@pytest.mark.parametrize("fresh", [1, 70])
+def test_negative_scale(gpu, fresh):
+    Step(gpu, [100, 333], [fresh, 1], 4, 2, 64, 16, "bf16").check(scale=-0.3)
+
+
 def not_finite_case(gpu, dt, fresh, lengths, seed, window=0):
     """Blocks of keys and values that are NaN reach the rows that see them, and no other."""
     s = Step(gpu, lengths, fresh, 4, 2, 128, 16, dt, seed=seed)

@@ -174,7 +174,7 @@ def test_attention_arguments():
     size, out = 10 * 2 * 16 * 136, C.c_size_t(0)
     good = [kv(), attn(), A, size, A, 9, 9, A, A, 2, A, 512, 3, A, 512, A, HUGE, None]
     bad_attn = ((dict(q_heads=0), -1), (dict(q_heads=5), -1), (dict(flags=4), -5), (dict(window=-1), -1), (dict(window=5, flags=0), -1),
-                (dict(max_fresh=0), -1), (dict(max_length=0), -1), (dict(scale=float("nan")), -1), (dict(scale=float("inf")), -1),
+                (dict(max_fresh=0), -1), (dict(max_length=0), -1), (dict(scale=float("nan")), -1), (dict(scale=float("inf")), -1), (dict(scale=0.0), -1),
                 (dict(q_heads=140000), -5))
     for kw, status in bad_attn:
         args = list(good)
