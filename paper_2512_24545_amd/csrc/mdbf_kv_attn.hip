@@ -27,7 +27,8 @@ struct AttnArgs {
   void* out;
   int64_t table_ld, ldq, ldo;
   float* part;
-  int32_t table_width, T, pages, kv_heads, group, head_dim, page_shift, causal, window, row_tiles, splits, chunk, join_rows;
+  int32_t table_width, requests, T, pages, kv_heads, group, head_dim, page_shift, causal, window, row_tiles, shares, join_rows;
+  uint32_t group_mul, group_shift;      // i / group = i * group_mul >> group_shift for i < 2^31
   float scale;                 // of the scores, times log2(e); its sign is the queries' (flip: 0x80008000)
   uint32_t flip;
   uint8_t wide_q, wide_o;
@@ -66,6 +67,9 @@ __device__ __forceinline__ void wave_lds_order() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
+// the new token that query row R of a request and kv head belongs to
+__device__ __forceinline__ int token_of(const AttnArgs& a, int R) { return (int)((uint64_t)(uint32_t)R * a.group_mul >> a.group_shift); }
+
 // A request's part of the step: its first row, its new tokens and its length, cut to what the buffers hold.
 struct Request {
   int start, fresh, len;
@@ -74,7 +78,7 @@ __device__ __forceinline__ Request request_of(const AttnArgs& a, int b) {
   Request r;
   r.start = min(max(a.cu[b], 0), a.T);
   r.fresh = (int)min(max((int64_t)a.cu[b + 1] - r.start, (int64_t)0), (int64_t)(a.T - r.start));
-  r.len = (int)min((int64_t)max(a.lengths[b], 0), min((int64_t)a.table_width << a.page_shift, (int64_t)0x7ffffe00));
+  r.len = (int)min((int64_t)max(a.lengths[b], 0), min((int64_t)a.table_width << a.page_shift, (int64_t)0x7ffffc00));
   return r;
 }
 // the tokens lo <= j < hi that new token i sees
@@ -89,17 +93,19 @@ __device__ __forceinline__ Sees sees(const AttnArgs& a, const Request& r, int i)
 
 // channels c0 .. c0 + N - 1 of a finished row: its sums over the sum of its numerators; zeros if it sees nothing
 template <int DT, int N>
-__device__ __forceinline__ void store_row(const AttnArgs& a, const Request& rq, int head, int64_t R, int c0, const float (&o)[N], float sum) {
-  const int i = (int)(R / a.group), g = (int)(R % a.group);
+__device__ __forceinline__ void store_row(const AttnArgs& a, const Request& rq, int head, int R, int c0, const float (&o)[N], float sum) {
+  const int i = token_of(a, R), g = R - i * a.group;
   const Sees s = sees(a, rq, i);
   const float inv = 1.0f / sum;
   uint32_t w[N / 2];
 #pragma unroll
   for (int c = 0; c < N / 2; ++c) w[c] = s.hi > s.lo ? round2<DT>(o[2 * c] * inv, o[2 * c + 1] * inv) : 0u;
   MDBF_GLOBAL uint16_t* to = (MDBF_GLOBAL uint16_t*)a.out + (int64_t)(rq.start + i) * a.ldo + (int64_t)(head * a.group + g) * a.head_dim + c0;
-  if (a.wide_o) {
+  if (a.wide_o && N == 2) {
+    *(MDBF_GLOBAL uint32_t*)to = w[0];
+  } else if (a.wide_o) {
 #pragma unroll
-    for (int c = 0; c < N / 4; ++c) ((MDBF_GLOBAL U32x2*)to)[c] = U32x2{w[2 * c], w[2 * c + 1]};
+    for (int c = 0; c < N / 4; ++c) ((MDBF_GLOBAL U32x2*)to)[c] = U32x2{w[2 * c], w[(2 * c + 1) % (N / 2)]};
   } else {
 #pragma unroll
     for (int c = 0; c < N / 2; ++c) {
@@ -109,110 +115,112 @@ __device__ __forceinline__ void store_row(const AttnArgs& a, const Request& rq, 
   }
 }
 
-constexpr int kTile = 32;        // tokens per step of a wave
+constexpr int kTile = 64;        // tokens per step of a wave
 constexpr int kWaves = 4;
 constexpr int kRows = 16;        // query rows of a workgroup
 constexpr float kSlack = 8;      // powers of two by which a score may exceed the running reference
 
-// The tokens that the rows of a tile of query rows see, and their part of each workgroup: `chunk` tokens from the first one's
-// tile on, the rest of them for the last workgroup.
+// The tokens that the rows of a tile of query rows see.
 struct Span {
   int lo, hi;              // what any row sees
   int all_lo, all_hi;      // what all rows see
-  int from;                // where the first part begins
-  int parts;
+  int from, units;         // the tiles of tokens from the first one's on; one where nothing is seen: the rows are written
 };
-__device__ __forceinline__ Span span_of(const AttnArgs& a, const Request& rq, int64_t tile, int64_t rows, int splits) {
-  const Sees s0 = sees(a, rq, (int)(tile * kRows / a.group)), s1 = sees(a, rq, (int)(min(tile * kRows + kRows - 1, rows - 1) / a.group));
+__device__ __forceinline__ Span span_of(const AttnArgs& a, const Request& rq, int tile, int rows) {
+  const Sees s0 = sees(a, rq, token_of(a, tile * kRows)), s1 = sees(a, rq, token_of(a, min(tile * kRows + kRows - 1, rows - 1)));
   Span s = {s0.lo, s1.hi, s1.lo, s0.hi, s0.lo & ~(kTile - 1), 1};
-  if (splits > 1 && s.hi > s.from) s.parts = (int)min((int64_t)splits, ((int64_t)s.hi - s.from + a.chunk - 1) / a.chunk);
+  if (s.hi > s.lo) s.units = (s.hi - s.from + kTile - 1) / kTile;
   return s;
 }
 
-// where the results of one part of a tile of rows go: kRows x D sums, then kRows maxima and kRows sums of numerators
+// Long caches: the units (tiles of 64 tokens) of all requests, row tiles and kv heads, one after the other, are cut into equal
+// shares, a workgroup's each, so that requests of any lengths keep the device evenly busy.  A workgroup finishes the row
+// tiles that lie whole in its share; of the first and the last one it may have a part only, whose sums it leaves in the
+// workspace (two places each), and where a row tile begins in a share and ends in a later one a note for the join.
+// (request, row tile, kv head, workgroups whose shares the row tile lies in, this one the first; 0: none begins here)
+typedef int32_t Note __attribute__((ext_vector_type(4)));
 template <int D>
-__device__ __forceinline__ int64_t part_floats() { return kRows * (D + 2); }
+constexpr int part_floats = kRows * (D + 2);      // kRows x D sums, then kRows maxima and kRows sums of numerators
+// the workgroups that the device holds at once
+template <int D>
+constexpr int share_count = 256 * (D == 64 ? 4 : D == 128 ? 3 : 2);
+constexpr int kLeastShare = 4;                    // units
+template <int D>
+constexpr size_t share_bytes() { return (size_t)share_count<D> * (sizeof(Note) + 2 * part_floats<D> * 4); }
 
 constexpr int kNonTemporal = 2;  // of the buffer loads: the cache is read once
 
-// One wave's tile of tokens: codes and scales of its keys and values as loaded.  It lies in one page (ONE), or its halves of 16
-// tokens lie in one each (pages of 16 tokens).
-template <int D, bool ONE>
+// Where a wave's tile of 64 tokens lies: NP pages' parts for the head (as buffers: a lane's place in the tile is the offset), and
+// whether those are pages of the pool.
+template <int NP>
+struct Place {
+  const uint8_t* base[NP];
+  __amdgpu_buffer_rsrc_t buf[NP];
+  int off[NP];               // of the first token in its page
+  bool there[NP];
+  __device__ __forceinline__ void set(const AttnArgs& a, int head, int head_bytes, int tok, const int (&page)[NP]) {
+#pragma unroll
+    for (int f = 0; f < NP; ++f) {
+      there[f] = (uint32_t)page[f] < (uint32_t)a.pages;
+      base[f] = a.cache + ((int64_t)(there[f] ? page[f] : 0) * a.kv_heads + head) * head_bytes;
+      buf[f] = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base[f]), 0, head_bytes, 0x00027000);
+      off[f] = (tok + kTile / NP * f) & ((1 << a.page_shift) - 1);
+    }
+  }
+};
+
+// Codes and scales of the tile's keys and values as loaded.  Nothing in the loads looks at what they bring: they are in flight
+// while the tile before is worked on.
+template <int D, int NP>
 struct Codes {
   static constexpr int KW = D / 32;                  // dwords of codes per lane and 16 keys = matrix steps over the channels
   static constexpr int KS = D <= 128 ? 1 : D / 128;  // scales among them
-  static constexpr int VU = D / 64;                  // 16-byte units of values per lane
-  static constexpr int VH = D == 64 ? 1 : VU / 2;    // of them in each half
-  uint32_t kc[2][KW], ks[2][KS];
-  U32x4 vc[VU];
-  uint32_t vs[VU];
-  // the half of a unit, and its place there: 16 tokens x D / 32 blocks
-  __device__ static __forceinline__ int half(int n, int lane) { return D == 64 ? lane >> 5 : n / VH; }
-  __device__ static __forceinline__ int unit(int n, int lane) { return D == 64 ? lane & 31 : (n % VH) * 64 + lane; }
+  static constexpr int VU = D / 64;                  // 16-byte units of values per lane and 32 tokens
+  uint32_t kc[4][KW], ks[4][KS];
+  U32x4 vc[2][VU];
+  uint32_t vs[2][VU];
 
-  bool there[2];             // whether the halves' pages are pages of the pool
-
-  // `page`: of the two halves' tokens, which begin at tok.  Nothing here looks at what the loads bring: they are in flight while
-  // the tile before is worked on.  (Buffer loads: a page's part for the head is the buffer, a lane's place in a tile the offset.)
-  __device__ __forceinline__ void load(const AttnArgs& a, int head, int64_t head_bytes, int tok, const int (&page)[2], int lane) {
-    const int P = 1 << a.page_shift, r = lane & 15, h = lane >> 4;
-    const uint8_t* base[2];
-    __amdgpu_buffer_rsrc_t buf[2];
-    int off[2];
+  __device__ __forceinline__ void load_keys(const Place<NP>& at, int page_shift, int lane) {
+    const int P = 1 << page_shift, r = lane & 15, h = lane >> 4;
 #pragma unroll
-    for (int f = 0; f < 2; ++f) {
-      if (ONE && f) {
-        there[1] = there[0], buf[1] = buf[0], off[1] = off[0] + 16;
-        continue;
-      }
-      there[f] = (uint32_t)page[f] < (uint32_t)a.pages;
-      base[f] = a.cache + ((int64_t)(there[f] ? page[f] : 0) * a.kv_heads + head) * head_bytes;
-      buf[f] = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base[f]), 0, (int)head_bytes, 0x00027000);
-      off[f] = (tok + 16 * f) & (P - 1);
-    }
-#pragma unroll
-    for (int f = 0; f < 2; ++f) {
-      const int at = r * (D / 2) + h * (D / 8);
+    for (int f = 0; f < 4; ++f) {
+      const int pg = f * NP / 4, off = at.off[pg] + 16 * (f - pg * (4 / NP));
       if (KW == 2) {
-        const U32x2 v = __builtin_amdgcn_raw_buffer_load_b64(buf[f], at, off[f] * (D / 2), kNonTemporal);
+        const U32x2 v = __builtin_amdgcn_raw_buffer_load_b64(at.buf[pg], r * (D / 2) + h * (D / 8), off * (D / 2), kNonTemporal);
         kc[f][0] = v[0], kc[f][1] = v[1];
       } else {
 #pragma unroll
         for (int s = 0; s < KW; s += 4) {
-          const U32x4 v = __builtin_amdgcn_raw_buffer_load_b128(buf[f], at + 4 * s, off[f] * (D / 2), kNonTemporal);
+          const U32x4 v = __builtin_amdgcn_raw_buffer_load_b128(at.buf[pg], r * (D / 2) + h * (D / 8) + 4 * s, off * (D / 2), kNonTemporal);
 #pragma unroll
           for (int w = 0; w < 4; ++w) kc[f][(s + w) % KW] = v[w];
         }
       }
 #pragma unroll
       for (int s = 0; s < KS; ++s)
-        ks[f][s] = __builtin_amdgcn_raw_buffer_load_b8(buf[f], r * (D / 32) + (D == 64 ? h >> 1 : h * KS + s), P * D + off[f] * (D / 32), 0);
-    }
-#pragma unroll
-    for (int n = 0; n < VU; ++n) {
-      if (!ONE && D == 64) {      // the halves of one load in different pages
-        const MDBF_GLOBAL uint8_t* at = (const MDBF_GLOBAL uint8_t*)(lane < 32 ? base[0] : base[1]);
-        const uint32_t o = lane < 32 ? off[0] : off[1], u = lane & 31;
-        vc[n] = __builtin_nontemporal_load((const MDBF_GLOBAL U32x4*)(at + (P + o) * (D / 2) + u * 16));
-        vs[n] = at[P * (D + D / 32) + o * (D / 32) + u];
-      } else {
-        const int f = ONE ? 0 : n / VH, u = (ONE ? n : n % VH) * 64 + lane;
-        vc[n] = __builtin_amdgcn_raw_buffer_load_b128(buf[f], u * 16, (P + off[f]) * (D / 2), kNonTemporal);
-        vs[n] = __builtin_amdgcn_raw_buffer_load_b8(buf[f], u, P * (D + D / 32) + off[f] * (D / 32), 0);
-      }
+        ks[f][s] = __builtin_amdgcn_raw_buffer_load_b8(at.buf[pg], r * (D / 32) + (D == 64 ? h >> 1 : h * KS + s), P * D + off * (D / 32), 0);
     }
   }
-  // a page that is none reads as NaN
-  __device__ __forceinline__ void check(int lane) {
-    if (there[0] && there[1]) return;
+  // a lane's units: 32 tokens x D / 32 blocks, one after the other
+  __device__ __forceinline__ void load_values(const Place<NP>& at, int page_shift, int lane) {
+    const int P = 1 << page_shift;
 #pragma unroll
-    for (int f = 0; f < 2; ++f)
+    for (int g = 0; g < 2; ++g)
 #pragma unroll
-      for (int s = 0; s < KS; ++s)
-        if (!there[f]) ks[f][s] = kKvNanScale;
-#pragma unroll
-    for (int n = 0; n < VU; ++n)
-      if (!(half(n, lane) ? there[1] : there[0])) vs[n] = kKvNanScale;
+      for (int n = 0; n < VU; ++n) {
+        if (NP == 4 && D == 64) {      // a load's halves lie in different pages
+          const MDBF_GLOBAL uint8_t* from = (const MDBF_GLOBAL uint8_t*)(lane < 32 ? at.base[2 * g % NP] : at.base[(2 * g + 1) % NP]);
+          const uint32_t o = lane < 32 ? at.off[2 * g % NP] : at.off[(2 * g + 1) % NP], u = lane & 31;
+          vc[g][n] = __builtin_nontemporal_load((const MDBF_GLOBAL U32x4*)(from + (P + o) * (D / 2) + u * 16));
+          vs[g][n] = from[P * (D + D / 32) + o * (D / 32) + u];
+        } else {
+          const int f = NP == 4 ? 2 * g + n / (VU / 2 ? VU / 2 : 1) : 2 * g;      // 16 tokens that the unit's page begins with
+          const int pg = f * NP / 4, first = at.off[pg] + 16 * (f - pg * (4 / NP));
+          const int u = (NP == 4 ? n % (VU / 2 ? VU / 2 : 1) : n) * 64 + lane;
+          vc[g][n] = __builtin_amdgcn_raw_buffer_load_b128(at.buf[pg], u * 16, (P + first) * (D / 2), kNonTemporal);
+          vs[g][n] = __builtin_amdgcn_raw_buffer_load_b8(at.buf[pg], u, P * (D + D / 32) + first * (D / 32), 0);
+        }
+      }
   }
 };
 
@@ -226,45 +234,146 @@ __device__ __forceinline__ float row_max(float x) {
   return fmaxf(__builtin_bit_cast(float, b0), __builtin_bit_cast(float, b1));
 }
 
-// One kv head, 16 query rows, one part of their tokens; the part's tiles are dealt out to the four waves, which meet at
-// the end.  A tile's loads are issued before the products of the one before it, and its page numbers a tile earlier still.
-template <int D, int DT, bool ONE>
+// units of a request over its row tiles and kv heads
+__device__ __forceinline__ int64_t request_units(const AttnArgs& a, int b) {
+  const Request rq = request_of(a, b);
+  const int rows = rq.fresh * a.group;
+  int64_t n = 0;
+  for (int rt = 0; rt * kRows < rows; ++rt) n += span_of(a, rq, rt, rows).units;
+  return n * a.kv_heads;
+}
+
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+  return ((int64_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
+}
+
+// sum over the workgroup's four waves up to and with this thread's x; `total` of all
+__device__ __forceinline__ int64_t scan_256(int64_t x, int64_t& total, int64_t* waves) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int64_t u = __shfl_up(x, o);
+    if (lane >= o) x += u;
+  }
+  __syncthreads();
+  if (lane == 63) waves[wave] = x;
+  __syncthreads();
+  total = 0;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    if (w < wave) x += waves[w];
+    total += waves[w];
+  }
+  return x;
+}
+
+// 16 query rows of one kv head at a time, the tiles of their tokens dealt out to the four waves, which meet at the end.  The
+// registers that a tile's keys were in take the next tile's as soon as the scores are there, those of its values once they
+// are in LDS; page numbers are looked up a tile earlier still.  NP: pages per tile of 64 tokens (1, 2 or 4).
+template <int D, int DT, int NP>
 __global__ __launch_bounds__(64 * kWaves, D == 64 ? 4 : D == 128 ? 3 : 2) void attn_few_kernel(AttnArgs a) {
-  using Tile = Codes<D, ONE>;
+  using Tile = Codes<D, NP>;
   constexpr int KW = Tile::KW, KS = Tile::KS, VU = Tile::VU;
+  constexpr int kGroup = 32;                  // tokens whose values are in LDS at a time
   // A token's values in LDS: 64 bytes per block, 16 more after each (D = 64) or every second one, rows an odd multiple of 32
   // bytes apart: neither the writes nor the transposing reads meet on a bank.
   constexpr int VROW = D == 64 ? 160 : D == 128 ? 288 : 608;
   auto block_at = [](int g) { return g * 64 + (D == 64 ? g : g >> 1) * 16; };
   constexpr int CT = D / 16;                  // channel tiles
   constexpr int OROW = D + 4;                 // floats of a row of results in LDS
-  static_assert(kTile * VROW >= kRows * OROW * 4, "the results fit the values' place");
-  __shared__ __attribute__((aligned(16))) unsigned char lds[kWaves][kTile * VROW];
+  static_assert(kGroup * VROW >= kRows * OROW * 4, "the results fit the values' place");
+  __shared__ __attribute__((aligned(16))) unsigned char lds[kWaves][kGroup * VROW];
   __shared__ float stat[kWaves][2][kRows];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, h = lane >> 4;
-  uint32_t idx = blockIdx.x;
-  const int part = idx % a.splits;
-  idx /= a.splits;
-  const int rt0 = idx % a.row_tiles;
-  idx /= a.row_tiles;
-  const int head = idx % a.kv_heads, b = idx / a.kv_heads;
-  const Request rq = request_of(a, b);
-  const int64_t rows = (int64_t)rq.fresh * a.group;
-  const int64_t head_bytes = kv_head_bytes(1 << a.page_shift, D);
-  const MDBF_CONST int32_t* table = (const MDBF_CONST int32_t*)a.table + b * a.table_ld;
+  const int head_bytes = (int)kv_head_bytes(1 << a.page_shift, D);
   unsigned char* vals = lds[wave];
 
-  // (tiles of rows beyond those that the launch was sized for are not split)
-  for (int64_t rt = rt0; rt * kRows < rows; rt += a.row_tiles) {
-    const Span sp = span_of(a, rq, rt, rows, rt == rt0 ? a.splits : 1);
-    if (part >= sp.parts) continue;
-    const int64_t R = rt * kRows + r;
+  // where this workgroup begins: a request, a tile of its rows and a kv head, and units of their tokens [u0, u1)
+  int b, head, u0 = 0, u1, rt;
+  int64_t left = 0, share = 0;
+  Request rq;
+  Span sp;
+  if (!a.shares) {
+    // a workgroup per row tile that the launch was sized for, with all of its tokens
+    uint32_t idx = blockIdx.x;
+    rt = idx % a.row_tiles;
+    idx /= a.row_tiles;
+    head = idx % a.kv_heads, b = idx / a.kv_heads;
+    rq = request_of(a, b);
+    const int rows = rq.fresh * a.group;
+    if (rt * kRows >= rows) return;
+    sp = span_of(a, rq, rt, rows);
+    u1 = sp.units;
+  } else {
+    // prefix sums over the requests: of up to 64 by every wave for itself, else by the workgroup, 256 at a time, first of all
+    // and then again up to the one where the share begins
+    int64_t* waves = reinterpret_cast<int64_t*>(lds[0]);
+    __shared__ int found_b;
+    __shared__ int64_t found_at;
+    const int tid = threadIdx.x;
+    const bool few = a.requests <= 64;
+    int64_t total = 0, sum, mine = 0, end = 0;
+    if (few) {
+      mine = end = lane < a.requests ? request_units(a, lane) : 0;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int64_t u = __shfl_up(end, o);
+        if (lane >= o) end += u;
+      }
+      total = __shfl(end, 63);
+    } else {
+      for (int r0 = 0; r0 < a.requests; r0 += 256) {
+        scan_256(r0 + tid < a.requests ? request_units(a, r0 + tid) : 0, sum, waves);
+        total += sum;
+      }
+    }
+    total = uniform(total);      // (what the loops below go by must be known to be the same in all lanes)
+    share = max((total + a.shares - 1) / a.shares, (int64_t)kLeastShare);
+    const int64_t start = blockIdx.x * share;
+    MDBF_GLOBAL Note* note = (MDBF_GLOBAL Note*)a.part + blockIdx.x;
+    if (tid == 0) *note = Note{0, 0, 0, 0};
+    if (start >= total) return;
+    left = min(share, total - start);
+    int64_t rest;
+    if (few) {
+      b = __builtin_ctzll(__ballot(start >= end - mine && start < end));
+      rest = start - __shfl(end - mine, b);
+    } else {
+      int64_t before = 0;
+      for (int r0 = 0; r0 < a.requests; r0 += 256) {
+        mine = r0 + tid < a.requests ? request_units(a, r0 + tid) : 0;
+        end = before + scan_256(mine, sum, waves);
+        if (start >= end - mine && start < end) found_b = r0 + tid, found_at = end - mine;
+        before += sum;
+        if (start < before) break;
+      }
+      __syncthreads();
+      b = found_b;
+      rest = start - found_at;
+      __syncthreads();
+    }
+    b = __builtin_amdgcn_readfirstlane(b);
+    rest = uniform(rest);
+    rq = request_of(a, b);
+    const int rows = rq.fresh * a.group;
+    for (rt = 0;; ++rt) {
+      sp = span_of(a, rq, rt, rows);
+      if (rest < (int64_t)sp.units * a.kv_heads) break;
+      rest -= (int64_t)sp.units * a.kv_heads;
+    }
+    head = (int)(rest / sp.units), u0 = (int)(rest % sp.units);
+    u1 = (int)min((int64_t)sp.units, u0 + left);
+  }
+
+  for (;;) {
+    const int rows = rq.fresh * a.group;
+    const MDBF_CONST int32_t* table = (const MDBF_CONST int32_t*)a.table + b * a.table_ld;
+    const int R = rt * kRows + r;
     const bool valid = R < rows;
-    const int i = valid ? (int)(R / a.group) : 0, g = valid ? (int)(R % a.group) : 0;
+    const int i = valid ? token_of(a, R) : 0, g = valid ? R - i * a.group : 0;
     Sees me = sees(a, rq, i);
     if (!valid) me.hi = me.lo = 0;
-    const int64_t first = sp.from + (int64_t)part * a.chunk;
-    const int tmin = max(sp.lo, (int)first), tmax = part == sp.parts - 1 ? sp.hi : (int)(first + a.chunk);
+    const int tmin = u0 ? sp.from + u0 * kTile : sp.lo, tmax = u1 < sp.units ? sp.from + u1 * kTile : sp.hi;
 
     U32x4 qf[KW];
     const int64_t q_at = (int64_t)(rq.start + i) * a.ldq + (int64_t)(head * a.group + g) * D + h * (D / 4);
@@ -289,107 +398,127 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 4 : D == 128 ? 3 : 2) void a
 #pragma unroll
     for (int c = 0; c < CT; ++c) acc[c] = F32x4{0, 0, 0, 0};
 
-    // page numbers of a tile's halves; behind the last token's none is looked up
-    auto pages_of = [&](int t, int (&page)[2]) __attribute__((always_inline)) {
+    // page numbers of a tile; behind the last token's none is looked up
+    auto pages_of = [&](int t, int (&page)[NP]) __attribute__((always_inline)) {
 #pragma unroll
-      for (int f = 0; f < (ONE ? 1 : 2); ++f) page[f] = table[min(t + 16 * f, rq.len - 1) >> a.page_shift];
-    };
-    auto work = [&](Tile& x, int t0) __attribute__((always_inline)) {
-      x.check(lane);
-      // scores (without their factor): a lane holds those of its row with tokens 4 h + 0 .. 3 of each half
-      F32x4 z[2];
-#pragma unroll
-      for (int f = 0; f < 2; ++f) {
-        z[f] = F32x4{0, 0, 0, 0};
-#pragma unroll
-        for (int s = 0; s < KW; ++s) z[f] = mma16<DT>(numbers<DT>(x.kc[f][s], unit_of(x.ks[f][KS == 1 ? 0 : s / 4])), qf[s], z[f]);
-      }
-      const bool inside = t0 >= sp.all_lo && t0 + kTile <= sp.all_hi;     // every row sees every token
-      if (!inside) {
-#pragma unroll
-        for (int f = 0; f < 2; ++f)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int tok = t0 + 16 * f + 4 * h + j;
-            if (tok < me.lo || tok >= me.hi) z[f][j] = -INFINITY;
-          }
-      }
-      // The reference m follows the maximum only where that has grown by more than kSlack (numerators stay below 2^kSlack, in
-      // reach of fp16): most tiles exchange nothing between lanes and rescale nothing.
-      const float top = fmaxf(fmaxf(fmaxf(z[0][0], z[0][1]), fmaxf(z[0][2], z[0][3])), fmaxf(fmaxf(z[1][0], z[1][1]), fmaxf(z[1][2], z[1][3]))) * a.scale;
-      if (__any(top > m + kSlack)) {
-        const float mn = fmaxf(m, row_max(top)), alpha = __builtin_amdgcn_exp2f(m - (mn == -INFINITY ? 0.0f : mn));
-        m = mn;
-        l *= alpha;
-#pragma unroll
-        for (int c = 0; c < CT; ++c) acc[c] *= alpha;
-      }
-      const float use = m == -INFINITY ? 0.0f : m;
-      F32x4 p[2];
-#pragma unroll
-      for (int f = 0; f < 2; ++f)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) p[f][j] = __builtin_amdgcn_exp2f(z[f][j] * a.scale - use);
-      l += ((p[0][0] + p[0][1]) + (p[0][2] + p[0][3])) + ((p[1][0] + p[1][1]) + (p[1][2] + p[1][3]));
-      const U32x4 pf = {round2<DT>(p[0][0], p[0][1]), round2<DT>(p[0][2], p[0][3]), round2<DT>(p[1][0], p[1][1]), round2<DT>(p[1][2], p[1][3])};
-
-      // values that no row sees are zeros; NaN among the others goes to the rows that see it, not through the product, where a
-      // zero weight would bring it to all rows
-#pragma unroll
-      for (int n = 0; n < VU; ++n) {
-        const int unit = Tile::unit(n, lane), row = 16 * Tile::half(n, lane) + unit / (D / 32), tok = t0 + row;
-        if (!inside && (tok < sp.lo || tok >= sp.hi)) {
-          x.vc[n] = U32x4{0, 0, 0, 0};
-          x.vs[n] = 127;
-        }
-        uint64_t bad = __ballot(x.vs[n] == kKvNanScale);
-        if (bad) {
-          if (x.vs[n] == kKvNanScale) {
-            x.vc[n] = U32x4{0, 0, 0, 0};
-            x.vs[n] = 127;
-          }
-          for (; bad; bad &= bad - 1) {
-            const int from = __builtin_ctzll(bad), bu = Tile::unit(n, from);
-            const int bt = t0 + 16 * Tile::half(n, from) + bu / (D / 32), bg = bu % (D / 32);
-            if (bt >= me.lo && bt < me.hi) nan_blocks |= 1u << bg;
-          }
-        }
-        const float unit_f = unit_of(x.vs[n]);
-        unsigned char* to = vals + row * VROW + block_at(unit % (D / 32));
-#pragma unroll
-        for (int w = 0; w < 4; ++w) *reinterpret_cast<U32x4*>(to + w * 16) = numbers<DT>(x.vc[n][w], unit_f);
-      }
-      wave_lds_order();
-      // a lane's channel of tokens 4 h + 0 .. 3 of each half: the order of the scores' registers
-#pragma unroll
-      for (int c = 0; c < CT; ++c) {
-        const unsigned char* from = vals + (4 * h + (r >> 2)) * VROW + block_at(c / 2) + (c & 1) * 32 + (r & 3) * 8;
-        const U32x2 v0 = __builtin_bit_cast(U32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((MDBF_LDS S16x4*)from));
-        const U32x2 v1 = __builtin_bit_cast(U32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((MDBF_LDS S16x4*)(from + 16 * VROW)));
-        acc[c] = mma16<DT>(U32x4{v0[0], v0[1], v1[0], v1[1]}, pf, acc[c]);
-      }
-      wave_lds_order();
+      for (int f = 0; f < NP; ++f) page[f] = table[min(t + kTile / NP * f, rq.len - 1) >> a.page_shift];
     };
 
     constexpr int kStep = kWaves * kTile;
     int t0 = (tmin & ~(kTile - 1)) + wave * kTile;
     if (t0 < tmax) {
-      Tile x, y;
-      int page[2];
+      Tile x;
+      Place<NP> at, next;
+      int page[NP];
       pages_of(t0, page);
-      x.load(a, head, head_bytes, t0, page, lane);
+      at.set(a, head, head_bytes, t0, page);
+      x.load_keys(at, a.page_shift, lane);
+      x.load_values(at, a.page_shift, lane);
       pages_of(t0 + kStep, page);
       for (;;) {
-        if (t0 + kStep < tmax) y.load(a, head, head_bytes, t0 + kStep, page, lane);
+        const bool more = t0 + kStep < tmax;
+        next.set(a, head, head_bytes, t0 + kStep, page);
         pages_of(t0 + 2 * kStep, page);
-        work(x, t0);
+
+        // scores (without their factor): a lane holds those of its row with tokens 4 h + 0 .. 3 of each 16
+        F32x4 z[4];
+#pragma unroll
+        for (int f = 0; f < 4; ++f) {
+          if (!at.there[f * NP / 4]) {      // a page that is none reads as NaN
+#pragma unroll
+            for (int s = 0; s < KS; ++s) x.ks[f][s] = kKvNanScale;
+          }
+          z[f] = F32x4{0, 0, 0, 0};
+#pragma unroll
+          for (int s = 0; s < KW; ++s) z[f] = mma16<DT>(numbers<DT>(x.kc[f][s], unit_of(x.ks[f][KS == 1 ? 0 : s / 4])), qf[s], z[f]);
+        }
+        if (more) x.load_keys(next, a.page_shift, lane);
+        const bool inside = t0 >= sp.all_lo && t0 + kTile <= sp.all_hi;     // every row sees every token
+        if (!inside) {
+#pragma unroll
+          for (int f = 0; f < 4; ++f)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const int tok = t0 + 16 * f + 4 * h + j;
+              if (tok < me.lo || tok >= me.hi) z[f][j] = -INFINITY;
+            }
+        }
+        // The reference m follows the maximum only where that has grown by more than kSlack (numerators stay below 2^kSlack, in
+        // reach of fp16): most tiles exchange nothing between lanes and rescale nothing.
+        float top = z[0][0];
+#pragma unroll
+        for (int f = 0; f < 4; ++f)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) top = fmaxf(top, z[f][j]);
+        top *= a.scale;
+        if (__any(top > m + kSlack)) {
+          const float mn = fmaxf(m, row_max(top)), alpha = __builtin_amdgcn_exp2f(m - (mn == -INFINITY ? 0.0f : mn));
+          m = mn;
+          l *= alpha;
+#pragma unroll
+          for (int c = 0; c < CT; ++c) acc[c] *= alpha;
+        }
+        const float use = m == -INFINITY ? 0.0f : m;
+        U32x4 pf[2];
+#pragma unroll
+        for (int f = 0; f < 4; ++f) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) z[f][j] = __builtin_amdgcn_exp2f(z[f][j] * a.scale - use);
+          l += (z[f][0] + z[f][1]) + (z[f][2] + z[f][3]);
+          pf[f / 2][f % 2 * 2] = round2<DT>(z[f][0], z[f][1]);
+          pf[f / 2][f % 2 * 2 + 1] = round2<DT>(z[f][2], z[f][3]);
+        }
+
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          // values that no row sees are zeros; NaN among the others goes to the rows that see it, not through the product, where
+          // a zero weight would bring it to all rows
+#pragma unroll
+          for (int n = 0; n < VU; ++n) {
+            const int unit = n * 64 + lane, row = unit / (D / 32), tok = t0 + kGroup * g + row;
+            if (NP > 1 || !at.there[0]) {
+              const int f = 2 * g + row / 16;
+              bool there = at.there[0];
+#pragma unroll
+              for (int k = 1; k < NP; ++k)
+                if (f * NP / 4 == k) there = at.there[k];
+              if (!there) x.vs[g][n] = kKvNanScale;
+            }
+            if (!inside && (tok < sp.lo || tok >= sp.hi)) {
+              x.vc[g][n] = U32x4{0, 0, 0, 0};
+              x.vs[g][n] = 127;
+            }
+            uint64_t bad = __ballot(x.vs[g][n] == kKvNanScale);
+            if (bad) {
+              if (x.vs[g][n] == kKvNanScale) {
+                x.vc[g][n] = U32x4{0, 0, 0, 0};
+                x.vs[g][n] = 127;
+              }
+              for (; bad; bad &= bad - 1) {
+                const int bu = n * 64 + __builtin_ctzll(bad), bt = t0 + kGroup * g + bu / (D / 32);
+                if (bt >= me.lo && bt < me.hi) nan_blocks |= 1u << bu % (D / 32);
+              }
+            }
+            const float unit_f = unit_of(x.vs[g][n]);
+            unsigned char* to = vals + row * VROW + block_at(unit % (D / 32));
+#pragma unroll
+            for (int w = 0; w < 4; ++w) *reinterpret_cast<U32x4*>(to + w * 16) = numbers<DT>(x.vc[g][n][w], unit_f);
+          }
+          if (g == 1 && more) x.load_values(next, a.page_shift, lane);
+          wave_lds_order();
+          // a lane's channel of tokens 4 h + 0 .. 3 of each 16: the order of the scores' registers
+#pragma unroll
+          for (int c = 0; c < CT; ++c) {
+            const unsigned char* from = vals + (4 * h + (r >> 2)) * VROW + block_at(c / 2) + (c & 1) * 32 + (r & 3) * 8;
+            const U32x2 v0 = __builtin_bit_cast(U32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((MDBF_LDS S16x4*)from));
+            const U32x2 v1 = __builtin_bit_cast(U32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((MDBF_LDS S16x4*)(from + 16 * VROW)));
+            acc[c] = mma16<DT>(U32x4{v0[0], v0[1], v1[0], v1[1]}, pf[g], acc[c]);
+          }
+          wave_lds_order();
+        }
+        if (!more) break;
+        at = next;
         t0 += kStep;
-        if (t0 >= tmax) break;
-        if (t0 + kStep < tmax) x.load(a, head, head_bytes, t0 + kStep, page, lane);
-        pages_of(t0 + 2 * kStep, page);
-        work(y, t0);
-        t0 += kStep;
-        if (t0 >= tmax) break;
       }
     }
 
@@ -410,7 +539,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 4 : D == 128 ? 3 : 2) void a
     {
       constexpr int N = D / 16;      // channels per thread
       const int row = threadIdx.x >> 4, piece = threadIdx.x & 15;
-      const int64_t Ro = rt * kRows + row;
+      const int Ro = rt * kRows + row;
       if (Ro < rows) {
         float top = stat[0][0][row];
 #pragma unroll
@@ -427,8 +556,8 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 4 : D == 128 ? 3 : 2) void a
 #pragma unroll
           for (int c = 0; c < N; ++c) o[c] += f * from[c];
         }
-        if (sp.parts > 1) {
-          MDBF_GLOBAL float* to = (MDBF_GLOBAL float*)a.part + (int64_t)blockIdx.x * part_floats<D>();
+        if (u1 - u0 < sp.units) {
+          MDBF_GLOBAL float* to = (MDBF_GLOBAL float*)((MDBF_GLOBAL Note*)a.part + a.shares) + (int64_t)(2 * blockIdx.x + (u0 == 0)) * part_floats<D>;
           if (piece == 0) {
             to[kRows * D + row] = top;
             to[kRows * (D + 1) + row] = sum;
@@ -441,86 +570,92 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 4 : D == 128 ? 3 : 2) void a
         }
       }
     }
+    if (u0 == 0 && u1 < sp.units && threadIdx.x == 0) {
+      ((MDBF_GLOBAL Note*)a.part)[blockIdx.x] = Note{b, rt, head, 1 + (int)((sp.units - u1 + share - 1) / share)};
+    }
+    // on to what is next
+    if (!a.shares) {
+      rt += a.row_tiles;
+      if (rt * kRows >= rows) break;
+      sp = span_of(a, rq, rt, rows);
+      u1 = sp.units;
+    } else {
+      left -= u1 - u0;
+      if (left <= 0) break;
+      if (++head == a.kv_heads) {
+        head = 0;
+        ++rt;
+        int n = rows;
+        while (rt * kRows >= n) {        // (units are left: there is a request with rows)
+          rq = request_of(a, ++b);
+          n = rq.fresh * a.group;
+          rt = 0;
+        }
+        sp = span_of(a, rq, rt, n);
+      }
+      u0 = 0;
+      u1 = (int)min((int64_t)sp.units, left);
+    }
     __syncthreads();
   }
 }
 
-// Joins the parts of a query row: a workgroup per row that the launch was sized for and CH of its channels, CH / 4 lanes side by
-// side on them; the groups of lanes take the parts in turn and meet in LDS, in one order.  A chain of two trips to memory at
-// most: the first parts' sums are requested before the weights are known.
-constexpr int kMostSplits = 1024;
-template <int D, int DT, int CH>
+// Joins the parts of the row tiles that several shares have: a wave per row and share where one begins.  D / 4 lanes side by side
+// on the channels take a part at a time, the others the next ones; the order is fixed.
+template <int D, int DT>
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
-  constexpr int L = CH / 4, GROUPS = 256 / L, AHEAD = 8;
-  uint32_t idx = blockIdx.x;
-  const int c0 = idx % (D / CH) * CH;
-  idx /= D / CH;
-  const int row0 = idx % a.join_rows;
-  idx /= a.join_rows;
-  const uint32_t tile = idx;               // of the launch before
-  const int rt = idx % a.row_tiles;
-  idx /= a.row_tiles;
-  const int head = idx % a.kv_heads, b = idx / a.kv_heads;
-  const Request rq = request_of(a, b);
-  const int64_t rows = (int64_t)rq.fresh * a.group;
-  if ((int64_t)rt * kRows + row0 >= rows) return;
-  const Span sp = span_of(a, rq, rt, rows, a.splits);
-  if (sp.parts <= 1) return;
-  const MDBF_GLOBAL float* from = (const MDBF_GLOBAL float*)a.part + (int64_t)tile * a.splits * part_floats<D>();
-  __shared__ float weight[kMostSplits], stat[4], total[4];
-  __shared__ F32x4 sums[GROUPS][L];
-  const int tid = threadIdx.x, l = tid % L, grp = tid / L;
-
-  for (int row = row0; row < kRows && (int64_t)rt * kRows + row < rows; row += a.join_rows) {
-    const MDBF_GLOBAL float* mine = from + row * D + c0 + l * 4;
-    F32x4 ahead[AHEAD];
+  constexpr int L = D / 4, GROUPS = 64 / L, AHEAD = 8;
+  const int lane = threadIdx.x & 63, l = lane % L, grp = lane / L;
+  const uint32_t idx = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int row0 = idx % a.join_rows, wg = idx / a.join_rows;
+  if (wg >= a.shares) return;
+  const Note note = ((const MDBF_GLOBAL Note*)a.part)[wg];
+  const int rt = note[1], head = note[2], count = note[3];
+  if (count < 2) return;
+  const Request rq = request_of(a, note[0]);
+  const int rows = rq.fresh * a.group;
+  const MDBF_GLOBAL float* parts = (const MDBF_GLOBAL float*)((const MDBF_GLOBAL Note*)a.part + a.shares);
+  // the first part lies in its workgroup's second place, the others in the first ones
+  auto part = [&](int p) { return parts + (int64_t)(2 * (wg + p) + (p == 0)) * part_floats<D>; };
+  for (int row = row0; row < kRows && rt * kRows + row < rows; row += a.join_rows) {
+    float top = -INFINITY;
+    for (int p = lane; p < count; p += 64) top = fmaxf(top, part(p)[kRows * D + row]);
 #pragma unroll
-    for (int k = 0; k < AHEAD; ++k)
-      if (grp + k * GROUPS < sp.parts) ahead[k] = *(const MDBF_GLOBAL F32x4*)(mine + (grp + k * GROUPS) * part_floats<D>());
-    float top = -INFINITY, tops[kMostSplits / 256], parts_sum[kMostSplits / 256];
-#pragma unroll
-    for (int k = 0; k < kMostSplits / 256; ++k) {
-      const int p = tid + k * 256;
-      tops[k] = -INFINITY, parts_sum[k] = 0;
-      if (p < sp.parts) {
-        tops[k] = from[p * part_floats<D>() + kRows * D + row];
-        parts_sum[k] = from[p * part_floats<D>() + kRows * (D + 1) + row];
-        top = fmaxf(top, tops[k]);
-      }
-    }
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
-    if ((tid & 63) == 0) stat[tid >> 6] = top;
-    __syncthreads();
-    top = fmaxf(fmaxf(stat[0], stat[1]), fmaxf(stat[2], stat[3]));
+    for (int w = 1; w < 64; w <<= 1) top = fmaxf(top, __shfl_xor(top, w));
     const float use = top == -INFINITY ? 0.0f : top;
-    float sum = 0;
-#pragma unroll
-    for (int k = 0; k < kMostSplits / 256; ++k)
-      if (tid + k * 256 < sp.parts) {
-        const float f = __builtin_amdgcn_exp2f(tops[k] - use);
-        weight[tid + k * 256] = f;
-        sum += f * parts_sum[k];
-      }
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
-    if ((tid & 63) == 0) total[tid >> 6] = sum;
-    __syncthreads();
-    sum = (total[0] + total[1]) + (total[2] + total[3]);
     F32x4 o = {0, 0, 0, 0};
+    float sum = 0;
+    for (int p0 = 0; p0 < count; p0 += 64) {
+      const int some = min(64, count - p0);
+      float f = 0;
+      if (lane < some) {
+        const MDBF_GLOBAL float* q = part(p0 + lane);
+        f = __builtin_amdgcn_exp2f(q[kRows * D + row] - use);
+        sum += f * q[kRows * (D + 1) + row];
+      }
+      for (int p = 0; p < some; p += GROUPS * AHEAD) {
+        F32x4 v[AHEAD];
 #pragma unroll
-    for (int k = 0; k < AHEAD; ++k)
-      if (grp + k * GROUPS < sp.parts) o += weight[grp + k * GROUPS] * ahead[k];
-    for (int p = grp + AHEAD * GROUPS; p < sp.parts; p += GROUPS) o += weight[p] * *(const MDBF_GLOBAL F32x4*)(mine + p * part_floats<D>());
-    sums[grp][l] = o;
-    __syncthreads();
-    if (grp == 0) {
+        for (int k = 0; k < AHEAD; ++k) {
+          const int at = p + k * GROUPS + grp;
+          if (at < some) v[k] = *(const MDBF_GLOBAL F32x4*)(part(p0 + at) + row * D + l * 4);
+        }
 #pragma unroll
-      for (int w = 1; w < GROUPS; ++w) o += sums[w][l];
-      const float v[4] = {o[0], o[1], o[2], o[3]};
-      store_row<DT, 4>(a, rq, head, (int64_t)rt * kRows + row, c0 + l * 4, v, sum);
+        for (int k = 0; k < AHEAD; ++k) {
+          const int at = p + k * GROUPS + grp;
+          const float w = __shfl(f, at & 63);
+          if (at < some) o += w * v[k];
+        }
+      }
     }
-    __syncthreads();
+#pragma unroll
+    for (int w = 1; w < 64; w <<= 1) sum += __shfl_xor(sum, w);
+#pragma unroll
+    for (int w = L; w < 64; w <<= 1)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) o[c] += __shfl_xor(o[c], w);
+    const float v[4] = {o[0], o[1], o[2], o[3]};
+    if (grp == 0) store_row<DT, 4>(a, rq, head, rt * kRows + row, l * 4, v, sum);
   }
 }
 
@@ -535,45 +670,42 @@ static int check_attn(const mdbf_kv_t* kv, const mdbf_attn_t* at, int requests, 
   return MDBF_OK;
 }
 
-// How a call is cut up: tiles of query rows per request and kv head, and parts of the tokens of each.
+// Whether a call is cut into shares, else a workgroup takes a row tile with all of its tokens: where no cache is longer than
+// kWhole tokens the second launch, the join, would cost more than the cut saves.
+#ifndef WH
+#define WH 1024
+#endif
+constexpr int kWhole = WH;
 struct AttnGeom {
-  int64_t tiles;           // over all requests and kv heads
-  int row_tiles, splits, chunk;
-  size_t part_bytes;
+  int row_tiles;           // of a request and kv head
+  bool shares;
 };
-// A part is one workgroup's: enough of them to fill the device several times over, so that requests of unequal length even
-// out, but none shorter than kLeastChunk tokens, two steps of its waves.
-constexpr int kLeastChunk = 256, kPartsWanted = 2048;
-static AttnGeom attn_geom(const mdbf_kv_t& kv, const mdbf_attn_t& at, int requests, int T) {
-  AttnGeom g;
+static AttnGeom attn_geom(const mdbf_kv_t& kv, const mdbf_attn_t& at, int T) {
   const int64_t group = at.q_heads / kv.kv_heads, most = std::min(at.max_fresh, T);
-  g.row_tiles = (int)std::min<int64_t>((most * group + kRows - 1) / kRows, 1 << 16);
-  g.tiles = (int64_t)requests * kv.kv_heads * g.row_tiles;
   int64_t span = at.max_length;
-  if (at.window) span = std::min<int64_t>(span, (int64_t)at.window + kRows + kTile);
-  const int64_t splits = std::max<int64_t>(1, std::min<int64_t>({kPartsWanted / g.tiles, span / kLeastChunk, kMostSplits}));
-  const int64_t step = kWaves * kTile;
-  g.chunk = (int)(((span + splits - 1) / splits + step - 1) / step * step);
-  g.splits = (int)((span + g.chunk - 1) / g.chunk);
-  g.part_bytes = g.splits > 1 ? (size_t)g.tiles * g.splits * kRows * (kv.head_dim + 2) * 4 : 0;
-  return g;
+  if (at.window) span = std::min<int64_t>(span, (int64_t)at.window + kRows);
+  return {(int)std::min<int64_t>((most * group + kRows - 1) / kRows, 1 << 16), span > kWhole};
+}
+static size_t attn_workspace(const mdbf_kv_t& kv, const AttnGeom& g) {
+  return !g.shares ? 0 : kv.head_dim == 64 ? share_bytes<64>() : kv.head_dim == 128 ? share_bytes<128>() : share_bytes<256>();
 }
 
 template <int D, int DT>
-static int launch_few(const AttnArgs& a, const AttnGeom& g, hipStream_t s) {
-  if (a.page_shift == 4) attn_few_kernel<D, DT, false><<<(unsigned)(g.tiles * g.splits), 64 * kWaves, 0, s>>>(a);
-  else attn_few_kernel<D, DT, true><<<(unsigned)(g.tiles * g.splits), 64 * kWaves, 0, s>>>(a);
+static int launch_few(AttnArgs& a, const AttnGeom& g, hipStream_t s) {
+  a.shares = g.shares ? share_count<D> : 0;
+  const unsigned grid = g.shares ? (unsigned)a.shares : (unsigned)((int64_t)a.requests * a.kv_heads * g.row_tiles);
+  if (a.page_shift == 4) attn_few_kernel<D, DT, 4><<<grid, 64 * kWaves, 0, s>>>(a);
+  else if (a.page_shift == 5) attn_few_kernel<D, DT, 2><<<grid, 64 * kWaves, 0, s>>>(a);
+  else attn_few_kernel<D, DT, 1><<<grid, 64 * kWaves, 0, s>>>(a);
   int e = (int)hipGetLastError();
-  if (e == 0 && g.splits > 1) {
-    // few parts: all channels in one workgroup
-    if (g.splits > 16) attn_join_kernel<D, DT, 32><<<(unsigned)(g.tiles * a.join_rows * (D / 32)), 256, 0, s>>>(a);
-    else attn_join_kernel<D, DT, D><<<(unsigned)(g.tiles * a.join_rows), 256, 0, s>>>(a);
+  if (e == 0 && g.shares) {
+    attn_join_kernel<D, DT><<<(unsigned)((a.shares * a.join_rows + 3) / 4), 256, 0, s>>>(a);
     e = (int)hipGetLastError();
   }
   return e;
 }
 template <int DT>
-static int launch_attn(int d, const AttnArgs& a, const AttnGeom& g, hipStream_t s) {
+static int launch_attn(int d, AttnArgs& a, const AttnGeom& g, hipStream_t s) {
   return d == 64 ? launch_few<64, DT>(a, g, s) : d == 128 ? launch_few<128, DT>(a, g, s) : launch_few<256, DT>(a, g, s);
 }
 
@@ -587,7 +719,7 @@ int mdbf_kv_attention_workspace_bytes(const mdbf_kv_t* kv, const mdbf_attn_t* at
   if (!bytes_out) return MDBF_EINVAL;
   int st = check_attn(kv, attn, requests, T);
   if (st) return st;
-  *bytes_out = attn_geom(*kv, *attn, requests, T).part_bytes;
+  *bytes_out = attn_workspace(*kv, attn_geom(*kv, *attn, T));
   return MDBF_OK;
 }
 
@@ -606,18 +738,23 @@ int mdbf_kv_attention(const mdbf_kv_t* kv, const mdbf_attn_t* attn, const void* 
     if (!kv_aligned(p, 16)) return MDBF_EALIGN;
   for (const void* p : ints)
     if (!kv_aligned(p, 4)) return MDBF_EALIGN;
-  const AttnGeom geom = attn_geom(*kv, *attn, requests, T);
-  if (geom.part_bytes && !workspace_dev) return MDBF_EINVAL;
-  if (workspace_bytes < geom.part_bytes) return MDBF_EWORKSPACE;
-  if (geom.tiles * std::max(geom.splits, kRows * 8) > 0x7fffffff) return MDBF_EUNSUPPORTED;
+  const AttnGeom geom = attn_geom(*kv, *attn, T);
+  const size_t need = attn_workspace(*kv, geom);
+  if (need && !workspace_dev) return MDBF_EINVAL;
+  if (workspace_bytes < need) return MDBF_EWORKSPACE;
+  const int group = attn->q_heads / kv->kv_heads;
+  if ((int64_t)requests * kv->kv_heads * geom.row_tiles > 0x7fffffff || (int64_t)T * group > 0x7fff0000) return MDBF_EUNSUPPORTED;
   AttnArgs a = {};
   a.cache = (const uint8_t*)cache_dev, a.table = table_dev, a.cu = cu_dev, a.lengths = lengths_dev, a.q = q_dev, a.out = out_dev;
-  a.table_ld = table_ld, a.ldq = ldq, a.ldo = ldo, a.table_width = table_width, a.T = T, a.pages = kv->pages;
-  a.kv_heads = kv->kv_heads, a.group = attn->q_heads / kv->kv_heads, a.head_dim = kv->head_dim;
+  a.table_ld = table_ld, a.ldq = ldq, a.ldo = ldo, a.table_width = table_width, a.requests = requests, a.T = T, a.pages = kv->pages;
+  a.kv_heads = kv->kv_heads, a.group = group, a.head_dim = kv->head_dim;
   a.page_shift = kv_page_shift(kv->page_size), a.causal = attn->flags & MDBF_ATTN_CAUSAL, a.window = attn->window;
-  a.row_tiles = geom.row_tiles, a.splits = geom.splits, a.chunk = geom.chunk, a.part = (float*)workspace_dev;
+  a.row_tiles = geom.row_tiles, a.part = (float*)workspace_dev;
   a.join_rows = (int)std::min<int64_t>((int64_t)std::min(attn->max_fresh, T) * a.group, kRows);
   a.scale = (float)(fabs((double)attn->scale) * 1.4426950408889634), a.flip = attn->scale < 0 ? 0x80008000u : 0u;
+  int bits = 0;
+  while ((1 << bits) < group) ++bits;
+  a.group_shift = 31 + bits, a.group_mul = (uint32_t)(((1ull << a.group_shift) + group - 1) / group);
   a.wide_q = ldq % 8 == 0, a.wide_o = ldo % 4 == 0;
   return hip_fail(kv->dtype == MDBF_F16 ? launch_attn<MDBF_F16>(kv->head_dim, a, geom, (hipStream_t)stream)
                                         : launch_attn<MDBF_BF16>(kv->head_dim, a, geom, (hipStream_t)stream));
