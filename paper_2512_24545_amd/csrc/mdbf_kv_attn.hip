@@ -120,11 +120,15 @@ constexpr int kWaves = 4;
 constexpr int kRows = 16;        // query rows of a workgroup
 constexpr float kSlack = 8;      // powers of two by which a score may exceed the running reference
 
+// What beginning and ending a tile of query rows costs, in tiles of tokens (see the shares below).  64 requests of up to 8192 tokens,
+// 8 kv heads of 128: 79 us with 0, 62.4 with 3, 59.2 with 6, 58.6 with 10, 60.5 with 16.
+constexpr int kRowsCost = 8;
 // The tokens that the rows of a tile of query rows see.
 struct Span {
   int lo, hi;              // what any row sees
   int all_lo, all_hi;      // what all rows see
   int from, units;         // the tiles of tokens from the first one's on; one where nothing is seen: the rows are written
+  __device__ __forceinline__ int cost() const { return units + kRowsCost; }
 };
 __device__ __forceinline__ Span span_of(const AttnArgs& a, const Request& rq, int tile, int rows) {
   const Sees s0 = sees(a, rq, token_of(a, tile * kRows)), s1 = sees(a, rq, token_of(a, min(tile * kRows + kRows - 1, rows - 1)));
@@ -133,8 +137,9 @@ __device__ __forceinline__ Span span_of(const AttnArgs& a, const Request& rq, in
   return s;
 }
 
-// Long caches: the units (tiles of 64 tokens) of all requests, row tiles and kv heads, one after the other, are cut into equal
-// shares, a workgroup's each, so that requests of any lengths keep the device evenly busy.  A workgroup finishes the row
+// Long caches: the units (tiles of 64 tokens, and kRowsCost more in front of them for each tile of rows) of all requests, row
+// tiles and kv heads, one after the other, are cut into equal shares, a workgroup's each, so that requests of any lengths keep
+// the device evenly busy.  A workgroup finishes the row
 // tiles that lie whole in its share; of the first and the last one it may have a part only, whose sums it leaves in the
 // workspace (two places each), and where a row tile begins in a share and ends in a later one a note for the join.
 // (request, row tile, kv head, workgroups whose shares the row tile lies in, this one the first; 0: none begins here)
@@ -239,7 +244,7 @@ __device__ __forceinline__ int64_t request_units(const AttnArgs& a, int b) {
   const Request rq = request_of(a, b);
   const int rows = rq.fresh * a.group;
   int64_t n = 0;
-  for (int rt = 0; rt * kRows < rows; ++rt) n += span_of(a, rq, rt, rows).units;
+  for (int rt = 0; rt * kRows < rows; ++rt) n += span_of(a, rq, rt, rows).cost();
   return n * a.kv_heads;
 }
 
@@ -293,6 +298,12 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 4 : D == 128 ? 3 : 2) void a
   int64_t left = 0, share = 0;
   Request rq;
   Span sp;
+  // units of the row tile that lie in the share, which goes on with this place of its cost
+  auto cut = [&](int place) __attribute__((always_inline)) {
+    const int most = (int)min((int64_t)(sp.cost() - place), left);
+    u0 = max(place - kRowsCost, 0), u1 = place + most - kRowsCost;
+    left -= most;
+  };
   if (!a.shares) {
     // a workgroup per row tile that the launch was sized for, with all of its tokens
     uint32_t idx = blockIdx.x;
@@ -358,14 +369,14 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 4 : D == 128 ? 3 : 2) void a
     const int rows = rq.fresh * a.group;
     for (rt = 0;; ++rt) {
       sp = span_of(a, rq, rt, rows);
-      if (rest < (int64_t)sp.units * a.kv_heads) break;
-      rest -= (int64_t)sp.units * a.kv_heads;
+      if (rest < (int64_t)sp.cost() * a.kv_heads) break;
+      rest -= (int64_t)sp.cost() * a.kv_heads;
     }
-    head = (int)(rest / sp.units), u0 = (int)(rest % sp.units);
-    u1 = (int)min((int64_t)sp.units, u0 + left);
+    head = (int)(rest / sp.cost());
+    cut((int)(rest % sp.cost()));
   }
 
-  for (;;) {
+  while (u1 > 0) {      // (a share may end in a row tile's cost, before its first unit)
     const int rows = rq.fresh * a.group;
     const MDBF_CONST int32_t* table = (const MDBF_CONST int32_t*)a.table + b * a.table_ld;
     const int R = rt * kRows + r;
@@ -580,7 +591,6 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 4 : D == 128 ? 3 : 2) void a
       sp = span_of(a, rq, rt, rows);
       u1 = sp.units;
     } else {
-      left -= u1 - u0;
       if (left <= 0) break;
       if (++head == a.kv_heads) {
         head = 0;
@@ -593,20 +603,21 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 4 : D == 128 ? 3 : 2) void a
         }
         sp = span_of(a, rq, rt, n);
       }
-      u0 = 0;
-      u1 = (int)min((int64_t)sp.units, left);
+      cut(0);
     }
     __syncthreads();
   }
 }
 
-// Joins the parts of the row tiles that several shares have: a wave per row and share where one begins.  D / 4 lanes side by side
-// on the channels take a part at a time, the others the next ones; the order is fixed.
-template <int D, int DT>
+// Joins the parts of the row tiles that several shares have: W waves per row and share where one begins.  D / 4 lanes side by
+// side on the channels take a part at a time, other lanes and waves the next ones; the order is fixed.
+template <int D, int DT, int W>
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
   constexpr int L = D / 4, GROUPS = 64 / L, AHEAD = 8;
-  const int lane = threadIdx.x & 63, l = lane % L, grp = lane / L;
-  const uint32_t idx = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  __shared__ F32x4 sums[W][L];
+  const int lane = threadIdx.x & 63, l = lane % L, grp = lane / L, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int mine = W == 1 ? 0 : wave;
+  const uint32_t idx = W == 1 ? blockIdx.x * 4 + wave : blockIdx.x;
   const int row0 = idx % a.join_rows, wg = idx / a.join_rows;
   if (wg >= a.shares) return;
   const Note note = ((const MDBF_GLOBAL Note*)a.part)[wg];
@@ -633,16 +644,16 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
         f = __builtin_amdgcn_exp2f(q[kRows * D + row] - use);
         sum += f * q[kRows * (D + 1) + row];
       }
-      for (int p = 0; p < some; p += GROUPS * AHEAD) {
+      for (int p = mine * GROUPS; p < some; p += GROUPS * W * AHEAD) {
         F32x4 v[AHEAD];
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) {
-          const int at = p + k * GROUPS + grp;
+          const int at = p + k * GROUPS * W + grp;
           if (at < some) v[k] = *(const MDBF_GLOBAL F32x4*)(part(p0 + at) + row * D + l * 4);
         }
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) {
-          const int at = p + k * GROUPS + grp;
+          const int at = p + k * GROUPS * W + grp;
           const float w = __shfl(f, at & 63);
           if (at < some) o += w * v[k];
         }
@@ -654,8 +665,16 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
     for (int w = L; w < 64; w <<= 1)
 #pragma unroll
       for (int c = 0; c < 4; ++c) o[c] += __shfl_xor(o[c], w);
+    if (W > 1) {
+      if (grp == 0) sums[mine][l] = o;
+      __syncthreads();
+      if (mine == 0)
+#pragma unroll
+        for (int w = 1; w < W; ++w) o += sums[w][l];
+    }
     const float v[4] = {o[0], o[1], o[2], o[3]};
-    if (grp == 0) store_row<DT, 4>(a, rq, head, rt * kRows + row, l * 4, v, sum);
+    if (grp == 0 && mine == 0) store_row<DT, 4>(a, rq, head, rt * kRows + row, l * 4, v, sum);
+    if (W > 1) __syncthreads();
   }
 }
 
@@ -672,10 +691,7 @@ static int check_attn(const mdbf_kv_t* kv, const mdbf_attn_t* at, int requests, 
 
 // Whether a call is cut into shares, else a workgroup takes a row tile with all of its tokens: where no cache is longer than
 // kWhole tokens the second launch, the join, would cost more than the cut saves.
-#ifndef WH
-#define WH 1024
-#endif
-constexpr int kWhole = WH;
+constexpr int kWhole = 1024;
 struct AttnGeom {
   int row_tiles;           // of a request and kv head
   bool shares;
@@ -699,7 +715,9 @@ static int launch_few(AttnArgs& a, const AttnGeom& g, hipStream_t s) {
   else attn_few_kernel<D, DT, 1><<<grid, 64 * kWaves, 0, s>>>(a);
   int e = (int)hipGetLastError();
   if (e == 0 && g.shares) {
-    attn_join_kernel<D, DT><<<(unsigned)((a.shares * a.join_rows + 3) / 4), 256, 0, s>>>(a);
+    // (few row tiles: each lies in many shares)
+    if (a.shares / ((int64_t)a.requests * a.kv_heads * g.row_tiles) >= 16) attn_join_kernel<D, DT, 4><<<(unsigned)(a.shares * a.join_rows), 256, 0, s>>>(a);
+    else attn_join_kernel<D, DT, 1><<<(unsigned)((a.shares * a.join_rows + 3) / 4), 256, 0, s>>>(a);
     e = (int)hipGetLastError();
   }
   return e;
