@@ -86,9 +86,9 @@ struct Sees {
   int lo, hi;
 };
 __device__ __forceinline__ Sees sees(const AttnArgs& a, const Request& r, int i) {
-  const int pos = r.len - r.fresh + i;
   if (!a.causal) return {0, r.len};
-  return {a.window ? max(pos - a.window + 1, 0) : 0, max(pos + 1, 0)};
+  const int end = max(r.len - r.fresh + i + 1, 0);
+  return {a.window ? max(end - a.window, 0) : 0, end};
 }
 
 // channels c0 .. c0 + N - 1 of a finished row: its sums over the sum of its numerators; zeros if it sees nothing
@@ -130,8 +130,9 @@ struct Span {
   int from, units;         // the tiles of tokens from the first one's on; one where nothing is seen: the rows are written
   __device__ __forceinline__ int cost() const { return units + kRowsCost; }
 };
+template <int ROWS = kRows>
 __device__ __forceinline__ Span span_of(const AttnArgs& a, const Request& rq, int tile, int rows) {
-  const Sees s0 = sees(a, rq, token_of(a, tile * kRows)), s1 = sees(a, rq, token_of(a, min(tile * kRows + kRows - 1, rows - 1)));
+  const Sees s0 = sees(a, rq, token_of(a, tile * ROWS)), s1 = sees(a, rq, token_of(a, min(tile * ROWS + ROWS - 1, rows - 1)));
   Span s = {s0.lo, s1.hi, s1.lo, s0.hi, s0.lo & ~(kTile - 1), 1};
   if (s.hi > s.lo) s.units = (s.hi - s.from + kTile - 1) / kTile;
   return s;
@@ -678,6 +679,261 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
   }
 }
 
+// ---- prompts ---------------------------------------------------------------------------------------------
+// 128 query rows of one kv head per workgroup, 32 per wave, which all read the tile of 64 tokens that the workgroup has in
+// LDS: key codes as they are (each wave makes numbers of them as it feeds its products), values as numbers.  Two buffers:
+// while one is worked on, the next tile's codes, which came in while the one before was, are written into the other.
+constexpr int kManyWaves = 4, kManyRows = 32 * kManyWaves;
+typedef float F32x16 __attribute__((ext_vector_type(16)));
+
+template <int DT>
+__device__ __forceinline__ F32x16 mma32(U32x4 a, U32x4 b, F32x16 c) {
+  if (DT == MDBF_F16) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(F16x8, a), __builtin_bit_cast(F16x8, b), c, 0, 0, 0);
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(Bf16x8, a), __builtin_bit_cast(Bf16x8, b), c, 0, 0, 0);
+}
+// max over the two lanes that hold a query row
+__device__ __forceinline__ float pair_max(float x) {
+  const auto a = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+  const uint32_t a0 = a[0], a1 = a[1];
+  return fmaxf(__builtin_bit_cast(float, a0), __builtin_bit_cast(float, a1));
+}
+
+template <int D, int DT>
+__global__ __launch_bounds__(64 * kManyWaves, D <= 128 ? 2 : 1) void attn_many_kernel(AttnArgs a) {
+  constexpr int BL = D / 32;                       // blocks of a token
+  constexpr int UNITS = kTile * BL;                // 16-byte units of a tile's keys, and of its values
+  constexpr int U = UNITS < 256 ? 1 : UNITS / 256; // of each per thread; with D = 64 half of the threads take keys, half values
+  constexpr int KROW = D / 2 + 16;                 // bytes of a token's key codes in LDS: reads of 16 bytes a lane meet on no bank
+  constexpr int VROW = D == 64 ? 160 : D == 128 ? 288 : 608;      // of its values, as in attn_few_kernel
+  auto block_at = [](int g) { return g * 64 + (D == 64 ? g : g >> 1) * 16; };
+  constexpr int ST = D / 64;                       // pairs of blocks
+  constexpr int CT = D / 32;                       // channel tiles
+  struct Buffer {
+    unsigned char keys[kTile * KROW];
+    unsigned char values[kTile * VROW];
+    unsigned char key_scales[kTile * BL], value_scales[kTile * BL];
+  };
+  __shared__ __attribute__((aligned(16))) Buffer lds[2];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 31, hh = lane >> 5;
+  const int P = 1 << a.page_shift, head_bytes = (int)kv_head_bytes(P, D);
+
+  // kv heads next to each other (their row tiles then share an XCD's cache), the row tiles that see most first
+  uint32_t idx = blockIdx.x;
+  const int head = idx % a.kv_heads;
+  idx /= a.kv_heads;
+  const int b = idx % a.requests, rt0 = a.row_tiles - 1 - idx / a.requests;
+  const Request rq = request_of(a, b);
+  const int rows = rq.fresh * a.group;
+  const MDBF_GLOBAL int32_t* table = (const MDBF_GLOBAL int32_t*)a.table + b * a.table_ld;
+  const MDBF_GLOBAL uint8_t* cache = (const MDBF_GLOBAL uint8_t*)a.cache + (int64_t)head * head_bytes;
+
+  for (int rt = rt0; rt * kManyRows < rows; rt += a.row_tiles) {
+    const Span sp = span_of<kManyRows>(a, rq, rt, rows);
+    const int R = rt * kManyRows + wave * 32 + r;
+    const bool valid = R < rows;
+    const int i = valid ? token_of(a, R) : 0, g = valid ? R - i * a.group : 0;
+    Sees me = sees(a, rq, i);
+    if (!valid) me.hi = me.lo = 0;
+
+    // queries: channels 64 s + 32 hh + 8 w + 0 .. 7 of the lane's row for step (s, w)
+    U32x4 qf[ST][4];
+    const int64_t q_at = (int64_t)(rq.start + i) * a.ldq + (int64_t)(head * a.group + g) * D + 32 * hh;
+#pragma unroll
+    for (int s = 0; s < ST; ++s)
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        qf[s][w] = U32x4{0, 0, 0, 0};
+        if (valid) {
+          const MDBF_GLOBAL uint16_t* p = (const MDBF_GLOBAL uint16_t*)a.q + q_at + 64 * s + 8 * w;
+          if (a.wide_q) {
+            qf[s][w] = *(const MDBF_GLOBAL U32x4*)p;
+          } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) qf[s][w][j] = (uint32_t)p[2 * j] | ((uint32_t)p[2 * j + 1] << 16);
+          }
+          qf[s][w] ^= a.flip;
+        }
+      }
+
+    // a thread's units of a tile: its page is looked up a tile before its codes are requested
+    U32x4 kc[U], vc[U];
+    uint32_t ks[U], vs[U];
+    int page[U];
+    bool there[U];
+    auto unit_of_thread = [&](int n) { return D == 64 ? tid & 127 : n * 256 + tid; };
+    auto look_up = [&](int t) __attribute__((always_inline)) {
+#pragma unroll
+      for (int n = 0; n < U; ++n) page[n] = table[max(min(t + unit_of_thread(n) / BL, rq.len - 1), 0) >> a.page_shift];
+    };
+    auto request = [&](int t) __attribute__((always_inline)) {
+#pragma unroll
+      for (int n = 0; n < U; ++n) {
+        const int u = unit_of_thread(n), off = (t + u / BL) & (P - 1), bl = u % BL;
+        there[n] = (uint32_t)page[n] < (uint32_t)a.pages;
+        const MDBF_GLOBAL uint8_t* from = cache + (int64_t)(there[n] ? page[n] : 0) * a.kv_heads * head_bytes;
+        if (D != 64 || tid < 128) {
+          kc[n] = *(const MDBF_GLOBAL U32x4*)(from + off * (D / 2) + bl * 16);
+          ks[n] = from[P * D + off * BL + bl];
+        }
+        if (D != 64 || tid >= 128) {
+          vc[n] = *(const MDBF_GLOBAL U32x4*)(from + (P + off) * (D / 2) + bl * 16);
+          vs[n] = from[P * (D + BL) + off * BL + bl];
+        }
+      }
+    };
+    // tokens that no row sees: their values are zeros; NaN among the others stays in value_scales
+    auto put = [&](Buffer& to, int t) __attribute__((always_inline)) {
+#pragma unroll
+      for (int n = 0; n < U; ++n) {
+        const int u = unit_of_thread(n), row = u / BL, bl = u % BL, tok = t + row;
+        if (D != 64 || tid < 128) {
+          *reinterpret_cast<U32x4*>(to.keys + row * KROW + bl * 16) = kc[n];
+          to.key_scales[u] = there[n] ? ks[n] : kKvNanScale;
+        }
+        if (D != 64 || tid >= 128) {
+          uint32_t sc = there[n] ? vs[n] : kKvNanScale;
+          if (tok < sp.lo || tok >= sp.hi) sc = 0;
+          to.value_scales[u] = sc;
+          if (sc == 0 || sc == kKvNanScale) vc[n] = U32x4{0, 0, 0, 0}, sc = 127;
+#pragma unroll
+          for (int w = 0; w < 4; ++w) *reinterpret_cast<U32x4*>(to.values + row * VROW + block_at(bl) + w * 16) = numbers<DT>(vc[n][w], unit_of(sc));
+        }
+      }
+    };
+
+    float m = -INFINITY, l = 0;
+    uint32_t nan_blocks = 0;
+    F32x16 acc[CT];
+#pragma unroll
+    for (int c = 0; c < CT; ++c)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) acc[c][j] = 0;
+
+    const int tiles = sp.hi > sp.lo ? sp.units : 0;
+    if (tiles) {
+      look_up(sp.from);
+      request(sp.from);
+      look_up(sp.from + kTile);
+      put(lds[0], sp.from);
+      if (tiles > 1) {
+        request(sp.from + kTile);
+        look_up(sp.from + 2 * kTile);
+      }
+      __syncthreads();
+    }
+    for (int n = 0; n < tiles; ++n) {
+      const int t0 = sp.from + n * kTile;
+      if (n + 1 < tiles) put(lds[(n + 1) & 1], t0 + kTile);
+      if (n + 2 < tiles) {
+        request(t0 + 2 * kTile);
+        look_up(t0 + 3 * kTile);
+      }
+      const Buffer& in = lds[n & 1];
+
+      // scores: a lane holds those of its row with tokens 32 f + 8 (j / 4) + 4 hh + j % 4
+      F32x16 z[2];
+#pragma unroll
+      for (int f = 0; f < 2; ++f) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) z[f][j] = 0;
+#pragma unroll
+        for (int s = 0; s < ST; ++s) {
+          const int row = 32 * f + r;
+          const U32x4 codes = *reinterpret_cast<const U32x4*>(in.keys + row * KROW + (2 * s + hh) * 16);
+          const float unit = unit_of(in.key_scales[row * BL + 2 * s + hh]);
+#pragma unroll
+          for (int w = 0; w < 4; ++w) z[f] = mma32<DT>(numbers<DT>(codes[w], unit), qf[s][w], z[f]);
+        }
+      }
+      if (t0 < sp.all_lo || t0 + kTile > sp.all_hi) {      // not every row sees every token
+#pragma unroll
+        for (int f = 0; f < 2; ++f)
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            const int tok = t0 + 32 * f + 8 * (j / 4) + 4 * hh + j % 4;
+            if (tok < me.lo || tok >= me.hi) z[f][j] = -INFINITY;
+          }
+      }
+      float top = z[0][0];
+#pragma unroll
+      for (int f = 0; f < 2; ++f)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) top = fmaxf(top, z[f][j]);
+      top *= a.scale;
+      if (__any(top > m + kSlack)) {      // as in attn_few_kernel
+        const float mn = fmaxf(m, pair_max(top)), alpha = __builtin_amdgcn_exp2f(m - (mn == -INFINITY ? 0.0f : mn));
+        m = mn;
+        l *= alpha;
+#pragma unroll
+        for (int c = 0; c < CT; ++c) acc[c] *= alpha;
+      }
+      const float use = m == -INFINITY ? 0.0f : m;
+      U32x4 pf[4];
+#pragma unroll
+      for (int f = 0; f < 2; ++f)
+#pragma unroll
+        for (int j = 0; j < 16; j += 4) {
+          float p[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) p[k] = __builtin_amdgcn_exp2f(z[f][j + k] * a.scale - use);
+          l += (p[0] + p[1]) + (p[2] + p[3]);
+          pf[2 * f + j / 8][j / 4 % 2 * 2] = round2<DT>(p[0], p[1]);
+          pf[2 * f + j / 8][j / 4 % 2 * 2 + 1] = round2<DT>(p[2], p[3]);
+        }
+
+      // NaN among the values: to the rows that see it
+      {
+        bool bad = false;
+#pragma unroll
+        for (int w = 0; w < UNITS / 256; ++w) {
+          const uint32_t x = *reinterpret_cast<const uint32_t*>(in.value_scales + w * 256 + lane * 4);
+          bad |= (x & 0xffu) == 0xffu || (x & 0xff00u) == 0xff00u || (x & 0xff0000u) == 0xff0000u || x >= 0xff000000u;
+        }
+        if (UNITS < 256) {
+          const uint32_t x = reinterpret_cast<const uint16_t*>(in.value_scales)[lane];
+          bad |= (x & 0xffu) == 0xffu || x >= 0xff00u;
+        }
+        if (__any(bad)) {
+          for (int u = 0; u < UNITS; ++u)
+            if (in.value_scales[u] == kKvNanScale) {
+              const int tok = t0 + u / BL;
+              if (tok >= me.lo && tok < me.hi) nan_blocks |= 1u << u % BL;
+            }
+        }
+      }
+
+      // results: 16 tokens at a time, in the order of the scores' registers; all channels' values of the 16 are read before the
+      // first product
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        U32x2 v[CT][2];
+        const unsigned char* from = in.values + (16 * k + 4 * hh + ((lane & 15) >> 2)) * VROW + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+#pragma unroll
+        for (int c = 0; c < CT; ++c) {
+          v[c][0] = __builtin_bit_cast(U32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((MDBF_LDS S16x4*)(from + block_at(c))));
+          v[c][1] = __builtin_bit_cast(U32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((MDBF_LDS S16x4*)(from + block_at(c) + 8 * VROW)));
+        }
+#pragma unroll
+        for (int c = 0; c < CT; ++c) acc[c] = mma32<DT>(U32x4{v[c][0][0], v[c][0][1], v[c][1][0], v[c][1][1]}, pf[k], acc[c]);
+      }
+      __syncthreads();
+    }
+
+    l += __shfl_xor(l, 32);
+    if (valid) {
+#pragma unroll
+      for (int c = 0; c < CT; ++c) {
+        const bool nan = nan_blocks >> c & 1;
+#pragma unroll
+        for (int j = 0; j < 16; j += 4) {
+          const float v[4] = {acc[c][j], acc[c][j + 1], acc[c][j + 2], acc[c][j + 3]};
+          store_row<DT, 4>(a, rq, head, R, 32 * c + 2 * j + 4 * hh, v, nan ? NAN : l);
+        }
+      }
+    }
+  }
+}
+
 static int check_attn(const mdbf_kv_t* kv, const mdbf_attn_t* at, int requests, int T) {
   int st = check_kv(kv);
   if (st) return st;
@@ -694,13 +950,18 @@ static int check_attn(const mdbf_kv_t* kv, const mdbf_attn_t* at, int requests, 
 constexpr int kWhole = 1024;
 struct AttnGeom {
   int row_tiles;           // of a request and kv head
-  bool shares;
+  bool shares, many;       // many: attn_many_kernel
 };
+#ifndef MR
+#define MR 33
+#endif
+constexpr int kManyFrom = MR;
 static AttnGeom attn_geom(const mdbf_kv_t& kv, const mdbf_attn_t& at, int T) {
   const int64_t group = at.q_heads / kv.kv_heads, most = std::min(at.max_fresh, T);
+  if (most * group >= kManyFrom) return {(int)std::min<int64_t>((most * group + kManyRows - 1) / kManyRows, 1 << 16), false, true};
   int64_t span = at.max_length;
   if (at.window) span = std::min<int64_t>(span, (int64_t)at.window + kRows);
-  return {(int)std::min<int64_t>((most * group + kRows - 1) / kRows, 1 << 16), span > kWhole};
+  return {(int)std::min<int64_t>((most * group + kRows - 1) / kRows, 1 << 16), span > kWhole, false};
 }
 static size_t attn_workspace(const mdbf_kv_t& kv, const AttnGeom& g) {
   return !g.shares ? 0 : kv.head_dim == 64 ? share_bytes<64>() : kv.head_dim == 128 ? share_bytes<128>() : share_bytes<256>();
@@ -710,7 +971,8 @@ template <int D, int DT>
 static int launch_few(AttnArgs& a, const AttnGeom& g, hipStream_t s) {
   a.shares = g.shares ? share_count<D> : 0;
   const unsigned grid = g.shares ? (unsigned)a.shares : (unsigned)((int64_t)a.requests * a.kv_heads * g.row_tiles);
-  if (a.page_shift == 4) attn_few_kernel<D, DT, 4><<<grid, 64 * kWaves, 0, s>>>(a);
+  if (g.many) attn_many_kernel<D, DT><<<grid, 64 * kManyWaves, 0, s>>>(a);
+  else if (a.page_shift == 4) attn_few_kernel<D, DT, 4><<<grid, 64 * kWaves, 0, s>>>(a);
   else if (a.page_shift == 5) attn_few_kernel<D, DT, 2><<<grid, 64 * kWaves, 0, s>>>(a);
   else attn_few_kernel<D, DT, 1><<<grid, 64 * kWaves, 0, s>>>(a);
   int e = (int)hipGetLastError();
