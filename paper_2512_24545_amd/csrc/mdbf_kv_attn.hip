@@ -11,7 +11,9 @@
 #include <math.h>
 
 #include <algorithm>
+#include <utility>
 
+#include "mdbf_fp6.h"
 #include "mdbf_kv.h"
 
 namespace mdbf {
@@ -691,6 +693,47 @@ __device__ __forceinline__ F32x16 mma32(U32x4 a, U32x4 b, F32x16 c) {
   if (DT == MDBF_F16) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(F16x8, a), __builtin_bit_cast(F16x8, b), c, 0, 0, 0);
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(Bf16x8, a), __builtin_bit_cast(Bf16x8, b), c, 0, 0, 0);
 }
+// Key codes (fp4, 32 per lane, with their block's scale byte at SA of `scales`) times limb L of the queries, summed into c.
+typedef int V8i __attribute__((ext_vector_type(8)));
+template <int SA, int L>
+__device__ __forceinline__ F32x16 mx32(U32x4 codes, uint32_t scales, v6u limb, uint32_t limb_scales, F32x16 c) {
+  const V8i x = {(int)codes[0], (int)codes[1], (int)codes[2], (int)codes[3], 0, 0, 0, 0};
+  const V8i y = {(int)limb[0], (int)limb[1], (int)limb[2], (int)limb[3], (int)limb[4], (int)limb[5], 0, 0};
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, c, 4, 2, SA, (int)scales, L, (int)limb_scales);
+}
+// f(0), f(1), ... with indices that are constants
+template <class F, int... I>
+__device__ __forceinline__ void each_of(F&& f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+
+// 32 channels of a query as a sum of NL fp6 numbers, each limb's scale 2^-4 of the one before: an absolute error of 2^-(4 NL + 2)
+// of the largest of the 32 at most.  Three limbs for bf16 and four for fp16: a value down to a 64th of the largest is exact.
+template <int NL>
+struct Limbs {
+  v6u limb[NL];
+  uint32_t scales = 0;      // a byte each
+  // whether all values are finite; where not, the limbs mean nothing
+  __device__ __forceinline__ bool set(float (&q)[32]) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int j = 0; j < 32; ++j) top = max(top, __builtin_bit_cast(uint32_t, q[j]) & 0x7fffffffu);
+    const int e = min(max((int)(top >> 23) - 2 + ((top & 0x7fffffu) > 0x700000u), 16), 254);      // at most 7.5 units
+#pragma unroll
+    for (int k = 0; k < NL; ++k) {
+      const float unit = __builtin_bit_cast(float, (uint32_t)(e - 4 * k) << 23);
+      scales |= (uint32_t)(e - 4 * k) << (8 * k);
+      limb[k] = fp6_encode32(q, unit);
+      if (k + 1 < NL) {
+        const v32f back = fp6_decode32(limb[k], unit);
+#pragma unroll
+        for (int j = 0; j < 32; ++j) q[j] -= back[j];
+      }
+    }
+    return (top >> 23) != 255;
+  }
+};
+
 // max over the two lanes that hold a query row
 __device__ __forceinline__ float pair_max(float x) {
   const auto a = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
@@ -704,9 +747,12 @@ __global__ __launch_bounds__(64 * kManyWaves, D <= 128 ? 2 : 1) void attn_many_k
   constexpr int UNITS = kTile * BL;                // 16-byte units of a tile's keys, and of its values
   constexpr int U = UNITS < 256 ? 1 : UNITS / 256; // of each per thread; with D = 64 half of the threads take keys, half values
   constexpr int KROW = D / 2 + 16;                 // bytes of a token's key codes in LDS: reads of 16 bytes a lane meet on no bank
-  constexpr int VROW = D == 64 ? 160 : D == 128 ? 288 : 608;      // of its values, as in attn_few_kernel
-  auto block_at = [](int g) { return g * 64 + (D == 64 ? g : g >> 1) * 16; };
+  // of its values: blocks 80 bytes apart and rows 64 more than a multiple of 256, so that neither the writes nor the transposing
+  // reads (which take two times 16 channels of four rows at once) meet on a bank
+  constexpr int VROW = D == 256 ? 832 : 320;
+  auto block_at = [](int g) { return g * 80; };
   constexpr int ST = D / 64;                       // pairs of blocks
+  constexpr int NL = DT == MDBF_F16 ? 4 : 3;       // limbs of the queries
   constexpr int CT = D / 32;                       // channel tiles
   struct Buffer {
     unsigned char keys[kTile * KROW];
@@ -735,25 +781,29 @@ __global__ __launch_bounds__(64 * kManyWaves, D <= 128 ? 2 : 1) void attn_many_k
     Sees me = sees(a, rq, i);
     if (!valid) me.hi = me.lo = 0;
 
-    // queries: channels 64 s + 32 hh + 8 w + 0 .. 7 of the lane's row for step (s, w)
-    U32x4 qf[ST][4];
+    // queries: channels 64 s + 32 hh + 0 .. 31 of the lane's row for step s
+    Limbs<NL> ql[ST];
+    bool finite = true;
     const int64_t q_at = (int64_t)(rq.start + i) * a.ldq + (int64_t)(head * a.group + g) * D + 32 * hh;
 #pragma unroll
-    for (int s = 0; s < ST; ++s)
+    for (int s = 0; s < ST; ++s) {
+      float q[32];
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        qf[s][w] = U32x4{0, 0, 0, 0};
+      for (int w = 0; w < 16; ++w) {
+        uint32_t x = 0;
         if (valid) {
-          const MDBF_GLOBAL uint16_t* p = (const MDBF_GLOBAL uint16_t*)a.q + q_at + 64 * s + 8 * w;
-          if (a.wide_q) {
-            qf[s][w] = *(const MDBF_GLOBAL U32x4*)p;
-          } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) qf[s][w][j] = (uint32_t)p[2 * j] | ((uint32_t)p[2 * j + 1] << 16);
-          }
-          qf[s][w] ^= a.flip;
+          const MDBF_GLOBAL uint16_t* p = (const MDBF_GLOBAL uint16_t*)a.q + q_at + 64 * s + 2 * w;
+          x = (a.wide_q ? *(const MDBF_GLOBAL uint32_t*)p : (uint32_t)p[0] | ((uint32_t)p[1] << 16)) ^ a.flip;
+        }
+        if (DT == MDBF_F16) {
+          const F16x2 v = __builtin_bit_cast(F16x2, x);
+          q[2 * w] = (float)v[0], q[2 * w + 1] = (float)v[1];
+        } else {
+          q[2 * w] = __builtin_bit_cast(float, x << 16), q[2 * w + 1] = __builtin_bit_cast(float, x & 0xffff0000u);
         }
       }
+      finite &= ql[s].set(q);
+    }
 
     // a thread's units of a tile: its page is looked up a tile before its codes are requested
     U32x4 kc[U], vc[U];
@@ -801,7 +851,7 @@ __global__ __launch_bounds__(64 * kManyWaves, D <= 128 ? 2 : 1) void attn_many_k
       }
     };
 
-    float m = -INFINITY, l = 0;
+    float m = -INFINITY, l = finite ? 0.0f : NAN;      // (a query that is not finite has no finite result)
     uint32_t nan_blocks = 0;
     F32x16 acc[CT];
 #pragma unroll
@@ -836,14 +886,20 @@ __global__ __launch_bounds__(64 * kManyWaves, D <= 128 ? 2 : 1) void attn_many_k
       for (int f = 0; f < 2; ++f) {
 #pragma unroll
         for (int j = 0; j < 16; ++j) z[f][j] = 0;
+        const int row = 32 * f + r;
+        // the blocks' scale bytes, this half's at the even places
+        uint32_t sc[(BL + 3) / 4];
 #pragma unroll
-        for (int s = 0; s < ST; ++s) {
-          const int row = 32 * f + r;
+        for (int w = 0; w < (BL + 3) / 4; ++w)
+          sc[w] = (BL == 2 ? *reinterpret_cast<const uint16_t*>(in.key_scales + row * BL) : reinterpret_cast<const uint32_t*>(in.key_scales + row * BL)[w]) >> (8 * hh);
+        each_of([&](auto st) __attribute__((always_inline)) {
+          constexpr int s = decltype(st)::value;
           const U32x4 codes = *reinterpret_cast<const U32x4*>(in.keys + row * KROW + (2 * s + hh) * 16);
-          const float unit = unit_of(in.key_scales[row * BL + 2 * s + hh]);
-#pragma unroll
-          for (int w = 0; w < 4; ++w) z[f] = mma32<DT>(numbers<DT>(codes[w], unit), qf[s][w], z[f]);
-        }
+          each_of([&](auto k) __attribute__((always_inline)) {
+            constexpr int L = NL - 1 - decltype(k)::value;      // the smallest first
+            z[f] = mx32<2 * (s & 1), L>(codes, sc[s / 2], ql[s].limb[L], ql[s].scales, z[f]);
+          }, std::make_integer_sequence<int, NL>{});
+        }, std::make_integer_sequence<int, ST>{});
       }
       if (t0 < sp.all_lo || t0 + kTile > sp.all_hi) {      // not every row sees every token
 #pragma unroll
