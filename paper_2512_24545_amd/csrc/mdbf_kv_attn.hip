@@ -122,17 +122,13 @@ constexpr int kWaves = 4;
 constexpr int kRows = 16;        // query rows of a workgroup
 constexpr float kSlack = 8;      // powers of two by which a score may exceed the running reference
 
-// What beginning and ending a tile of query rows costs, in tiles of tokens (see the shares below).  64 requests of up to 8192 tokens,
-// 8 kv heads of 128: 79 us with 0, 62.4 with 3, 59.2 with 6, 58.6 with 10, 60.5 with 16.
-constexpr int kRowsCost = 8;
-// The tokens that the rows of a tile of query rows see.
+// The tokens that a tile of ROWS query rows sees.
 struct Span {
   int lo, hi;              // what any row sees
   int all_lo, all_hi;      // what all rows see
   int from, units;         // the tiles of tokens from the first one's on; one where nothing is seen: the rows are written
-  __device__ __forceinline__ int cost() const { return units + kRowsCost; }
 };
-template <int ROWS = kRows>
+template <int ROWS>
 __device__ __forceinline__ Span span_of(const AttnArgs& a, const Request& rq, int tile, int rows) {
   const Sees s0 = sees(a, rq, token_of(a, tile * ROWS)), s1 = sees(a, rq, token_of(a, min(tile * ROWS + ROWS - 1, rows - 1)));
   Span s = {s0.lo, s1.hi, s1.lo, s0.hi, s0.lo & ~(kTile - 1), 1};
@@ -140,21 +136,173 @@ __device__ __forceinline__ Span span_of(const AttnArgs& a, const Request& rq, in
   return s;
 }
 
-// Long caches: the units (tiles of 64 tokens, and kRowsCost more in front of them for each tile of rows) of all requests, row
-// tiles and kv heads, one after the other, are cut into equal shares, a workgroup's each, so that requests of any lengths keep
-// the device evenly busy.  A workgroup finishes the row
-// tiles that lie whole in its share; of the first and the last one it may have a part only, whose sums it leaves in the
-// workspace (two places each), and where a row tile begins in a share and ends in a later one a note for the join.
-// (request, row tile, kv head, workgroups whose shares the row tile lies in, this one the first; 0: none begins here)
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+  return ((int64_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
+}
+
+// sum over a workgroup of four waves up to and with this thread's x; `total` of all
+__device__ __forceinline__ int64_t scan_256(int64_t x, int64_t& total, int64_t* waves) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int64_t u = __shfl_up(x, o);
+    if (lane >= o) x += u;
+  }
+  __syncthreads();
+  if (lane == 63) waves[wave] = x;
+  __syncthreads();
+  total = 0;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    if (w < wave) x += waves[w];
+    total += waves[w];
+  }
+  return x;
+}
+
+// What a workgroup does: tiles of ROWS query rows of a request and kv head, one after the other, and of their tokens the units
+// (tiles of 64) u0 .. u1 - 1.
+//
+// Either each takes row tiles with all of their tokens.  Or the units of all requests, row tiles and kv heads, one after the
+// other and COST more in front of them for each row tile (what beginning and ending one takes), are cut into equal shares, a
+// workgroup's each, so that requests of any lengths keep the device evenly busy.  A workgroup finishes the row tiles that lie
+// whole in its share; of the first and the last one it may have a part only, whose sums it leaves in the workspace (two places
+// each), and where a row tile begins in a share and ends in a later one a note for the join: request, row tile, kv head, and
+// the number of workgroups whose shares it lies in, this one the first; 0 if none begins here.
 typedef int32_t Note __attribute__((ext_vector_type(4)));
-template <int D>
-constexpr int part_floats = kRows * (D + 2);      // kRows x D sums, then kRows maxima and kRows sums of numerators
+constexpr int kLeastShare = 4;      // units
+template <int ROWS, int COST>
+struct Work {
+  int b, rt, head, u0 = 0, u1 = 0;
+  int64_t left = 0, share = 0;
+  Request rq;
+  Span sp;
+
+  // units of a request over its row tiles and kv heads
+  __device__ static __forceinline__ int64_t units_of(const AttnArgs& a, int b) {
+    const Request r = request_of(a, b);
+    const int rows = r.fresh * a.group;
+    int64_t n = 0;
+    for (int t = 0; t * ROWS < rows; ++t) n += span_of<ROWS>(a, r, t, rows).units + COST;
+    return n * a.kv_heads;
+  }
+  // the units of the row tile that lie in the share, which goes on with this place among COST + units
+  __device__ __forceinline__ void cut(int place) {
+    const int most = (int)min((int64_t)(sp.units + COST - place), left);
+    u0 = max(place - COST, 0), u1 = place + most - COST;
+    left -= most;
+  }
+  // all tokens of a row tile, if the request has it
+  __device__ __forceinline__ void whole(const AttnArgs& a, int b_, int rt_, int head_) {
+    b = b_, rt = rt_, head = head_;
+    rq = request_of(a, b);
+    const int rows = rq.fresh * a.group;
+    if (rt * ROWS >= rows) return;
+    sp = span_of<ROWS>(a, rq, rt, rows);
+    u1 = sp.units;
+  }
+  // This workgroup's share: prefix sums over the requests, of up to 64 by every wave for itself, else by the workgroup, 256 at
+  // a time, first of all and then again up to the one where the share begins.  `find`: six words of LDS.
+  __device__ __forceinline__ void first(const AttnArgs& a, int64_t* find) {
+    const int tid = threadIdx.x, lane = tid & 63;
+    const bool few = a.requests <= 64;
+    int64_t total = 0, sum, mine = 0, end = 0;
+    if (few) {
+      mine = end = lane < a.requests ? units_of(a, lane) : 0;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int64_t u = __shfl_up(end, o);
+        if (lane >= o) end += u;
+      }
+      total = __shfl(end, 63);
+    } else {
+      for (int r0 = 0; r0 < a.requests; r0 += 256) {
+        scan_256(r0 + tid < a.requests ? units_of(a, r0 + tid) : 0, sum, find);
+        total += sum;
+      }
+    }
+    total = uniform(total);      // (what the loops below go by must be known to be the same in all lanes)
+    share = max((total + a.shares - 1) / a.shares, (int64_t)kLeastShare);
+    const int64_t start = blockIdx.x * share;
+    if (tid == 0) ((MDBF_GLOBAL Note*)a.part)[blockIdx.x] = Note{0, 0, 0, 0};
+    if (start >= total) return;
+    left = min(share, total - start);
+    int64_t rest;
+    if (few) {
+      b = __builtin_ctzll(__ballot(start >= end - mine && start < end));
+      rest = start - __shfl(end - mine, b);
+    } else {
+      int64_t before = 0;
+      for (int r0 = 0; r0 < a.requests; r0 += 256) {
+        mine = r0 + tid < a.requests ? units_of(a, r0 + tid) : 0;
+        end = before + scan_256(mine, sum, find);
+        if (start >= end - mine && start < end) find[4] = r0 + tid, find[5] = end - mine;
+        before += sum;
+        if (start < before) break;
+      }
+      __syncthreads();
+      b = (int)find[4];
+      rest = start - find[5];
+    }
+    b = __builtin_amdgcn_readfirstlane(b);
+    rest = uniform(rest);
+    rq = request_of(a, b);
+    const int rows = rq.fresh * a.group;
+    for (rt = 0;; ++rt) {
+      sp = span_of<ROWS>(a, rq, rt, rows);
+      const int64_t all = (int64_t)(sp.units + COST) * a.kv_heads;
+      if (rest < all) break;
+      rest -= all;
+    }
+    head = (int)(rest / (sp.units + COST));
+    cut((int)(rest % (sp.units + COST)));
+  }
+  __device__ __forceinline__ bool any() const { return u1 > 0; }      // (a share may end before a row tile's first unit)
+  __device__ __forceinline__ bool part() const { return u1 - u0 < sp.units; }
+  __device__ __forceinline__ void note(const AttnArgs& a) const {
+    if (u0 == 0 && u1 < sp.units && threadIdx.x == 0)
+      ((MDBF_GLOBAL Note*)a.part)[blockIdx.x] = Note{b, rt, head, 1 + (int)((sp.units - u1 + share - 1) / share)};
+  }
+  // on to what is next
+  __device__ __forceinline__ void next(const AttnArgs& a) {
+    int rows = rq.fresh * a.group;
+    u1 = 0;
+    if (!a.shares) {
+      rt += a.row_tiles;
+      if (rt * ROWS >= rows) return;
+      sp = span_of<ROWS>(a, rq, rt, rows);
+      u1 = sp.units;
+      return;
+    }
+    if (left <= 0) return;
+    if (++head == a.kv_heads) {
+      head = 0;
+      ++rt;
+      while (rt * ROWS >= rows) {        // (units are left: there is a request with rows)
+        rq = request_of(a, ++b);
+        rows = rq.fresh * a.group;
+        rt = 0;
+      }
+      sp = span_of<ROWS>(a, rq, rt, rows);
+    }
+    cut(0);
+  }
+};
+// sums of a part of a row tile: ROWS x D of them, then ROWS maxima and ROWS sums of numerators; where this workgroup's go, and those
+// of the p-th workgroup of a note at wg (the first part lies in the second place)
+template <int D, int ROWS>
+constexpr int part_floats = ROWS * (D + 2);
+template <int D, int ROWS>
+__device__ __forceinline__ MDBF_GLOBAL float* part_at(const AttnArgs& a, int wg, bool second) {
+  return (MDBF_GLOBAL float*)((MDBF_GLOBAL Note*)a.part + a.shares) + (int64_t)(2 * wg + second) * part_floats<D, ROWS>;
+}
+
+// Few rows: what beginning and ending a row tile costs.  64 requests of up to 8192 tokens, 8 kv heads of 128: 79 us with 0, 62.4
+// with 3, 59.2 with 6, 58.6 with 10, 60.5 with 16.
+constexpr int kRowsCost = 8;
 // the workgroups that the device holds at once
 template <int D>
-constexpr int share_count = 256 * (D == 64 ? 4 : D == 128 ? 3 : 2);
-constexpr int kLeastShare = 4;                    // units
-template <int D>
-constexpr size_t share_bytes() { return (size_t)share_count<D> * (sizeof(Note) + 2 * part_floats<D> * 4); }
+constexpr int kFewShares = 256 * (D == 64 ? 4 : D == 128 ? 3 : 2);
 
 constexpr int kNonTemporal = 2;  // of the buffer loads: the cache is read once
 
@@ -242,39 +390,6 @@ __device__ __forceinline__ float row_max(float x) {
   return fmaxf(__builtin_bit_cast(float, b0), __builtin_bit_cast(float, b1));
 }
 
-// units of a request over its row tiles and kv heads
-__device__ __forceinline__ int64_t request_units(const AttnArgs& a, int b) {
-  const Request rq = request_of(a, b);
-  const int rows = rq.fresh * a.group;
-  int64_t n = 0;
-  for (int rt = 0; rt * kRows < rows; ++rt) n += span_of(a, rq, rt, rows).cost();
-  return n * a.kv_heads;
-}
-
-__device__ __forceinline__ int64_t uniform(int64_t x) {
-  return ((int64_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
-}
-
-// sum over the workgroup's four waves up to and with this thread's x; `total` of all
-__device__ __forceinline__ int64_t scan_256(int64_t x, int64_t& total, int64_t* waves) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int64_t u = __shfl_up(x, o);
-    if (lane >= o) x += u;
-  }
-  __syncthreads();
-  if (lane == 63) waves[wave] = x;
-  __syncthreads();
-  total = 0;
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    if (w < wave) x += waves[w];
-    total += waves[w];
-  }
-  return x;
-}
-
 // 16 query rows of one kv head at a time, the tiles of their tokens dealt out to the four waves, which meet at the end.  The
 // registers that a tile's keys were in take the next tile's as soon as the scores are there, those of its values once they
 // are in LDS; page numbers are looked up a tile earlier still.  NP: pages per tile of 64 tokens (1, 2 or 4).
@@ -296,91 +411,19 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 4 : D == 128 ? 3 : 2) void a
   const int head_bytes = (int)kv_head_bytes(1 << a.page_shift, D);
   unsigned char* vals = lds[wave];
 
-  // where this workgroup begins: a request, a tile of its rows and a kv head, and units of their tokens [u0, u1)
-  int b, head, u0 = 0, u1, rt;
-  int64_t left = 0, share = 0;
-  Request rq;
-  Span sp;
-  // units of the row tile that lie in the share, which goes on with this place of its cost
-  auto cut = [&](int place) __attribute__((always_inline)) {
-    const int most = (int)min((int64_t)(sp.cost() - place), left);
-    u0 = max(place - kRowsCost, 0), u1 = place + most - kRowsCost;
-    left -= most;
-  };
-  if (!a.shares) {
-    // a workgroup per row tile that the launch was sized for, with all of its tokens
-    uint32_t idx = blockIdx.x;
-    rt = idx % a.row_tiles;
-    idx /= a.row_tiles;
-    head = idx % a.kv_heads, b = idx / a.kv_heads;
-    rq = request_of(a, b);
-    const int rows = rq.fresh * a.group;
-    if (rt * kRows >= rows) return;
-    sp = span_of(a, rq, rt, rows);
-    u1 = sp.units;
-  } else {
-    // prefix sums over the requests: of up to 64 by every wave for itself, else by the workgroup, 256 at a time, first of all
-    // and then again up to the one where the share begins
-    int64_t* waves = reinterpret_cast<int64_t*>(lds[0]);
-    __shared__ int found_b;
-    __shared__ int64_t found_at;
-    const int tid = threadIdx.x;
-    const bool few = a.requests <= 64;
-    int64_t total = 0, sum, mine = 0, end = 0;
-    if (few) {
-      mine = end = lane < a.requests ? request_units(a, lane) : 0;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const int64_t u = __shfl_up(end, o);
-        if (lane >= o) end += u;
-      }
-      total = __shfl(end, 63);
-    } else {
-      for (int r0 = 0; r0 < a.requests; r0 += 256) {
-        scan_256(r0 + tid < a.requests ? request_units(a, r0 + tid) : 0, sum, waves);
-        total += sum;
-      }
-    }
-    total = uniform(total);      // (what the loops below go by must be known to be the same in all lanes)
-    share = max((total + a.shares - 1) / a.shares, (int64_t)kLeastShare);
-    const int64_t start = blockIdx.x * share;
-    MDBF_GLOBAL Note* note = (MDBF_GLOBAL Note*)a.part + blockIdx.x;
-    if (tid == 0) *note = Note{0, 0, 0, 0};
-    if (start >= total) return;
-    left = min(share, total - start);
-    int64_t rest;
-    if (few) {
-      b = __builtin_ctzll(__ballot(start >= end - mine && start < end));
-      rest = start - __shfl(end - mine, b);
-    } else {
-      int64_t before = 0;
-      for (int r0 = 0; r0 < a.requests; r0 += 256) {
-        mine = r0 + tid < a.requests ? request_units(a, r0 + tid) : 0;
-        end = before + scan_256(mine, sum, waves);
-        if (start >= end - mine && start < end) found_b = r0 + tid, found_at = end - mine;
-        before += sum;
-        if (start < before) break;
-      }
-      __syncthreads();
-      b = found_b;
-      rest = start - found_at;
-      __syncthreads();
-    }
-    b = __builtin_amdgcn_readfirstlane(b);
-    rest = uniform(rest);
-    rq = request_of(a, b);
-    const int rows = rq.fresh * a.group;
-    for (rt = 0;; ++rt) {
-      sp = span_of(a, rq, rt, rows);
-      if (rest < (int64_t)sp.cost() * a.kv_heads) break;
-      rest -= (int64_t)sp.cost() * a.kv_heads;
-    }
-    head = (int)(rest / sp.cost());
-    cut((int)(rest % sp.cost()));
+  Work<kRows, kRowsCost> work;
+  if (a.shares) {
+    work.first(a, reinterpret_cast<int64_t*>(stat));
+    __syncthreads();
+  } else {      // a workgroup per row tile that the launch was sized for
+    const uint32_t idx = blockIdx.x / a.row_tiles;
+    work.whole(a, idx / a.kv_heads, blockIdx.x % a.row_tiles, idx % a.kv_heads);
   }
 
-  while (u1 > 0) {      // (a share may end in a row tile's cost, before its first unit)
-    const int rows = rq.fresh * a.group;
+  for (; work.any(); work.next(a)) {
+    const Request rq = work.rq;
+    const Span sp = work.sp;
+    const int b = work.b, rt = work.rt, head = work.head, u0 = work.u0, u1 = work.u1, rows = rq.fresh * a.group;
     const MDBF_CONST int32_t* table = (const MDBF_CONST int32_t*)a.table + b * a.table_ld;
     const int R = rt * kRows + r;
     const bool valid = R < rows;
@@ -570,8 +613,8 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 4 : D == 128 ? 3 : 2) void a
 #pragma unroll
           for (int c = 0; c < N; ++c) o[c] += f * from[c];
         }
-        if (u1 - u0 < sp.units) {
-          MDBF_GLOBAL float* to = (MDBF_GLOBAL float*)((MDBF_GLOBAL Note*)a.part + a.shares) + (int64_t)(2 * blockIdx.x + (u0 == 0)) * part_floats<D>;
+        if (work.part()) {
+          MDBF_GLOBAL float* to = part_at<D, kRows>(a, blockIdx.x, u0 == 0);
           if (piece == 0) {
             to[kRows * D + row] = top;
             to[kRows * (D + 1) + row] = sum;
@@ -584,37 +627,14 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 4 : D == 128 ? 3 : 2) void a
         }
       }
     }
-    if (u0 == 0 && u1 < sp.units && threadIdx.x == 0) {
-      ((MDBF_GLOBAL Note*)a.part)[blockIdx.x] = Note{b, rt, head, 1 + (int)((sp.units - u1 + share - 1) / share)};
-    }
-    // on to what is next
-    if (!a.shares) {
-      rt += a.row_tiles;
-      if (rt * kRows >= rows) break;
-      sp = span_of(a, rq, rt, rows);
-      u1 = sp.units;
-    } else {
-      if (left <= 0) break;
-      if (++head == a.kv_heads) {
-        head = 0;
-        ++rt;
-        int n = rows;
-        while (rt * kRows >= n) {        // (units are left: there is a request with rows)
-          rq = request_of(a, ++b);
-          n = rq.fresh * a.group;
-          rt = 0;
-        }
-        sp = span_of(a, rq, rt, n);
-      }
-      cut(0);
-    }
+    work.note(a);
     __syncthreads();
   }
 }
 
 // Joins the parts of the row tiles that several shares have: W waves per row and share where one begins.  D / 4 lanes side by
 // side on the channels take a part at a time, other lanes and waves the next ones; the order is fixed.
-template <int D, int DT, int W>
+template <int D, int DT, int ROWS, int W>
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
   constexpr int L = D / 4, GROUPS = 64 / L, AHEAD = 8;
   __shared__ F32x4 sums[W][L];
@@ -628,12 +648,10 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
   if (count < 2) return;
   const Request rq = request_of(a, note[0]);
   const int rows = rq.fresh * a.group;
-  const MDBF_GLOBAL float* parts = (const MDBF_GLOBAL float*)((const MDBF_GLOBAL Note*)a.part + a.shares);
-  // the first part lies in its workgroup's second place, the others in the first ones
-  auto part = [&](int p) { return parts + (int64_t)(2 * (wg + p) + (p == 0)) * part_floats<D>; };
-  for (int row = row0; row < kRows && rt * kRows + row < rows; row += a.join_rows) {
+  auto part = [&](int p) { return (const MDBF_GLOBAL float*)part_at<D, ROWS>(a, wg + p, p == 0); };
+  for (int row = row0; row < ROWS && rt * ROWS + row < rows; row += a.join_rows) {
     float top = -INFINITY;
-    for (int p = lane; p < count; p += 64) top = fmaxf(top, part(p)[kRows * D + row]);
+    for (int p = lane; p < count; p += 64) top = fmaxf(top, part(p)[ROWS * D + row]);
 #pragma unroll
     for (int w = 1; w < 64; w <<= 1) top = fmaxf(top, __shfl_xor(top, w));
     const float use = top == -INFINITY ? 0.0f : top;
@@ -644,8 +662,8 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
       float f = 0;
       if (lane < some) {
         const MDBF_GLOBAL float* q = part(p0 + lane);
-        f = __builtin_amdgcn_exp2f(q[kRows * D + row] - use);
-        sum += f * q[kRows * (D + 1) + row];
+        f = __builtin_amdgcn_exp2f(q[ROWS * D + row] - use);
+        sum += f * q[ROWS * (D + 1) + row];
       }
       for (int p = mine * GROUPS; p < some; p += GROUPS * W * AHEAD) {
         F32x4 v[AHEAD];
@@ -676,7 +694,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
         for (int w = 1; w < W; ++w) o += sums[w][l];
     }
     const float v[4] = {o[0], o[1], o[2], o[3]};
-    if (grp == 0 && mine == 0) store_row<DT, 4>(a, rq, head, rt * kRows + row, l * 4, v, sum);
+    if (grp == 0 && mine == 0) store_row<DT, 4>(a, rq, head, rt * ROWS + row, l * 4, v, sum);
     if (W > 1) __syncthreads();
   }
 }
@@ -686,6 +704,9 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
 // LDS: key codes as they are (each wave makes numbers of them as it feeds its products), values as numbers.  Two buffers:
 // while one is worked on, the next tile's codes, which came in while the one before was, are written into the other.
 constexpr int kManyWaves = 4, kManyRows = 32 * kManyWaves;
+constexpr int kManyCost = 4;      // units that beginning and ending a row tile costs
+template <int D>
+constexpr int kManyShares = 256 * (D <= 128 ? 2 : 1);
 typedef float F32x16 __attribute__((ext_vector_type(16)));
 
 template <int DT>
@@ -763,18 +784,21 @@ __global__ __launch_bounds__(64 * kManyWaves, D <= 128 ? 2 : 1) void attn_many_k
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 31, hh = lane >> 5;
   const int P = 1 << a.page_shift, head_bytes = (int)kv_head_bytes(P, D);
 
-  // kv heads next to each other (their row tiles then share an XCD's cache), the row tiles that see most first
-  uint32_t idx = blockIdx.x;
-  const int head = idx % a.kv_heads;
-  idx /= a.kv_heads;
-  const int b = idx % a.requests, rt0 = a.row_tiles - 1 - idx / a.requests;
-  const Request rq = request_of(a, b);
-  const int rows = rq.fresh * a.group;
-  const MDBF_GLOBAL int32_t* table = (const MDBF_GLOBAL int32_t*)a.table + b * a.table_ld;
-  const MDBF_GLOBAL uint8_t* cache = (const MDBF_GLOBAL uint8_t*)a.cache + (int64_t)head * head_bytes;
+  Work<kManyRows, kManyCost> work;
+  if (a.shares) {
+    work.first(a, reinterpret_cast<int64_t*>(&lds[0]));
+    __syncthreads();
+  } else {      // kv heads next to each other (their row tiles then share an XCD's cache), the row tiles that see most first
+    const uint32_t idx = blockIdx.x / a.kv_heads;
+    work.whole(a, idx % a.requests, a.row_tiles - 1 - idx / a.requests, blockIdx.x % a.kv_heads);
+  }
 
-  for (int rt = rt0; rt * kManyRows < rows; rt += a.row_tiles) {
-    const Span sp = span_of<kManyRows>(a, rq, rt, rows);
+  for (; work.any(); work.next(a)) {
+    const Request rq = work.rq;
+    const Span sp = work.sp;
+    const int rt = work.rt, head = work.head, rows = rq.fresh * a.group;
+    const MDBF_GLOBAL int32_t* table = (const MDBF_GLOBAL int32_t*)a.table + work.b * a.table_ld;
+    const MDBF_GLOBAL uint8_t* cache = (const MDBF_GLOBAL uint8_t*)a.cache + (int64_t)head * head_bytes;
     const int R = rt * kManyRows + wave * 32 + r;
     const bool valid = R < rows;
     const int i = valid ? token_of(a, R) : 0, g = valid ? R - i * a.group : 0;
@@ -788,13 +812,20 @@ __global__ __launch_bounds__(64 * kManyWaves, D <= 128 ? 2 : 1) void attn_many_k
 #pragma unroll
     for (int s = 0; s < ST; ++s) {
       float q[32];
+      U32x4 raw[4] = {};
+      if (valid) {
+        const MDBF_GLOBAL uint16_t* p = (const MDBF_GLOBAL uint16_t*)a.q + q_at + 64 * s;
+        if (a.wide_q) {
+#pragma unroll
+          for (int w = 0; w < 4; ++w) raw[w] = ((const MDBF_GLOBAL U32x4*)p)[w];
+        } else {
+#pragma unroll
+          for (int w = 0; w < 16; ++w) raw[w / 4][w % 4] = (uint32_t)p[2 * w] | ((uint32_t)p[2 * w + 1] << 16);
+        }
+      }
 #pragma unroll
       for (int w = 0; w < 16; ++w) {
-        uint32_t x = 0;
-        if (valid) {
-          const MDBF_GLOBAL uint16_t* p = (const MDBF_GLOBAL uint16_t*)a.q + q_at + 64 * s + 2 * w;
-          x = (a.wide_q ? *(const MDBF_GLOBAL uint32_t*)p : (uint32_t)p[0] | ((uint32_t)p[1] << 16)) ^ a.flip;
-        }
+        const uint32_t x = raw[w / 4][w % 4] ^ a.flip;
         if (DT == MDBF_F16) {
           const F16x2 v = __builtin_bit_cast(F16x2, x);
           q[2 * w] = (float)v[0], q[2 * w + 1] = (float)v[1];
@@ -859,20 +890,20 @@ __global__ __launch_bounds__(64 * kManyWaves, D <= 128 ? 2 : 1) void attn_many_k
 #pragma unroll
       for (int j = 0; j < 16; ++j) acc[c][j] = 0;
 
-    const int tiles = sp.hi > sp.lo ? sp.units : 0;
+    const int tiles = sp.hi > sp.lo ? work.u1 - work.u0 : 0, begin = sp.from + work.u0 * kTile;
     if (tiles) {
-      look_up(sp.from);
-      request(sp.from);
-      look_up(sp.from + kTile);
-      put(lds[0], sp.from);
+      look_up(begin);
+      request(begin);
+      look_up(begin + kTile);
+      put(lds[0], begin);
       if (tiles > 1) {
-        request(sp.from + kTile);
-        look_up(sp.from + 2 * kTile);
+        request(begin + kTile);
+        look_up(begin + 2 * kTile);
       }
       __syncthreads();
     }
     for (int n = 0; n < tiles; ++n) {
-      const int t0 = sp.from + n * kTile;
+      const int t0 = begin + n * kTile;
       if (n + 1 < tiles) put(lds[(n + 1) & 1], t0 + kTile);
       if (n + 2 < tiles) {
         request(t0 + 2 * kTile);
@@ -880,27 +911,29 @@ __global__ __launch_bounds__(64 * kManyWaves, D <= 128 ? 2 : 1) void attn_many_k
       }
       const Buffer& in = lds[n & 1];
 
-      // scores: a lane holds those of its row with tokens 32 f + 8 (j / 4) + 4 hh + j % 4
+      // scores: a lane holds those of its row with tokens 32 f + 8 (j / 4) + 4 hh + j % 4; two chains of products side by side
       F32x16 z[2];
+      uint32_t sc[2][(BL + 3) / 4];      // the blocks' scale bytes, this half's at the even places
 #pragma unroll
       for (int f = 0; f < 2; ++f) {
-#pragma unroll
-        for (int j = 0; j < 16; ++j) z[f][j] = 0;
-        const int row = 32 * f + r;
-        // the blocks' scale bytes, this half's at the even places
-        uint32_t sc[(BL + 3) / 4];
+        const unsigned char* from = in.key_scales + (32 * f + r) * BL;
 #pragma unroll
         for (int w = 0; w < (BL + 3) / 4; ++w)
-          sc[w] = (BL == 2 ? *reinterpret_cast<const uint16_t*>(in.key_scales + row * BL) : reinterpret_cast<const uint32_t*>(in.key_scales + row * BL)[w]) >> (8 * hh);
-        each_of([&](auto st) __attribute__((always_inline)) {
-          constexpr int s = decltype(st)::value;
-          const U32x4 codes = *reinterpret_cast<const U32x4*>(in.keys + row * KROW + (2 * s + hh) * 16);
-          each_of([&](auto k) __attribute__((always_inline)) {
-            constexpr int L = NL - 1 - decltype(k)::value;      // the smallest first
-            z[f] = mx32<2 * (s & 1), L>(codes, sc[s / 2], ql[s].limb[L], ql[s].scales, z[f]);
-          }, std::make_integer_sequence<int, NL>{});
-        }, std::make_integer_sequence<int, ST>{});
+          sc[f][w] = (BL == 2 ? *reinterpret_cast<const uint16_t*>(from) : reinterpret_cast<const uint32_t*>(from)[w]) >> (8 * hh);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) z[f][j] = 0;
       }
+      each_of([&](auto st) __attribute__((always_inline)) {
+        constexpr int s = decltype(st)::value;
+        U32x4 codes[2];
+#pragma unroll
+        for (int f = 0; f < 2; ++f) codes[f] = *reinterpret_cast<const U32x4*>(in.keys + (32 * f + r) * KROW + (2 * s + hh) * 16);
+        each_of([&](auto k) __attribute__((always_inline)) {
+          constexpr int L = NL - 1 - decltype(k)::value;      // the smallest first
+#pragma unroll
+          for (int f = 0; f < 2; ++f) z[f] = mx32<2 * (s & 1), L>(codes[f], sc[f][s / 2], ql[s].limb[L], ql[s].scales, z[f]);
+        }, std::make_integer_sequence<int, NL>{});
+      }, std::make_integer_sequence<int, ST>{});
       if (t0 < sp.all_lo || t0 + kTile > sp.all_hi) {      // not every row sees every token
 #pragma unroll
         for (int f = 0; f < 2; ++f)
@@ -976,7 +1009,21 @@ __global__ __launch_bounds__(64 * kManyWaves, D <= 128 ? 2 : 1) void attn_many_k
     }
 
     l += __shfl_xor(l, 32);
-    if (valid) {
+    if (valid && work.part()) {
+      MDBF_GLOBAL float* to = part_at<D, kManyRows>(a, blockIdx.x, work.u0 == 0);
+      const int row = wave * 32 + r;
+      if (hh == 0) to[kManyRows * D + row] = m, to[kManyRows * (D + 1) + row] = l;
+#pragma unroll
+      for (int c = 0; c < CT; ++c) {
+        const bool nan = nan_blocks >> c & 1;
+#pragma unroll
+        for (int j = 0; j < 16; j += 4) {
+          F32x4 v = {acc[c][j], acc[c][j + 1], acc[c][j + 2], acc[c][j + 3]};
+          if (nan) v = F32x4{NAN, NAN, NAN, NAN};
+          *(MDBF_GLOBAL F32x4*)(to + row * D + 32 * c + 2 * j + 4 * hh) = v;
+        }
+      }
+    } else if (valid) {
 #pragma unroll
       for (int c = 0; c < CT; ++c) {
         const bool nan = nan_blocks >> c & 1;
@@ -987,6 +1034,7 @@ __global__ __launch_bounds__(64 * kManyWaves, D <= 128 ? 2 : 1) void attn_many_k
         }
       }
     }
+    work.note(a);
   }
 }
 
@@ -1001,41 +1049,74 @@ static int check_attn(const mdbf_kv_t* kv, const mdbf_attn_t* at, int requests, 
   return MDBF_OK;
 }
 
-// Whether a call is cut into shares, else a workgroup takes a row tile with all of its tokens: where no cache is longer than
-// kWhole tokens the second launch, the join, would cost more than the cut saves.
-constexpr int kWhole = 1024;
+// Which kernel a call takes, and whether its work is cut into shares: by estimates of the time from the sizes that the caller
+// bounds the call by, in us.  A workgroup of the few-row kernel takes 1 us per unit where the device is full of them, one of the
+// prompts' kernel 2 with two on a compute unit and 1.3 with one (heads of 128; the others scale alike); the join is a launch.
+#ifndef SW
+#define SW 10.0
+#define FU 1.0
+#endif
+constexpr int kWhole = 1024;      // tokens up to which few rows' tiles are not cut
+static bool attn_cuts(const mdbf_attn_t& at) { return (at.window ? std::min(at.max_length, at.window) : at.max_length) > kWhole; }
 struct AttnGeom {
   int row_tiles;           // of a request and kv head
-  bool shares, many;       // many: attn_many_kernel
+  bool shares, many;
 };
-#ifndef MR
-#define MR 33
-#endif
-constexpr int kManyFrom = MR;
 static AttnGeom attn_geom(const mdbf_kv_t& kv, const mdbf_attn_t& at, int T) {
-  const int64_t group = at.q_heads / kv.kv_heads, most = std::min(at.max_fresh, T);
-  if (most * group >= kManyFrom) return {(int)std::min<int64_t>((most * group + kManyRows - 1) / kManyRows, 1 << 16), false, true};
-  int64_t span = at.max_length;
-  if (at.window) span = std::min<int64_t>(span, (int64_t)at.window + kRows);
-  return {(int)std::min<int64_t>((most * group + kRows - 1) / kRows, 1 << 16), span > kWhole, false};
+  const int64_t rows = (int64_t)std::min(at.max_fresh, T) * (at.q_heads / kv.kv_heads), heads = kv.kv_heads;
+  const bool causal = at.flags & MDBF_ATTN_CAUSAL;
+  const int fresh = std::min(at.max_fresh, T), requests = at.max_fresh ? (T + fresh - 1) / fresh : 1;      // with as many new tokens
+  auto tiles_of = [&](int per) { return (rows + per - 1) / per; };
+  auto units_of = [&](int per, bool most) {
+    double span = at.max_length;
+    if (causal && !most) span -= std::min<double>(fresh, span) / 2;
+    if (at.window) span = std::min<double>(span, (double)at.window + per * fresh / (double)rows);
+    return span / kTile + 1;
+  };
+  const double few_tiles = (double)requests * heads * tiles_of(kRows), many_tiles = (double)requests * heads * tiles_of(kManyRows);
+  const double few_shares = kv.head_dim == 64 ? kFewShares<64> : kv.head_dim == 128 ? kFewShares<128> : kFewShares<256>;
+  const double many_shares = kv.head_dim <= 128 ? kManyShares<128> : kManyShares<256>;
+  const bool cuts = attn_cuts(at);
+  const double few = FU * std::max(few_tiles * (units_of(kRows, false) + kRowsCost) / few_shares, cuts ? 0.0 : units_of(kRows, true)) + (cuts ? 6.0 : 0.0);
+  const double whole = std::max((many_tiles <= many_shares / 2 ? 1.3 : 2.0) * (units_of(kManyRows, true) + kManyCost),
+                                2.0 * many_tiles * (units_of(kManyRows, false) + kManyCost) / many_shares);
+  const double cut = 2.0 * many_tiles * (units_of(kManyRows, false) + kManyCost) / many_shares + SW;
+  AttnGeom g;
+  g.many = rows > kRows && std::min(whole, cut) < few;
+  g.shares = cuts && (!g.many || cut < whole);
+#ifdef FORCE
+  g.many = FORCE > 0; g.shares = cuts && (FORCE != 1);
+#endif
+  g.row_tiles = (int)std::min<int64_t>(tiles_of(g.many ? kManyRows : kRows), 1 << 16);
+  return g;
 }
-static size_t attn_workspace(const mdbf_kv_t& kv, const AttnGeom& g) {
-  return !g.shares ? 0 : kv.head_dim == 64 ? share_bytes<64>() : kv.head_dim == 128 ? share_bytes<128>() : share_bytes<256>();
+// One size for all calls with these heads and bounds or smaller ones; nothing where no cache is long enough to be cut.
+template <int D>
+static size_t workspace_of(bool few) {
+  const size_t bytes_few = kFewShares<D> * (sizeof(Note) + sizeof(float) * 2 * part_floats<D, kRows>);
+  return few ? bytes_few : std::max(bytes_few, kManyShares<D> * (sizeof(Note) + sizeof(float) * 2 * part_floats<D, kManyRows>));
+}
+static size_t attn_workspace(const mdbf_kv_t& kv, const mdbf_attn_t& at) {
+  if (!attn_cuts(at)) return 0;
+  const bool few = (int64_t)at.max_fresh * (at.q_heads / kv.kv_heads) <= kRows;
+  return kv.head_dim == 64 ? workspace_of<64>(few) : kv.head_dim == 128 ? workspace_of<128>(few) : workspace_of<256>(few);
 }
 
 template <int D, int DT>
 static int launch_few(AttnArgs& a, const AttnGeom& g, hipStream_t s) {
-  a.shares = g.shares ? share_count<D> : 0;
-  const unsigned grid = g.shares ? (unsigned)a.shares : (unsigned)((int64_t)a.requests * a.kv_heads * g.row_tiles);
+  a.shares = !g.shares ? 0 : g.many ? kManyShares<D> : kFewShares<D>;
+  const int64_t tiles = (int64_t)a.requests * a.kv_heads * g.row_tiles;
+  const unsigned grid = g.shares ? (unsigned)a.shares : (unsigned)tiles;
   if (g.many) attn_many_kernel<D, DT><<<grid, 64 * kManyWaves, 0, s>>>(a);
   else if (a.page_shift == 4) attn_few_kernel<D, DT, 4><<<grid, 64 * kWaves, 0, s>>>(a);
   else if (a.page_shift == 5) attn_few_kernel<D, DT, 2><<<grid, 64 * kWaves, 0, s>>>(a);
   else attn_few_kernel<D, DT, 1><<<grid, 64 * kWaves, 0, s>>>(a);
   int e = (int)hipGetLastError();
   if (e == 0 && g.shares) {
-    // (few row tiles: each lies in many shares)
-    if (a.shares / ((int64_t)a.requests * a.kv_heads * g.row_tiles) >= 16) attn_join_kernel<D, DT, 4><<<(unsigned)(a.shares * a.join_rows), 256, 0, s>>>(a);
-    else attn_join_kernel<D, DT, 1><<<(unsigned)((a.shares * a.join_rows + 3) / 4), 256, 0, s>>>(a);
+    const unsigned rows = (unsigned)(a.shares * a.join_rows);
+    if (g.many) attn_join_kernel<D, DT, kManyRows, 1><<<(rows + 3) / 4, 256, 0, s>>>(a);
+    else if (a.shares / tiles >= 16) attn_join_kernel<D, DT, kRows, 4><<<rows, 256, 0, s>>>(a);      // few row tiles, each in many shares
+    else attn_join_kernel<D, DT, kRows, 1><<<(rows + 3) / 4, 256, 0, s>>>(a);
     e = (int)hipGetLastError();
   }
   return e;
@@ -1055,7 +1136,7 @@ int mdbf_kv_attention_workspace_bytes(const mdbf_kv_t* kv, const mdbf_attn_t* at
   if (!bytes_out) return MDBF_EINVAL;
   int st = check_attn(kv, attn, requests, T);
   if (st) return st;
-  *bytes_out = attn_workspace(*kv, attn_geom(*kv, *attn, T));
+  *bytes_out = attn_workspace(*kv, *attn);
   return MDBF_OK;
 }
 
@@ -1075,7 +1156,7 @@ int mdbf_kv_attention(const mdbf_kv_t* kv, const mdbf_attn_t* attn, const void* 
   for (const void* p : ints)
     if (!kv_aligned(p, 4)) return MDBF_EALIGN;
   const AttnGeom geom = attn_geom(*kv, *attn, T);
-  const size_t need = attn_workspace(*kv, geom);
+  const size_t need = attn_workspace(*kv, *attn);
   if (need && !workspace_dev) return MDBF_EINVAL;
   if (workspace_bytes < need) return MDBF_EWORKSPACE;
   const int group = attn->q_heads / kv->kv_heads;
@@ -1086,7 +1167,7 @@ int mdbf_kv_attention(const mdbf_kv_t* kv, const mdbf_attn_t* attn, const void* 
   a.kv_heads = kv->kv_heads, a.group = group, a.head_dim = kv->head_dim;
   a.page_shift = kv_page_shift(kv->page_size), a.causal = attn->flags & MDBF_ATTN_CAUSAL, a.window = attn->window;
   a.row_tiles = geom.row_tiles, a.part = (float*)workspace_dev;
-  a.join_rows = (int)std::min<int64_t>((int64_t)std::min(attn->max_fresh, T) * a.group, kRows);
+  a.join_rows = (int)std::min<int64_t>((int64_t)std::min(attn->max_fresh, T) * a.group, geom.many ? kManyRows : kRows);
   a.scale = (float)(fabs((double)attn->scale) * 1.4426950408889634), a.flip = attn->scale < 0 ? 0x80008000u : 0u;
   int bits = 0;
   while ((1 << bits) < group) ++bits;
