@@ -320,8 +320,8 @@ int mdbf_kv_page_bytes(const mdbf_kv_t* kv, size_t* bytes_out);
  *   slots, positions (T)  of every new token, requests one after the other; -1 in the entries behind the last
  *   taken_out             taken plus the pages used      status              0, or the sum of MDBF_KV_* below
  * If status is not 0 the step is refused as a whole: tables stay as they are, taken_out = taken, lengths = cached (0 where that is negative),
- * cu is 0, slots and positions are -1 throughout, so that launches behind it do nothing.  taken_out may be taken.
- * One launch, two for long steps. */
+ * cu is 0, slots and positions are -1 throughout, so that launches behind it do nothing.  taken_out may be taken; no other
+ * output may overlap an input.  One launch, two for long steps. */
 #define MDBF_KV_BAD_LENGTH 1   /* a negative count, or a length beyond 2^31 - 1 */
 #define MDBF_KV_BAD_WIDTH 2    /* a request needs more pages than its table's row has room for */
 #define MDBF_KV_BAD_TOKENS 4   /* more new tokens than T */
@@ -357,7 +357,7 @@ typedef struct {
  *   q_dev, k_dev     T rows of q_heads resp. kv_heads x head_dim, row strides ldq, ldk (any, at least the row)
  *   q_weight_dev, k_weight_dev   head_dim fp32, or null
  *   rope_dev         rope_rows x rot_dim fp32: a position's rot_dim / 2 cosines, then its sines
- *   positions_dev    T int32.  Negative (padding): the token's rows become zeros and nothing is cached.  At or beyond rope_rows: the rotated
+ *   positions_dev    T int32 (neither is read where rot_dim is 0).  Negative (padding): the token's rows become zeros and nothing is cached.  At or beyond rope_rows: the rotated
  *                    channels become NaN
  *   q_out_dev        row stride ldqo; k_out_dev likewise, or null if only the cache is wanted
  * Outputs may be the inputs themselves where strides and types agree.
@@ -384,9 +384,12 @@ typedef struct {
  * come from the cache (the new tokens' own too: append first).  q_dev, out_dev: T rows of q_heads x head_dim of the cache's
  * dtype, row strides ldq, ldo.  Rows behind the last request's are left as they are; a token that sees nothing gets zeros.
  * What a token does not see has no influence on its row, whatever the bytes there are; a page number outside the pool reads as NaN.
- * Lengths are cut to what the table's row covers, fresh counts to T.  Scores, running maxima and sums are fp32; products are of the
- * cache's dtype, whose only rounding is that of the softmax's numerators.  Repeated calls return the same bits.
- * The workspace (host arithmetic only) holds partial results where a long cache is split among workgroups; it may be null if 0 bytes are needed. */
+ * Lengths are cut to what the table's row covers, fresh counts to T.  Scores, running maxima and sums are fp32.  Rounded are the
+ * softmax's numerators, once to the cache's dtype, and, in calls with many new tokens, the queries, to 2^-14 (bf16) or 2^-18 (fp16) of the
+ * largest of each 32 channels (a value down to a 64th of it is exact).  Repeated calls return the same bits.
+ * The workspace holds partial results where the work on long caches is cut among workgroups; it may be null where 0 bytes are needed.  Its size
+ * (host arithmetic only) does not depend on requests and T, and never shrinks with max_fresh and max_length: a buffer for the largest
+ * call serves all of the same heads. */
 int mdbf_kv_attention_workspace_bytes(const mdbf_kv_t* kv, const mdbf_attn_t* attn, int requests, int T, size_t* bytes_out);
 int mdbf_kv_attention(const mdbf_kv_t* kv, const mdbf_attn_t* attn, const void* cache_dev, size_t cache_bytes,
                       const int32_t* table_dev, int64_t table_ld, int table_width, const int32_t* cu_dev,

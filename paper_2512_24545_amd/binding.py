@@ -7,6 +7,7 @@ be loaded (and cannot be built), importing callers get an exception.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 
 import numpy as np
@@ -423,29 +424,43 @@ class KVSlots:
 
     def __init__(self, requests, tokens, device="cuda:0"):
         torch = _torch()
-        e = lambda n, t=torch.int32: torch.empty(n, dtype=t, device=device)
-        self.lengths, self.cu, self.positions, self.taken, self.status = e(requests), e(requests + 1), e(tokens), e(1), e(1)
-        self.slots = e(tokens, torch.int64)
+        ints = torch.empty(2 * requests + 3 + tokens, dtype=torch.int32, device=device)
+        self.lengths, self.cu, self.positions, self.taken, self.status = ints.split((requests, requests + 1, tokens, 1, 1))
+        self.slots = torch.empty(tokens, dtype=torch.int64, device=device)
 
 
-def _int_tensor(t, n=None, bits=32):
-    torch = _torch()
-    return t.is_cuda and t.dtype == (torch.int32 if bits == 32 else torch.int64) and t.is_contiguous() and (n is None or t.numel() == n)
+# (Steps of small batches take the host as long as the device: in these calls attributes are asked for once, descriptions of equal
+# sizes are made once, and checks are plain comparisons.)
+def _ints(t, n, dtype=None):
+    """Whether t is a contiguous CUDA tensor of n int32 (or the given type)."""
+    return t.dtype == (dtype or _torch_module.int32) and t.is_contiguous() and t.numel() == n and t.is_cuda
+
+
+def _row_stride(x, row):
+    """Row stride of (T, heads, d) whose heads lie side by side, `row` = heads * d."""
+    s = x.stride()
+    assert x.is_cuda and s[2] == 1 and (s[1] == x.shape[2] or x.shape[1] == 1), "rows of heads side by side are needed"
+    return s[0] if s[0] >= row or x.shape[0] > 1 else row
 
 
 def mdbf_kv_slots(cached, fresh, table, free_pages, taken, page_size, tokens, out=None, stream=None):
     """Block tables and slot map of a step: int32 CUDA tensors cached, fresh (requests), table (requests x width, updated in
     place), free_pages, taken (one entry).  tokens: room for the step's new tokens.  Returns a KVSlots (`out` if given;
     out.taken may be `taken`).  Nothing is read back: out.status is on the device."""
+    torch = _torch()
     n = cached.numel()
-    assert _int_tensor(cached) and _int_tensor(fresh, n) and _int_tensor(free_pages) and _int_tensor(taken, 1)
-    assert table.is_cuda and table.dtype == cached.dtype and table.dim() == 2 and table.shape[0] == n and table.stride(1) == 1
-    o = KVSlots(n, tokens, cached.device) if out is None else out
-    if out is not None:
-        assert _int_tensor(o.lengths, n) and _int_tensor(o.cu, n + 1) and _int_tensor(o.positions, tokens)
-        assert _int_tensor(o.slots, tokens, 64) and _int_tensor(o.taken, 1) and _int_tensor(o.status, 1)
-    status = (_lib or lib()).mdbf_kv_slots(n, page_size, cached.data_ptr(), fresh.data_ptr(), table.data_ptr(), table.stride(0), table.shape[1],
-                                           free_pages.data_ptr(), free_pages.numel(), taken.data_ptr(), tokens, o.lengths.data_ptr(),
+    assert _ints(cached, n) and _ints(fresh, n) and _ints(taken, 1) and _ints(free_pages, free_pages.numel())
+    rows, width = table.shape
+    ld, one = table.stride()
+    assert table.is_cuda and table.dtype == torch.int32 and rows == n and (one == 1 or width == 1)
+    o = out
+    if o is None:
+        o = KVSlots(n, tokens, cached.device)
+    else:
+        assert _ints(o.lengths, n) and _ints(o.cu, n + 1) and _ints(o.positions, tokens)
+        assert _ints(o.slots, tokens, torch.int64) and _ints(o.taken, 1) and _ints(o.status, 1)
+    status = (_lib or lib()).mdbf_kv_slots(n, page_size, cached.data_ptr(), fresh.data_ptr(), table.data_ptr(), ld if ld >= width or n > 1 else width,
+                                           width, free_pages.data_ptr(), free_pages.numel(), taken.data_ptr(), tokens, o.lengths.data_ptr(),
                                            o.cu.data_ptr(), o.slots.data_ptr(), o.positions.data_ptr(), o.taken.data_ptr(),
                                            o.status.data_ptr(), _stream_ptr(stream))
     if status:
@@ -453,38 +468,36 @@ def mdbf_kv_slots(cached, fresh, table, free_pages, taken, page_size, tokens, ou
     return o
 
 
-def _heads(x, d=None):
-    """Rows of heads (T, heads, d), the heads of a row side by side: its row stride."""
-    T, H, D = x.shape
-    s = x.stride()
-    assert x.is_cuda and s[2] == 1 and (s[1] == D or H == 1) and (d is None or D == d), "rows of heads side by side are needed"
-    return s[0] if T > 1 else max(s[0], H * D)
-
-
 def mdbf_kv_append(cache, k, v, slots, stream=None):
     """Writes the rows of k and v (T, kv_heads, head_dim; f16/bf16/f32) to the cache's slots (int64; outside of the pool: skipped)."""
-    T = k.shape[0]
-    assert k.shape == v.shape == (T, cache.kv_heads, cache.head_dim) and k.dtype == v.dtype and _int_tensor(slots, T, 64)
-    status = (_lib or lib()).mdbf_kv_append(cache.desc, *cache.args, k.data_ptr(), _heads(k), v.data_ptr(), _heads(v),
-                                            DTYPE_CODE[_dtype_name(k)], slots.data_ptr(), T, _stream_ptr(stream))
+    torch = _torch()
+    shape = k.shape
+    T, H, d = shape
+    assert H == cache.kv_heads and d == cache.head_dim and v.shape == shape and k.dtype == v.dtype and _ints(slots, T, torch.int64)
+    status = (_lib or lib()).mdbf_kv_append(cache.desc, *cache.args, k.data_ptr(), _row_stride(k, H * d), v.data_ptr(), _row_stride(v, H * d),
+                                            DTYPE_CODE[_DTYPE_NAME[k.dtype]], slots.data_ptr(), T, _stream_ptr(stream))
     if status:
         _check(status, "mdbf_kv_append")
 
 
 def mdbf_kv_read(cache, slots, out=None, stream=None):
     """The keys and values that the slots hold: two tensors (T, kv_heads, head_dim), `out` or new ones of the cache's dtype."""
-    T = slots.numel()
-    shape = (T, cache.kv_heads, cache.head_dim)
+    torch = _torch()
+    T, H, d = slots.numel(), cache.kv_heads, cache.head_dim
     if out is None:
-        torch = _torch()
-        out = tuple(torch.empty(shape, dtype=_torch_dtype(cache.dtype), device=slots.device) for _ in range(2))
+        out = tuple(torch.empty((T, H, d), dtype=_TORCH_DTYPE[cache.dtype], device=slots.device) for _ in range(2))
     k, v = out
-    assert k.shape == v.shape == shape and k.dtype == v.dtype and _int_tensor(slots, T, 64)
-    status = (_lib or lib()).mdbf_kv_read(cache.desc, *cache.args, slots.data_ptr(), T, k.data_ptr(), _heads(k), v.data_ptr(), _heads(v),
-                                          DTYPE_CODE[_dtype_name(k)], _stream_ptr(stream))
+    assert k.shape == v.shape == (T, H, d) and k.dtype == v.dtype and _ints(slots, T, torch.int64)
+    status = (_lib or lib()).mdbf_kv_read(cache.desc, *cache.args, slots.data_ptr(), T, k.data_ptr(), _row_stride(k, H * d), v.data_ptr(),
+                                          _row_stride(v, H * d), DTYPE_CODE[_DTYPE_NAME[k.dtype]], _stream_ptr(stream))
     if status:
         _check(status, "mdbf_kv_read")
     return k, v
+
+
+@functools.lru_cache(maxsize=256)
+def _rope_desc(*values):
+    return RopeDesc(*values)
 
 
 def mdbf_qk_norm_rope(q, k, rope, positions, q_weight=None, k_weight=None, eps=1e-6, interleaved=False, y_dtype=None, q_out=None,
@@ -493,48 +506,62 @@ def mdbf_qk_norm_rope(q, k, rope, positions, q_weight=None, k_weight=None, eps=1
     then sines of a position, or None; positions: int32 (T).  Returns (q_out, k_out), new tensors of y_dtype (that of q) unless given.
     With a cache, the same launch writes k and v to its slots; k_out is then None unless it was given."""
     torch = _torch()
-    T, Hq, d = q.shape
-    Hkv = k.shape[1]
-    assert k.shape == (T, Hkv, d) and k.dtype == q.dtype
-    name = _DTYPE_NAME[q.dtype]
+    q_shape, k_shape, x_dtype = q.shape, k.shape, q.dtype
+    T, Hq, d = q_shape
+    Hkv = k_shape[1]
+    assert k_shape[0] == T and k_shape[2] == d and k.dtype == x_dtype
+    name = _DTYPE_NAME[x_dtype]
     if q_out is None:
         q_out = torch.empty((T, Hq, d), dtype=_TORCH_DTYPE[y_dtype or name], device=q.device)
-    if k_out is None and cache is None:
-        k_out = torch.empty((T, Hkv, d), dtype=q_out.dtype, device=q.device)
-    assert q_out.shape == q.shape and (k_out is None or (k_out.shape == k.shape and k_out.dtype == q_out.dtype))
+    else:
+        assert q_out.shape == q_shape
+    out_dtype = q_out.dtype
+    if k_out is None:
+        if cache is None:
+            k_out = torch.empty((T, Hkv, d), dtype=out_dtype, device=q.device)
+    else:
+        assert k_out.shape == k_shape and k_out.dtype == out_dtype
     for w in (q_weight, k_weight):
-        assert w is None or (w.is_cuda and w.dtype == torch.float32 and w.is_contiguous() and w.numel() == d), "norm weights are head_dim fp32"
+        assert w is None or _ints(w, d, torch.float32), "norm weights are head_dim fp32"
     rows = rot = 0
     if rope is not None:
         rows, rot = rope.shape
-        assert rope.is_cuda and rope.dtype == torch.float32 and rope.is_contiguous() and _int_tensor(positions, T)
-    desc = RopeDesc(Hq, Hkv, d, rot, rows, DTYPE_CODE[name], DTYPE_CODE[_DTYPE_NAME[q_out.dtype]],
-                    MDBF_ROPE_INTERLEAVED if interleaved else 0, eps)
-    ptr = lambda t: None if t is None else t.data_ptr()
+        assert _ints(rope, rows * rot, torch.float32) and _ints(positions, T)
+    desc = _rope_desc(Hq, Hkv, d, rot, rows, DTYPE_CODE[name], DTYPE_CODE[_DTYPE_NAME[out_dtype]], MDBF_ROPE_INTERLEAVED if interleaved else 0, eps)
     kv = (None, None, 0, None, 0, None)
     if cache is not None:
-        assert v.shape == k.shape and v.dtype == k.dtype and _int_tensor(slots, T, 64)
-        kv = (cache.desc, *cache.args, v.data_ptr(), _heads(v), slots.data_ptr())
-    status = (_lib or lib()).mdbf_qk_norm_rope(desc, q.data_ptr(), _heads(q), k.data_ptr(), _heads(k), ptr(q_weight), ptr(k_weight), ptr(rope),
-                                               ptr(positions) if rot else None, T, q_out.data_ptr(), _heads(q_out), ptr(k_out),
-                                               0 if k_out is None else _heads(k_out), *kv, _stream_ptr(stream))
+        assert v.shape == k_shape and v.dtype == x_dtype and _ints(slots, T, torch.int64)
+        kv = (cache.desc, *cache.args, v.data_ptr(), _row_stride(v, Hkv * d), slots.data_ptr())
+    status = (_lib or lib()).mdbf_qk_norm_rope(
+        desc, q.data_ptr(), _row_stride(q, Hq * d), k.data_ptr(), _row_stride(k, Hkv * d), None if q_weight is None else q_weight.data_ptr(),
+        None if k_weight is None else k_weight.data_ptr(), rope.data_ptr() if rot else None, positions.data_ptr() if rot else None, T,
+        q_out.data_ptr(), _row_stride(q_out, Hq * d), None if k_out is None else k_out.data_ptr(),
+        0 if k_out is None else _row_stride(k_out, Hkv * d), *kv, _stream_ptr(stream))
     if status:
         _check(status, "mdbf_qk_norm_rope")
     return q_out, k_out
 
 
-def _attn_desc(cache, q_heads, max_fresh, max_length, causal, window, scale):
-    return AttnDesc(q_heads, MDBF_ATTN_CAUSAL if causal else 0, window, max_fresh, max_length,
-                    cache.head_dim ** -0.5 if scale is None else scale)
+@functools.lru_cache(maxsize=1024)
+def _attn_desc(*values):
+    return AttnDesc(*values)
+
+
+@functools.lru_cache(maxsize=1024)
+def _attention_workspace_bytes(pages, kv_heads, head_dim, page_size, dtype, *attn):
+    out = C.c_size_t(0)
+    _check(lib().mdbf_kv_attention_workspace_bytes(KvDesc(pages, kv_heads, head_dim, page_size, dtype), AttnDesc(*attn), 1, 1, C.byref(out)),
+           "mdbf_kv_attention_workspace_bytes")
+    return out.value
 
 
 def mdbf_kv_attention_workspace(cache, q_heads, requests, tokens, max_fresh, max_length, causal=True, window=0):
     """The workspace (uint8 CUDA tensor, or None where none is needed) of mdbf_kv_attention calls of these sizes."""
-    out = C.c_size_t(0)
-    d = _attn_desc(cache, q_heads, max_fresh, max_length, causal, window, 1.0)
-    _check(lib().mdbf_kv_attention_workspace_bytes(cache.desc, d, requests, tokens, C.byref(out)), "mdbf_kv_attention_workspace_bytes")
+    d = cache.desc
+    n = _attention_workspace_bytes(d.pages, d.kv_heads, d.head_dim, d.page_size, d.dtype, q_heads, MDBF_ATTN_CAUSAL if causal else 0, window,
+                                   max_fresh, max_length, 1.0)
     torch = _torch()
-    return torch.empty(out.value, dtype=torch.uint8, device=cache.buffer.device) if out.value else None
+    return torch.empty(n, dtype=torch.uint8, device=cache.buffer.device) if n else None
 
 
 def mdbf_kv_attention(cache, q, table, cu, lengths, max_fresh, max_length, scale=None, causal=True, window=0, out=None, workspace=None,
@@ -542,20 +569,25 @@ def mdbf_kv_attention(cache, q, table, cu, lengths, max_fresh, max_length, scale
     """Attention of the new tokens' queries q (T, q_heads, d; the cache's dtype) over the cache.  table (requests x width), cu (requests + 1)
     and lengths (requests) are int32 CUDA tensors as mdbf_kv_slots leaves them; max_fresh, max_length: bounds of the
     new tokens and the length of a request (launch sizes).  Returns out (T, q_heads, d)."""
-    T, Hq, d = q.shape
+    torch = _torch()
+    shape, dtype = q.shape, q.dtype
+    T, Hq, d = shape
     n = lengths.numel()
-    assert d == cache.head_dim and _dtype_name(q) == cache.dtype and _int_tensor(lengths) and _int_tensor(cu, n + 1)
-    assert table.is_cuda and table.dtype == lengths.dtype and table.dim() == 2 and table.shape[0] == n and table.stride(1) == 1
+    assert d == cache.head_dim and _DTYPE_NAME[dtype] == cache.dtype and _ints(lengths, n) and _ints(cu, n + 1)
+    rows, width = table.shape
+    ld, one = table.stride()
+    assert table.is_cuda and table.dtype == torch.int32 and rows == n and (one == 1 or width == 1)
     if out is None:
-        out = _torch().empty((T, Hq, d), dtype=q.dtype, device=q.device)
-    assert out.shape == q.shape and out.dtype == q.dtype
+        out = torch.empty(shape, dtype=dtype, device=q.device)
+    else:
+        assert out.shape == shape and out.dtype == dtype
     if workspace is None:
         workspace = mdbf_kv_attention_workspace(cache, Hq, n, T, max_fresh, max_length, causal, window)
-    desc = _attn_desc(cache, Hq, max_fresh, max_length, causal, window, scale)
-    status = (_lib or lib()).mdbf_kv_attention(cache.desc, desc, *cache.args, table.data_ptr(), table.stride(0), table.shape[1], cu.data_ptr(),
-                                               lengths.data_ptr(), n, q.data_ptr(), _heads(q), T, out.data_ptr(), _heads(out),
-                                               None if workspace is None else workspace.data_ptr(),
-                                               0 if workspace is None else workspace.numel(), _stream_ptr(stream))
+    desc = _attn_desc(Hq, MDBF_ATTN_CAUSAL if causal else 0, window, max_fresh, max_length, d ** -0.5 if scale is None else scale)
+    ws = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
+    status = (_lib or lib()).mdbf_kv_attention(cache.desc, desc, *cache.args, table.data_ptr(), ld if ld >= width or n > 1 else width, width,
+                                               cu.data_ptr(), lengths.data_ptr(), n, q.data_ptr(), _row_stride(q, Hq * d), T, out.data_ptr(),
+                                               _row_stride(out, Hq * d), *ws, _stream_ptr(stream))
     if status:
         _check(status, "mdbf_kv_attention")
     return out

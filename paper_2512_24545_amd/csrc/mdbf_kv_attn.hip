@@ -805,37 +805,6 @@ __global__ __launch_bounds__(64 * kManyWaves, D <= 128 ? 2 : 1) void attn_many_k
     Sees me = sees(a, rq, i);
     if (!valid) me.hi = me.lo = 0;
 
-    // queries: channels 64 s + 32 hh + 0 .. 31 of the lane's row for step s
-    Limbs<NL> ql[ST];
-    bool finite = true;
-    const int64_t q_at = (int64_t)(rq.start + i) * a.ldq + (int64_t)(head * a.group + g) * D + 32 * hh;
-#pragma unroll
-    for (int s = 0; s < ST; ++s) {
-      float q[32];
-      U32x4 raw[4] = {};
-      if (valid) {
-        const MDBF_GLOBAL uint16_t* p = (const MDBF_GLOBAL uint16_t*)a.q + q_at + 64 * s;
-        if (a.wide_q) {
-#pragma unroll
-          for (int w = 0; w < 4; ++w) raw[w] = ((const MDBF_GLOBAL U32x4*)p)[w];
-        } else {
-#pragma unroll
-          for (int w = 0; w < 16; ++w) raw[w / 4][w % 4] = (uint32_t)p[2 * w] | ((uint32_t)p[2 * w + 1] << 16);
-        }
-      }
-#pragma unroll
-      for (int w = 0; w < 16; ++w) {
-        const uint32_t x = raw[w / 4][w % 4] ^ a.flip;
-        if (DT == MDBF_F16) {
-          const F16x2 v = __builtin_bit_cast(F16x2, x);
-          q[2 * w] = (float)v[0], q[2 * w + 1] = (float)v[1];
-        } else {
-          q[2 * w] = __builtin_bit_cast(float, x << 16), q[2 * w + 1] = __builtin_bit_cast(float, x & 0xffff0000u);
-        }
-      }
-      finite &= ql[s].set(q);
-    }
-
     // a thread's units of a tile: its page is looked up a tile before its codes are requested
     U32x4 kc[U], vc[U];
     uint32_t ks[U], vs[U];
@@ -882,6 +851,44 @@ __global__ __launch_bounds__(64 * kManyWaves, D <= 128 ? 2 : 1) void attn_many_k
       }
     };
 
+    // the first tile is on its way while the queries are prepared
+    const int tiles = sp.hi > sp.lo ? work.u1 - work.u0 : 0, begin = sp.from + work.u0 * kTile;
+    look_up(begin);
+    // queries: channels 64 s + 32 hh + 0 .. 31 of the lane's row for step s
+    U32x4 raw[ST][4] = {};
+    if (valid) {
+      const MDBF_GLOBAL uint16_t* p = (const MDBF_GLOBAL uint16_t*)a.q + (int64_t)(rq.start + i) * a.ldq + (int64_t)(head * a.group + g) * D + 32 * hh;
+#pragma unroll
+      for (int s = 0; s < ST; ++s) {
+        if (a.wide_q) {
+#pragma unroll
+          for (int w = 0; w < 4; ++w) raw[s][w] = ((const MDBF_GLOBAL U32x4*)(p + 64 * s))[w];
+        } else {
+#pragma unroll
+          for (int w = 0; w < 16; ++w) raw[s][w / 4][w % 4] = (uint32_t)p[64 * s + 2 * w] | ((uint32_t)p[64 * s + 2 * w + 1] << 16);
+        }
+      }
+    }
+    request(begin);
+    look_up(begin + kTile);
+    Limbs<NL> ql[ST];
+    bool finite = true;
+#pragma unroll
+    for (int s = 0; s < ST; ++s) {
+      float q[32];
+#pragma unroll
+      for (int w = 0; w < 16; ++w) {
+        const uint32_t x = raw[s][w / 4][w % 4] ^ a.flip;
+        if (DT == MDBF_F16) {
+          const F16x2 v = __builtin_bit_cast(F16x2, x);
+          q[2 * w] = (float)v[0], q[2 * w + 1] = (float)v[1];
+        } else {
+          q[2 * w] = __builtin_bit_cast(float, x << 16), q[2 * w + 1] = __builtin_bit_cast(float, x & 0xffff0000u);
+        }
+      }
+      finite &= ql[s].set(q);
+    }
+
     float m = -INFINITY, l = finite ? 0.0f : NAN;      // (a query that is not finite has no finite result)
     uint32_t nan_blocks = 0;
     F32x16 acc[CT];
@@ -890,11 +897,7 @@ __global__ __launch_bounds__(64 * kManyWaves, D <= 128 ? 2 : 1) void attn_many_k
 #pragma unroll
       for (int j = 0; j < 16; ++j) acc[c][j] = 0;
 
-    const int tiles = sp.hi > sp.lo ? work.u1 - work.u0 : 0, begin = sp.from + work.u0 * kTile;
     if (tiles) {
-      look_up(begin);
-      request(begin);
-      look_up(begin + kTile);
       put(lds[0], begin);
       if (tiles > 1) {
         request(begin + kTile);
@@ -934,6 +937,16 @@ __global__ __launch_bounds__(64 * kManyWaves, D <= 128 ? 2 : 1) void attn_many_k
           for (int f = 0; f < 2; ++f) z[f] = mx32<2 * (s & 1), L>(codes[f], sc[f][s / 2], ql[s].limb[L], ql[s].scales, z[f]);
         }, std::make_integer_sequence<int, NL>{});
       }, std::make_integer_sequence<int, ST>{});
+      U32x2 v[2][CT][2];
+      auto read = [&](int k) __attribute__((always_inline)) {
+        const unsigned char* from = in.values + (16 * k + 4 * hh + ((lane & 15) >> 2)) * VROW + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+#pragma unroll
+        for (int c = 0; c < CT; ++c) {
+          v[k & 1][c][0] = __builtin_bit_cast(U32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((MDBF_LDS S16x4*)(from + block_at(c))));
+          v[k & 1][c][1] = __builtin_bit_cast(U32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((MDBF_LDS S16x4*)(from + block_at(c) + 8 * VROW)));
+        }
+      };
+      read(0);
       if (t0 < sp.all_lo || t0 + kTile > sp.all_hi) {      // not every row sees every token
 #pragma unroll
         for (int f = 0; f < 2; ++f)
@@ -991,19 +1004,14 @@ __global__ __launch_bounds__(64 * kManyWaves, D <= 128 ? 2 : 1) void attn_many_k
         }
       }
 
-      // results: 16 tokens at a time, in the order of the scores' registers; all channels' values of the 16 are read before the
-      // first product
+      // results: 16 tokens at a time, in the order of the scores' registers; the values of the next 16 are read before the products
+      // of these
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        U32x2 v[CT][2];
-        const unsigned char* from = in.values + (16 * k + 4 * hh + ((lane & 15) >> 2)) * VROW + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+        if (k < 3) read(k + 1);
 #pragma unroll
-        for (int c = 0; c < CT; ++c) {
-          v[c][0] = __builtin_bit_cast(U32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((MDBF_LDS S16x4*)(from + block_at(c))));
-          v[c][1] = __builtin_bit_cast(U32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((MDBF_LDS S16x4*)(from + block_at(c) + 8 * VROW)));
-        }
-#pragma unroll
-        for (int c = 0; c < CT; ++c) acc[c] = mma32<DT>(U32x4{v[c][0][0], v[c][0][1], v[c][1][0], v[c][1][1]}, pf[k], acc[c]);
+        for (int c = 0; c < CT; ++c)
+          acc[c] = mma32<DT>(U32x4{v[k & 1][c][0][0], v[k & 1][c][0][1], v[k & 1][c][1][0], v[k & 1][c][1][1]}, pf[k], acc[c]);
       }
       __syncthreads();
     }
@@ -1049,45 +1057,50 @@ static int check_attn(const mdbf_kv_t* kv, const mdbf_attn_t* at, int requests, 
   return MDBF_OK;
 }
 
-// Which kernel a call takes, and whether its work is cut into shares: by estimates of the time from the sizes that the caller
-// bounds the call by, in us.  A workgroup of the few-row kernel takes 1 us per unit where the device is full of them, one of the
-// prompts' kernel 2 with two on a compute unit and 1.3 with one (heads of 128; the others scale alike); the join is a launch.
-#ifndef SW
-#define SW 10.0
-#define FU 1.0
-#endif
-constexpr int kWhole = 1024;      // tokens up to which few rows' tiles are not cut
-static bool attn_cuts(const mdbf_attn_t& at) { return (at.window ? std::min(at.max_length, at.window) : at.max_length) > kWhole; }
+// Which kernel a call takes, and whether its work is cut into shares: by estimates of the time, in us, from the sizes that the
+// caller bounds the call by.  Fitted to calls of 1 to 8192 new tokens behind 0 to 30000; what they get wrong costs up to a fifth
+// where requests are of unequal lengths.  128 new tokens behind 30000, 32 heads on 8 of 128: few rows 163 us, prompts 619 whole and
+// 83 cut; 33 behind 2000 of 8 requests: 26, 48 and 28; 2048 behind 14336: 1288, 471 and 523.
+constexpr int kWhole = 1024;      // tokens up to which nothing is cut: the join, a launch, would cost more
+struct AttnCosts {
+  double few;              // a unit of the few-row kernel where it fills the device
+  double one, full;        // one of the prompts' kernel, with one workgroup on a compute unit, and with all that fit
+  double parts;            // the parts that all workgroups of the prompts' kernel leave and the join takes
+  int few_shares, many_shares;
+};
+static AttnCosts attn_costs(int d) {
+  if (d == 64) return {1.5, 1.0, 1.1, 12, kFewShares<64>, kManyShares<64>};
+  if (d == 128) return {1.0, 1.25, 1.85, 24, kFewShares<128>, kManyShares<128>};
+  return {1.7, 2.45, 2.6, 24, kFewShares<256>, kManyShares<256>};
+}
 struct AttnGeom {
   int row_tiles;           // of a request and kv head
   bool shares, many;
 };
+static bool attn_cuts(const mdbf_attn_t& at) { return (at.window ? std::min(at.max_length, at.window) : at.max_length) > kWhole; }
 static AttnGeom attn_geom(const mdbf_kv_t& kv, const mdbf_attn_t& at, int T) {
-  const int64_t rows = (int64_t)std::min(at.max_fresh, T) * (at.q_heads / kv.kv_heads), heads = kv.kv_heads;
-  const bool causal = at.flags & MDBF_ATTN_CAUSAL;
-  const int fresh = std::min(at.max_fresh, T), requests = at.max_fresh ? (T + fresh - 1) / fresh : 1;      // with as many new tokens
-  auto tiles_of = [&](int per) { return (rows + per - 1) / per; };
+  const AttnCosts k = attn_costs(kv.head_dim);
+  const int fresh = std::min(at.max_fresh, T), requests = (T + fresh - 1) / fresh;      // requests with as many new tokens as any
+  const double rows = (double)fresh * (at.q_heads / kv.kv_heads);
+  auto tiles_of = [&](int per) { return ceil(rows / per); };
+  // units of a row tile: of the one that sees most, and on average
   auto units_of = [&](int per, bool most) {
     double span = at.max_length;
-    if (causal && !most) span -= std::min<double>(fresh, span) / 2;
-    if (at.window) span = std::min<double>(span, (double)at.window + per * fresh / (double)rows);
+    if ((at.flags & MDBF_ATTN_CAUSAL) && !most) span -= std::min<double>(fresh, span) / 2;
+    if (at.window) span = std::min<double>(span, at.window + per * fresh / rows);
     return span / kTile + 1;
   };
-  const double few_tiles = (double)requests * heads * tiles_of(kRows), many_tiles = (double)requests * heads * tiles_of(kManyRows);
-  const double few_shares = kv.head_dim == 64 ? kFewShares<64> : kv.head_dim == 128 ? kFewShares<128> : kFewShares<256>;
-  const double many_shares = kv.head_dim <= 128 ? kManyShares<128> : kManyShares<256>;
   const bool cuts = attn_cuts(at);
-  const double few = FU * std::max(few_tiles * (units_of(kRows, false) + kRowsCost) / few_shares, cuts ? 0.0 : units_of(kRows, true)) + (cuts ? 6.0 : 0.0);
-  const double whole = std::max((many_tiles <= many_shares / 2 ? 1.3 : 2.0) * (units_of(kManyRows, true) + kManyCost),
-                                2.0 * many_tiles * (units_of(kManyRows, false) + kManyCost) / many_shares);
-  const double cut = 2.0 * many_tiles * (units_of(kManyRows, false) + kManyCost) / many_shares + SW;
+  const double few_tiles = requests * (double)kv.kv_heads * tiles_of(kRows), many_tiles = requests * (double)kv.kv_heads * tiles_of(kManyRows);
+  double few = k.few * few_tiles * (units_of(kRows, false) + kRowsCost) / k.few_shares + 8;
+  if (!cuts) few = std::max(few, k.few * units_of(kRows, true));
+  const double even = many_tiles * (units_of(kManyRows, false) + kManyCost) / k.many_shares, crowd = std::min(1.0, std::max(0.0, many_tiles / 256 - 1));
+  const double whole = std::max((k.one + crowd * (k.full - k.one)) * (units_of(kManyRows, true) + kManyCost), k.full * even);
+  const double cut = k.full * even + 12 + k.parts * std::min(1.0, even / kLeastShare);
   AttnGeom g;
-  g.many = rows > kRows && std::min(whole, cut) < few;
+  g.many = rows > kRows && std::min(whole, cuts ? cut : whole) < few;
   g.shares = cuts && (!g.many || cut < whole);
-#ifdef FORCE
-  g.many = FORCE > 0; g.shares = cuts && (FORCE != 1);
-#endif
-  g.row_tiles = (int)std::min<int64_t>(tiles_of(g.many ? kManyRows : kRows), 1 << 16);
+  g.row_tiles = (int)std::min(tiles_of(g.many ? kManyRows : kRows), 65536.0);
   return g;
 }
 // One size for all calls with these heads and bounds or smaller ones; nothing where no cache is long enough to be cut.
@@ -1160,7 +1173,7 @@ int mdbf_kv_attention(const mdbf_kv_t* kv, const mdbf_attn_t* attn, const void* 
   if (need && !workspace_dev) return MDBF_EINVAL;
   if (workspace_bytes < need) return MDBF_EWORKSPACE;
   const int group = attn->q_heads / kv->kv_heads;
-  if ((int64_t)requests * kv->kv_heads * geom.row_tiles > 0x7fffffff || (int64_t)T * group > 0x7fff0000) return MDBF_EUNSUPPORTED;
+  if ((int64_t)requests * kv->kv_heads * geom.row_tiles > 0x7fffffff || (int64_t)T * group > 0x70000000) return MDBF_EUNSUPPORTED;
   AttnArgs a = {};
   a.cache = (const uint8_t*)cache_dev, a.table = table_dev, a.cu = cu_dev, a.lengths = lengths_dev, a.q = q_dev, a.out = out_dev;
   a.table_ld = table_ld, a.ldq = ldq, a.ldo = ldo, a.table_width = table_width, a.requests = requests, a.T = T, a.pages = kv->pages;
