@@ -140,14 +140,20 @@ __device__ __forceinline__ int64_t uniform(int64_t x) {
   return ((int64_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
 }
 
-// sum over a workgroup of four waves up to and with this thread's x; `total` of all
-__device__ __forceinline__ int64_t scan_256(int64_t x, int64_t& total, int64_t* waves) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// sum over a wave up to and with this lane's x
+__device__ __forceinline__ int64_t scan_64(int64_t x) {
+  const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
     const int64_t u = __shfl_up(x, o);
     if (lane >= o) x += u;
   }
+  return x;
+}
+// sum over a workgroup of four waves up to and with this thread's x; `total` of all
+__device__ __forceinline__ int64_t scan_256(int64_t x, int64_t& total, int64_t* waves) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  x = scan_64(x);
   __syncthreads();
   if (lane == 63) waves[wave] = x;
   __syncthreads();
@@ -178,12 +184,12 @@ struct Work {
   Request rq;
   Span sp;
 
-  // units of a request over its row tiles and kv heads
-  __device__ static __forceinline__ int64_t units_of(const AttnArgs& a, int b) {
+  // of a request's row tiles from, from + step, ..., in all kv heads
+  __device__ static __forceinline__ int64_t units_of(const AttnArgs& a, int b, int from, int step) {
     const Request r = request_of(a, b);
     const int rows = r.fresh * a.group;
     int64_t n = 0;
-    for (int t = 0; t * ROWS < rows; ++t) n += span_of<ROWS>(a, r, t, rows).units + COST;
+    for (int t = from; t * ROWS < rows; t += step) n += span_of<ROWS>(a, r, t, rows).units + COST;
     return n * a.kv_heads;
   }
   // the units of the row tile that lie in the share, which goes on with this place among COST + units
@@ -201,23 +207,26 @@ struct Work {
     sp = span_of<ROWS>(a, rq, rt, rows);
     u1 = sp.units;
   }
-  // This workgroup's share: prefix sums over the requests, of up to 64 by every wave for itself, else by the workgroup, 256 at
-  // a time, first of all and then again up to the one where the share begins.  `find`: six words of LDS.
+  // This workgroup's share: prefix sums over the requests, of up to 64 by every wave for itself, which deals its lanes out to
+  // them, else by the workgroup, 256 at a time, first of all and then again up to the one where the share begins; and in that
+  // one over its row tiles, 64 at a time.  1500 rows of 8 heads and 1 kv head of 128 against 9500 tokens, 94 row tiles: 74 us, 93
+  // where a lane went over them one by one.  `find`: six words of LDS.
   __device__ __forceinline__ void first(const AttnArgs& a, int64_t* find) {
     const int tid = threadIdx.x, lane = tid & 63;
     const bool few = a.requests <= 64;
     int64_t total = 0, sum, mine = 0, end = 0;
     if (few) {
-      mine = end = lane < a.requests ? units_of(a, lane) : 0;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const int64_t u = __shfl_up(end, o);
-        if (lane >= o) end += u;
-      }
+      int bits = 6;                    // one lane each, or where there are row tiles to go over 64 >> bits, of 2^bits requests or less
+      if (a.row_tiles > 1) bits = 32 - __builtin_clz(a.requests) - !(a.requests & (a.requests - 1));
+      const int of = lane & ((1 << bits) - 1);
+      if (of < a.requests) mine = units_of(a, of, lane >> bits, 64 >> bits);
+      for (int o = 1 << bits; o < 64; o <<= 1) mine += __shfl_xor(mine, o);
+      if (lane >> bits) mine = 0;
+      end = scan_64(mine);
       total = __shfl(end, 63);
     } else {
       for (int r0 = 0; r0 < a.requests; r0 += 256) {
-        scan_256(r0 + tid < a.requests ? units_of(a, r0 + tid) : 0, sum, find);
+        scan_256(r0 + tid < a.requests ? units_of(a, r0 + tid, 0, 1) : 0, sum, find);
         total += sum;
       }
     }
@@ -234,7 +243,7 @@ struct Work {
     } else {
       int64_t before = 0;
       for (int r0 = 0; r0 < a.requests; r0 += 256) {
-        mine = r0 + tid < a.requests ? units_of(a, r0 + tid) : 0;
+        mine = r0 + tid < a.requests ? units_of(a, r0 + tid, 0, 1) : 0;
         end = before + scan_256(mine, sum, find);
         if (start >= end - mine && start < end) find[4] = r0 + tid, find[5] = end - mine;
         before += sum;
@@ -248,12 +257,20 @@ struct Work {
     rest = uniform(rest);
     rq = request_of(a, b);
     const int rows = rq.fresh * a.group;
-    for (rt = 0;; ++rt) {
-      sp = span_of<ROWS>(a, rq, rt, rows);
-      const int64_t all = (int64_t)(sp.units + COST) * a.kv_heads;
-      if (rest < all) break;
-      rest -= all;
+    rt = 0;
+    for (int t0 = 0; rows > ROWS; t0 += 64) {      // (rest is less than the request's units: one of its row tiles has it)
+      mine = 0;
+      if ((t0 + lane) * ROWS < rows) mine = (int64_t)(span_of<ROWS>(a, rq, t0 + lane, rows).units + COST) * a.kv_heads;
+      end = scan_64(mine);
+      const uint64_t past = __ballot(rest < end);
+      if (past) {
+        rt = t0 + __builtin_ctzll(past);
+        rest = uniform(rest - __shfl(end - mine, rt - t0));
+        break;
+      }
+      rest = uniform(rest - __shfl(end, 63));
     }
+    sp = span_of<ROWS>(a, rq, rt, rows);
     head = (int)(rest / (sp.units + COST));
     cut((int)(rest % (sp.units + COST)));
   }

@@ -47,6 +47,13 @@ def test_many_prompts(gpu, n):
     Step(gpu, lengths, fresh, 4, 1, 64, 16, "f16", seed=n).check()
 
 
+@pytest.mark.parametrize("lengths,fresh", [([4000], [300]), ([2000, 80, 5000], [270, 80, 300])])
+@pytest.mark.parametrize("window", [0, 700])
+def test_more_row_tiles_than_a_wave_has_lanes(gpu, lengths, fresh, window):
+    """32 query heads share one of 64 channels: 300 tokens are 75 tiles of 128 rows or 600 of 16."""
+    Step(gpu, lengths, fresh, 32, 1, 64, 32, "f16", seed=len(fresh)).check(window=window)
+
+
 @pytest.mark.parametrize("heads", [(16, 1), (17, 1), (24, 8)])
 def test_very_unequal_lengths(gpu, heads):
     """Shares that begin and end inside the cost of a row tile, row tiles in one share, in two and in many."""
