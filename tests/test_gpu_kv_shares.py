@@ -101,3 +101,45 @@ def test_a_workspace_for_the_largest_call_serves_smaller_ones(gpu):
             for window in (1, 500, 2000):
                 assert size(fresh, length, window=window) <= size(fresh, length)
     s.check(workspace=torch.empty(largest, dtype=torch.uint8, device="cuda:0"))
+
+
+@pytest.mark.parametrize("requests,cached,fresh,kv_heads", [(3, 100, 1, 8), (2, 0, 40, 32), (1, 1500, 20, 4)])
+def test_the_attention_block_of_a_layer(gpu, requests, cached, fresh, kv_heads):
+    """The whole block as workloads.py runs it, eagerly and from a graph, against the oracles of its parts."""
+    torch, mb = gpu
+    from oracle import kv_oracle as kvo
+    from paper_2512_24545_amd.workloads import AttentionBlock
+    g = torch.Generator(device="cuda:0")
+    g.manual_seed(cached + fresh)
+    b = AttentionBlock(torch, g, requests, cached, fresh, kv_heads)
+    Y = b.step().clone()
+    torch.cuda.synchronize()
+    assert b.places.status.item() == 0
+    # the attention's inputs: what the projections gave, normed and turned; its result against the cache's contents
+    table, d, group = b.table.cpu().numpy(), 128, 32 // kv_heads
+    for r in range(requests):
+        pos = np.arange(cached + fresh)
+        slots = torch.from_numpy(table[r, pos // 64].astype(np.int64) * 64 + pos % 64).cuda()
+        k, v = (x.double().cpu().numpy() for x in mb.mdbf_kv_read(b.cache, slots))
+        rows = slice(r * fresh, (r + 1) * fresh)
+        q_in, k_in, v_in = (x[rows].double().cpu().numpy() for x in b.heads)
+        norm, rope = [w.cpu().numpy() for w in b.norm], b.rope.cpu().numpy()
+        q_ref = kvo.norm_rope(q_in, norm[0], rope, pos[cached:], 1e-6, False)
+        q = b.turned[rows].double().cpu().numpy()
+        assert np.abs(q - q_ref).max() <= 2.0 ** -11 * np.abs(q_ref).max() + 4e-6 * np.abs(q_ref).max()
+        assert np.array_equal(v[cached:], kvo.values(*kvo.quantise(v_in, "f16")))
+        k_ref = kvo.norm_rope(k_in, norm[1], rope, pos[cached:], 1e-6, False)
+        assert np.abs(k[cached:] - k_ref).max() <= np.abs(k_ref).max() / 4        # 4 bits: at most half a step of the largest numbers
+        out = b.out[rows].double().cpu().numpy()
+        for h in (0, 13, 31):
+            ref, mag, den = kvo.attention(q[:, h], k[:, h // group], v[:, h // group], pos[cached:], True, 0, d ** -0.5)
+            from test_gpu_kv import attention_tolerance
+            assert (np.abs(out[:, h] - ref) <= attention_tolerance("f16", ref, mag, den, q[:, h], k[:, h // group], v[:, h // group], d ** -0.5)).all()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        b.step()
+    for _ in range(3):
+        b.Y.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(b.Y, Y)
