@@ -33,7 +33,7 @@ struct AttnArgs {
   uint32_t group_mul, group_shift;      // i / group = i * group_mul >> group_shift for i < 2^31
   float scale;                 // of the scores, times log2(e); its sign is the queries' (flip: 0x80008000)
   uint32_t flip;
-  uint8_t wide_q, wide_o;
+  uint8_t wide_q, wide_o, nth;
 };
 
 template <int DT>
@@ -207,6 +207,29 @@ struct Work {
     sp = span_of<ROWS>(a, rq, rt, rows);
     u1 = sp.units;
   }
+  // All tokens of a row tile, the idx-th of those that 64 requests or less have in a kv head: last ones first (which see most), of
+  // all requests.  A lane counts a request's, then, for a place in the requests, the row tiles at later ones.
+  __device__ __forceinline__ void whole_nth(const AttnArgs& a, int idx, int head_) {
+    const int lane = threadIdx.x & 63;
+    const int mine = lane < a.requests ? (request_of(a, lane).fresh * a.group + ROWS - 1) / ROWS : 0;
+    int all = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) all += __shfl_xor(all, o);
+    if (idx >= __builtin_amdgcn_readfirstlane(all)) return;
+#pragma unroll 1
+    for (int t = 0;; t += 64) {        // (later than a request's last are none: some place has idx or less)
+      int later = 0;
+#pragma unroll 1
+      for (int r = 0; r < a.requests; ++r) later += max(__builtin_amdgcn_readlane(mine, r) - (t + lane + 1), 0);
+      const uint64_t here = __ballot(later <= idx);
+      if (!here) continue;
+      const int l = __builtin_ctzll(here), nth = idx - __builtin_amdgcn_readlane(later, l);
+      const bool has = mine > t + l;
+      const uint64_t have = __ballot(has);
+      whole(a, __builtin_ctzll(__ballot(has && __popcll(have & ((1ull << lane) - 1)) == nth)), t + l, head_);
+      return;
+    }
+  }
   // This workgroup's share: prefix sums over the requests, of up to 64 by every wave for itself, which deals its lanes out to
   // them, else by the workgroup, 256 at a time, first of all and then again up to the one where the share begins; and in that
   // one over its row tiles, 64 at a time.  1500 rows of 8 heads and 1 kv head of 128 against 9500 tokens, 94 row tiles: 74 us, 93
@@ -286,7 +309,7 @@ struct Work {
     u1 = 0;
     if (!a.shares) {
       rt += a.row_tiles;
-      if (rt * ROWS >= rows) return;
+      if ((int64_t)rt * ROWS >= rows) return;
       sp = span_of<ROWS>(a, rq, rt, rows);
       u1 = sp.units;
       return;
@@ -807,7 +830,8 @@ __global__ __launch_bounds__(64 * kManyWaves, D <= 128 ? 2 : 1) void attn_many_k
     __syncthreads();
   } else {      // kv heads next to each other (their row tiles then share an XCD's cache), the row tiles that see most first
     const uint32_t idx = blockIdx.x / a.kv_heads;
-    work.whole(a, idx % a.requests, a.row_tiles - 1 - idx / a.requests, blockIdx.x % a.kv_heads);
+    if (a.nth) work.whole_nth(a, idx, blockIdx.x % a.kv_heads);
+    else work.whole(a, idx % a.requests, a.row_tiles - 1 - idx / a.requests, blockIdx.x % a.kv_heads);
   }
 
   for (; work.any(); work.next(a)) {
@@ -1091,11 +1115,11 @@ static AttnCosts attn_costs(int d) {
   return {1.7, 2.45, 2.6, 24, kFewShares<256>, kManyShares<256>};
 }
 struct AttnGeom {
-  int row_tiles;           // of a request and kv head
-  bool shares, many;
+  int row_tiles;           // of a request and kv head; nth: of all requests and a kv head
+  bool shares, many, nth;
 };
 static bool attn_cuts(const mdbf_attn_t& at) { return (at.window ? std::min(at.max_length, at.window) : at.max_length) > kWhole; }
-static AttnGeom attn_geom(const mdbf_kv_t& kv, const mdbf_attn_t& at, int T) {
+static AttnGeom attn_geom(const mdbf_kv_t& kv, const mdbf_attn_t& at, int all, int T) {
   const AttnCosts k = attn_costs(kv.head_dim);
   const int fresh = std::min(at.max_fresh, T), requests = (T + fresh - 1) / fresh;      // requests with as many new tokens as any
   const double rows = (double)fresh * (at.q_heads / kv.kv_heads);
@@ -1118,6 +1142,13 @@ static AttnGeom attn_geom(const mdbf_kv_t& kv, const mdbf_attn_t& at, int T) {
   g.many = rows > kRows && std::min(whole, cuts ? cut : whole) < few;
   g.shares = cuts && (!g.many || cut < whole);
   g.row_tiles = (int)std::min(tiles_of(g.many ? kManyRows : kRows), 65536.0);
+  // Row tiles without shares: each workgroup takes one that its request may have, or the n-th of those that there are, for which
+  // it looks through the requests.  That takes 0.5 to 2 us but spreads them evenly where most requests are much shorter than the
+  // bound: else a compute unit gets two and three while others, whose workgroups had none, are idle.  Five requests of 1 to 997 new
+  // tokens (14 heads on 2 of 64, 1111 visible): 38 -> 34 us, of 1 to 500: 32 -> 26; but 8 of 1 to 1024, 32 heads: 51.5 -> 53.5.
+  const int64_t there = (int64_t)T * (at.q_heads / kv.kv_heads) / kManyRows + all;
+  g.nth = g.many && !g.shares && all <= 64 && there * kv.kv_heads <= 512 && there < 0.75 * all * g.row_tiles;
+  if (g.nth) g.row_tiles = (int)there;
   return g;
 }
 // One size for all calls with these heads and bounds or smaller ones; nothing where no cache is long enough to be cut.
@@ -1135,7 +1166,7 @@ static size_t attn_workspace(const mdbf_kv_t& kv, const mdbf_attn_t& at) {
 template <int D, int DT>
 static int launch_few(AttnArgs& a, const AttnGeom& g, hipStream_t s) {
   a.shares = !g.shares ? 0 : g.many ? kManyShares<D> : kFewShares<D>;
-  const int64_t tiles = (int64_t)a.requests * a.kv_heads * g.row_tiles;
+  const int64_t tiles = (int64_t)(g.nth ? 1 : a.requests) * a.kv_heads * g.row_tiles;
   const unsigned grid = g.shares ? (unsigned)a.shares : (unsigned)tiles;
   if (g.many) attn_many_kernel<D, DT><<<grid, 64 * kManyWaves, 0, s>>>(a);
   else if (a.page_shift == 4) attn_few_kernel<D, DT, 4><<<grid, 64 * kWaves, 0, s>>>(a);
@@ -1185,7 +1216,7 @@ int mdbf_kv_attention(const mdbf_kv_t* kv, const mdbf_attn_t* attn, const void* 
     if (!kv_aligned(p, 16)) return MDBF_EALIGN;
   for (const void* p : ints)
     if (!kv_aligned(p, 4)) return MDBF_EALIGN;
-  const AttnGeom geom = attn_geom(*kv, *attn, T);
+  const AttnGeom geom = attn_geom(*kv, *attn, requests, T);
   const size_t need = attn_workspace(*kv, *attn);
   if (need && !workspace_dev) return MDBF_EINVAL;
   if (workspace_bytes < need) return MDBF_EWORKSPACE;
@@ -1196,7 +1227,7 @@ int mdbf_kv_attention(const mdbf_kv_t* kv, const mdbf_attn_t* attn, const void* 
   a.table_ld = table_ld, a.ldq = ldq, a.ldo = ldo, a.table_width = table_width, a.requests = requests, a.T = T, a.pages = kv->pages;
   a.kv_heads = kv->kv_heads, a.group = group, a.head_dim = kv->head_dim;
   a.page_shift = kv_page_shift(kv->page_size), a.causal = attn->flags & MDBF_ATTN_CAUSAL, a.window = attn->window;
-  a.row_tiles = geom.row_tiles, a.part = (float*)workspace_dev;
+  a.row_tiles = geom.row_tiles, a.nth = geom.nth, a.part = (float*)workspace_dev;
   a.join_rows = (int)std::min<int64_t>((int64_t)std::min(attn->max_fresh, T) * a.group, geom.many ? kManyRows : kRows);
   a.scale = (float)(fabs((double)attn->scale) * 1.4426950408889634), a.flip = attn->scale < 0 ? 0x80008000u : 0u;
   int bits = 0;

@@ -54,6 +54,24 @@ def test_more_row_tiles_than_a_wave_has_lanes(gpu, lengths, fresh, window):
     Step(gpu, lengths, fresh, 32, 1, 64, 32, "f16", seed=len(fresh)).check(window=window)
 
 
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("Hq,Hkv,d", [(7, 1, 64), (6, 2, 128), (4, 1, 256)])
+@pytest.mark.parametrize("window", [0, 100])
+def test_one_long_prompt_among_short_ones(gpu, dt, Hq, Hkv, d, window):
+    """Row tiles without shares, far fewer than the longest prompt would have in every request; requests without any."""
+    fresh = [3, 0, 500, 20, 130, 0, 60, 129, 1]
+    s = Step(gpu, [n + extra for n, extra in zip(fresh, [200, 0, 90, 7, 0, 300, 64, 1, 400])], fresh, Hq, Hkv, d, 32, dt, seed=d)
+    s.check(window=window)
+    s.check(window=window, causal=True, max_fresh=713)
+
+
+@pytest.mark.parametrize("Hkv", [1, 5])
+def test_a_very_long_prompt_among_short_ones(gpu, Hkv):
+    """More row tiles in a request than a wave has lanes."""
+    fresh = [30, 5, 700, 1, 1]
+    Step(gpu, [n + 40 for n in fresh], fresh, 16 * Hkv, Hkv, 64, 16, "bf16").check()
+
+
 @pytest.mark.parametrize("heads", [(16, 1), (17, 1), (24, 8)])
 def test_very_unequal_lengths(gpu, heads):
     """Shares that begin and end inside the cost of a row tile, row tiles in one share, in two and in many."""
