@@ -6,8 +6,11 @@
 //
 // On the matrix cores the scores are K Q^T (tokens x rows) and the results V^T P^T (channels x rows): a lane holds one
 // query row throughout, the scores' registers are the second product's operand as they lie, and maxima and sums need two
-// exchanges between lanes.  Codes become fp16 or bf16 numbers, exactly, with their block's scale by the conversion
-// instruction: keys in the registers that feed the product, values on their way into LDS, where transposing reads take them.
+// exchanges between lanes.  Values become fp16 or bf16 numbers, exactly, with their block's scale by the conversion
+// instruction on their way into LDS, where transposing reads take them.  So do keys for few query rows, in the registers that
+// feed the product; for prompts their codes are an operand as they are (below).  Scores, maxima, sums and results are fp32; the
+// numerators e^(z_j - m) are rounded to the values' type, at most half a unit of its last place each, and the sum is of what was
+// not rounded.
 #include <math.h>
 
 #include <algorithm>
@@ -433,6 +436,11 @@ __device__ __forceinline__ float row_max(float x) {
 // 16 query rows of one kv head at a time, the tiles of their tokens dealt out to the four waves, which meet at the end.  The
 // registers that a tile's keys were in take the next tile's as soon as the scores are there, those of its values once they
 // are in LDS; page numbers are looked up a tile earlier still.  NP: pages per tile of 64 tokens (1, 2 or 4).
+//
+// Bound by the cache's bytes where that is long: 64 requests of up to 8192 tokens, 32 heads on 8 of 128 (295 MB), 55 us and 5 for
+// the join, 5.2 TB/s of the 6.0 that a plain read reaches; one of 200000 tokens (218 MB) 41 and 6 us.  Matrix cores are busy for an
+// eighth of that.  Short caches are a launch's latency and each wave's chain of page number, codes, scores, values and the meeting of the
+// waves: 4 requests of up to 701 tokens, 32 heads of 128 (8 MB), 10 us.
 template <int D, int DT, int NP>
 __global__ __launch_bounds__(64 * kWaves, D == 64 ? 4 : D == 128 ? 3 : 2) void attn_few_kernel(AttnArgs a) {
   using Tile = Codes<D, NP>;
@@ -741,8 +749,17 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
 
 // ---- prompts ---------------------------------------------------------------------------------------------
 // 128 query rows of one kv head per workgroup, 32 per wave, which all read the tile of 64 tokens that the workgroup has in
-// LDS: key codes as they are (each wave makes numbers of them as it feeds its products), values as numbers.  Two buffers:
+// LDS: key codes as they are, values as numbers.  Two buffers:
 // while one is worked on, the next tile's codes, which came in while the one before was, are written into the other.
+//
+// K Q^T are block-scaled products of fp4 and fp6, at four times the 16-bit rate, so that three or four of them, one for each limb
+// of the queries, are no dearer than one of 16 bits and its conversions of the keys.  Long prompts are bound by instruction
+// issue: two waves a SIMD, for whose softmax and values the vector unit is busy 53 % of the cycles and the matrix core 41 %, seldom
+// both.  2048 tokens behind 14336, 32 heads on 8 of 128 (515 Gflop): 457 to 492 us, 1.05 to 1.13 Pflop/s of the 1.26 that a large
+// 16-bit product reaches.
+// Short ones are latency: 1.0 us (D = 64) or 1.25 (128) per tile of tokens with one workgroup on a compute unit, 1.1 or 1.85 for two.
+// Tried: eight waves in two halves that take turns at the tiles and add up at the end, half as many workgroups: 512 tokens of 32
+// heads 17.0 -> 16.3 us, calls in shares as before, prompts of 300 tokens of 4 requests 42 -> 48: not kept.
 constexpr int kManyWaves = 4, kManyRows = 32 * kManyWaves;
 constexpr int kManyCost = 4;      // units that beginning and ending a row tile costs
 template <int D>
