@@ -119,7 +119,7 @@ __global__ __launch_bounds__(kSlotThreads) void slots_kernel(SlotArgs a) {
     return;
   }
 
-  int tok0 = 0, page0 = taken;              // of the requests before this round's
+  int tok0 = 0, page0 = taken;              // of the requests before this pass
   for (int64_t r0 = 0; r0 < a.requests; r0 += kSlotThreads) {
     const int64_t r = r0 + tid;
     const int n = (int)min((int64_t)kSlotThreads, a.requests - r0);

@@ -786,7 +786,8 @@ __device__ __forceinline__ void each_of(F&& f, std::integer_sequence<int, I...>)
 }
 
 // 32 channels of a query as a sum of NL fp6 numbers, each limb's scale 2^-4 of the one before: an absolute error of 2^-(4 NL + 2)
-// of the largest of the 32 at most.  Three limbs for bf16 and four for fp16: a value down to a 64th of the largest is exact.
+// of the largest of the 32 at most.  Three limbs for bf16 and four for fp16: in a score of ten that is no more than the rounding of its
+// numerator, 2^-9 and 2^-12.
 template <int NL>
 struct Limbs {
   v6u limb[NL];
@@ -939,15 +940,21 @@ __global__ __launch_bounds__(64 * kManyWaves, D <= 128 ? 2 : 1) void attn_many_k
         const uint32_t x = raw[s][w / 4][w % 4] ^ a.flip;
         if (DT == MDBF_F16) {
           const F16x2 v = __builtin_bit_cast(F16x2, x);
-          q[2 * w] = (float)v[0], q[2 * w + 1] = (float)v[1];
+          q[2 * w] = (float)v[0] * a.scale, q[2 * w + 1] = (float)v[1] * a.scale;
         } else {
-          q[2 * w] = __builtin_bit_cast(float, x << 16), q[2 * w + 1] = __builtin_bit_cast(float, x & 0xffff0000u);
+          q[2 * w] = __builtin_bit_cast(float, x << 16) * a.scale, q[2 * w + 1] = __builtin_bit_cast(float, x & 0xffff0000u) * a.scale;
         }
       }
       finite &= ql[s].set(q);
     }
 
-    float m = -INFINITY, l = finite ? 0.0f : NAN;      // (a query that is not finite has no finite result)
+    // The products' sums begin at -m, so that they end as the exponentials' arguments; with D = 256 no registers are left for
+    // that.
+    constexpr bool FROM_M = D <= 128;
+    F32x16 from_m;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) from_m[j] = 0;
+    float m = -INFINITY, use = 0, l = finite ? 0.0f : NAN;      // (a query that is not finite has no finite result)
     uint32_t nan_blocks = 0;
     F32x16 acc[CT];
 #pragma unroll
@@ -981,8 +988,7 @@ __global__ __launch_bounds__(64 * kManyWaves, D <= 128 ? 2 : 1) void attn_many_k
 #pragma unroll
         for (int w = 0; w < (BL + 3) / 4; ++w)
           sc[f][w] = (BL == 2 ? *reinterpret_cast<const uint16_t*>(from) : reinterpret_cast<const uint32_t*>(from)[w]) >> (8 * hh);
-#pragma unroll
-        for (int j = 0; j < 16; ++j) z[f][j] = 0;
+        z[f] = from_m;
       }
       each_of([&](auto st) __attribute__((always_inline)) {
         constexpr int s = decltype(st)::value;
@@ -1019,15 +1025,20 @@ __global__ __launch_bounds__(64 * kManyWaves, D <= 128 ? 2 : 1) void attn_many_k
       for (int f = 0; f < 2; ++f)
 #pragma unroll
         for (int j = 0; j < 16; ++j) top = fmaxf(top, z[f][j]);
-      top *= a.scale;
+      if (FROM_M) top += use;
       if (__any(top > m + kSlack)) {      // as in attn_few_kernel
         const float mn = fmaxf(m, pair_max(top)), alpha = __builtin_amdgcn_exp2f(m - (mn == -INFINITY ? 0.0f : mn));
+        const float before = use;
         m = mn;
+        use = m == -INFINITY ? 0.0f : m;
         l *= alpha;
 #pragma unroll
         for (int c = 0; c < CT; ++c) acc[c] *= alpha;
+        if (FROM_M) {
+#pragma unroll
+          for (int j = 0; j < 16; ++j) from_m[j] = -use, z[0][j] -= use - before, z[1][j] -= use - before;
+        }
       }
-      const float use = m == -INFINITY ? 0.0f : m;
       U32x4 pf[4];
 #pragma unroll
       for (int f = 0; f < 2; ++f)
@@ -1035,7 +1046,7 @@ __global__ __launch_bounds__(64 * kManyWaves, D <= 128 ? 2 : 1) void attn_many_k
         for (int j = 0; j < 16; j += 4) {
           float p[4];
 #pragma unroll
-          for (int k = 0; k < 4; ++k) p[k] = __builtin_amdgcn_exp2f(z[f][j + k] * a.scale - use);
+          for (int k = 0; k < 4; ++k) p[k] = __builtin_amdgcn_exp2f(FROM_M ? z[f][j + k] : z[f][j + k] - use);
           l += (p[0] + p[1]) + (p[2] + p[3]);
           pf[2 * f + j / 8][j / 4 % 2 * 2] = round2<DT>(p[0], p[1]);
           pf[2 * f + j / 8][j / 4 % 2 * 2 + 1] = round2<DT>(p[2], p[3]);
