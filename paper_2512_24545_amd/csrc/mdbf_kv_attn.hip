@@ -820,7 +820,8 @@ __device__ __forceinline__ float pair_max(float x) {
   return fmaxf(__builtin_bit_cast(float, a0), __builtin_bit_cast(float, a1));
 }
 
-template <int D, int DT>
+// CROWD: waves that feed products go first (see launch_few).
+template <int D, int DT, bool CROWD>
 __global__ __launch_bounds__(64 * kManyWaves, D <= 128 ? 2 : 1) void attn_many_kernel(AttnArgs a) {
   constexpr int BL = D / 32;                       // blocks of a token
   constexpr int UNITS = kTile * BL;                // 16-byte units of a tile's keys, and of its values
@@ -990,6 +991,7 @@ __global__ __launch_bounds__(64 * kManyWaves, D <= 128 ? 2 : 1) void attn_many_k
           sc[f][w] = (BL == 2 ? *reinterpret_cast<const uint16_t*>(from) : reinterpret_cast<const uint32_t*>(from)[w]) >> (8 * hh);
         z[f] = from_m;
       }
+      if (CROWD) __builtin_amdgcn_s_setprio(1);
       each_of([&](auto st) __attribute__((always_inline)) {
         constexpr int s = decltype(st)::value;
         U32x4 codes[2];
@@ -1011,6 +1013,7 @@ __global__ __launch_bounds__(64 * kManyWaves, D <= 128 ? 2 : 1) void attn_many_k
         }
       };
       read(0);
+      if (CROWD) __builtin_amdgcn_s_setprio(0);
       if (t0 < sp.all_lo || t0 + kTile > sp.all_hi) {      // not every row sees every token
 #pragma unroll
         for (int f = 0; f < 2; ++f)
@@ -1073,6 +1076,7 @@ __global__ __launch_bounds__(64 * kManyWaves, D <= 128 ? 2 : 1) void attn_many_k
         }
       }
 
+      if (CROWD) __builtin_amdgcn_s_setprio(1);
       // results: 16 tokens at a time, in the order of the scores' registers; the values of the next 16 are read before the products
       // of these
 #pragma unroll
@@ -1082,6 +1086,7 @@ __global__ __launch_bounds__(64 * kManyWaves, D <= 128 ? 2 : 1) void attn_many_k
         for (int c = 0; c < CT; ++c)
           acc[c] = mma32<DT>(U32x4{v[k & 1][c][0][0], v[k & 1][c][0][1], v[k & 1][c][1][0], v[k & 1][c][1][1]}, pf[k], acc[c]);
       }
+      if (CROWD) __builtin_amdgcn_s_setprio(0);
       __syncthreads();
     }
 
@@ -1145,6 +1150,7 @@ static AttnCosts attn_costs(int d) {
 struct AttnGeom {
   int row_tiles;           // of a request and kv head; nth: of all requests and a kv head
   bool shares, many, nth;
+  bool distant;            // a row tile of the prompts' kernel sees 4096 tokens or more on average
 };
 static bool attn_cuts(const mdbf_attn_t& at) { return (at.window ? std::min(at.max_length, at.window) : at.max_length) > kWhole; }
 static AttnGeom attn_geom(const mdbf_kv_t& kv, const mdbf_attn_t& at, int all, int T) {
@@ -1175,6 +1181,7 @@ static AttnGeom attn_geom(const mdbf_kv_t& kv, const mdbf_attn_t& at, int all, i
   // bound: else a compute unit gets two and three while others, whose workgroups had none, are idle.  Five requests of 1 to 997 new
   // tokens (14 heads on 2 of 64, 1111 visible): 38 -> 34 us, of 1 to 500: 32 -> 26; but 8 of 1 to 1024, 32 heads: 51.5 -> 53.5.
   const int64_t there = (int64_t)T * (at.q_heads / kv.kv_heads) / kManyRows + all;
+  g.distant = units_of(kManyRows, false) >= 64;
   g.nth = g.many && !g.shares && all <= 64 && there * kv.kv_heads <= 512 && there < 0.75 * all * g.row_tiles;
   if (g.nth) g.row_tiles = (int)there;
   return g;
@@ -1196,7 +1203,13 @@ static int launch_few(AttnArgs& a, const AttnGeom& g, hipStream_t s) {
   a.shares = !g.shares ? 0 : g.many ? kManyShares<D> : kFewShares<D>;
   const int64_t tiles = (int64_t)(g.nth ? 1 : a.requests) * a.kv_heads * g.row_tiles;
   const unsigned grid = g.shares ? (unsigned)a.shares : (unsigned)tiles;
-  if (g.many) attn_many_kernel<D, DT><<<grid, 64 * kManyWaves, 0, s>>>(a);
+  // Where two workgroups share a compute unit, a wave of each a SIMD, the one that feeds products goes before the one that is at its
+  // softmax, if row tiles see much: 32 heads on 8 of 128, 2048 tokens behind 14336 464 -> 441 us (fp16 513 -> 487), 7000 252 -> 243,
+  // 4000 165 -> 161, 2000 108 -> 108.4, none 50.6 -> 53.9: the instructions' order that it keeps costs something too.  With one
+  // workgroup on a compute unit it only costs (512 tokens 16.9 -> 17.3, D = 256 705 -> 745), with D = 64 nothing is gained.
+  constexpr bool kCrowds = D == 128;
+  if (g.many && kCrowds && g.distant && grid >= 512) attn_many_kernel<D, DT, kCrowds><<<grid, 64 * kManyWaves, 0, s>>>(a);
+  else if (g.many) attn_many_kernel<D, DT, false><<<grid, 64 * kManyWaves, 0, s>>>(a);
   else if (a.page_shift == 4) attn_few_kernel<D, DT, 4><<<grid, 64 * kWaves, 0, s>>>(a);
   else if (a.page_shift == 5) attn_few_kernel<D, DT, 2><<<grid, 64 * kWaves, 0, s>>>(a);
   else attn_few_kernel<D, DT, 1><<<grid, 64 * kWaves, 0, s>>>(a);

@@ -65,6 +65,12 @@ def test_one_long_prompt_among_short_ones(gpu, dt, Hq, Hkv, d, window):
     s.check(window=window, causal=True, max_fresh=713)
 
 
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("lengths,fresh,heads,window", [([5000], [70], 4, 0), ([6000, 4500], [33, 66], 4, 4400)])
+def test_prompts_that_see_much(gpu, dt, lengths, fresh, heads, window):
+    Step(gpu, lengths, fresh, heads, heads // 4, 128, 64, dt, seed=heads).check(window=window)
+
+
 @pytest.mark.parametrize("Hkv", [1, 5])
 def test_a_very_long_prompt_among_short_ones(gpu, Hkv):
     """More row tiles in a request than a wave has lanes."""
