@@ -754,8 +754,8 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
 //
 // K Q^T are block-scaled products of fp4 and fp6, at four times the 16-bit rate, so that three or four of them, one for each limb
 // of the queries, are no dearer than one of 16 bits and its conversions of the keys.  Long prompts are bound by instruction
-// issue: two waves a SIMD, for whose softmax and values the vector unit is busy 53 % of the cycles and the matrix core 41 %, seldom
-// both.  2048 tokens behind 14336, 32 heads on 8 of 128 (515 Gflop): 457 to 492 us, 1.05 to 1.13 Pflop/s of the 1.26 that a large
+// issue: two waves a SIMD, for whose softmax and values the vector unit is busy 55 % of the cycles and the matrix core 47 %, seldom
+// both.  2048 tokens behind 14336, 32 heads on 8 of 128 (515 Gflop): 433 to 441 us, 1.17 to 1.19 Pflop/s of the 1.26 that a large
 // 16-bit product reaches.
 // Short ones are latency: 1.0 us (D = 64) or 1.25 (128) per tile of tokens with one workgroup on a compute unit, 1.1 or 1.85 for two.
 // Tried: eight waves in two halves that take turns at the tiles and add up at the end, half as many workgroups: 512 tokens of 32
@@ -1134,7 +1134,7 @@ static int check_attn(const mdbf_kv_t* kv, const mdbf_attn_t* at, int requests, 
 // Which kernel a call takes, and whether its work is cut into shares: by estimates of the time, in us, from the sizes that the
 // caller bounds the call by.  Fitted to calls of 1 to 8192 new tokens behind 0 to 30000; what they get wrong costs up to a fifth
 // where requests are of unequal lengths.  128 new tokens behind 30000, 32 heads on 8 of 128: few rows 163 us, prompts 619 whole and
-// 83 cut; 33 behind 2000 of 8 requests: 26, 48 and 28; 2048 behind 14336: 1288, 471 and 523.
+// 78 cut; 40 behind 3000 of 8 requests: 32, 64 and 34; 1000 behind 4000: 188, 100 and 99.
 constexpr int kWhole = 1024;      // tokens up to which nothing is cut: the join, a launch, would cost more
 struct AttnCosts {
   double few;              // a unit of the few-row kernel where it fills the device
