@@ -1132,7 +1132,7 @@ static int check_attn(const mdbf_kv_t* kv, const mdbf_attn_t* at, int requests, 
 }
 
 // Which kernel a call takes, and whether its work is cut into shares: by estimates of the time, in us, from the sizes that the
-// caller bounds the call by.  Fitted to calls of 1 to 8192 new tokens behind 0 to 30000; what they get wrong costs up to a fifth
+// caller bounds the call by.  Fitted to calls of 1 to 8192 new tokens behind 0 to 30000; what they get wrong costs up to a quarter
 // where requests are of unequal lengths.  128 new tokens behind 30000, 32 heads on 8 of 128: few rows 163 us, prompts 619 whole and
 // 78 cut; 40 behind 3000 of 8 requests: 32, 64 and 34; 1000 behind 4000: 188, 100 and 99.
 constexpr int kWhole = 1024;      // tokens up to which nothing is cut: the join, a launch, would cost more
