@@ -6,6 +6,7 @@ be loaded (and cannot be built), importing callers get an exception.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import functools
 import os
@@ -183,6 +184,24 @@ def _stream_ptr(stream=None):
     return c._cuda_getCurrentRawStream(c._cuda_getDevice())
 
 
+def _on(stream):
+    """Where a call on `stream` makes its workspace.  Memory from the current stream's pool would go back there when the call
+    returns, and to that stream's next operation while `stream` still works in it; and what the current stream has yet to do with
+    an earlier tensor of that memory would go on beside it."""
+    return contextlib.nullcontext() if stream is None else _torch().cuda.stream(stream)
+
+
+def _result(make, stream):
+    """A result tensor of a call on `stream`, from make(): of that stream's memory likewise, and not reused before what the current
+    stream, the caller's, has been given to do by the time that it is dropped is done."""
+    if stream is None:
+        return make()
+    with _on(stream):
+        t = make()
+    t.record_stream(_torch().cuda.current_stream(t.device))
+    return t
+
+
 def _torch_dtype(name):
     _torch()
     return _TORCH_DTYPE[name]
@@ -199,7 +218,7 @@ def mdbf_pack(signs, stream=None):
     assert signs.is_cuda and signs.dtype == torch.int8 and signs.dim() == 2 and signs.stride(1) == 1
     rows, cols = signs.shape
     nbytes = mdbf_packed_bytes(rows, cols)
-    packed = torch.empty(nbytes, dtype=torch.uint8, device=signs.device)
+    packed = _result(lambda: torch.empty(nbytes, dtype=torch.uint8, device=signs.device), stream)
     _check(lib().mdbf_pack(signs.data_ptr(), rows, cols, signs.stride(0), packed.data_ptr(), nbytes,
                            _stream_ptr(stream)), "mdbf_pack")
     return packed
@@ -207,7 +226,7 @@ def mdbf_pack(signs, stream=None):
 
 def mdbf_unpack(packed, rows, cols, stream=None):
     torch = _torch()
-    out = torch.empty((rows, cols), dtype=torch.int8, device=packed.device)
+    out = _result(lambda: torch.empty((rows, cols), dtype=torch.int8, device=packed.device), stream)
     _check(lib().mdbf_unpack(packed.data_ptr(), rows, cols, out.data_ptr(), out.stride(0), _stream_ptr(stream)),
            "mdbf_unpack")
     return out
@@ -217,7 +236,7 @@ def mdbf_pad_envelope(env, l_to, stream=None):
     """env: CUDA tensor (rows, l), contiguous.  Returns (rows, l_to) with zero modes appended."""
     torch = _torch()
     assert env.is_cuda and env.dim() == 2 and env.is_contiguous()
-    out = torch.empty((env.shape[0], l_to), dtype=env.dtype, device=env.device)
+    out = _result(lambda: torch.empty((env.shape[0], l_to), dtype=env.dtype, device=env.device), stream)
     _check(lib().mdbf_pad_envelope(env.data_ptr(), env.shape[0], env.shape[1], DTYPE_CODE[_dtype_name(env)],
                                    out.data_ptr(), l_to, _stream_ptr(stream)), "mdbf_pad_envelope")
     return out
@@ -287,9 +306,10 @@ def mdbf_forward(layer, X, y_dtype="f32", precise=False, Y=None, workspace=None,
     d = layer.desc(_DTYPE_NAME[X.dtype], y_dtype, precise, block_scaled, accumulate, fp16_staged)
     assert not (accumulate and Y is None), "accumulate needs the Y to add to"
     if Y is None:
-        Y = torch.empty((T, layer.m), dtype=_torch_dtype(y_dtype), device=X.device)
+        Y = _result(lambda: torch.empty((T, layer.m), dtype=_torch_dtype(y_dtype), device=X.device), stream)
     if workspace is None:
-        workspace = torch.empty(mdbf_workspace_bytes(d, T), dtype=torch.uint8, device=X.device)
+        with _on(stream):
+            workspace = torch.empty(mdbf_workspace_bytes(d, T), dtype=torch.uint8, device=X.device)
     status = (_lib or lib()).mdbf_forward(d, layer.SA_packed.data_ptr(), layer.SB_packed.data_ptr(), layer.env(), X.data_ptr(), ldx,
                                           Y.data_ptr(), Y.stride(0), T, workspace.data_ptr(), workspace.numel(), _stream_ptr(stream))
     if status:
@@ -388,11 +408,12 @@ def mdbf_msvid(Z, l, X0, iters=8, stream=None, workspace=None):
     need = C.c_size_t(0)
     _check(lib().mdbf_msvid_workspace_bytes(rows, cols, l, C.byref(need)), "mdbf_msvid_workspace_bytes")
     if workspace is None:
-        workspace = torch.empty(need.value, dtype=torch.uint8, device=Z.device)
-    S = torch.empty((rows, cols), dtype=torch.int8, device=Z.device)
-    A = torch.empty((rows, l), dtype=torch.float32, device=Z.device)
-    Q = torch.empty((cols, l), dtype=torch.float32, device=Z.device)
-    sigma = torch.empty((b,), dtype=torch.float32, device=Z.device)
+        with _on(stream):
+            workspace = torch.empty(need.value, dtype=torch.uint8, device=Z.device)
+    S = _result(lambda: torch.empty((rows, cols), dtype=torch.int8, device=Z.device), stream)
+    A = _result(lambda: torch.empty((rows, l), dtype=torch.float32, device=Z.device), stream)
+    Q = _result(lambda: torch.empty((cols, l), dtype=torch.float32, device=Z.device), stream)
+    sigma = _result(lambda: torch.empty((b,), dtype=torch.float32, device=Z.device), stream)
     _check(lib().mdbf_msvid(Z.data_ptr(), rows, cols, Z.stride(0), l, iters, X0.data_ptr(), S.data_ptr(), A.data_ptr(),
                             Q.data_ptr(), sigma.data_ptr(), workspace.data_ptr(), workspace.numel(),
                             _stream_ptr(stream)), "mdbf_msvid")
@@ -422,11 +443,11 @@ class KVSlots:
     """What mdbf_kv_slots writes: lengths, cu, slots, positions, taken, status.  Made once for `requests` and `tokens`, it can be
     handed to every step's call."""
 
-    def __init__(self, requests, tokens, device="cuda:0"):
+    def __init__(self, requests, tokens, device="cuda:0", stream=None):
         torch = _torch()
-        ints = torch.empty(2 * requests + 3 + tokens, dtype=torch.int32, device=device)
+        ints = _result(lambda: torch.empty(2 * requests + 3 + tokens, dtype=torch.int32, device=device), stream)
         self.lengths, self.cu, self.positions, self.taken, self.status = ints.split((requests, requests + 1, tokens, 1, 1))
-        self.slots = torch.empty(tokens, dtype=torch.int64, device=device)
+        self.slots = _result(lambda: torch.empty(tokens, dtype=torch.int64, device=device), stream)
 
 
 # (Steps of small batches take the host as long as the device: in these calls attributes are asked for once, descriptions of equal
@@ -455,7 +476,7 @@ def mdbf_kv_slots(cached, fresh, table, free_pages, taken, page_size, tokens, ou
     assert table.is_cuda and table.dtype == torch.int32 and rows == n and (one == 1 or width == 1)
     o = out
     if o is None:
-        o = KVSlots(n, tokens, cached.device)
+        o = KVSlots(n, tokens, cached.device, stream)
     else:
         assert _ints(o.lengths, n) and _ints(o.cu, n + 1) and _ints(o.positions, tokens)
         assert _ints(o.slots, tokens, torch.int64) and _ints(o.taken, 1) and _ints(o.status, 1)
@@ -485,7 +506,7 @@ def mdbf_kv_read(cache, slots, out=None, stream=None):
     torch = _torch()
     T, H, d = slots.numel(), cache.kv_heads, cache.head_dim
     if out is None:
-        out = tuple(torch.empty((T, H, d), dtype=_TORCH_DTYPE[cache.dtype], device=slots.device) for _ in range(2))
+        out = tuple(_result(lambda: torch.empty((T, H, d), dtype=_TORCH_DTYPE[cache.dtype], device=slots.device), stream) for _ in range(2))
     k, v = out
     assert k.shape == v.shape == (T, H, d) and k.dtype == v.dtype and _ints(slots, T, torch.int64)
     status = (_lib or lib()).mdbf_kv_read(cache.desc, *cache.args, slots.data_ptr(), T, k.data_ptr(), _row_stride(k, H * d), v.data_ptr(),
@@ -512,13 +533,13 @@ def mdbf_qk_norm_rope(q, k, rope, positions, q_weight=None, k_weight=None, eps=1
     assert k_shape[0] == T and k_shape[2] == d and k.dtype == x_dtype
     name = _DTYPE_NAME[x_dtype]
     if q_out is None:
-        q_out = torch.empty((T, Hq, d), dtype=_TORCH_DTYPE[y_dtype or name], device=q.device)
+        q_out = _result(lambda: torch.empty((T, Hq, d), dtype=_TORCH_DTYPE[y_dtype or name], device=q.device), stream)
     else:
         assert q_out.shape == q_shape
     out_dtype = q_out.dtype
     if k_out is None:
         if cache is None:
-            k_out = torch.empty((T, Hkv, d), dtype=out_dtype, device=q.device)
+            k_out = _result(lambda: torch.empty((T, Hkv, d), dtype=out_dtype, device=q.device), stream)
     else:
         assert k_out.shape == k_shape and k_out.dtype == out_dtype
     for w in (q_weight, k_weight):
@@ -578,11 +599,12 @@ def mdbf_kv_attention(cache, q, table, cu, lengths, max_fresh, max_length, scale
     ld, one = table.stride()
     assert table.is_cuda and table.dtype == torch.int32 and rows == n and (one == 1 or width == 1)
     if out is None:
-        out = torch.empty(shape, dtype=dtype, device=q.device)
+        out = _result(lambda: torch.empty(shape, dtype=dtype, device=q.device), stream)
     else:
         assert out.shape == shape and out.dtype == dtype
     if workspace is None:
-        workspace = mdbf_kv_attention_workspace(cache, Hq, n, T, max_fresh, max_length, causal, window)
+        with _on(stream):
+            workspace = mdbf_kv_attention_workspace(cache, Hq, n, T, max_fresh, max_length, causal, window)
     desc = _attn_desc(Hq, MDBF_ATTN_CAUSAL if causal else 0, window, max_fresh, max_length, d ** -0.5 if scale is None else scale)
     ws = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
     status = (_lib or lib()).mdbf_kv_attention(cache.desc, desc, *cache.args, table.data_ptr(), ld if ld >= width or n > 1 else width, width,
