@@ -391,6 +391,10 @@ typedef struct {
  * (host arithmetic only) does not depend on requests and T, and never shrinks with max_fresh and max_length: a buffer for the largest
  * call serves all of the same heads. */
 int mdbf_kv_attention_workspace_bytes(const mdbf_kv_t* kv, const mdbf_attn_t* attn, int requests, int T, size_t* bytes_out);
+/* What a call of these sizes runs (host only): "few rows" (16 query rows of a kv head at a time) or "prompts" (128), then
+ * ", shares" where the work is cut, ", n-th row tiles" where workgroups take the row tiles that there are instead of those that there may
+ * be, and ", products first" where waves that feed products have priority; "" for what a call would refuse. */
+const char* mdbf_kv_attention_kernel(const mdbf_kv_t* kv, const mdbf_attn_t* attn, int requests, int T);
 int mdbf_kv_attention(const mdbf_kv_t* kv, const mdbf_attn_t* attn, const void* cache_dev, size_t cache_bytes,
                       const int32_t* table_dev, int64_t table_ld, int table_width, const int32_t* cu_dev,
                       const int32_t* lengths_dev, int requests, const void* q_dev, int64_t ldq, int T, void* out_dev,

@@ -34,7 +34,7 @@ EXPORTS = [
     "mdbf_forward_batch", "mdbf_forward_batch_part", "mdbf_batch_plan_kernel", "mdbf_batch_plan_launches", "mdbf_strerror", "mdbf_last_hip_error", "mdbf_version",
     "mdbf_msvid_block", "mdbf_msvid_workspace_bytes", "mdbf_msvid",
     "mdbf_kv_page_bytes", "mdbf_kv_slots", "mdbf_kv_append", "mdbf_kv_read", "mdbf_qk_norm_rope",
-    "mdbf_kv_attention_workspace_bytes", "mdbf_kv_attention",
+    "mdbf_kv_attention_workspace_bytes", "mdbf_kv_attention_kernel", "mdbf_kv_attention",
 ]
 
 
@@ -124,6 +124,8 @@ def lib():
     L.mdbf_qk_norm_rope.argtypes = [C.POINTER(RopeDesc), vp, i64, vp, i64, vp, vp, vp, vp, C.c_int, vp, i64, vp, i64,
                                     C.POINTER(KvDesc), vp, sz, vp, i64, vp, vp]
     L.mdbf_kv_attention_workspace_bytes.argtypes = [C.POINTER(KvDesc), C.POINTER(AttnDesc), C.c_int, C.c_int, C.POINTER(sz)]
+    L.mdbf_kv_attention_kernel.restype = C.c_char_p
+    L.mdbf_kv_attention_kernel.argtypes = [C.POINTER(KvDesc), C.POINTER(AttnDesc), C.c_int, C.c_int]
     L.mdbf_kv_attention.argtypes = [C.POINTER(KvDesc), C.POINTER(AttnDesc), vp, sz, vp, i64, C.c_int, vp, vp, C.c_int, vp, i64,
                                     C.c_int, vp, i64, vp, sz, vp]
     L.mdbf_strerror.restype = C.c_char_p
@@ -583,6 +585,12 @@ def mdbf_kv_attention_workspace(cache, q_heads, requests, tokens, max_fresh, max
                                    max_fresh, max_length, 1.0)
     torch = _torch()
     return torch.empty(n, dtype=torch.uint8, device=cache.buffer.device) if n else None
+
+
+def mdbf_kv_attention_kernel(cache, q_heads, requests, tokens, max_fresh, max_length, causal=True, window=0):
+    """What an mdbf_kv_attention call of these sizes runs (include/mdbf.h has the names)."""
+    attn = AttnDesc(q_heads, MDBF_ATTN_CAUSAL if causal else 0, window, max_fresh, max_length, 1.0)
+    return lib().mdbf_kv_attention_kernel(cache.desc, attn, requests, tokens).decode()
 
 
 def mdbf_kv_attention(cache, q, table, cu, lengths, max_fresh, max_length, scale=None, causal=True, window=0, out=None, workspace=None,

@@ -1186,6 +1186,16 @@ static AttnGeom attn_geom(const mdbf_kv_t& kv, const mdbf_attn_t& at, int all, i
   if (g.nth) g.row_tiles = (int)there;
   return g;
 }
+static unsigned attn_grid(const AttnGeom& g, int shares, int requests, int kv_heads) {
+  return g.shares ? (unsigned)shares : (unsigned)((int64_t)(g.nth ? 1 : requests) * kv_heads * g.row_tiles);
+}
+// Where two workgroups share a compute unit, a wave of each a SIMD, the one that feeds products goes before the one that is at its
+// softmax, if row tiles see much: 32 heads on 8 of 128, 2048 tokens behind 14336 464 -> 441 us (fp16 513 -> 487), 7000 252 -> 243,
+// 4000 165 -> 161, 2000 108 -> 108.4, none 50.6 -> 53.9: the instructions' order that it keeps costs something too.  With one
+// workgroup on a compute unit it only costs (512 tokens 16.9 -> 17.3, D = 256 705 -> 745), with D = 64 nothing is gained.
+template <int D>
+constexpr bool kCrowds = D == 128;
+static bool attn_crowds(const AttnGeom& g, unsigned grid) { return g.many && g.distant && grid >= 512; }
 // One size for all calls with these heads and bounds or smaller ones; nothing where no cache is long enough to be cut.
 template <int D>
 static size_t workspace_of(bool few) {
@@ -1201,14 +1211,8 @@ static size_t attn_workspace(const mdbf_kv_t& kv, const mdbf_attn_t& at) {
 template <int D, int DT>
 static int launch_few(AttnArgs& a, const AttnGeom& g, hipStream_t s) {
   a.shares = !g.shares ? 0 : g.many ? kManyShares<D> : kFewShares<D>;
-  const int64_t tiles = (int64_t)(g.nth ? 1 : a.requests) * a.kv_heads * g.row_tiles;
-  const unsigned grid = g.shares ? (unsigned)a.shares : (unsigned)tiles;
-  // Where two workgroups share a compute unit, a wave of each a SIMD, the one that feeds products goes before the one that is at its
-  // softmax, if row tiles see much: 32 heads on 8 of 128, 2048 tokens behind 14336 464 -> 441 us (fp16 513 -> 487), 7000 252 -> 243,
-  // 4000 165 -> 161, 2000 108 -> 108.4, none 50.6 -> 53.9: the instructions' order that it keeps costs something too.  With one
-  // workgroup on a compute unit it only costs (512 tokens 16.9 -> 17.3, D = 256 705 -> 745), with D = 64 nothing is gained.
-  constexpr bool kCrowds = D == 128;
-  if (g.many && kCrowds && g.distant && grid >= 512) attn_many_kernel<D, DT, kCrowds><<<grid, 64 * kManyWaves, 0, s>>>(a);
+  const unsigned grid = attn_grid(g, a.shares, a.requests, a.kv_heads);
+  if (kCrowds<D> && attn_crowds(g, grid)) attn_many_kernel<D, DT, kCrowds<D>><<<grid, 64 * kManyWaves, 0, s>>>(a);
   else if (g.many) attn_many_kernel<D, DT, false><<<grid, 64 * kManyWaves, 0, s>>>(a);
   else if (a.page_shift == 4) attn_few_kernel<D, DT, 4><<<grid, 64 * kWaves, 0, s>>>(a);
   else if (a.page_shift == 5) attn_few_kernel<D, DT, 2><<<grid, 64 * kWaves, 0, s>>>(a);
@@ -1217,7 +1221,7 @@ static int launch_few(AttnArgs& a, const AttnGeom& g, hipStream_t s) {
   if (e == 0 && g.shares) {
     const unsigned rows = (unsigned)(a.shares * a.join_rows);
     if (g.many) attn_join_kernel<D, DT, kManyRows, 1><<<(rows + 3) / 4, 256, 0, s>>>(a);
-    else if (a.shares / tiles >= 16) attn_join_kernel<D, DT, kRows, 4><<<rows, 256, 0, s>>>(a);      // few row tiles, each in many shares
+    else if (a.shares / ((int64_t)a.requests * a.kv_heads * g.row_tiles) >= 16) attn_join_kernel<D, DT, kRows, 4><<<rows, 256, 0, s>>>(a);      // few row tiles, each in many shares
     else attn_join_kernel<D, DT, kRows, 1><<<(rows + 3) / 4, 256, 0, s>>>(a);
     e = (int)hipGetLastError();
   }
@@ -1240,6 +1244,18 @@ int mdbf_kv_attention_workspace_bytes(const mdbf_kv_t* kv, const mdbf_attn_t* at
   if (st) return st;
   *bytes_out = attn_workspace(*kv, *attn);
   return MDBF_OK;
+}
+
+const char* mdbf_kv_attention_kernel(const mdbf_kv_t* kv, const mdbf_attn_t* attn, int requests, int T) {
+  if (check_attn(kv, attn, requests, T)) return "";
+  const AttnGeom g = attn_geom(*kv, *attn, requests, T);
+  if (!g.many) return g.shares ? "few rows, shares" : "few rows";
+  const AttnCosts k = attn_costs(kv->head_dim);
+  const bool crowd = (kv->head_dim == 64 ? kCrowds<64> : kv->head_dim == 128 ? kCrowds<128> : kCrowds<256>) &&
+                     attn_crowds(g, attn_grid(g, k.many_shares, requests, kv->kv_heads));
+  if (g.shares) return crowd ? "prompts, shares, products first" : "prompts, shares";
+  if (g.nth) return crowd ? "prompts, n-th row tiles, products first" : "prompts, n-th row tiles";
+  return crowd ? "prompts, products first" : "prompts";
 }
 
 int mdbf_kv_attention(const mdbf_kv_t* kv, const mdbf_attn_t* attn, const void* cache_dev, size_t cache_bytes,
