@@ -548,8 +548,9 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 4 : D == 128 ? 3 : 2) void a
               if (tok < me.lo || tok >= me.hi) z[f][j] = -INFINITY;
             }
         }
-        // The reference m follows the maximum only where that has grown by more than kSlack (numerators stay below 2^kSlack, in
-        // reach of fp16): most tiles exchange nothing between lanes and rescale nothing.
+        // A row's reference m follows its maximum only where that has grown by more than kSlack (numerators stay below 2^kSlack, in
+        // reach of fp16): most tiles exchange nothing between lanes and rescale nothing.  Rows that others bring here keep theirs
+        // (a factor of 1): a row's bits depend on its own scores alone.
         float top = z[0][0];
 #pragma unroll
         for (int f = 0; f < 4; ++f)
@@ -557,7 +558,8 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 4 : D == 128 ? 3 : 2) void a
           for (int j = 0; j < 4; ++j) top = fmaxf(top, z[f][j]);
         top *= a.scale;
         if (__any(top > m + kSlack)) {
-          const float mn = fmaxf(m, row_max(top)), alpha = __builtin_amdgcn_exp2f(m - (mn == -INFINITY ? 0.0f : mn));
+          const float high = row_max(top), mn = high > m + kSlack ? high : m;
+          const float alpha = __builtin_amdgcn_exp2f(m - (mn == -INFINITY ? 0.0f : mn));
           m = mn;
           l *= alpha;
 #pragma unroll
@@ -1030,7 +1032,8 @@ __global__ __launch_bounds__(64 * kManyWaves, D <= 128 ? 2 : 1) void attn_many_k
         for (int j = 0; j < 16; ++j) top = fmaxf(top, z[f][j]);
       if (FROM_M) top += use;
       if (__any(top > m + kSlack)) {      // as in attn_few_kernel
-        const float mn = fmaxf(m, pair_max(top)), alpha = __builtin_amdgcn_exp2f(m - (mn == -INFINITY ? 0.0f : mn));
+        const float high = pair_max(top), mn = high > m + kSlack ? high : m;
+        const float alpha = __builtin_amdgcn_exp2f(m - (mn == -INFINITY ? 0.0f : mn));
         const float before = use;
         m = mn;
         use = m == -INFINITY ? 0.0f : m;

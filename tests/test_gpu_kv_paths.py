@@ -132,6 +132,58 @@ def test_rows_that_see_everything(gpu, path):
 
 @both_types
 @every_path
+def test_what_a_row_does_not_see_does_not_change_its_bits(gpu, path, dt):
+    """Later tokens with large keys and values, earlier ones than the window has, and other rows' queries."""
+    p = Path(gpu, path, dt, seed=6)
+    s = p.s
+    clean = p.run().double().cpu().numpy()
+    rng = np.random.default_rng(6)
+    changed = []
+    for r, (n, f) in enumerate(zip(s.lengths, s.fresh)):
+        for tok in sorted({n - 1, n - 1 - f // 3, n - 1 - f // 2, 1 if p.window else n - 1} & set(range(n))):
+            changed.append((r, tok))
+            for part in range(4):
+                to = s.views[part][s.table_host[r, tok // s.P], :, tok % s.P]
+                to[:] = rng.integers(0, 256, to.shape) if part < 2 else rng.integers(128, 132, to.shape)
+    s.upload()
+    big = {(t, h) for t in range(0, p.real, 5) for h in range(t % 3, s.Hq, 3)}
+    for t, h in big:
+        s.q[t, h] *= 16
+    got = p.run().double().cpu().numpy()
+    same = 0
+    for r, (n, f) in enumerate(zip(s.lengths, s.fresh)):
+        for i in range(f):
+            pos = n - f + i
+            if any(b == r and tok <= pos and (not p.window or tok > pos - p.window) for b, tok in changed):
+                continue
+            for h in range(s.Hq):
+                if (s.cu[r] + i, h) not in big:
+                    same += 1
+                    assert np.array_equal(got[s.cu[r] + i, h], clean[s.cu[r] + i, h]), (r, i, h)
+    assert same > p.real * s.Hq // 10
+
+
+@both_types
+@every_path
+def test_queries_that_are_not_finite(gpu, path, dt):
+    p = Path(gpu, path, dt, seed=3)
+    s = p.s
+    clean = p.run().double().cpu().numpy()
+    seen = np.concatenate([n - f + np.arange(f) >= 0 for n, f in zip(s.lengths, s.fresh)])
+    bad = {(t, h) for t in range(0, p.real, 7) for h in range(t % 3, s.Hq, 3)}
+    for i, (t, h) in enumerate(sorted(bad)):
+        s.q[t, h, (5 * i) % s.d] = [float("nan"), float("inf"), -float("inf")][i % 3]
+    got = p.run().double().cpu().numpy()
+    for t in range(p.real):
+        for h in range(s.Hq):
+            if (t, h) in bad and seen[t]:
+                assert np.isnan(got[t, h]).all(), (t, h)
+            else:
+                assert np.array_equal(got[t, h], clean[t, h]), (t, h)
+
+
+@both_types
+@every_path
 def test_blocks_that_are_not_finite(gpu, path, dt):
     """NaN in a key reaches the rows that see it, in a value its block of their channels; no other bit changes."""
     p = Path(gpu, path, dt, seed=4)
