@@ -385,7 +385,7 @@ typedef struct {
  * dtype, row strides ldq, ldo.  Rows behind the last request's are left as they are; a token that sees nothing gets zeros.
  * What a token does not see has no influence on its row, whatever the bytes there are; a page number outside the pool reads as NaN.
  * Lengths are cut to what the table's row covers, fresh counts to T.  Scores, running maxima and sums are fp32.  Rounded are the
- * softmax's numerators, once to the cache's dtype, and, in calls with many new tokens, the queries (times scale), to 2^-14 (bf16) or 2^-18 (fp16) of the
+ * softmax's numerators, once to the cache's dtype (fp16: no finer than 2^-31 of the largest), and, in calls with many new tokens, the queries (times scale), to 2^-14 (bf16) or 2^-18 (fp16) of the
  * largest of each 32 channels.  Repeated calls return the same bits.
  * The workspace holds partial results where the work on long caches is cut among workgroups; it may be null where 0 bytes are needed.  Its size
  * (host arithmetic only) does not depend on requests and T, and never shrinks with max_fresh and max_length: a buffer for the largest

@@ -9,8 +9,10 @@
 // exchanges between lanes.  Values become fp16 or bf16 numbers, exactly, with their block's scale by the conversion
 // instruction on their way into LDS, where transposing reads take them.  So do keys for few query rows, in the registers that
 // feed the product; for prompts their codes are an operand as they are (below).  Scores, maxima, sums and results are fp32; the
-// numerators e^(z_j - m) are rounded to the values' type, at most half a unit of its last place each, and the sum is of what was
-// not rounded.
+// numerators e^(z_j - m) are rounded to the values' type and the sum is of what was not rounded.  The rounding errs by half a unit
+// of a numerator's last place; in fp16 also by 2^-32 of the reference's numerator at most, where the type's exponents end: numerators carry a
+// factor of 2^7 there (kLift), so that 200000 tokens at that end are 5e-5 of the sum (without it: 0.6 %, and a third of the result
+// where the token at the reference has small values).
 #include <math.h>
 
 #include <algorithm>
@@ -124,6 +126,10 @@ constexpr int kTile = 64;        // tokens per step of a wave
 constexpr int kWaves = 4;
 constexpr int kRows = 16;        // query rows of a workgroup
 constexpr float kSlack = 8;      // powers of two by which a score may exceed the running reference
+// powers of two by which numerators are larger than e^(z - m), a factor that the division takes out again: with kSlack they stay
+// below 2^15 in fp16; bf16 has fp32's exponents
+template <int DT>
+constexpr float kLift = DT == MDBF_F16 ? 7 : 0;
 
 // The tokens that a tile of ROWS query rows sees.
 struct Span {
@@ -548,8 +554,8 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 4 : D == 128 ? 3 : 2) void a
               if (tok < me.lo || tok >= me.hi) z[f][j] = -INFINITY;
             }
         }
-        // A row's reference m follows its maximum only where that has grown by more than kSlack (numerators stay below 2^kSlack, in
-        // reach of fp16): most tiles exchange nothing between lanes and rescale nothing.  Rows that others bring here keep theirs
+        // A row's reference m follows its maximum only where that has grown by more than kSlack (numerators stay below
+        // 2^(kSlack + kLift), in reach of fp16): most tiles exchange nothing between lanes and rescale nothing.  Rows that others bring here keep theirs
         // (a factor of 1): a row's bits depend on its own scores alone.
         float top = z[0][0];
 #pragma unroll
@@ -565,7 +571,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 4 : D == 128 ? 3 : 2) void a
 #pragma unroll
           for (int c = 0; c < CT; ++c) acc[c] *= alpha;
         }
-        const float use = m == -INFINITY ? 0.0f : m;
+        const float use = m == -INFINITY ? 0.0f : m - kLift<DT>;
         U32x4 pf[2];
 #pragma unroll
         for (int f = 0; f < 4; ++f) {
@@ -1036,7 +1042,7 @@ __global__ __launch_bounds__(64 * kManyWaves, D <= 128 ? 2 : 1) void attn_many_k
         const float alpha = __builtin_amdgcn_exp2f(m - (mn == -INFINITY ? 0.0f : mn));
         const float before = use;
         m = mn;
-        use = m == -INFINITY ? 0.0f : m;
+        use = m == -INFINITY ? 0.0f : m - kLift<DT>;
         l *= alpha;
 #pragma unroll
         for (int c = 0; c < CT; ++c) acc[c] *= alpha;
