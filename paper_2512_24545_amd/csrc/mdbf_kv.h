@@ -13,7 +13,8 @@ typedef __bf16 Bf16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kKvBlock = 32;              // channels that share a scale
 constexpr uint32_t kKvNanScale = 255;
-// scale bytes (2^(b - 127)) that a cache of fp16 resp. bf16 values uses: all of the block's values are numbers of that type
+// scale bytes (2^(b - 127)) that a cache of fp16 resp. bf16 values uses: all of the block's values are numbers of that type; larger
+// ones are read as NaN
 constexpr uint32_t kKvScaleMin[2] = {104, 2}, kKvScaleMax[2] = {140, 252};
 
 // bytes of one kv head's part of a page: key codes, value codes, key scales, value scales

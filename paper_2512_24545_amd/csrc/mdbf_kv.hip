@@ -413,6 +413,7 @@ struct ReadArgs {
   void *k, *v;
   int64_t ldk, ldv, slot_count;
   int32_t T, kv_heads, page_shift;
+  uint32_t scale_max;
   uint8_t wide_k, wide_v, stream;
 };
 
@@ -430,7 +431,8 @@ __global__ __launch_bounds__(256) void read_kernel(ReadArgs a) {
     if (there) {
       const KvPlace at = kv_place(slot, h, value, a.kv_heads, a.page_shift, D);
       const uint32_t codes = *(const MDBF_GLOBAL uint32_t*)((const MDBF_GLOBAL uint8_t*)a.cache + at.codes + e * 4);
-      const float unit = __builtin_bit_cast(float, (uint32_t)((const MDBF_GLOBAL uint8_t*)a.cache)[at.scales + (e >> 2)] << 23);
+      const uint32_t scale = ((const MDBF_GLOBAL uint8_t*)a.cache)[at.scales + (e >> 2)];
+      const float unit = __builtin_bit_cast(float, (scale > a.scale_max ? kKvNanScale : scale) << 23);
       const F32x2 p0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, unit, 0), p1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, unit, 1),
                   p2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, unit, 2), p3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, unit, 3);
       x[0] = p0[0], x[1] = p0[1], x[2] = p1[0], x[3] = p1[1], x[4] = p2[0], x[5] = p2[1], x[6] = p3[0], x[7] = p3[1];
@@ -580,7 +582,7 @@ int mdbf_kv_read(const mdbf_kv_t* kv, const void* cache_dev, size_t cache_bytes,
   ReadArgs a;
   a.cache = (const uint8_t*)cache_dev, a.slots = slots_dev, a.k = k_dev, a.v = v_dev, a.ldk = ldk, a.ldv = ldv;
   a.slot_count = (int64_t)kv->pages * kv->page_size, a.T = T, a.kv_heads = kv->kv_heads;
-  a.page_shift = kv_page_shift(kv->page_size);
+  a.page_shift = kv_page_shift(kv->page_size), a.scale_max = kKvScaleMax[kv->dtype];
   a.wide_k = wide_rows(ldk, y_dtype), a.wide_v = wide_rows(ldv, y_dtype);
   a.stream = 2 * T * row * dtype_size(y_dtype) > kStreamBytes;
   if (y_dtype == MDBF_F16) launch_read_d<MDBF_F16>(kv->head_dim, a, (hipStream_t)stream);

@@ -65,6 +65,10 @@ __device__ __forceinline__ uint32_t round2(float a, float b) {
   if (DT == MDBF_F16) return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, F16x2));
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, Bf16x2));
 }
+// a scale byte as loaded: beyond the type's largest it stands for NaN (as it is, its block's numbers could be infinite, and a weight of
+// zero would carry them to rows that do not see the token)
+template <int DT>
+__device__ __forceinline__ uint32_t known_scale(uint32_t scale_byte) { return scale_byte > kKvScaleMax[DT] ? kKvNanScale : scale_byte; }
 __device__ __forceinline__ float unit_of(uint32_t scale_byte) { return __builtin_bit_cast(float, scale_byte << 23); }
 
 // a wave's LDS operations execute in order: this keeps the compiler from moving them across
@@ -541,7 +545,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 4 : D == 128 ? 3 : 2) void a
           }
           z[f] = F32x4{0, 0, 0, 0};
 #pragma unroll
-          for (int s = 0; s < KW; ++s) z[f] = mma16<DT>(numbers<DT>(x.kc[f][s], unit_of(x.ks[f][KS == 1 ? 0 : s / 4])), qf[s], z[f]);
+          for (int s = 0; s < KW; ++s) z[f] = mma16<DT>(numbers<DT>(x.kc[f][s], unit_of(known_scale<DT>(x.ks[f][KS == 1 ? 0 : s / 4]))), qf[s], z[f]);
         }
         if (more) x.load_keys(next, a.page_shift, lane);
         const bool inside = t0 >= sp.all_lo && t0 + kTile <= sp.all_hi;     // every row sees every token
@@ -601,9 +605,9 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 4 : D == 128 ? 3 : 2) void a
               x.vc[g][n] = U32x4{0, 0, 0, 0};
               x.vs[g][n] = 127;
             }
-            uint64_t bad = __ballot(x.vs[g][n] == kKvNanScale);
+            uint64_t bad = __ballot(x.vs[g][n] > kKvScaleMax[DT]);
             if (bad) {
-              if (x.vs[g][n] == kKvNanScale) {
+              if (x.vs[g][n] > kKvScaleMax[DT]) {
                 x.vc[g][n] = U32x4{0, 0, 0, 0};
                 x.vs[g][n] = 127;
               }
@@ -906,13 +910,13 @@ __global__ __launch_bounds__(64 * kManyWaves, D <= 128 ? 2 : 1) void attn_many_k
         const int u = unit_of_thread(n), row = u / BL, bl = u % BL, tok = t + row;
         if (D != 64 || tid < 128) {
           *reinterpret_cast<U32x4*>(to.keys + row * KROW + bl * 16) = kc[n];
-          to.key_scales[u] = there[n] ? ks[n] : kKvNanScale;
+          to.key_scales[u] = there[n] ? known_scale<DT>(ks[n]) : kKvNanScale;
         }
         if (D != 64 || tid >= 128) {
           uint32_t sc = there[n] ? vs[n] : kKvNanScale;
           if (tok < sp.lo || tok >= sp.hi) sc = 0;
           to.value_scales[u] = sc;
-          if (sc == 0 || sc == kKvNanScale) vc[n] = U32x4{0, 0, 0, 0}, sc = 127;
+          if (sc - 1 >= kKvScaleMax[DT]) vc[n] = U32x4{0, 0, 0, 0}, sc = 127;      // 0, or read as NaN
 #pragma unroll
           for (int w = 0; w < 4; ++w) *reinterpret_cast<U32x4*>(to.values + row * VROW + block_at(bl) + w * 16) = numbers<DT>(vc[n][w], unit_of(sc));
         }
@@ -1066,19 +1070,22 @@ __global__ __launch_bounds__(64 * kManyWaves, D <= 128 ? 2 : 1) void attn_many_k
 
       // NaN among the values: to the rows that see it
       {
-        bool bad = false;
+        // bytes beyond the type's largest, four at a time: the high bit, and a carry from the other seven into it
+        constexpr uint32_t kRest = 0x7f7f7f7fu, kTo = (0xffu - kKvScaleMax[DT]) * 0x01010101u;
+        uint32_t bad = 0;
 #pragma unroll
         for (int w = 0; w < UNITS / 256; ++w) {
           const uint32_t x = *reinterpret_cast<const uint32_t*>(in.value_scales + w * 256 + lane * 4);
-          bad |= (x & 0xffu) == 0xffu || (x & 0xff00u) == 0xff00u || (x & 0xff0000u) == 0xff0000u || x >= 0xff000000u;
+          bad |= ((x & kRest) + kTo) & x;
         }
         if (UNITS < 256) {
           const uint32_t x = reinterpret_cast<const uint16_t*>(in.value_scales)[lane];
-          bad |= (x & 0xffu) == 0xffu || x >= 0xff00u;
+          bad |= ((x & kRest) + kTo) & x;
         }
+        bad &= 0x80808080u;
         if (__any(bad)) {
           for (int u = 0; u < UNITS; ++u)
-            if (in.value_scales[u] == kKvNanScale) {
+            if (in.value_scales[u] > kKvScaleMax[DT]) {
               const int tok = t0 + u / BL;
               if (tok >= me.lo && tok < me.hi) nan_blocks |= 1u << u % BL;
             }

@@ -50,3 +50,70 @@ def test_a_long_tail_behind_tokens_of_high_score_and_no_value(gpu, path, dt, gap
                 tol += (seen * 2.0 ** -32 * np.abs(v).max(initial=0) / den)[:, None]
             err = np.abs(got[s.cu[r]:s.cu[r] + f, h] - ref)
             assert (err <= tol).all(), (r, h, (err / tol).max())
+
+
+BEYOND = {"f16": [141, 160, 200, 254, 255], "bf16": [253, 254, 255]}      # scale bytes of numbers that the type does not have
+
+
+@both_types
+@every_path
+def test_scale_bytes_beyond_the_type_are_nan(gpu, path, dt):
+    """In a key for the rows that see it, in a value for its block of their channels; no other bit changes, with all codes at their
+    largest."""
+    p = Path(gpu, path, dt, seed=8)
+    s = p.s
+    clean = p.run().double().cpu().numpy()
+    keys, values, i = [], [], 0         # (request, token, kv head, block)
+    for r, (n, f) in enumerate(zip(s.lengths, s.fresh)):
+        for tok in sorted({0, n // 2, n - 1 - f // 2, n - 2, n - 1} & set(range(n))):
+            (keys if i % 3 == 0 else values).append((r, tok, (r + i) % s.Hkv, (r + 2 * i) % (s.d // 32)))
+            i += 1
+    for part, where in ((2, keys), (3, values)):
+        for i, (r, tok, head, block) in enumerate(where):
+            page, at = s.table_host[r, tok // s.P], tok % s.P
+            s.views[part][page, head, at, block] = BEYOND[dt][i % len(BEYOND[dt])]
+            s.views[part - 2][page, head, at, 16 * block:16 * block + 16] = 0xF7 if i % 2 else 0x77
+    s.upload()
+    got = p.run().double().cpu().numpy()
+    for r, (n, f) in enumerate(zip(s.lengths, s.fresh)):
+        for i in range(f):
+            pos = n - f + i
+            sees = lambda tok: tok <= pos and (not p.window or tok > pos - p.window)
+            for h in range(s.Hq):
+                head, want = h // (s.Hq // s.Hkv), np.zeros(s.d, bool)
+                for b, tok, kv_head, block in keys:
+                    if b == r and kv_head == head and sees(tok):
+                        want[:] = True
+                for b, tok, kv_head, block in values:
+                    if b == r and kv_head == head and sees(tok):
+                        want[32 * block:32 * block + 32] = True
+                t = s.cu[r] + i
+                assert np.array_equal(np.isnan(got[t, h]), want), (r, i, h)
+                assert np.array_equal(got[t, h][~want], clean[t, h][~want]), (r, i, h)
+
+
+@pytest.mark.parametrize("dt,largest", [("f16", 140), ("bf16", 252)])
+@pytest.mark.parametrize("y_dt", ["f16", "bf16", "f32"])
+def test_every_scale_byte_read_back(gpu, dt, largest, y_dt):
+    torch, mb = gpu
+    cache = mb.KVCache(16, 1, 64, 16, dt)
+    views = kvo.page_views(cache.buffer.cpu().numpy(), 16, 1, 16, 64)
+    rng = np.random.default_rng(9)
+    codes, scales = rng.integers(0, 256, (2, 256, 32)).astype(np.uint8), np.arange(256, dtype=np.uint8)
+    slot = rng.permutation(256)
+    for part in (0, 1):
+        views[part][slot // 16, 0, slot % 16] = codes[part]
+        views[part + 2][slot // 16, 0, slot % 16] = scales[:, None]
+    pool = np.concatenate([x.reshape(16, 1, -1) for x in views], 2).reshape(-1)
+    cache = mb.KVCache(16, 1, 64, 16, dt, buffer=torch.from_numpy(pool).cuda())
+    ttype = {"f16": torch.float16, "bf16": torch.bfloat16, "f32": torch.float32}[y_dt]
+    out = [torch.empty((256, 1, 64), dtype=ttype, device="cuda:0") for _ in range(2)]
+    for y, c in zip(mb.mdbf_kv_read(cache, torch.from_numpy(slot).cuda(), out=out), codes):
+        y = y.double().cpu().numpy()[:, 0]
+        assert np.isnan(y[largest + 1:]).all()
+        known = slice({"f16": 104, "bf16": 2}[dt], largest + 1)
+        with np.errstate(over="ignore"):
+            want = kvo.values(kvo.unpack(c), np.repeat(scales[:, None], 2, 1))[known]
+            if y_dt == "f16" and dt == "bf16":
+                want = want.astype(np.float16).astype(np.float64)
+        assert np.array_equal(y[known], want)
