@@ -373,6 +373,7 @@ int mdbf_qk_norm_rope(const mdbf_rope_t* desc, const void* q_dev, int64_t ldq, c
 
 #define MDBF_ATTN_CAUSAL 1u   /* a token sees the ones up to its own position (the new tokens are the request's last);
                                  without it all of the request */
+#define MDBF_ATTN_EXACT_QUERIES 2u   /* queries are not rounded, whatever a call runs: see there */
 typedef struct {
   int32_t q_heads;      /* a multiple of kv_heads: query head h reads kv head h / (q_heads / kv_heads) */
   uint32_t flags;
@@ -387,8 +388,9 @@ typedef struct {
  * dtype, row strides ldq, ldo.  Rows behind the last request's are left as they are; a token that sees nothing gets zeros.
  * What a token does not see has no influence on its row, whatever the bytes there are; a page number outside the pool reads as NaN.
  * Lengths are cut to what the table's row covers, fresh counts to T.  Scores, running maxima and sums are fp32.  Rounded are the
- * softmax's numerators, once to the cache's dtype (fp16: no finer than 2^-31 of the largest), and, in calls with many new tokens, the queries (times scale), to 2^-14 (bf16) or 2^-18 (fp16) of the
- * largest of each 32 channels.  Repeated calls return the same bits.
+ * softmax's numerators, once to the cache's dtype (fp16: no finer than 2^-31 of the largest), and, in calls with many new tokens, the queries (times scale), to
+ * 1.07 * 2^-14 (bf16) or 2^-18 (fp16) of the largest of each 32 channels.  With MDBF_ATTN_EXACT_QUERIES they are not: for queries with channels far
+ * beyond their neighbours' (some 30 times and more); such calls take up to 15 % longer.  Repeated calls return the same bits.
  * The workspace holds partial results where the work on long caches is cut among workgroups; it may be null where 0 bytes are needed.  Its size
  * (host arithmetic only) does not depend on requests and T, and never shrinks with max_fresh and max_length: a buffer for the largest
  * call serves all of the same heads. */

@@ -23,6 +23,7 @@ MDBF_FLAG_FP16_STAGED = 8
 MDBF_KV_BAD_LENGTH, MDBF_KV_BAD_WIDTH, MDBF_KV_BAD_TOKENS, MDBF_KV_NO_PAGES = 1, 2, 4, 8
 MDBF_ROPE_INTERLEAVED = 1
 MDBF_ATTN_CAUSAL = 1
+MDBF_ATTN_EXACT_QUERIES = 2
 DTYPE_CODE = {"f16": MDBF_F16, "bf16": MDBF_BF16, "f32": MDBF_F32}
 
 STATUS = {0: "MDBF_OK", -1: "MDBF_EINVAL", -2: "MDBF_EALIGN", -3: "MDBF_EDTYPE", -4: "MDBF_EWORKSPACE",
@@ -594,10 +595,11 @@ def mdbf_kv_attention_kernel(cache, q_heads, requests, tokens, max_fresh, max_le
 
 
 def mdbf_kv_attention(cache, q, table, cu, lengths, max_fresh, max_length, scale=None, causal=True, window=0, out=None, workspace=None,
-                      stream=None):
+                      stream=None, exact_queries=False):
     """Attention of the new tokens' queries q (T, q_heads, d; the cache's dtype) over the cache.  table (requests x width), cu (requests + 1)
     and lengths (requests) are int32 CUDA tensors as mdbf_kv_slots leaves them; max_fresh, max_length: bounds of the
-    new tokens and the length of a request (launch sizes).  Returns out (T, q_heads, d)."""
+    new tokens and the length of a request (launch sizes).  exact_queries: not rounded in calls with many new tokens either.  Returns
+    out (T, q_heads, d)."""
     torch = _torch()
     shape, dtype = q.shape, q.dtype
     T, Hq, d = shape
@@ -613,7 +615,7 @@ def mdbf_kv_attention(cache, q, table, cu, lengths, max_fresh, max_length, scale
     if workspace is None:
         with _on(stream):
             workspace = mdbf_kv_attention_workspace(cache, Hq, n, T, max_fresh, max_length, causal, window)
-    desc = _attn_desc(Hq, MDBF_ATTN_CAUSAL if causal else 0, window, max_fresh, max_length, d ** -0.5 if scale is None else scale)
+    desc = _attn_desc(Hq, (MDBF_ATTN_CAUSAL if causal else 0) | (MDBF_ATTN_EXACT_QUERIES if exact_queries else 0), window, max_fresh, max_length, d ** -0.5 if scale is None else scale)
     ws = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
     status = (_lib or lib()).mdbf_kv_attention(cache.desc, desc, *cache.args, table.data_ptr(), ld if ld >= width or n > 1 else width, width,
                                                cu.data_ptr(), lengths.data_ptr(), n, q.data_ptr(), _row_stride(q, Hq * d), T, out.data_ptr(),

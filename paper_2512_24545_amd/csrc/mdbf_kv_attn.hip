@@ -797,9 +797,11 @@ __device__ __forceinline__ void each_of(F&& f, std::integer_sequence<int, I...>)
   (f(std::integral_constant<int, I>{}), ...);
 }
 
-// 32 channels of a query as a sum of NL fp6 numbers, each limb's scale 2^-4 of the one before: an absolute error of 2^-(4 NL + 2)
+// 32 channels of a query as a sum of NL fp6 numbers, each limb's scale 2^-4 of the one before: an absolute error of 1.07 * 2^-(4 NL + 2)
 // of the largest of the 32 at most.  Three limbs for bf16 and four for fp16: in a score of ten that is no more than the rounding of its
-// numerator, 2^-9 and 2^-12.
+// numerator, 2^-9 and 2^-12, and for a channel down to a 32nd (bf16) or 64th (fp16) of the largest no more than half a spacing of the
+// type.  Where one channel is far beyond the others it is much of what those are (a thousand times: 2.4 % of the result in bf16 if
+// the keys are as far the other way, 0.17 in fp16; 32 times: 0.1 and 0.007): MDBF_ATTN_EXACT_QUERIES.
 template <int NL>
 struct Limbs {
   v6u limb[NL];
@@ -832,8 +834,10 @@ __device__ __forceinline__ float pair_max(float x) {
   return fmaxf(__builtin_bit_cast(float, a0), __builtin_bit_cast(float, a1));
 }
 
-// CROWD: waves that feed products go first (see launch_few).
-template <int D, int DT, bool CROWD>
+// CROWD: waves that feed products go first (see kCrowds).  EXACT: queries as they are, in 16-bit products for which every wave makes
+// numbers of the key codes: 2048 tokens behind 14336, 32 heads on 8 of 128, 432 -> 480 us (fp16 479 -> 497), 1000 behind 5000, 32 of
+// 64, 85 -> 98.
+template <int D, int DT, bool CROWD, bool EXACT>
 __global__ __launch_bounds__(64 * kManyWaves, D <= 128 ? 2 : 1) void attn_many_kernel(AttnArgs a) {
   constexpr int BL = D / 32;                       // blocks of a token
   constexpr int UNITS = kTile * BL;                // 16-byte units of a tile's keys, and of its values
@@ -945,6 +949,12 @@ __global__ __launch_bounds__(64 * kManyWaves, D <= 128 ? 2 : 1) void attn_many_k
     look_up(begin + kTile);
     Limbs<NL> ql[ST];
     bool finite = true;
+    if constexpr (EXACT) {
+#pragma unroll
+      for (int s = 0; s < ST; ++s)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) raw[s][w] ^= a.flip;
+    } else
 #pragma unroll
     for (int s = 0; s < ST; ++s) {
       float q[32];
@@ -962,8 +972,8 @@ __global__ __launch_bounds__(64 * kManyWaves, D <= 128 ? 2 : 1) void attn_many_k
     }
 
     // The products' sums begin at -m, so that they end as the exponentials' arguments; with D = 256 no registers are left for
-    // that.
-    constexpr bool FROM_M = D <= 128;
+    // that, and 16-bit queries do not carry the scale.
+    constexpr bool FROM_M = D <= 128 && !EXACT;
     F32x16 from_m;
 #pragma unroll
     for (int j = 0; j < 16; ++j) from_m[j] = 0;
@@ -1009,7 +1019,13 @@ __global__ __launch_bounds__(64 * kManyWaves, D <= 128 ? 2 : 1) void attn_many_k
         U32x4 codes[2];
 #pragma unroll
         for (int f = 0; f < 2; ++f) codes[f] = *reinterpret_cast<const U32x4*>(in.keys + (32 * f + r) * KROW + (2 * s + hh) * 16);
-        each_of([&](auto k) __attribute__((always_inline)) {
+        if constexpr (EXACT) {
+#pragma unroll
+          for (int w = 0; w < 4; ++w)
+#pragma unroll
+            for (int f = 0; f < 2; ++f)
+              z[f] = mma32<DT>(numbers<DT>(codes[f][w], unit_of(sc[f][s / 2] >> (16 * (s & 1)) & 255u)), raw[s][w], z[f]);
+        } else each_of([&](auto k) __attribute__((always_inline)) {
           constexpr int L = NL - 1 - decltype(k)::value;      // the smallest first
 #pragma unroll
           for (int f = 0; f < 2; ++f) z[f] = mx32<2 * (s & 1), L>(codes[f], sc[f][s / 2], ql[s].limb[L], ql[s].scales, z[f]);
@@ -1040,6 +1056,7 @@ __global__ __launch_bounds__(64 * kManyWaves, D <= 128 ? 2 : 1) void attn_many_k
       for (int f = 0; f < 2; ++f)
 #pragma unroll
         for (int j = 0; j < 16; ++j) top = fmaxf(top, z[f][j]);
+      if (EXACT) top *= a.scale;
       if (FROM_M) top += use;
       if (__any(top > m + kSlack)) {      // as in attn_few_kernel
         const float high = pair_max(top), mn = high > m + kSlack ? high : m;
@@ -1062,7 +1079,7 @@ __global__ __launch_bounds__(64 * kManyWaves, D <= 128 ? 2 : 1) void attn_many_k
         for (int j = 0; j < 16; j += 4) {
           float p[4];
 #pragma unroll
-          for (int k = 0; k < 4; ++k) p[k] = __builtin_amdgcn_exp2f(FROM_M ? z[f][j + k] : z[f][j + k] - use);
+          for (int k = 0; k < 4; ++k) p[k] = __builtin_amdgcn_exp2f(FROM_M ? z[f][j + k] : EXACT ? z[f][j + k] * a.scale - use : z[f][j + k] - use);
           l += (p[0] + p[1]) + (p[2] + p[3]);
           pf[2 * f + j / 8][j / 4 % 2 * 2] = round2<DT>(p[0], p[1]);
           pf[2 * f + j / 8][j / 4 % 2 * 2 + 1] = round2<DT>(p[2], p[3]);
@@ -1143,7 +1160,7 @@ static int check_attn(const mdbf_kv_t* kv, const mdbf_attn_t* at, int requests, 
   if (at->q_heads <= 0 || at->q_heads % kv->kv_heads || at->window < 0 || at->max_fresh < 1 || at->max_length < 1 || !isfinite(at->scale) || at->scale == 0.0f)
     return MDBF_EINVAL;
   if (at->window && !(at->flags & MDBF_ATTN_CAUSAL)) return MDBF_EINVAL;
-  if ((at->flags & ~MDBF_ATTN_CAUSAL) || at->q_heads > (1 << 16)) return MDBF_EUNSUPPORTED;
+  if ((at->flags & ~(MDBF_ATTN_CAUSAL | MDBF_ATTN_EXACT_QUERIES)) || at->q_heads > (1 << 16)) return MDBF_EUNSUPPORTED;
   return MDBF_OK;
 }
 
@@ -1165,7 +1182,7 @@ static AttnCosts attn_costs(int d) {
 }
 struct AttnGeom {
   int row_tiles;           // of a request and kv head; nth: of all requests and a kv head
-  bool shares, many, nth;
+  bool shares, many, nth, exact;
   bool distant;            // a row tile of the prompts' kernel sees 4096 tokens or more on average
 };
 static bool attn_cuts(const mdbf_attn_t& at) { return (at.window ? std::min(at.max_length, at.window) : at.max_length) > kWhole; }
@@ -1188,9 +1205,10 @@ static AttnGeom attn_geom(const mdbf_kv_t& kv, const mdbf_attn_t& at, int all, i
   const double even = many_tiles * (units_of(kManyRows, false) + kManyCost) / k.many_shares, crowd = std::min(1.0, std::max(0.0, many_tiles / 256 - 1));
   const double whole = std::max((k.one + crowd * (k.full - k.one)) * (units_of(kManyRows, true) + kManyCost), k.full * even);
   const double cut = k.full * even + 12 + k.parts * std::min(1.0, even / kLeastShare);
-  AttnGeom g;
+  AttnGeom g = {};
   g.many = rows > kRows && std::min(whole, cuts ? cut : whole) < few;
   g.shares = cuts && (!g.many || cut < whole);
+  g.exact = at.flags & MDBF_ATTN_EXACT_QUERIES;
   g.row_tiles = (int)std::min(tiles_of(g.many ? kManyRows : kRows), 65536.0);
   // Row tiles without shares: each workgroup takes one that its request may have, or the n-th of those that there are, for which
   // it looks through the requests.  That takes 0.5 to 2 us but spreads them evenly where most requests are much shorter than the
@@ -1224,12 +1242,17 @@ static size_t attn_workspace(const mdbf_kv_t& kv, const mdbf_attn_t& at) {
   return kv.head_dim == 64 ? workspace_of<64>(few) : kv.head_dim == 128 ? workspace_of<128>(few) : workspace_of<256>(few);
 }
 
+template <int D, int DT, bool EXACT>
+static void launch_many(unsigned grid, const AttnArgs& a, const AttnGeom& g, hipStream_t s) {
+  if (kCrowds<D> && attn_crowds(g, grid)) attn_many_kernel<D, DT, kCrowds<D>, EXACT><<<grid, 64 * kManyWaves, 0, s>>>(a);
+  else attn_many_kernel<D, DT, false, EXACT><<<grid, 64 * kManyWaves, 0, s>>>(a);
+}
 template <int D, int DT>
-static int launch_few(AttnArgs& a, const AttnGeom& g, hipStream_t s) {
+static int launch_kernels(AttnArgs& a, const AttnGeom& g, hipStream_t s) {
   a.shares = !g.shares ? 0 : g.many ? kManyShares<D> : kFewShares<D>;
   const unsigned grid = attn_grid(g, a.shares, a.requests, a.kv_heads);
-  if (kCrowds<D> && attn_crowds(g, grid)) attn_many_kernel<D, DT, kCrowds<D>><<<grid, 64 * kManyWaves, 0, s>>>(a);
-  else if (g.many) attn_many_kernel<D, DT, false><<<grid, 64 * kManyWaves, 0, s>>>(a);
+  if (g.many && g.exact) launch_many<D, DT, true>(grid, a, g, s);
+  else if (g.many) launch_many<D, DT, false>(grid, a, g, s);
   else if (a.page_shift == 4) attn_few_kernel<D, DT, 4><<<grid, 64 * kWaves, 0, s>>>(a);
   else if (a.page_shift == 5) attn_few_kernel<D, DT, 2><<<grid, 64 * kWaves, 0, s>>>(a);
   else attn_few_kernel<D, DT, 1><<<grid, 64 * kWaves, 0, s>>>(a);
@@ -1245,7 +1268,7 @@ static int launch_few(AttnArgs& a, const AttnGeom& g, hipStream_t s) {
 }
 template <int DT>
 static int launch_attn(int d, AttnArgs& a, const AttnGeom& g, hipStream_t s) {
-  return d == 64 ? launch_few<64, DT>(a, g, s) : d == 128 ? launch_few<128, DT>(a, g, s) : launch_few<256, DT>(a, g, s);
+  return d == 64 ? launch_kernels<64, DT>(a, g, s) : d == 128 ? launch_kernels<128, DT>(a, g, s) : launch_kernels<256, DT>(a, g, s);
 }
 
 }  // namespace mdbf

@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 
 from oracle import kv_oracle as kvo
-from test_gpu_kv import U, gpu  # noqa: F401  (gpu: the fixture)
+from test_gpu_kv import U, attention_tolerance, gpu, rows  # noqa: F401  (gpu: the fixture)
 from test_gpu_kv_paths import Path, both_types, every_path
 
 pytestmark = pytest.mark.gpu
@@ -117,3 +117,58 @@ def test_every_scale_byte_read_back(gpu, dt, largest, y_dt):
             if y_dt == "f16" and dt == "bf16":
                 want = want.astype(np.float16).astype(np.float64)
         assert np.array_equal(y[known], want)
+
+
+@both_types
+@every_path
+@pytest.mark.parametrize("times,exact", [(1, True), (32, True), (1000, True), (1, False), (32, False)])
+def test_queries_with_channels_far_beyond_the_others(gpu, path, dt, times, exact):
+    """One channel of 32 that many times the others, where all keys are zero: what is left of the scores must be that of the other
+    channels.  Exact queries: the tolerance of few rows in every form; else with the rounding that prompts have (test_gpu_kv_paths.py)."""
+    torch, _ = gpu
+    p = Path(gpu, path, dt, seed=10)
+    s = p.s
+    q = np.random.default_rng(10).standard_normal((p.T, s.Hq, s.d))
+    q[:, :, 3::32] *= times
+    s.q, s.q64 = rows(torch, q, dt)
+    s.views[0][..., 1::16] &= 0x0F                       # channels 3, 35, ...: the odd half of bytes 1, 17, ...
+    for r in range(len(s.lengths)):
+        s.k[r][..., 3::32] = 0
+    s.upload()
+    out = torch.full(s.q.shape, 5.0, dtype=s.q.dtype, device="cuda:0")
+    got = p.run(out=out, exact_queries=exact).double().cpu().numpy()
+    assert (got[p.real:] == 5.0).all()
+    e = 0.0 if exact or not p.name.startswith("prompts") else 1.07 * 2.0 ** (-14 if dt == "bf16" else -18)
+    for r, (n, f) in enumerate(zip(s.lengths, s.fresh)):
+        at, pos = slice(s.cu[r], s.cu[r] + f), n - f + np.arange(f)
+        for h in range(s.Hq if f else 0):
+            x, k, v = s.q64[at, h], s.k[r][:, h // (s.Hq // s.Hkv)], s.v[r][:, h // (s.Hq // s.Hkv)]
+            ref, mag, den = kvo.attention(x, k, v, pos, True, p.window, s.d ** -0.5)
+            tol = attention_tolerance(dt, ref, mag, den, x, k, v, s.d ** -0.5) + n * 2.0 ** -126 * np.abs(v).max(initial=0)
+            if e and n:
+                dz = s.d ** -0.5 * e * np.abs(x).reshape(f, -1, 32).max(2) @ np.abs(k).reshape(n, -1, 32).sum(2).max(0)
+                tol = tol + (np.exp(2 * dz) - 1)[:, None] * mag
+            err = np.abs(got[at, h] - ref)
+            assert (err <= tol).all(), (r, h, (err / tol).max())
+
+
+@both_types
+@every_path
+def test_exact_queries_that_are_not_finite_and_lie_apart(gpu, path, dt):
+    """NaN in the rows with such queries, the other rows' bits as they were; the same bits from strides that no wide access fits."""
+    p = Path(gpu, path, dt, seed=11)
+    s = p.s
+    clean = p.run(scale=-0.2, exact_queries=True).double().cpu().numpy()
+    seen = np.concatenate([n - f + np.arange(f) >= 0 for n, f in zip(s.lengths, s.fresh)])
+    q = p.torch.zeros((p.T, s.Hq * s.d + 3), dtype=s.q.dtype, device="cuda:0")[:, :s.Hq * s.d].unflatten(1, (s.Hq, s.d))
+    q.copy_(s.q)
+    bad = {(t, h) for t in range(0, p.real, 7) for h in range(t % 3, s.Hq, 3)}
+    for i, (t, h) in enumerate(sorted(bad)):
+        q[t, h, (5 * i) % s.d] = [float("nan"), float("inf"), -float("inf")][i % 3]
+    got = p.run(scale=-0.2, exact_queries=True, q=q).double().cpu().numpy()
+    for t in range(p.real):
+        for h in range(s.Hq):
+            if (t, h) in bad and seen[t]:
+                assert np.isnan(got[t, h]).all(), (t, h)
+            else:
+                assert np.array_equal(got[t, h], clean[t, h]), (t, h)

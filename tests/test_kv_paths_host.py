@@ -22,12 +22,12 @@ def test_every_form_is_run(d):
     assert taken == {name for dd, name, *_ in paths.PATHS if dd == d} == (NAMES | FIRST if d == 128 else NAMES)
 
 
-def test_the_type_does_not_matter():
+def test_the_type_and_the_queries_form_do_not_matter():
     for d, name, Hq, Hkv, n, T, fresh, length, window, _ in paths.PATHS:
-        assert kernel(d, Hq, Hkv, n, T, fresh, length, window, dtype=0) == kernel(d, Hq, Hkv, n, T, fresh, length, window) == name
+        assert kernel(d, Hq, Hkv, n, T, fresh, length, window, dtype=0) == kernel(d, Hq, Hkv, n, T, fresh, length, window, flags=3) == kernel(d, Hq, Hkv, n, T, fresh, length, window) == name
 
 
 def test_what_is_refused_has_no_name():
     assert kernel(96, 4, 2, 1, 1, 1, 1) == kernel(128, 5, 2, 1, 1, 1, 1) == kernel(128, 4, 2, 0, 1, 1, 1) == kernel(128, 4, 2, 1, 1, 0, 1) == ""
-    assert kernel(128, 4, 2, 1, 1, 1, 1, flags=2) == kernel(128, 4, 2, 1, 1, 1, 1, dtype=2) == kernel(128, 4, 2, 1, 1, 1, 1, window=-1) == ""
+    assert kernel(128, 4, 2, 1, 1, 1, 1, flags=4) == kernel(128, 4, 2, 1, 1, 1, 1, dtype=2) == kernel(128, 4, 2, 1, 1, 1, 1, window=-1) == ""
     assert mb.lib().mdbf_kv_attention_kernel(None, None, 1, 1) == b""
