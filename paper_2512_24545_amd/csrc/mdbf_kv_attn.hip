@@ -246,7 +246,7 @@ struct Work {
   // This workgroup's share: prefix sums over the requests, of up to 64 by every wave for itself, which deals its lanes out to
   // them, else by the workgroup, 256 at a time, first of all and then again up to the one where the share begins; and in that
   // one over its row tiles, 64 at a time.  1500 rows of 8 heads and 1 kv head of 128 against 9500 tokens, 94 row tiles: 74 us, 93
-  // where a lane went over them one by one.  `find`: six words of LDS.
+  // where a lane went over them one by one.  `find`: six words of LDS that nothing else uses.
   __device__ __forceinline__ void first(const AttnArgs& a, int64_t* find) {
     const int tid = threadIdx.x, lane = tid & 63;
     const bool few = a.requests <= 64;
@@ -471,8 +471,8 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 4 : D == 128 ? 3 : 2) void a
 
   Work<kRows, kRowsCost> work;
   if (a.shares) {
-    work.first(a, reinterpret_cast<int64_t*>(stat));
-    __syncthreads();
+    __shared__ int64_t find[6];
+    work.first(a, find);
   } else {      // a workgroup per row tile that the launch was sized for
     const uint32_t idx = blockIdx.x / a.row_tiles;
     work.whole(a, idx / a.kv_heads, blockIdx.x % a.row_tiles, idx % a.kv_heads);
@@ -861,8 +861,8 @@ __global__ __launch_bounds__(64 * kManyWaves, D <= 128 ? 2 : 1) void attn_many_k
 
   Work<kManyRows, kManyCost> work;
   if (a.shares) {
-    work.first(a, reinterpret_cast<int64_t*>(&lds[0]));
-    __syncthreads();
+    __shared__ int64_t find[6];
+    work.first(a, find);
   } else {      // kv heads next to each other (their row tiles then share an XCD's cache), the row tiles that see most first
     const uint32_t idx = blockIdx.x / a.kv_heads;
     if (a.nth) work.whole_nth(a, idx, blockIdx.x % a.kv_heads);
