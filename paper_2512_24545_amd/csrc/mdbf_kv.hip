@@ -63,7 +63,7 @@ template <class P>
 __device__ __forceinline__ int last_at_most(P start, int n, int t) {
   int lo = 0, hi = n;
   while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
+    const int mid = lo + ((hi - lo) >> 1);
     if (start[mid] <= t) lo = mid;
     else hi = mid;
   }
@@ -138,7 +138,8 @@ __global__ __launch_bounds__(kSlotThreads) void slots_kernel(SlotArgs a) {
       a.cu[r] = first;
     }
     __syncthreads();
-    for (int i = tid; i < (int)total[1]; i += kSlotThreads) {
+    for (int64_t j = tid; j < total[1]; j += kSlotThreads) {
+      const int i = (int)j;
       const int q = last_at_most(page_start, n, page0 + i);
       a.table[(r0 + q) * a.table_ld + held[q] + (page0 + i - page_start[q])] = a.free_pages[page0 + i];
     }
@@ -492,7 +493,7 @@ static int launch_qkv(int xd, int yd, int d, QkvArgs& a, hipStream_t s) {
   int parts = (int)std::min<int64_t>((a.units + per - 1) / per, std::max<int64_t>(1, waves / a.T));
   a.units_per_wave = ((a.units + parts - 1) / parts + per - 1) / per * per;
   parts = (a.units + a.units_per_wave - 1) / a.units_per_wave;
-  const dim3 grid((unsigned)((a.T + 3) / 4), (unsigned)parts);
+  const dim3 grid((unsigned)(((int64_t)a.T + 3) / 4), (unsigned)parts);
   if (xd == MDBF_F16) launch_qkv_x<MDBF_F16>(yd, d, grid, a, s);
   else if (xd == MDBF_BF16) launch_qkv_x<MDBF_BF16>(yd, d, grid, a, s);
   else launch_qkv_x<MDBF_F32>(yd, d, grid, a, s);
@@ -501,7 +502,7 @@ static int launch_qkv(int xd, int yd, int d, QkvArgs& a, hipStream_t s) {
 
 template <int YD, bool STREAM>
 static void launch_read_s(int d, const ReadArgs& a, hipStream_t s) {
-  const dim3 grid((unsigned)((a.T + 3) / 4));
+  const dim3 grid((unsigned)(((int64_t)a.T + 3) / 4));
   if (d == 64) read_kernel<YD, 64, STREAM><<<grid, 256, 0, s>>>(a);
   else if (d == 128) read_kernel<YD, 128, STREAM><<<grid, 256, 0, s>>>(a);
   else read_kernel<YD, 256, STREAM><<<grid, 256, 0, s>>>(a);
@@ -584,7 +585,7 @@ int mdbf_kv_read(const mdbf_kv_t* kv, const void* cache_dev, size_t cache_bytes,
   a.slot_count = (int64_t)kv->pages * kv->page_size, a.T = T, a.kv_heads = kv->kv_heads;
   a.page_shift = kv_page_shift(kv->page_size), a.scale_max = kKvScaleMax[kv->dtype];
   a.wide_k = wide_rows(ldk, y_dtype), a.wide_v = wide_rows(ldv, y_dtype);
-  a.stream = 2 * T * row * dtype_size(y_dtype) > kStreamBytes;
+  a.stream = 2 * (int64_t)T * row * dtype_size(y_dtype) > kStreamBytes;
   if (y_dtype == MDBF_F16) launch_read_d<MDBF_F16>(kv->head_dim, a, (hipStream_t)stream);
   else if (y_dtype == MDBF_BF16) launch_read_d<MDBF_BF16>(kv->head_dim, a, (hipStream_t)stream);
   else launch_read_d<MDBF_F32>(kv->head_dim, a, (hipStream_t)stream);

@@ -1188,14 +1188,14 @@ struct AttnGeom {
 static bool attn_cuts(const mdbf_attn_t& at) { return (at.window ? std::min(at.max_length, at.window) : at.max_length) > kWhole; }
 static AttnGeom attn_geom(const mdbf_kv_t& kv, const mdbf_attn_t& at, int all, int T) {
   const AttnCosts k = attn_costs(kv.head_dim);
-  const int fresh = std::min(at.max_fresh, T), requests = (T + fresh - 1) / fresh;      // requests with as many new tokens as any
+  const int fresh = std::min(at.max_fresh, T), requests = (int)(((int64_t)T + fresh - 1) / fresh);      // requests with as many new tokens as any
   const double rows = (double)fresh * (at.q_heads / kv.kv_heads);
   auto tiles_of = [&](int per) { return ceil(rows / per); };
   // units of a row tile: of the one that sees most, and on average
   auto units_of = [&](int per, bool most) {
     double span = at.max_length;
     if ((at.flags & MDBF_ATTN_CAUSAL) && !most) span -= std::min<double>(fresh, span) / 2;
-    if (at.window) span = std::min<double>(span, at.window + per * fresh / rows);
+    if (at.window) span = std::min<double>(span, at.window + (double)per * fresh / rows);
     return span / kTile + 1;
   };
   const bool cuts = attn_cuts(at);
@@ -1317,7 +1317,8 @@ int mdbf_kv_attention(const mdbf_kv_t* kv, const mdbf_attn_t* attn, const void* 
   if (need && !workspace_dev) return MDBF_EINVAL;
   if (workspace_bytes < need) return MDBF_EWORKSPACE;
   const int group = attn->q_heads / kv->kv_heads;
-  if ((int64_t)requests * kv->kv_heads * geom.row_tiles > 0x7fffffff || (int64_t)T * group > 0x70000000) return MDBF_EUNSUPPORTED;
+  // (rows and requests are counted in steps of up to 8192, by 32 bits)
+  if ((int64_t)requests * kv->kv_heads * geom.row_tiles > 0x7fffffff || (int64_t)T * group > 0x70000000 || requests > 0x70000000) return MDBF_EUNSUPPORTED;
   AttnArgs a = {};
   a.cache = (const uint8_t*)cache_dev, a.table = table_dev, a.cu = cu_dev, a.lengths = lengths_dev, a.q = q_dev, a.out = out_dev;
   a.table_ld = table_ld, a.ldq = ldq, a.ldo = ldo, a.table_width = table_width, a.requests = requests, a.T = T, a.pages = kv->pages;
