@@ -14,7 +14,7 @@ namespace mdbf {
 // the first one's results are still there), whose prefixes stay in LDS for the tokens and the new pages, which find their
 // request by bisection.  Long steps leave the tokens to a second launch that bisects cu, in LDS where that has room.  All
 // latency: the kernel takes 5.1 us for 64 requests with a token each, 7.4 and 6.5 for 500 prompts of 250000 tokens (3 MB, 0.6 us at
-// the rate of a copy): dependent loads, two scans and their barriers.
+// the rate of a copy): dependent loads, a scan (a second one and more from 1025 requests on) and its barriers.
 constexpr int kSlotThreads = 1024;
 constexpr int kSlotOneLaunch = 8192;      // new tokens up to which the first launch writes the slots too
 constexpr int kSlotTokens = 1024;         // tokens per workgroup of the second launch
@@ -308,8 +308,8 @@ struct QkvArgs {
 };
 
 // Rows in, rows out and codes out, each once: x / sqrt(mean x^2 + eps) * w, then pairs (p, q) -> (p c - q s, q c + p s), in fp32 and
-// rounded once, at the store; keys and values that go into the cache are first rounded to its type, as a program that stored
-// them in between would.  D / 8 lanes hold a head, eight channels each: the sum of squares is a few exchanges among them, a rotated
+// rounded once, at the store; keys that go into the cache are first rounded to the outputs' type, as by a program that stored them in
+// between; values go in as they come.  D / 8 lanes hold a head, eight channels each: the sum of squares is a few exchanges among them, a rotated
 // pair lies in one lane or in two of the same head, and the lanes' cosines and sines serve all heads of a token.  Bound by HBM where
 // it is large: 8192 tokens of 64 heads of 128 (273 MB) 54 us, the keys and values of 32 heads into the cache and back (340 MB) 69 us,
 // 4.9 to 5.1 TB/s, what a copy reaches; 64 tokens of 40 heads are the latency of a launch and its loads, 4.1 us.

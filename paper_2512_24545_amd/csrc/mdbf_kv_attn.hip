@@ -112,11 +112,9 @@ __device__ __forceinline__ void store_row(const AttnArgs& a, const Request& rq, 
 #pragma unroll
   for (int c = 0; c < N / 2; ++c) w[c] = s.hi > s.lo ? round2<DT>(o[2 * c] * inv, o[2 * c + 1] * inv) : 0u;
   MDBF_GLOBAL uint16_t* to = (MDBF_GLOBAL uint16_t*)a.out + (int64_t)(rq.start + i) * a.ldo + (int64_t)(head * a.group + g) * a.head_dim + c0;
-  if (a.wide_o && N == 2) {
-    *(MDBF_GLOBAL uint32_t*)to = w[0];
-  } else if (a.wide_o) {
+  if (a.wide_o) {
 #pragma unroll
-    for (int c = 0; c < N / 4; ++c) ((MDBF_GLOBAL U32x2*)to)[c] = U32x2{w[2 * c], w[(2 * c + 1) % (N / 2)]};
+    for (int c = 0; c < N / 4; ++c) ((MDBF_GLOBAL U32x2*)to)[c] = U32x2{w[2 * c], w[2 * c + 1]};
   } else {
 #pragma unroll
     for (int c = 0; c < N / 2; ++c) {
@@ -450,7 +448,7 @@ __device__ __forceinline__ float row_max(float x) {
 // Bound by the cache's bytes where that is long: 64 requests of up to 8192 tokens, 32 heads on 8 of 128 (295 MB), 55 us and 5 for
 // the join, 5.2 TB/s of the 6.0 that a plain read reaches; one of 200000 tokens (218 MB) 41 and 6 us.  Matrix cores are busy for an
 // eighth of that.  Short caches are a launch's latency and each wave's chain of page number, codes, scores, values and the meeting of the
-// waves: 4 requests of up to 701 tokens, 32 heads of 128 (8 MB), 10 us.
+// waves: 4 requests of up to 701 tokens, 32 heads of 128 (8 MB), 10.6 us.
 template <int D, int DT, int NP>
 __global__ __launch_bounds__(64 * kWaves, D == 64 ? 4 : D == 128 ? 3 : 2) void attn_few_kernel(AttnArgs a) {
   using Tile = Codes<D, NP>;
@@ -766,9 +764,9 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
 //
 // K Q^T are block-scaled products of fp4 and fp6, at four times the 16-bit rate, so that three or four of them, one for each limb
 // of the queries, are no dearer than one of 16 bits and its conversions of the keys.  Long prompts are bound by instruction
-// issue: two waves a SIMD, for whose softmax and values the vector unit is busy 55 % of the cycles and the matrix core 47 %, seldom
-// both.  2048 tokens behind 14336, 32 heads on 8 of 128 (515 Gflop): 433 to 441 us, 1.17 to 1.19 Pflop/s of the 1.26 that a large
-// 16-bit product reaches.
+// issue: two waves a SIMD, for whose softmax and values the vector unit is busy 57 % of the cycles and the matrix core 49 %, seldom
+// both.  2048 tokens behind 14336, 32 heads on 8 of 128 (515 Gflop): 425 to 444 us, 1.16 to 1.21 Pflop/s of the 1.26 that a large
+// 16-bit product reaches; in fp16, a limb more, 485 to 500.
 // Short ones are latency: 1.0 us (D = 64) or 1.25 (128) per tile of tokens with one workgroup on a compute unit, 1.1 or 1.85 for two.
 // Tried: eight waves in two halves that take turns at the tiles and add up at the end, half as many workgroups: 512 tokens of 32
 // heads 17.0 -> 16.3 us, calls in shares as before, prompts of 300 tokens of 4 requests 42 -> 48: not kept.
@@ -843,8 +841,9 @@ __global__ __launch_bounds__(64 * kManyWaves, D <= 128 ? 2 : 1) void attn_many_k
   constexpr int UNITS = kTile * BL;                // 16-byte units of a tile's keys, and of its values
   constexpr int U = UNITS < 256 ? 1 : UNITS / 256; // of each per thread; with D = 64 half of the threads take keys, half values
   constexpr int KROW = D / 2 + 16;                 // bytes of a token's key codes in LDS: reads of 16 bytes a lane meet on no bank
-  // of its values: blocks 80 bytes apart and rows 64 more than a multiple of 256, so that neither the writes nor the transposing
-  // reads (which take two times 16 channels of four rows at once) meet on a bank
+  // of its values: blocks 80 bytes apart and rows 64 more than a multiple of 256, so that the writes and the transposing reads
+  // (which take two times 16 channels of four rows at once) do not meet on a bank where a row has four blocks.  With D = 64, two
+  // blocks a row, writes of rows four apart do: 22 % of the LDS' cycles in prompts of odd lengths (D = 128: 6 %).
   constexpr int VROW = D == 256 ? 832 : 320;
   auto block_at = [](int g) { return g * 80; };
   constexpr int ST = D / 64;                       // pairs of blocks
@@ -1165,9 +1164,9 @@ static int check_attn(const mdbf_kv_t* kv, const mdbf_attn_t* at, int requests, 
 }
 
 // Which kernel a call takes, and whether its work is cut into shares: by estimates of the time, in us, from the sizes that the
-// caller bounds the call by.  Fitted to calls of 1 to 8192 new tokens behind 0 to 30000; what they get wrong costs up to a quarter
-// where requests are of unequal lengths.  128 new tokens behind 30000, 32 heads on 8 of 128: few rows 163 us, prompts 619 whole and
-// 78 cut; 40 behind 3000 of 8 requests: 32, 64 and 34; 1000 behind 4000: 188, 100 and 99.
+// caller bounds the call by.  Fitted to calls of 1 to 8192 new tokens behind 0 to 30000; what they get wrong costs up to a fifth
+// where requests are of unequal lengths.  128 new tokens behind 30000, 32 heads on 8 of 128: few rows 161 us, prompts 515 whole and
+// 78 cut; 40 behind 3000 of 8 requests: 32, 60 and 34; 1000 behind 4000: 188, 93 and 99.
 constexpr int kWhole = 1024;      // tokens up to which nothing is cut: the join, a launch, would cost more
 struct AttnCosts {
   double few;              // a unit of the few-row kernel where it fills the device
@@ -1212,8 +1211,8 @@ static AttnGeom attn_geom(const mdbf_kv_t& kv, const mdbf_attn_t& at, int all, i
   g.row_tiles = (int)std::min(tiles_of(g.many ? kManyRows : kRows), 65536.0);
   // Row tiles without shares: each workgroup takes one that its request may have, or the n-th of those that there are, for which
   // it looks through the requests.  That takes 0.5 to 2 us but spreads them evenly where most requests are much shorter than the
-  // bound: else a compute unit gets two and three while others, whose workgroups had none, are idle.  Five requests of 1 to 997 new
-  // tokens (14 heads on 2 of 64, 1111 visible): 38 -> 34 us, of 1 to 500: 32 -> 26; but 8 of 1 to 1024, 32 heads: 51.5 -> 53.5.
+  // bound: else a compute unit gets two and three while others, whose workgroups had none, are idle.  Five requests of 1 to 500 new
+  // tokens behind 1501 (14 heads on 2 of 64, 1111 visible): 30.7 -> 24.7 us, of 1 to 997: 31.9 -> 32.1.
   const int64_t there = (int64_t)T * (at.q_heads / kv.kv_heads) / kManyRows + all;
   g.distant = units_of(kManyRows, false) >= 64;
   g.nth = g.many && !g.shares && all <= 64 && there * kv.kv_heads <= 512 && there < 0.75 * all * g.row_tiles;
@@ -1224,9 +1223,10 @@ static unsigned attn_grid(const AttnGeom& g, int shares, int requests, int kv_he
   return g.shares ? (unsigned)shares : (unsigned)((int64_t)(g.nth ? 1 : requests) * kv_heads * g.row_tiles);
 }
 // Where two workgroups share a compute unit, a wave of each a SIMD, the one that feeds products goes before the one that is at its
-// softmax, if row tiles see much: 32 heads on 8 of 128, 2048 tokens behind 14336 464 -> 441 us (fp16 513 -> 487), 7000 252 -> 243,
-// 4000 165 -> 161, 2000 108 -> 108.4, none 50.6 -> 53.9: the instructions' order that it keeps costs something too.  With one
-// workgroup on a compute unit it only costs (512 tokens 16.9 -> 17.3, D = 256 705 -> 745), with D = 64 nothing is gained.
+// softmax, if row tiles see much: 32 heads on 8 of 128, 2048 tokens behind 14336 455 -> 435 us (fp16 511 -> 486), 7000 248 -> 239,
+// 4000 163 -> 158, 2000 107 -> 106, none 49 -> 52: the instructions' order that it keeps costs something too.  With one
+// workgroup on a compute unit it only costs (512 tokens 16.4 -> 17.1; D = 256, 2000 behind 8000, 655 -> 691); with D = 64 nothing
+// is gained (32 on 32, 1000 behind 5000, 84.5 -> 84.7).
 template <int D>
 constexpr bool kCrowds = D == 128;
 static bool attn_crowds(const AttnGeom& g, unsigned grid) { return g.many && g.distant && grid >= 512; }
