@@ -296,7 +296,7 @@ int mdbf_msvid(const float* Z_dev, int rows, int cols, int64_t ld, int l, int it
  * (it may round to 6: least error at 4 bits, 11 % of a normally distributed block's norm); values round to the nearest number, ties to
  * the even code.  A block with a NaN or an infinity in it becomes NaN.  dtype bounds the scales, to 2^-23 .. 2^13 (MDBF_F16) or
  * 2^-125 .. 2^125 (MDBF_BF16), so that every stored value is a number of that type: larger magnitudes saturate.
- * (Nothing here writes other scale bytes.  Where a pool holds them, those beyond the bound are read as NaN, and values of those below it are
+ * (Nothing here writes other scale bytes.  Where a pool holds them, those beyond the bound are read as NaN, and values of those below it may be
  * rounded to the type.)
  * 4.25 bits a channel.  A token's place is its slot, page * page_size + offset.
  *
