@@ -833,8 +833,8 @@ __device__ __forceinline__ float pair_max(float x) {
 }
 
 // CROWD: waves that feed products go first (see kCrowds).  EXACT: queries as they are, in 16-bit products for which every wave makes
-// numbers of the key codes: 2048 tokens behind 14336, 32 heads on 8 of 128, 432 -> 480 us (fp16 479 -> 497), 1000 behind 5000, 32 of
-// 64, 85 -> 98.
+// numbers of the key codes: 2048 tokens behind 14336, 32 heads on 8 of 128, 427 -> 479 us (fp16 476 -> 500), 1000 behind 5000, 32 of
+// 64, 84 -> 97; 300 behind 2000 of 2 requests, 16 on 4 of 256 in fp16, 50 -> 47.
 template <int D, int DT, bool CROWD, bool EXACT>
 __global__ __launch_bounds__(64 * kManyWaves, D <= 128 ? 2 : 1) void attn_many_kernel(AttnArgs a) {
   constexpr int BL = D / 32;                       // blocks of a token
@@ -948,14 +948,13 @@ __global__ __launch_bounds__(64 * kManyWaves, D <= 128 ? 2 : 1) void attn_many_k
     look_up(begin + kTile);
     Limbs<NL> ql[ST];
     bool finite = true;
-    if constexpr (EXACT) {
-#pragma unroll
-      for (int s = 0; s < ST; ++s)
-#pragma unroll
-        for (int w = 0; w < 4; ++w) raw[s][w] ^= a.flip;
-    } else
 #pragma unroll
     for (int s = 0; s < ST; ++s) {
+      if constexpr (EXACT) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) raw[s][w] ^= a.flip;
+        continue;
+      }
       float q[32];
 #pragma unroll
       for (int w = 0; w < 16; ++w) {
