@@ -50,7 +50,10 @@ typedef enum {
   MDBF_EHIP = -6           /* a HIP call failed; mdbf_last_hip_error() gives the text */
 } mdbf_status;
 
-typedef enum { MDBF_F16 = 0, MDBF_BF16 = 1, MDBF_F32 = 2 } mdbf_dtype;
+typedef enum {
+  MDBF_F16 = 0, MDBF_BF16 = 1, MDBF_F32 = 2,
+  MDBF_E4M3 = 3            /* 8-bit floating point numbers with scales: results of mdbf_add_norm only */
+} mdbf_dtype;
 
 /* flags of mdbf_desc_t */
 #define MDBF_FLAG_PRECISE 1u   /* fp32 vector arithmetic throughout (no fp16 staging, no matrix cores); slow */
@@ -403,6 +406,94 @@ int mdbf_kv_attention(const mdbf_kv_t* kv, const mdbf_attn_t* attn, const void* 
                       const int32_t* table_dev, int64_t table_ld, int table_width, const int32_t* cu_dev,
                       const int32_t* lengths_dev, int requests, const void* q_dev, int64_t ldq, int T, void* out_dev,
                       int64_t ldo, void* workspace_dev, size_t workspace_bytes, void* stream);
+
+/* ---- around the projections of a serving step --------------------------------------------------
+ * In front of the projections the residual's addition and the norm (mdbf_add_norm), beside them the low-rank adapters of the
+ * requests (mdbf_adapter_rows once a step, mdbf_adapters after mdbf_forward), behind the head the next tokens (mdbf_sample). */
+typedef struct {
+  int32_t n;                       /* channels of a row, 1 .. 65536 */
+  int32_t x_dtype, h_dtype, y_dtype;   /* of x; of residual and residual_out: that of x or MDBF_F32; of y: also MDBF_E4M3 */
+  int32_t scale_group;             /* of MDBF_E4M3: 0, a fp32 scale per row, or 32, a scale byte per 32 channels; otherwise 0 */
+  float eps;
+} mdbf_norm_t;
+
+/* h = x + residual,  y = h / sqrt(mean(h^2) + eps) * weight  for each of T rows; h is x where residual is null, and the weight (n fp32) is
+ * left out where it is null.  h in fp32, the mean in fp64, rounded to fp32 as 1 / sqrt; results are rounded once, residual_out too (y is made of
+ * the sum that was not rounded).  residual_out may be null.
+ * y of MDBF_E4M3 (bias 7, largest 448, no infinities) is the nearest such number to y / scale, ties to even:
+ *   scale_group 0    scales_dev: fp32, one per row, lds apart: the row's largest |y| / 448; 1 where that is 0.  A row with a NaN or an infinity in y has
+ *                    NaN for its scale and codes
+ *   scale_group 32   scales_dev: a byte b per 32 channels (the last of a row may be fewer), rows lds bytes apart: 2^(b - 127), the
+ *                    smallest power of two (from 2^-126 on) that leaves the largest magnitude at most 448; 255 and NaN codes for a block with a NaN or an infinity
+ * in it.
+ * Rows are ldx, ldr, ldro, ldy elements apart (any, at least n).  Outputs may be the inputs themselves where strides and
+ * types agree, and otherwise overlap nothing.  One launch. */
+int mdbf_add_norm(const mdbf_norm_t* desc, const void* x_dev, int64_t ldx, const void* residual_dev, int64_t ldr,
+                  const float* weight_dev, int T, void* residual_out_dev, int64_t ldro, void* y_dev, int64_t ldy,
+                  void* scales_dev, int64_t lds, void* stream);
+
+/* Low-rank adapters.  A projection's pool has `adapters` pairs A (r x n) and B (m x r); a request has one of them or none.
+ * mdbf_adapter_rows puts a step's rows in the order of their adapters: request i has the rows cu[i] .. cu[i + 1) (as
+ * mdbf_kv_slots leaves cu) and the adapter adapter[i]; one outside 0 .. adapters - 1 is none.  Writes
+ *   rows   (T)             rows with an adapter, adapter by adapter, each one's in their order; -1 behind the last
+ *   tiles  (tile_room x 4) (adapter, place of its first row in rows, rows of the tile, 0): an adapter's rows in tiles of
+ *                          MDBF_ADAPTER_TILE, its last one shorter, in the order of rows; (-1, 0, 0, 0) behind the last
+ *   places (requests)      the place of each request's first row in rows; requests without an adapter come behind the others
+ * For mdbf_adapters rows and tiles may be made by other means.  cu must not fall and lies in 0 .. T; where it does not, nothing outside of the
+ * tables is written, but they are of no use.  At most 8192 adapters.  One launch, two for long steps.
+ * tile_room: at least mdbf_adapter_tiles(T, requests, adapters), as many as there can be (host only; a negative mdbf_status for
+ * bad arguments). */
+#define MDBF_ADAPTER_TILE 64
+int64_t mdbf_adapter_tiles(int T, int requests, int adapters);
+int mdbf_adapter_rows(int T, int requests, int adapters, const int32_t* cu_dev, const int32_t* adapter_dev, int32_t* rows_dev,
+                      int32_t* tiles_dev, int64_t tile_room, int32_t* places_dev, void* stream);
+
+/* One projection's adapters, and what they are applied to. */
+typedef struct {
+  int32_t n, m, r;         /* rank r 1 .. 256; adapters of lower ranks are filled up with zeros */
+  int32_t y_dtype;
+  const void* A_dev;       /* adapters x r x n, contiguous */
+  const void* B_dev;       /* adapters x m x r, contiguous */
+  const float* scale_dev;  /* adapters, or null: 1 */
+  const void* X_dev;       /* T x n, row stride ldx >= n */
+  int64_t ldx;
+  void* Y_dev;             /* T x m, row stride ldy >= m */
+  int64_t ldy;
+} mdbf_adapter_t;
+
+/* Y[t] += scale[a] B[a] (A[a] X[t]) for the rows t in the tiles, a the tile's adapter: the rows of requests without one stay as
+ * they are.  `count` projections (1 .. MDBF_ADAPTER_MAX) of one step in one call, `dtype` that of all X, A and B (MDBF_F16 or MDBF_BF16); they may
+ * share X, not Y.  Y overlaps nothing else that the call reads.  Sums are fp32; the inner values A X are rounded to three (fp32 Y) or two numbers of 16 bits that add up to
+ * them to 2^-23 or 2^-16, in fp16 after a row's largest is brought to 1; Y is rounded once.  A row, a tile or an adapter outside of what T, tile_room and
+ * `adapters` say is left out; a row must not be listed twice.  Repeated calls return the same bits; two launches. */
+#define MDBF_ADAPTER_MAX 8
+int mdbf_adapters_workspace_bytes(int count, const mdbf_adapter_t* list, int dtype, int adapters, int T, int64_t tile_room,
+                                  size_t* bytes_out);
+int mdbf_adapters(int count, const mdbf_adapter_t* list, int dtype, int adapters, int T, const int32_t* rows_dev,
+                  const int32_t* tiles_dev, int64_t tile_room, void* workspace_dev, size_t workspace_bytes, void* stream);
+
+/* The next token of each of T rows of logits (`vocab` of them, rows ld elements apart), from given numbers.
+ * A row's tokens in the order of their logits, the largest first, equal ones by index, have the weights exp((logit - largest) / temperature).  Of them are
+ * kept the first top_k; of those the fewest whose weights add up to top_p of theirs, but one at least; of those the ones
+ * whose weight is at least min_p (the largest weight is 1), but the first in any case.  The token is the first one
+ * at which the kept weights up to and with it add up to more than u times those of all kept ones.
+ *   u              T fp32, cut to 0 .. 1 - 2^-24 (NaN: 0)
+ *   temperature    T fp32 or null (1).  0 and less, or NaN: the largest logit's token
+ *   top_k          T int32 or null; 0 and less: no bound       top_p   T fp32 or null; 1 and more, or NaN: no bound
+ *   min_p          T fp32 or null; NaN: no bound
+ *   tokens         T int32; -1 in a row that holds nothing but -inf and NaN (NaN counts as -inf, whose weight is 0)
+ *   probs          T fp32 or null: the token's weight over that of all kept ones; 0 with token -1
+ * Among infinite logits each has the weight 1, and finite ones none.  Weights are fp64, held to 2^-50 of the largest of each 16384 neighbours or better; sums are
+ * fp64 in a fixed order: repeated calls return the same bits.  The workspace (host arithmetic only) never shrinks with T and vocab. */
+typedef struct {
+  const float* temperature_dev;
+  const int32_t* top_k_dev;
+  const float* top_p_dev;
+  const float* min_p_dev;
+} mdbf_sample_t;
+int mdbf_sample_workspace_bytes(int T, int vocab, size_t* bytes_out);
+int mdbf_sample(const mdbf_sample_t* settings, const void* logits_dev, int64_t ld, int dtype, int T, int vocab, const float* u_dev,
+                int32_t* tokens_dev, float* probs_dev, void* workspace_dev, size_t workspace_bytes, void* stream);
 
 /* ---- misc ----------------------------------------------------------------------------- */
 const char* mdbf_strerror(int status);

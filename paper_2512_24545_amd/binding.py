@@ -15,7 +15,7 @@ import numpy as np
 
 from . import build as _build
 
-MDBF_F16, MDBF_BF16, MDBF_F32 = 0, 1, 2
+MDBF_F16, MDBF_BF16, MDBF_F32, MDBF_E4M3 = 0, 1, 2, 3
 MDBF_FLAG_PRECISE = 1
 MDBF_FLAG_BLOCK_SCALED = 2
 MDBF_FLAG_ACCUMULATE = 4
@@ -24,6 +24,7 @@ MDBF_KV_BAD_LENGTH, MDBF_KV_BAD_WIDTH, MDBF_KV_BAD_TOKENS, MDBF_KV_NO_PAGES = 1,
 MDBF_ROPE_INTERLEAVED = 1
 MDBF_ATTN_CAUSAL = 1
 MDBF_ATTN_EXACT_QUERIES = 2
+MDBF_ADAPTER_TILE, MDBF_ADAPTER_MAX = 64, 8
 DTYPE_CODE = {"f16": MDBF_F16, "bf16": MDBF_BF16, "f32": MDBF_F32}
 
 STATUS = {0: "MDBF_OK", -1: "MDBF_EINVAL", -2: "MDBF_EALIGN", -3: "MDBF_EDTYPE", -4: "MDBF_EWORKSPACE",
@@ -36,6 +37,8 @@ EXPORTS = [
     "mdbf_msvid_block", "mdbf_msvid_workspace_bytes", "mdbf_msvid",
     "mdbf_kv_page_bytes", "mdbf_kv_slots", "mdbf_kv_append", "mdbf_kv_read", "mdbf_qk_norm_rope",
     "mdbf_kv_attention_workspace_bytes", "mdbf_kv_attention_kernel", "mdbf_kv_attention",
+    "mdbf_add_norm", "mdbf_adapter_tiles", "mdbf_adapter_rows", "mdbf_adapters_workspace_bytes", "mdbf_adapters",
+    "mdbf_sample_workspace_bytes", "mdbf_sample",
 ]
 
 
@@ -78,6 +81,21 @@ class RopeDesc(C.Structure):
 class AttnDesc(C.Structure):
     _fields_ = [("q_heads", C.c_int32), ("flags", C.c_uint32), ("window", C.c_int32), ("max_fresh", C.c_int32),
                 ("max_length", C.c_int32), ("scale", C.c_float)]
+
+
+class NormDesc(C.Structure):
+    _fields_ = [("n", C.c_int32), ("x_dtype", C.c_int32), ("h_dtype", C.c_int32), ("y_dtype", C.c_int32),
+                ("scale_group", C.c_int32), ("eps", C.c_float)]
+
+
+class AdapterDesc(C.Structure):
+    _fields_ = [("n", C.c_int32), ("m", C.c_int32), ("r", C.c_int32), ("y_dtype", C.c_int32), ("A_dev", C.c_void_p),
+                ("B_dev", C.c_void_p), ("scale_dev", C.c_void_p), ("X_dev", C.c_void_p), ("ldx", C.c_int64),
+                ("Y_dev", C.c_void_p), ("ldy", C.c_int64)]
+
+
+class SampleDesc(C.Structure):
+    _fields_ = [("temperature_dev", C.c_void_p), ("top_k_dev", C.c_void_p), ("top_p_dev", C.c_void_p), ("min_p_dev", C.c_void_p)]
 
 
 _lib = None
@@ -129,6 +147,14 @@ def lib():
     L.mdbf_kv_attention_kernel.argtypes = [C.POINTER(KvDesc), C.POINTER(AttnDesc), C.c_int, C.c_int]
     L.mdbf_kv_attention.argtypes = [C.POINTER(KvDesc), C.POINTER(AttnDesc), vp, sz, vp, i64, C.c_int, vp, vp, C.c_int, vp, i64,
                                     C.c_int, vp, i64, vp, sz, vp]
+    L.mdbf_add_norm.argtypes = [C.POINTER(NormDesc), vp, i64, vp, i64, vp, C.c_int, vp, i64, vp, i64, vp, i64, vp]
+    L.mdbf_adapter_tiles.restype = i64
+    L.mdbf_adapter_tiles.argtypes = [C.c_int, C.c_int, C.c_int]
+    L.mdbf_adapter_rows.argtypes = [C.c_int, C.c_int, C.c_int, vp, vp, vp, vp, i64, vp, vp]
+    L.mdbf_adapters_workspace_bytes.argtypes = [C.c_int, C.POINTER(AdapterDesc), C.c_int, C.c_int, C.c_int, i64, C.POINTER(sz)]
+    L.mdbf_adapters.argtypes = [C.c_int, C.POINTER(AdapterDesc), C.c_int, C.c_int, C.c_int, vp, vp, i64, vp, sz, vp]
+    L.mdbf_sample_workspace_bytes.argtypes = [C.c_int, C.c_int, C.POINTER(sz)]
+    L.mdbf_sample.argtypes = [C.POINTER(SampleDesc), vp, i64, C.c_int, C.c_int, C.c_int, vp, vp, vp, vp, sz, vp]
     L.mdbf_strerror.restype = C.c_char_p
     L.mdbf_strerror.argtypes = [C.c_int]
     L.mdbf_last_hip_error.restype = C.c_char_p
@@ -172,7 +198,7 @@ def _torch():
     global _torch_module
     if _torch_module is None:
         import torch
-        _TORCH_DTYPE.update(f16=torch.float16, bf16=torch.bfloat16, f32=torch.float32)
+        _TORCH_DTYPE.update(f16=torch.float16, bf16=torch.bfloat16, f32=torch.float32, e4m3=torch.float8_e4m3fn)
         _DTYPE_NAME.update({torch.float16: "f16", torch.bfloat16: "bf16", torch.float32: "f32"})
         _torch_module = torch
     return _torch_module
@@ -623,3 +649,212 @@ def mdbf_kv_attention(cache, q, table, cu, lengths, max_fresh, max_length, scale
     if status:
         _check(status, "mdbf_kv_attention")
     return out
+
+
+# ---- around the projections of a serving step --------------------------------------------------
+def _here(*tensors):
+    """Tensors (or None) of the current device, whose stream a call goes to."""
+    dev = _torch_module._C._cuda_getDevice()
+    for t in tensors:
+        assert t is None or t.get_device() == dev, "tensors of the current device are needed"
+
+
+def _rows_of(x, n=None):
+    """Row stride of a matrix whose rows' elements lie side by side."""
+    ld, one = x.stride()
+    rows, cols = x.shape
+    assert (one == 1 or cols == 1) and (n is None or cols == n), "a matrix with contiguous rows is needed"
+    return ld if ld >= cols or rows > 1 else cols
+
+
+@functools.lru_cache(maxsize=256)
+def _norm_desc(*values):
+    return NormDesc(*values)
+
+
+def mdbf_add_norm(x, residual=None, weight=None, eps=1e-6, y_dtype=None, scale_group=0, residual_out=None, out=None, scales=None, stream=None):
+    """h = x + residual (T, n), y = h / sqrt(mean(h^2) + eps) * weight.  x f16/bf16/f32; residual of that type or f32; weight n fp32; y_dtype that of x unless
+    given, "e4m3" for 8-bit numbers with scales: one fp32 a row (scale_group 0), or a byte b, 2^(b - 127), per 32 channels (32).  Returns
+    (y, h, scales): h of the residual's type (None without residual), scales None but for e4m3; residual_out (may be the residual), out and
+    scales are used where given."""
+    torch = _torch()
+    T, n = x.shape
+    name = _DTYPE_NAME[x.dtype]
+    y_dtype = y_dtype or (name if out is None else "e4m3" if out.dtype == torch.float8_e4m3fn else _DTYPE_NAME[out.dtype])
+    eight = y_dtype == "e4m3"
+    if out is None:
+        out = _result(lambda: torch.empty((T, n), dtype=_TORCH_DTYPE[y_dtype], device=x.device), stream)
+    else:
+        assert out.shape == (T, n) and out.dtype == _TORCH_DTYPE[y_dtype]
+    h_name, ldr, ldro = name, 0, 0
+    if residual is not None:
+        assert residual.shape == (T, n)
+        h_name, ldr = _DTYPE_NAME[residual.dtype], _rows_of(residual)
+        if residual_out is None:
+            residual_out = _result(lambda: torch.empty((T, n), dtype=residual.dtype, device=x.device), stream)
+        else:
+            assert residual_out.shape == (T, n) and residual_out.dtype == residual.dtype
+        ldro = _rows_of(residual_out)
+    else:
+        assert residual_out is None, "residual_out needs a residual"
+    lds = 0
+    if eight:
+        shape, dtype = ((T, -(-n // 32)), torch.uint8) if scale_group else ((T, 1), torch.float32)
+        if scales is None:
+            scales = _result(lambda: torch.empty(shape, dtype=dtype, device=x.device), stream)
+        else:
+            assert scales.shape == shape and scales.dtype == dtype
+        lds = _rows_of(scales)
+    else:
+        assert scales is None, "scales go with e4m3"
+    assert weight is None or _ints(weight, n, torch.float32), "the weight is n fp32"
+    _here(x, residual, weight, residual_out, out, scales)
+    desc = _norm_desc(n, DTYPE_CODE[name], DTYPE_CODE[h_name], MDBF_E4M3 if eight else DTYPE_CODE[y_dtype], scale_group, eps)
+    status = (_lib or lib()).mdbf_add_norm(
+        desc, x.data_ptr(), _rows_of(x), None if residual is None else residual.data_ptr(), ldr, None if weight is None else weight.data_ptr(), T,
+        None if residual_out is None else residual_out.data_ptr(), ldro, out.data_ptr(), _rows_of(out), None if scales is None else scales.data_ptr(),
+        lds, _stream_ptr(stream))
+    if status:
+        _check(status, "mdbf_add_norm")
+    return out, residual_out, scales
+
+
+class AdapterRows:
+    """A step's rows in the order of their adapters: rows (tokens), tiles (room x 4) and places (requests), int32 (include/mdbf.h has their
+    contents).  Made once for these sizes, it can be handed to every step's mdbf_adapter_rows; rows and tiles may also be
+    given."""
+
+    def __init__(self, tokens, requests, adapters, device="cuda:0", stream=None, rows=None, tiles=None):
+        self.tokens, self.requests, self.adapters = tokens, requests, adapters
+        self.rows, self.tiles, self.places = rows, tiles, None
+        if rows is None or tiles is None:
+            torch = _torch()
+            room = (_lib or lib()).mdbf_adapter_tiles(tokens, requests, adapters)
+            if room < 0:
+                _check(int(room), "mdbf_adapter_tiles")
+            # (tiles first: their entries are read 16 bytes at a time)
+            ints = _result(lambda: torch.empty(4 * room + tokens + requests, dtype=torch.int32, device=device), stream)
+            self.tiles, self.rows, self.places = ints.split((4 * room, tokens, requests))
+            self.tiles = self.tiles.view(room, 4)
+        else:
+            assert _ints(rows, tokens) and tiles.shape[1:] == (4,) and _ints(tiles, tiles.shape[0] * 4)
+
+
+def mdbf_adapter_rows(cu, adapter, adapters, tokens, out=None, stream=None):
+    """Rows in the order of their requests' adapters.  cu (requests + 1; as mdbf_kv_slots leaves it) and adapter (requests; outside 0 .. adapters - 1: none)
+    are int32 CUDA tensors; tokens: room for the step's rows.  Returns an AdapterRows (`out` if given)."""
+    _torch()
+    n = adapter.numel()
+    assert _ints(adapter, n) and _ints(cu, n + 1)
+    o = out
+    if o is None:
+        o = AdapterRows(tokens, n, adapters, adapter.device, stream)
+    else:
+        assert (o.tokens, o.requests, o.adapters) == (tokens, n, adapters) and o.places is not None
+    _here(cu, adapter, o.rows)
+    status = (_lib or lib()).mdbf_adapter_rows(tokens, n, adapters, cu.data_ptr(), adapter.data_ptr(), o.rows.data_ptr(), o.tiles.data_ptr(),
+                                               o.tiles.shape[0], o.places.data_ptr(), _stream_ptr(stream))
+    if status:
+        _check(status, "mdbf_adapter_rows")
+    return o
+
+
+class Adapters:
+    """The low-rank adapters of one projection (m x n): A (adapters, r, n), B (adapters, m, r), f16 or bf16, and scale (adapters fp32, or None)."""
+
+    def __init__(self, A, B, scale=None):
+        self.count, self.r, self.n = A.shape
+        self.m = B.shape[1]
+        assert B.shape == (self.count, self.m, self.r) and A.dtype == B.dtype and A.is_contiguous() and B.is_contiguous()
+        _torch()
+        assert scale is None or _ints(scale, self.count, _torch_module.float32)
+        self.A, self.B, self.scale = A, B, scale
+        self.args = (A.data_ptr(), B.data_ptr(), None if scale is None else scale.data_ptr())
+
+
+def _adapter_list(rows, adapters, Xs, Ys):
+    count, T = len(adapters), rows.tokens
+    assert 0 < count == len(Xs) == len(Ys)
+    arr = (AdapterDesc * count)()
+    dtype = adapters[0].A.dtype
+    for d, p, X, Y in zip(arr, adapters, Xs, Ys):
+        assert p.count == rows.adapters and p.A.dtype == X.dtype == dtype and X.shape == (T, p.n) and Y.shape == (T, p.m)
+        _here(X, Y, p.A, p.B, p.scale)
+        d.n, d.m, d.r, d.y_dtype = p.n, p.m, p.r, DTYPE_CODE[_DTYPE_NAME[Y.dtype]]
+        d.A_dev, d.B_dev, d.scale_dev = p.args
+        d.X_dev, d.ldx, d.Y_dev, d.ldy = X.data_ptr(), _rows_of(X), Y.data_ptr(), _rows_of(Y)
+    return arr, DTYPE_CODE[_DTYPE_NAME[dtype]]
+
+
+def mdbf_adapters_workspace(rows, adapters, Xs, Ys):
+    """The workspace (uint8 CUDA tensor) of an mdbf_adapters call with these arguments."""
+    torch = _torch()
+    arr, dtype = _adapter_list(rows, adapters, Xs, Ys)
+    return torch.empty(_adapters_need(arr, dtype, rows), dtype=torch.uint8, device=Xs[0].device)
+
+
+def _adapters_need(arr, dtype, rows):
+    need = C.c_size_t(0)
+    status = (_lib or lib()).mdbf_adapters_workspace_bytes(len(arr), arr, dtype, rows.adapters, rows.tokens, rows.tiles.shape[0], C.byref(need))
+    if status:
+        _check(status, "mdbf_adapters_workspace_bytes")
+    return need.value
+
+
+def mdbf_adapters(rows, adapters, Xs, Ys, workspace=None, stream=None):
+    """Ys[i][t] += scale[a] B[a] (A[a] Xs[i][t]) with a the adapter of row t: up to 8 projections of one step in one call, after the shared
+    projections have written Ys.  rows: an AdapterRows; adapters: an Adapters per projection; Xs (T, n) of the adapters' type, Ys (T, m)
+    f16/bf16/f32.  Rows without an adapter stay as they are.  Returns Ys."""
+    torch = _torch()
+    arr, dtype = _adapter_list(rows, adapters, Xs, Ys)
+    _here(rows.rows, rows.tiles, workspace)
+    if workspace is None:
+        with _on(stream):
+            workspace = torch.empty(_adapters_need(arr, dtype, rows), dtype=torch.uint8, device=Xs[0].device)
+    status = (_lib or lib()).mdbf_adapters(len(arr), arr, dtype, rows.adapters, rows.tokens, rows.rows.data_ptr(), rows.tiles.data_ptr(),
+                                           rows.tiles.shape[0], workspace.data_ptr(), workspace.numel(), _stream_ptr(stream))
+    if status:
+        _check(status, "mdbf_adapters")
+    return Ys
+
+
+@functools.lru_cache(maxsize=256)
+def _sample_need(T, vocab):
+    out = C.c_size_t(0)
+    _check(lib().mdbf_sample_workspace_bytes(T, vocab, C.byref(out)), "mdbf_sample_workspace_bytes")
+    return out.value
+
+
+def mdbf_sample_workspace(T, vocab, device="cuda:0"):
+    """The workspace (uint8 CUDA tensor, or None where none is needed) of mdbf_sample calls of up to these sizes."""
+    torch = _torch()
+    n = _sample_need(T, vocab)
+    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
+
+
+def mdbf_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, tokens=None, probs=None, workspace=None, stream=None):
+    """The next token of each row of logits (T, vocab; f16/bf16/f32), drawn with the numbers u (T fp32 in [0, 1)).  temperature (0: the largest
+    logit's token), top_k (int32; 0: no bound), top_p, min_p: one per row, or None.  Returns (tokens int32, -1 in a row of nothing but -inf and NaN;
+    probs fp32, the token's share among those kept)."""
+    torch = _torch()
+    T, vocab = logits.shape
+    f32 = torch.float32
+    assert _ints(u, T, f32) and (top_k is None or _ints(top_k, T))
+    for s in (temperature, top_p, min_p):
+        assert s is None or _ints(s, T, f32)
+    if tokens is None:
+        tokens = _result(lambda: torch.empty(T, dtype=torch.int32, device=logits.device), stream)
+    if probs is None:
+        probs = _result(lambda: torch.empty(T, dtype=f32, device=logits.device), stream)
+    assert _ints(tokens, T) and _ints(probs, T, f32)
+    if workspace is None:
+        with _on(stream):
+            workspace = mdbf_sample_workspace(T, vocab, logits.device)
+    _here(logits, u, temperature, top_k, top_p, min_p, tokens, probs, workspace)
+    desc = SampleDesc(*(None if s is None else s.data_ptr() for s in (temperature, top_k, top_p, min_p)))
+    ws = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
+    status = (_lib or lib()).mdbf_sample(desc, logits.data_ptr(), _rows_of(logits), DTYPE_CODE[_DTYPE_NAME[logits.dtype]], T, vocab, u.data_ptr(),
+                                         tokens.data_ptr(), probs.data_ptr(), *ws, _stream_ptr(stream))
+    if status:
+        _check(status, "mdbf_sample")
+    return tokens, probs
