@@ -725,10 +725,10 @@ class AdapterRows:
     given."""
 
     def __init__(self, tokens, requests, adapters, device="cuda:0", stream=None, rows=None, tiles=None):
+        torch = _torch()
         self.tokens, self.requests, self.adapters = tokens, requests, adapters
         self.rows, self.tiles, self.places = rows, tiles, None
         if rows is None or tiles is None:
-            torch = _torch()
             room = (_lib or lib()).mdbf_adapter_tiles(tokens, requests, adapters)
             if room < 0:
                 _check(int(room), "mdbf_adapter_tiles")

@@ -138,64 +138,294 @@ __global__ __launch_bounds__(kRowChunk) void adapter_places_kernel(RowArgs a) {
 }
 
 // ---- products -------------------------------------------------------------------------------------------
-struct AdapterProj {
-  const void *A, *B, *X;
+// Two launches: V = A X by tiles of rows, ranks and parts of the channels, then Y += scale B V by tiles of rows and columns of
+// Y.  Both on 16x16x32 products.  What has to be moved is X, the adapters in use and Y, twice: a tile of rows shares its adapter, and what
+// a projection shares with the next one, X, is read once for up to four tiles of ranks.
+constexpr int kInSlots = 4;                    // tiles of 16 ranks per workgroup of the first launch
+constexpr int kMaxRank = 256;
+constexpr int kMaxGroups = MDBF_ADAPTER_MAX * kMaxRank / 16 / kInSlots;
+constexpr int kOutBlock = 64;                  // columns of Y that a wave takes at a time
+
+typedef float Acc4 __attribute__((ext_vector_type(4)));
+typedef __bf16 Bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 F16x8 __attribute__((ext_vector_type(8)));
+
+template <int DT>
+__device__ __forceinline__ Acc4 product(const U32x4& a, const U32x4& b, const Acc4& c) {
+  if (DT == MDBF_F16) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(F16x8, a), __builtin_bit_cast(F16x8, b), c, 0, 0, 0);
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(Bf16x8, a), __builtin_bit_cast(Bf16x8, b), c, 0, 0, 0);
+}
+
+// workgroups of the first launch that share X: tiles of 16 ranks, of one projection or of several
+struct InGroup {
+  const void* X;
+  int64_t ldx;
+  int32_t n, slots;
+  uint8_t proj[kInSlots], tile[kInSlots];
+};
+struct InArgs {
+  InGroup g[kMaxGroups];
+  const void* A[MDBF_ADAPTER_MAX];
+  int32_t r[MDBF_ADAPTER_MAX], column[MDBF_ADAPTER_MAX];   // rank, and the projection's first column of V
+  const int32_t *rows, *tiles;
+  float* V;                                    // splits x T x width, by place
+  int32_t adapters, T, width, splits;
+};
+struct OutProj {
+  const void* B;
   void* Y;
   const float* scale;
-  float* V;                      // workspace: T x r, by place
-  int64_t ldx, ldy;
-  int32_t n, m, r, yd;
+  int64_t ldy;
+  int32_t m, r, column, yd, chunk;             // chunk: columns of Y per workgroup
 };
-struct AdapterArgs {
-  AdapterProj p[MDBF_ADAPTER_MAX];
+struct OutArgs {
+  OutProj p[MDBF_ADAPTER_MAX];
   const int32_t *rows, *tiles;
-  int32_t adapters, T;
+  const float* V;
+  int32_t adapters, T, width, splits;
 };
 
 // the tile's adapter, first place and rows; false for one that is none
-__device__ __forceinline__ bool tile_of(const AdapterArgs& a, int64_t t, int& adapter, int& first, int& count) {
-  const U32x4 w = *((const MDBF_GLOBAL U32x4*)a.tiles + t);
+__device__ __forceinline__ bool tile_of(const int32_t* tiles, int64_t t, int adapters, int T, int& adapter, int& first, int& count) {
+  const U32x4 w = *((const MDBF_GLOBAL U32x4*)tiles + t);
   adapter = (int)w[0], first = (int)w[1], count = min((int)w[2], MDBF_ADAPTER_TILE);
-  if (adapter < 0 || adapter >= a.adapters || first < 0 || first >= a.T || count <= 0) return false;
-  count = min(count, a.T - first);
+  if (adapter < 0 || adapter >= adapters || first < 0 || first >= T || count <= 0) return false;
+  count = min(count, T - first);
   return true;
 }
 
-// The simplest form: a wave per row and rank, then a thread per result.
-template <int DT>
-__global__ __launch_bounds__(256) void adapter_in_kernel(AdapterArgs a) {
-  const AdapterProj& p = a.p[blockIdx.y];
-  int adapter, first, count;
-  if (!tile_of(a, blockIdx.x, adapter, first, count)) return;
-  const int lane = threadIdx.x & 63;
-  for (int i = threadIdx.x >> 6; i < count * p.r; i += 4) {
-    const int row = a.rows[first + i / p.r], j = i % p.r;
-    if (row < 0 || row >= a.T) continue;
-    float sum = 0;
-    for (int c = lane; c < p.n; c += 64)
-      sum += load_as_float(p.X, row * p.ldx + c, DT) * load_as_float(p.A, ((int64_t)adapter * p.r + j) * p.n + c, DT);
+// V[split][place][rank] = sum over the split's channels of A[rank][c] X[row][c].  A wave has 16 rows; where a tile has fewer than 64 the other
+// waves take parts of the channels, and their sums meet in LDS.
+template <int DT, int NS>
+__device__ __forceinline__ void in_tile(const InArgs& a, const InGroup& g, int adapter, int first, int count, int split, Acc4 (*part)[NS][64]) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, kg = lane >> 4;
+  const int subs = count <= 16 ? 1 : count <= 32 ? 2 : 4, sub = wave & (subs - 1), piece = wave / subs, pieces = 4 / subs;
+  const int steps = (g.n + 31) / 32, all = a.splits * pieces, at = split * pieces + piece;
+  const int s0 = (int)((int64_t)steps * at / all), s1 = (int)((int64_t)steps * (at + 1) / all);
+
+  const int place = first + min(sub * 16 + i, count - 1);
+  const int row = cut(a.rows[place], a.T - 1);          // (a row that is none is left out at the end)
+  const int64_t x0 = (int64_t)row * g.ldx;
+  int64_t a0[NS];
+  const void* A[NS];
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
-    if (lane == 0) p.V[(int64_t)(first + i / p.r) * p.r + j] = sum;
+  for (int s = 0; s < NS; ++s) {
+    const int p = g.proj[s], r = a.r[p];
+    A[s] = a.A[p];
+    a0[s] = ((int64_t)adapter * r + min(g.tile[s] * 16 + i, r - 1)) * g.n;
+  }
+  Acc4 acc[NS] = {};
+  const int full = min(s1, g.n / 32);
+  int s = s0;
+  constexpr int U = 4;
+  for (; s + U <= full; s += U) {
+    Raw8<DT> x[U], w[U][NS];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int c = (s + u) * 32 + kg * 8;
+      load_raw8<DT>(g.X, x0 + c, 8, x[u]);
+#pragma unroll
+      for (int q = 0; q < NS; ++q) load_raw8<DT>(A[q], a0[q] + c, 8, w[u][q]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int q = 0; q < NS; ++q) acc[q] = product<DT>(x[u].w[0], w[u][q].w[0], acc[q]);
+  }
+  for (; s < s1; ++s) {
+    const int c = s * 32 + kg * 8;
+    Raw8<DT> x, w;
+    load_raw8<DT>(g.X, x0 + c, g.n - c, x);
+#pragma unroll
+    for (int q = 0; q < NS; ++q) {
+      load_raw8<DT>(A[q], a0[q] + c, g.n - c, w);
+      acc[q] = product<DT>(x.w[0], w.w[0], acc[q]);
+    }
+  }
+  if (pieces > 1) {
+    if (piece) {
+#pragma unroll
+      for (int q = 0; q < NS; ++q) part[wave - subs][q][lane] = acc[q];
+    }
+    __syncthreads();
+    if (piece) return;
+    for (int w = sub; w < 4 - subs; w += subs)
+#pragma unroll
+      for (int q = 0; q < NS; ++q) acc[q] += part[w][q][lane];
+  }
+  // lane: rank i of the tile, rows 4 kg ..
+#pragma unroll
+  for (int q = 0; q < NS; ++q) {
+    const int p = g.proj[q], rank = g.tile[q] * 16 + i;
+    float* v = a.V + ((int64_t)split * a.T + first + sub * 16 + kg * 4) * a.width + a.column[p] + rank;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (sub * 16 + kg * 4 + e < count) v[(int64_t)e * a.width] = rank < a.r[p] ? acc[q][e] : 0.0f;
   }
 }
 
 template <int DT>
-__global__ __launch_bounds__(256) void adapter_out_kernel(AdapterArgs a) {
-  const AdapterProj& p = a.p[blockIdx.y];
+__global__ __launch_bounds__(256) void adapter_in_kernel(InArgs a) {
+  __shared__ Acc4 part[3][kInSlots][64];
   int adapter, first, count;
-  if (!tile_of(a, blockIdx.x, adapter, first, count)) return;
-  const float scale = p.scale ? p.scale[adapter] : 1.0f;
-  for (int i = 0; i < count; ++i) {
-    const int row = a.rows[first + i];
-    if (row < 0 || row >= a.T) continue;
-    for (int c = threadIdx.x; c < p.m; c += 256) {
-      float sum = 0;
-      for (int j = 0; j < p.r; ++j)
-        sum += p.V[(int64_t)(first + i) * p.r + j] * load_as_float(p.B, ((int64_t)adapter * p.m + c) * p.r + j, DT);
-      store_from_float(p.Y, row * p.ldy + c, p.yd, load_as_float(p.Y, row * p.ldy + c, p.yd) + scale * sum);
+  if (!tile_of(a.tiles, blockIdx.x, a.adapters, a.T, adapter, first, count)) return;
+  const InGroup& g = a.g[blockIdx.z];
+  if (g.slots == 1) in_tile<DT, 1>(a, g, adapter, first, count, blockIdx.y, (Acc4(*)[1][64])part);
+  else if (g.slots == 2) in_tile<DT, 2>(a, g, adapter, first, count, blockIdx.y, (Acc4(*)[2][64])part);
+  else if (g.slots == 3) in_tile<DT, 3>(a, g, adapter, first, count, blockIdx.y, (Acc4(*)[3][64])part);
+  else in_tile<DT, 4>(a, g, adapter, first, count, blockIdx.y, part);
+}
+
+// Y[row][c] += scale sum over ranks of V[row][rank] B[c][rank].  V, a sum of the splits', is written as NL numbers of 16 bits that add up to it, one after
+// the other along the contraction in pieces of eight ranks, so that a rank of 16 with two of them is one product deep.  fp16 has not fp32's
+// exponents: there a row is brought to a largest of 1 first.  The columns of the products' tiles are laid out so that a lane ends with 16
+// neighbouring columns of one row.
+template <int DT, int YD, int NL>
+__global__ __launch_bounds__(256) void adapter_out_kernel(OutArgs a) {
+  extern __shared__ U32x4 limbs[];             // [sub][step][lane]
+  __shared__ uint32_t top[MDBF_ADAPTER_TILE];
+  __shared__ int32_t rows[MDBF_ADAPTER_TILE];
+  const OutProj& p = a.p[blockIdx.z];
+  int adapter, first, count;
+  if (p.yd != YD || (int64_t)blockIdx.y * p.chunk >= p.m) return;
+  if (!tile_of(a.tiles, blockIdx.x, a.adapters, a.T, adapter, first, count)) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, kg = lane >> 4;
+  const int eights = (p.r + 7) / 8, pieces = eights * NL, steps = (pieces + 3) / 4, subs = (count + 15) / 16;
+
+  if (tid < MDBF_ADAPTER_TILE) {
+    const int row = tid < count ? a.rows[first + tid] : -1;
+    rows[tid] = row < a.T ? row : -1;
+    top[tid] = 0;
+  }
+  // (V's columns behind a rank are zeros up to a multiple of 16)
+  const auto sum8 = [&](int t, int j, float (&v)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = 0.0f;
+    for (int s = 0; s < a.splits; ++s) {
+      const float* src = a.V + ((int64_t)s * a.T + first + t) * a.width + p.column + j * 8;
+      const F32x4 x = *(const MDBF_GLOBAL F32x4*)src, y = *((const MDBF_GLOBAL F32x4*)src + 1);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] += x[e], v[4 + e] += y[e];
+    }
+  };
+  if (DT == MDBF_F16) {
+    __syncthreads();
+    for (int w = tid; w < count * eights; w += 256) {
+      const int t = w / eights;
+      float v[8];
+      sum8(t, w - t * eights, v);
+      uint32_t m = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) m = max(m, __builtin_bit_cast(uint32_t, v[e]) & 0x7fffffffu);
+      atomicMax(&top[t], m);
+    }
+    __syncthreads();
+  }
+  // the power of two that brings a row's largest into [1, 2); rows that are not finite stay
+  const auto exponent = [&](int t) { const int e = (int)(top[t] >> 23); return e == 255 || e == 0 ? 0 : e - 127; };
+  const int cells = subs * 16 * eights;
+  for (int w = tid; w < cells; w += 256) {
+    const int t = w / eights, j = w - t * eights;
+    float v[8] = {};
+    if (t < count) sum8(t, j, v);
+    if (DT == MDBF_F16) {
+      const int e = t < count ? exponent(t) : 0;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) v[q] = __builtin_ldexpf(v[q], -e);
+    }
+#pragma unroll
+    for (int l = 0; l < NL; ++l) {
+      const int piece = l * eights + j;
+      U32x4 out;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const uint32_t h = round2<DT>(v[2 * q], v[2 * q + 1]);
+        out[q] = h;
+        float lo, hi;
+        if (DT == MDBF_F16) {
+          const F16x2 f = __builtin_bit_cast(F16x2, h);
+          lo = (float)f[0], hi = (float)f[1];
+        } else {
+          lo = __builtin_bit_cast(float, h << 16), hi = __builtin_bit_cast(float, h & 0xffff0000u);
+        }
+        // (what is not finite is carried by the first number alone)
+        v[2 * q] = __builtin_isfinite(lo) ? v[2 * q] - lo : 0.0f;
+        v[2 * q + 1] = __builtin_isfinite(hi) ? v[2 * q + 1] - hi : 0.0f;
+      }
+      limbs[((t >> 4) * steps + (piece >> 2)) * 64 + (piece & 3) * 16 + (t & 15)] = out;
     }
   }
+  for (int w = tid; w < subs * 16 * (steps * 4 - pieces); w += 256) {        // pieces behind the last
+    const int gap = steps * 4 - pieces, t = w / gap, piece = pieces + w - t * gap;
+    limbs[((t >> 4) * steps + (piece >> 2)) * 64 + (piece & 3) * 16 + (t & 15)] = U32x4{0, 0, 0, 0};
+  }
+  __syncthreads();
+
+  const float scale = p.scale ? p.scale[adapter] : 1.0f;
+  const int c_end = min((int64_t)p.m, ((int64_t)blockIdx.y + 1) * p.chunk);
+  for (int cb = (int)blockIdx.y * p.chunk + wave * kOutBlock; cb < c_end; cb += 4 * kOutBlock) {
+    // product row i of tile j is the column cb + (i / 4) * 16 + j * 4 + i % 4
+    int64_t b0[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) b0[j] = ((int64_t)adapter * p.m + min(cb + (i >> 2) * 16 + j * 4 + (i & 3), p.m - 1)) * p.r;
+    for (int sub = 0; sub < subs; ++sub) {
+      const int t = sub * 16 + i, row = rows[t], c = cb + kg * 16;
+      const bool there = t < count && row >= 0 && c < p.m;
+      Raw8<YD> y[2];
+      const int64_t at = (int64_t)max(row, 0) * p.ldy + c;
+      if (there) {
+        load_raw8<YD>(p.Y, at, p.m - c, y[0]);
+        if (c + 8 < p.m) load_raw8<YD>(p.Y, at + 8, p.m - c - 8, y[1]);
+      }
+      Acc4 acc[4] = {};
+      for (int s = 0; s < steps; ++s) {
+        const int piece = s * 4 + kg, j8 = (piece % eights) * 8;
+        const U32x4 v = limbs[(sub * steps + s) * 64 + lane];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          Raw8<DT> w = {};
+          if (piece < pieces) load_raw8<DT>(p.B, b0[j] + j8, p.r - j8, w);
+          acc[j] = product<DT>(w.w[0], v, acc[j]);
+        }
+      }
+      if (!there) continue;
+      float factor = scale;
+      if (DT == MDBF_F16) factor = __builtin_ldexpf(factor, exponent(t));
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if (c + 8 * h >= p.m) break;
+        float out[8];
+        to_float8<YD>(y[h], out);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) out[e] = fmaf(factor, acc[2 * h + e / 4][e % 4], out[e]);
+        store_float8<YD, false>(p.Y, at + 8 * h, p.m - c - 8 * h, out);
+      }
+    }
+  }
+}
+
+// How a call is cut.
+struct AdapterShape {
+  int width, splits;
+  size_t bytes;
+};
+static AdapterShape adapter_shape(int count, const mdbf_adapter_t* list, int T, int64_t tile_room) {
+  AdapterShape sh = {0, 1, 0};
+  int64_t slots = 0;
+  int n = 1;
+  for (int i = 0; i < count; ++i) {
+    sh.width += (list[i].r + 15) / 16 * 16;
+    slots += (list[i].r + 15) / 16;
+    n = list[i].n > n ? list[i].n : n;
+  }
+  // enough workgroups to fill the device twice, eight at most: the second launch reads every split's sums once per chunk of columns
+  const int64_t groups = (slots + kInSlots - 1) / kInSlots;
+  const int64_t want = 512 / (tile_room * groups);
+  const int most = n / 256 < 16 ? n / 256 : 16;
+  sh.splits = (int)(want < most ? want : most);
+  if (sh.splits < 1) sh.splits = 1;
+  sh.bytes = (size_t)sh.splits * T * sh.width * 4;
+  return sh;
 }
 
 static int check_adapters(int count, const mdbf_adapter_t* list, int dtype, int adapters, int T, int64_t tile_room) {
@@ -205,14 +435,60 @@ static int check_adapters(int count, const mdbf_adapter_t* list, int dtype, int 
     const mdbf_adapter_t& l = list[i];
     if (l.n < 1 || l.m < 1 || l.r < 1) return MDBF_EINVAL;
     if (!row_dtype(l.y_dtype)) return MDBF_EDTYPE;
-    if (l.r > 256) return MDBF_EUNSUPPORTED;
+    if (l.r > kMaxRank) return MDBF_EUNSUPPORTED;
   }
   return tile_room > (1ll << 30) ? MDBF_EUNSUPPORTED : MDBF_OK;
 }
-static size_t adapter_ws_bytes(int count, const mdbf_adapter_t* list, int T) {
-  size_t n = 0;
-  for (int i = 0; i < count; ++i) n += ((size_t)T * list[i].r * 4 + 255) / 256 * 256;
-  return n;
+
+template <int DT, int YD>
+static int launch_out(const OutArgs& o, int count, int64_t tile_room, int chunks, int eights, hipStream_t s) {
+  constexpr int NL = DT == MDBF_BF16 && YD == MDBF_F32 ? 3 : 2;
+  const size_t lds = (size_t)(MDBF_ADAPTER_TILE / 16) * ((eights * NL + 3) / 4) * 1024;
+  static KernelSetup setup;
+  const int e = kernel_setup(setup, [] {
+    return hipFuncSetAttribute((const void*)adapter_out_kernel<DT, YD, NL>, hipFuncAttributeMaxDynamicSharedMemorySize,
+                               MDBF_ADAPTER_TILE / 16 * (kMaxRank / 8 * NL / 4) * 1024);
+  });
+  if (e) return e;
+  adapter_out_kernel<DT, YD, NL><<<dim3((unsigned)tile_room, chunks, count), 256, lds, s>>>(o);
+  return (int)hipGetLastError();
+}
+
+template <int DT>
+static int launch_adapters(int count, const mdbf_adapter_t* list, int adapters, int T, const int32_t* rows, const int32_t* tiles, int64_t tile_room,
+                           float* V, hipStream_t s) {
+  const AdapterShape sh = adapter_shape(count, list, T, tile_room);
+  InArgs in = {};
+  OutArgs out = {};
+  in.rows = out.rows = rows, in.tiles = out.tiles = tiles, in.V = V, out.V = V;
+  in.adapters = out.adapters = adapters, in.T = out.T = T, in.width = out.width = sh.width, in.splits = out.splits = sh.splits;
+  int groups = 0, column = 0, yds = 0, eights[3] = {}, chunks[3] = {};
+  for (int i = 0; i < count; ++i) {
+    const mdbf_adapter_t& l = list[i];
+    in.A[i] = l.A_dev, in.r[i] = l.r, in.column[i] = column;
+    for (int t = 0; t < (l.r + 15) / 16; ++t) {
+      InGroup* g = groups ? &in.g[groups - 1] : nullptr;
+      if (!g || g->slots == kInSlots || g->X != l.X_dev || g->ldx != l.ldx || g->n != l.n) {
+        g = &in.g[groups++];
+        g->X = l.X_dev, g->ldx = l.ldx, g->n = l.n;
+      }
+      g->proj[g->slots] = (uint8_t)i, g->tile[g->slots] = (uint8_t)t;
+      ++g->slots;
+    }
+    const int chunk = 4 * kOutBlock;
+    out.p[i] = {l.B_dev, l.Y_dev, l.scale_dev, l.ldy, l.m, l.r, column, l.y_dtype, chunk};
+    column += (l.r + 15) / 16 * 16;
+    yds |= 1 << l.y_dtype;
+    const int c = (l.m + chunk - 1) / chunk, e = (l.r + 7) / 8;
+    if (c > chunks[l.y_dtype]) chunks[l.y_dtype] = c;
+    if (e > eights[l.y_dtype]) eights[l.y_dtype] = e;
+  }
+  adapter_in_kernel<DT><<<dim3((unsigned)tile_room, sh.splits, groups), 256, 0, s>>>(in);
+  int e = (int)hipGetLastError();
+  if (!e && (yds & 1 << MDBF_F16)) e = launch_out<DT, MDBF_F16>(out, count, tile_room, chunks[MDBF_F16], eights[MDBF_F16], s);
+  if (!e && (yds & 1 << MDBF_BF16)) e = launch_out<DT, MDBF_BF16>(out, count, tile_room, chunks[MDBF_BF16], eights[MDBF_BF16], s);
+  if (!e && (yds & 1 << MDBF_F32)) e = launch_out<DT, MDBF_F32>(out, count, tile_room, chunks[MDBF_F32], eights[MDBF_F32], s);
+  return e;
 }
 
 }  // namespace mdbf
@@ -255,7 +531,7 @@ int mdbf_adapters_workspace_bytes(int count, const mdbf_adapter_t* list, int dty
   if (!bytes_out) return MDBF_EINVAL;
   const int st = check_adapters(count, list, dtype, adapters, T, tile_room);
   if (st) return st;
-  *bytes_out = adapter_ws_bytes(count, list, T);
+  *bytes_out = adapter_shape(count, list, T, tile_room).bytes;
   return MDBF_OK;
 }
 
@@ -265,8 +541,6 @@ int mdbf_adapters(int count, const mdbf_adapter_t* list, int dtype, int adapters
   if (st) return st;
   if (!rows_dev || !tiles_dev || !workspace_dev) return MDBF_EINVAL;
   if (!ptr_aligned(rows_dev, 4) || !ptr_aligned(tiles_dev, 16) || !ptr_aligned(workspace_dev, 16)) return MDBF_EALIGN;
-  AdapterArgs a = {};
-  char* ws = (char*)workspace_dev;
   for (int i = 0; i < count; ++i) {
     const mdbf_adapter_t& l = list[i];
     if (!l.A_dev || !l.B_dev || !l.X_dev || !l.Y_dev || l.ldx < l.n || l.ldy < l.m) return MDBF_EINVAL;
@@ -276,20 +550,12 @@ int mdbf_adapters(int count, const mdbf_adapter_t* list, int dtype, int adapters
     if (!ptr_aligned(l.scale_dev, 4)) return MDBF_EALIGN;
     for (int j = 0; j < i; ++j)
       if (list[j].Y_dev == l.Y_dev) return MDBF_EINVAL;
-    a.p[i] = {l.A_dev, l.B_dev, l.X_dev, l.Y_dev, l.scale_dev, (float*)ws, l.ldx, l.ldy, l.n, l.m, l.r, l.y_dtype};
-    ws += ((size_t)T * l.r * 4 + 255) / 256 * 256;
   }
-  if (workspace_bytes < adapter_ws_bytes(count, list, T)) return MDBF_EWORKSPACE;
-  a.rows = rows_dev, a.tiles = tiles_dev, a.adapters = adapters, a.T = T;
-  const dim3 grid((unsigned)tile_room, count);
-  if (dtype == MDBF_F16) {
-    adapter_in_kernel<MDBF_F16><<<grid, 256, 0, (hipStream_t)stream>>>(a);
-    adapter_out_kernel<MDBF_F16><<<grid, 256, 0, (hipStream_t)stream>>>(a);
-  } else {
-    adapter_in_kernel<MDBF_BF16><<<grid, 256, 0, (hipStream_t)stream>>>(a);
-    adapter_out_kernel<MDBF_BF16><<<grid, 256, 0, (hipStream_t)stream>>>(a);
-  }
-  return hip_fail((int)hipGetLastError());
+  if (workspace_bytes < adapter_shape(count, list, T, tile_room).bytes) return MDBF_EWORKSPACE;
+  float* V = (float*)workspace_dev;
+  return hip_fail(dtype == MDBF_F16
+                      ? launch_adapters<MDBF_F16>(count, list, adapters, T, rows_dev, tiles_dev, tile_room, V, (hipStream_t)stream)
+                      : launch_adapters<MDBF_BF16>(count, list, adapters, T, rows_dev, tiles_dev, tile_room, V, (hipStream_t)stream));
 }
 
 }  // extern "C"
