@@ -30,7 +30,7 @@ constexpr uint32_t kKeyNone = 0x007fffffu;      // -inf
 
 // a row's settings
 struct RowSetting {
-  double largest, per_degree, top_p, min_p, u;
+  double largest, per_degree, grid, top_p, min_p, u;
   uint32_t top, top_k;
   bool greedy;
 };
@@ -39,6 +39,7 @@ __device__ __forceinline__ RowSetting row_setting(const SampleArgs& a, int64_t t
   const float temperature = a.temperature ? a.temperature[t] : 1.0f;
   r.greedy = !(temperature > 0.0f);
   r.per_degree = 1.0 / (double)temperature;
+  r.grid = 16 * 1.44269504088896340736 / (double)temperature;   // sixteenths of a factor of two per unit of the logits
   r.top = top;
   r.largest = (double)key_value(top);
   const int k = a.top_k ? a.top_k[t] : 0;
@@ -68,7 +69,7 @@ struct PickShared {
   uint32_t count[256];
   unsigned long long mass[256];
   unsigned long long sum[kPickThreads / 64];
-  uint32_t top[kPickThreads / 64];
+  uint32_t found[kPickThreads / 64];
   uint32_t digit, count_before;
   unsigned long long mass_before;
 };
@@ -129,31 +130,13 @@ __device__ Place descend(const SampleArgs& a, int64_t t, const RowSetting& r, Pi
     at.ties = s.count[s.digit];
   }
   return at;
-}
-
-// One workgroup a row, the row read again for every digit.
+}// A row that nothing else serves: read again for every digit.
 template <int DT>
-__global__ __launch_bounds__(kPickThreads) void sample_kernel(SampleArgs a) {
-  __shared__ PickShared s;
+__device__ void sample_digits(const SampleArgs& a, int64_t t, const RowSetting& r, PickShared& s) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t t = blockIdx.x;
-  uint32_t top = 0;
-  for (int i = tid; i < a.vocab; i += kPickThreads) top = max(top, key_at<DT>(a, t, i));
-  for (int o = 1; o < 64; o <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
-  if (lane == 0) s.top[wave] = top;
-  __syncthreads();
-  for (int w = 0; w < kPickThreads / 64; ++w) top = max(top, s.top[w]);
-  if (top <= kKeyNone) {
-    if (tid == 0) {
-      a.tokens[t] = -1;
-      if (a.probs) a.probs[t] = 0.0f;
-    }
-    return;
-  }
-  const RowSetting r = row_setting(a, t, top);
-  uint32_t key = top, tie = 0;
+  uint32_t key = r.top, tie = 0;
   double prob = 1.0;
-  if (!r.greedy) {
+  {
     // what is kept is a first part of the order, and so is what each bound leaves: the least of their masses
     unsigned long long total = 0, likely = 0;
     for (int i = tid; i < a.vocab; i += kPickThreads) {
@@ -197,19 +180,18 @@ __global__ __launch_bounds__(kPickThreads) void sample_kernel(SampleArgs a) {
     prob = w / kept;
   }
   // the index of that one among equal logits
-  __shared__ uint32_t found[kPickThreads / 64];
   uint32_t before = 0;
   for (int i0 = 0; i0 < a.vocab; i0 += kPickThreads) {
     const int i = i0 + tid;
     const bool eq = i < a.vocab && key_at<DT>(a, t, i) == key;
     const unsigned long long b = __ballot(eq);
     __syncthreads();
-    if (lane == 0) found[wave] = __popcll(b);
+    if (lane == 0) s.found[wave] = __popcll(b);
     __syncthreads();
     uint32_t mine = before, all = before;
     for (int w = 0; w < kPickThreads / 64; ++w) {
-      if (w < wave) mine += found[w];
-      all += found[w];
+      if (w < wave) mine += s.found[w];
+      all += s.found[w];
     }
     if (eq && mine + __popcll(b & ((1ull << lane) - 1)) == tie) {
       a.tokens[t] = i;
@@ -220,6 +202,434 @@ __global__ __launch_bounds__(kPickThreads) void sample_kernel(SampleArgs a) {
   }
 }
 
+// ---- the two launches -----------------------------------------------------------------------------------
+// With t = logit * 16 log2(e) / temperature a weight is 2^(t / 16) over the largest one's.  The first launch sorts the tokens of each part of a row into buckets
+// of a sixteenth of a factor of two, floor(t), from the part's largest down, and sums there how many they are and their 2^(frac(t) / 16): one 64-bit whole
+// number a bucket, whose additions in LDS have no order.  The buckets of all parts of a row lie on one grid, so the second launch, a workgroup a
+// row, adds them up; prefix sums then tell in which bucket each bound and the drawn number lie.  Only the tokens of those few are looked
+// at by themselves: parts that have some are read again, their tokens put in order, and the bounds applied exactly.  Tokens that equal the part's
+// largest are counted apart, so that those that equal the row's largest, of weight 1, make up a bucket of an exact mass: where many are alike,
+// bounds fall on borders between them.
+constexpr int kBuckets = 768;                    // of a row: the largest, then 767 sixteenths, down to 2^-47 of it; less weighs nothing
+constexpr int kPerOctave = 16;
+constexpr int kFracBits = 39;                    // of 2^(frac / 16) - 1 < 0.0443: 16384 of them stay below 2^49, where the count begins
+constexpr int kCountBit = 49;
+constexpr int kList = 8192;                      // tokens that the second launch puts in order; rows that have more go by digits
+constexpr int kPartThreads = 1024;
+constexpr double kSlack = 1e-9;                  // by which sums of buckets and of tokens may differ, and more
+
+struct PartHead {
+  unsigned long long top;                        // key of the part's largest, ~its index: the largest with the lowest index is the largest number
+  unsigned long long equal;                      // tokens that equal it
+};
+
+__device__ __forceinline__ double degrees(const RowSetting& r, float x) { return (double)x * r.grid; }
+
+// 2^(x / 16) - 1 for x in [0, 1): the exponential's series, to 6e-14
+__device__ __forceinline__ double sixteenth(double x) {
+  constexpr double q = 0.69314718055994530942 / kPerOctave;
+  constexpr double c1 = q, c2 = q * q / 2, c3 = q * q * q / 6, c4 = q * q * q * q / 24, c5 = q * q * q * q * q / 120, c6 = q * q * q * q * q * q / 720;
+  return x * fma(x, fma(x, fma(x, fma(x, fma(x, c6, c5), c4), c3), c2), c1);
+}
+
+template <int DT, int EPT>
+__global__ __launch_bounds__(kPartThreads) void sample_parts_kernel(SampleArgs a, PartHead* heads, unsigned long long* hists) {
+  __shared__ unsigned long long hist[kBuckets];
+  __shared__ unsigned long long tops[kPartThreads / 64];
+  __shared__ uint32_t equal;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t t = blockIdx.y, part = t * gridDim.x + blockIdx.x;
+  const int i0 = blockIdx.x * (kPartThreads * EPT);
+
+  Raw8<DT> raw[EPT / 8];
+#pragma unroll
+  for (int p = 0; p < EPT / 8; ++p) {
+    const int i = i0 + (p * kPartThreads + tid) * 8;
+    if (i < a.vocab) load_raw8<DT>(a.logits, t * a.ld + i, a.vocab - i, raw[p]);
+  }
+  for (int o = tid; o < kBuckets; o += kPartThreads) hist[o] = 0;
+  if (tid == 0) equal = 0;
+  float v[EPT], best = -__builtin_inff();
+  int at = 0x7fffffff;
+#pragma unroll
+  for (int p = 0; p < EPT / 8; ++p) {
+    const int i = i0 + (p * kPartThreads + tid) * 8;
+    float x[8];
+    to_float8<DT>(raw[p], x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float y = i + e < a.vocab && x[e] == x[e] ? x[e] : -__builtin_inff();
+      v[p * 8 + e] = y;
+      if (y > best) best = y, at = i + e;
+    }
+  }
+  unsigned long long top = (unsigned long long)order_key(best) << 32 | (uint32_t)~at;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const unsigned long long u = __shfl_xor(top, o);
+    if (u > top) top = u;
+  }
+  if (lane == 0) tops[wave] = top;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kPartThreads / 64; ++w)
+    if (tops[w] > top) top = tops[w];
+  if (tid == 0) heads[part].top = top;
+  const uint32_t key = (uint32_t)(top >> 32);
+  const RowSetting r = row_setting(a, t, key);
+  if (key <= kKeyNone || r.greedy) return;
+  const float largest = key_value(key);
+  const bool infinite = largest == __builtin_inff();    // then nothing else weighs
+  const double base = floor(degrees(r, largest));
+  uint32_t alike = 0;
+#pragma unroll
+  for (int e = 0; e < EPT; ++e) {
+    const bool same = v[e] == largest;
+    alike += (uint32_t)__popcll(__ballot(same));
+    if (infinite || same) continue;
+    const double d = degrees(r, v[e]), f = floor(d), down = base - f;
+    if (down < kBuckets && v[e] > -__builtin_inff()) {
+      // (the sum with 2^52 has the whole number in its last bits)
+      const double g = fma(sixteenth(d - f), (double)(1ull << kFracBits), 0x1p52);
+      atomicAdd(&hist[(int)down], __builtin_bit_cast(unsigned long long, g) - 0x4330000000000000ull + (1ull << kCountBit));
+    }
+  }
+  if (lane == 0) atomicAdd(&equal, alike);
+  __syncthreads();
+  if (tid == 0) heads[part].equal = equal;
+  for (int o = tid; o < kBuckets; o += kPartThreads) hists[part * kBuckets + o] = hist[o];
+}
+
+// What the second launch has in LDS.
+struct RowShared {
+  unsigned long long list[kList];                // ~key, index: the order of the tokens
+  double before[kBuckets], seg_mass[kBuckets];   // mass in front of a bucket, and of the list in front of a bucket's first
+  uint32_t count_before[kBuckets], seg_at[kBuckets];
+  uint32_t flags[(kBuckets + 31) / 32];
+  double sums[kPickThreads / 64];
+  uint32_t counts[kPickThreads / 64];
+  unsigned long long tops[kPickThreads / 64];
+  double klo, khi, plo, phi, mlo, mhi, total;
+  int k, p0, p1, m0, m1, u0, u1;
+  uint32_t n, all, found;
+};
+
+template <class Op>
+__device__ __forceinline__ double block_fold(double v, double* part, Op op) {
+  for (int o = 1; o < 64; o <<= 1) v = op(v, __shfl_xor(v, o));
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = part[0];
+  for (int w = 1; w < kPickThreads / 64; ++w) v = op(v, part[w]);
+  return v;
+}
+
+// Which buckets have to be looked at: those of the bounds and of the drawn number, the latter ones' ends by the least and the most that the bounds
+// may leave.
+__device__ void choose_buckets(const RowSetting& r, RowShared& s, double before, double upto, uint32_t count_before, uint32_t count_to, double frac) {
+  const int o = threadIdx.x;
+  const bool in = o < kBuckets;
+  const double total = s.total;
+  if (o == 0) {
+    s.k = -1, s.p0 = s.m0 = s.u0 = 0, s.p1 = s.m1 = s.u1 = -1;
+    s.klo = s.khi = s.plo = s.phi = s.mlo = s.mhi = total;
+  }
+  __syncthreads();
+  if (in && r.top_k && count_before < r.top_k && count_to >= r.top_k) s.k = o, s.klo = before, s.khi = upto;
+  __syncthreads();
+  const double klo = s.klo, khi = s.khi;
+  __syncthreads();
+  if (r.top_p < 1.0) {
+    const double lo = r.top_p * klo * (1 - kSlack), hi = r.top_p * khi * (1 + kSlack);
+    if (o == 0) s.p1 = kBuckets - 1, s.plo = 0;
+    __syncthreads();
+    if (in && before < lo && upto >= lo) s.p0 = o, s.plo = before;
+    if (in && before <= hi && upto > hi) s.p1 = o, s.phi = upto;
+  }
+  if (r.min_p > 0.0 && in) {
+    const double last = -floor(frac + kPerOctave * log2(r.min_p));      // the bucket of that weight, or its neighbour, is `last` + 1
+    const int m0 = (int)fmin(fmax(last, 0.0), (double)kBuckets), m1 = (int)fmin(fmax(last + 2, 0.0), (double)(kBuckets - 1));
+    if (m0 < kBuckets) {
+      if (o == m0) s.m0 = o, s.mlo = before;
+      if (o == m1) s.m1 = o, s.mhi = upto;
+    }
+  }
+  __syncthreads();
+  const double lo = fmin(klo, fmin(s.plo, s.mlo)), hi = fmin(khi, fmin(s.phi, s.mhi));
+  const double ulo = r.u * lo * (1 - kSlack), uhi = r.u * hi * (1 + kSlack);
+  __syncthreads();
+  if (o == 0) s.u1 = kBuckets - 1;
+  __syncthreads();
+  if (in && before <= ulo && upto > ulo) s.u0 = o;
+  if (in && before <= uhi && upto > uhi) s.u1 = o;
+  __syncthreads();
+  // (a bound that another one is sure to undercut needs none of its tokens)
+  const bool least = s.mlo >= fmin(khi, s.phi), other = s.mhi <= fmin(klo, s.plo);
+  const bool flag = in && ((!other && (o == s.k || (o >= s.p0 && o <= s.p1))) || (!least && o >= s.m0 && o <= s.m1) || (o >= s.u0 && o <= s.u1));
+  const unsigned long long b = __ballot(flag);
+  if (in && (o & 63) == 0) s.flags[o >> 5] = (uint32_t)b, s.flags[(o >> 5) + 1] = (uint32_t)(b >> 32);
+  __syncthreads();
+}
+
+// The list in order: bitonic, in LDS.
+__device__ void sort_list(RowShared& s, int n) {
+  int size = 1;
+  while (size < n) size <<= 1;
+  for (int i = n + threadIdx.x; i < size; i += kPickThreads) s.list[i] = ~0ull;
+  __syncthreads();
+  for (int k = 2; k <= size; k <<= 1)
+    for (int j = k >> 1; j > 0; j >>= 1) {
+      for (int i = threadIdx.x; i < size / 2; i += kPickThreads) {
+        const int x = ((i & ~(j - 1)) << 1) | (i & (j - 1)), y = x | j;
+        const unsigned long long p = s.list[x], q = s.list[y];
+        if ((p > q) == ((x & k) == 0)) s.list[x] = q, s.list[y] = p;
+      }
+      __syncthreads();
+    }
+}
+
+template <int DT>
+__global__ __launch_bounds__(kPickThreads) void sample_rows_kernel(SampleArgs a, const PartHead* heads, const unsigned long long* hists, int parts, int part_size) {
+  extern __shared__ char shared[];
+  RowShared& s = *(RowShared*)shared;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t t = blockIdx.x;
+  unsigned long long top = 0;
+  for (int c = tid; c < parts; c += kPickThreads) {
+    const unsigned long long u = heads[t * parts + c].top;
+    if (u > top) top = u;
+  }
+  for (int o = 1; o < 64; o <<= 1) {
+    const unsigned long long u = __shfl_xor(top, o);
+    if (u > top) top = u;
+  }
+  if (lane == 0) s.tops[wave] = top;
+  if (tid == 0) s.n = 0;
+  __syncthreads();
+  for (int w = 0; w < kPickThreads / 64; ++w)
+    if (s.tops[w] > top) top = s.tops[w];
+  const uint32_t key = (uint32_t)(top >> 32);
+  const RowSetting r = row_setting(a, t, key);
+  if (key <= kKeyNone || r.greedy) {
+    if (tid == 0) {
+      a.tokens[t] = key <= kKeyNone ? -1 : (int)~(uint32_t)top;
+      if (a.probs) a.probs[t] = key <= kKeyNone ? 0.0f : 1.0f;
+    }
+    return;
+  }
+  const float largest = key_value(key);
+  const bool infinite = largest == __builtin_inff();
+  const double most = infinite ? 0.0 : degrees(r, largest), base = floor(most), frac = most - base;
+
+  const auto bucket_of = [&](float x) { return x == largest ? 0 : 1 + (int)fmin(base - floor(degrees(r, x)), (double)kBuckets); };
+
+  // a thread's bucket, of all parts
+  uint32_t count = 0;
+  unsigned long long extra = 0;
+  if (tid < kBuckets)
+    for (int c = 0; c < parts; ++c) {
+      const float its = key_value((uint32_t)(heads[t * parts + c].top >> 32));
+      if (its == -__builtin_inff() || (infinite && its != largest)) continue;
+      const int top_bucket = bucket_of(its);
+      if (tid == top_bucket) {
+        const uint32_t equal = (uint32_t)heads[t * parts + c].equal;
+        count += equal;
+        const double d = degrees(r, its);
+        if (tid) extra += equal * (unsigned long long)(sixteenth(d - floor(d)) * (double)(1ull << kFracBits) + 0.5);
+      }
+      // (its buckets begin with that of its largest, of the row's with bucket 1)
+      const int shift = max(top_bucket, 1);
+      if (infinite || tid < shift) continue;
+      const unsigned long long h = hists[(t * parts + c) * kBuckets + tid - shift];
+      count += (uint32_t)(h >> kCountBit);
+      extra += h & ((1ull << kCountBit) - 1);
+    }
+  const double mass = tid == 0 ? (double)count
+                               : ((double)count + (double)extra * (1.0 / (double)(1ull << kFracBits))) * exp2(-(tid - 1 + frac) / kPerOctave);
+  uint32_t count_to = count;
+  double upto = mass;
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint32_t uc = __shfl_up(count_to, o);
+    const double um = __shfl_up(upto, o);
+    if (lane >= o) count_to += uc, upto += um;
+  }
+  if (lane == 63) s.sums[wave] = upto, s.counts[wave] = count_to;
+  __syncthreads();
+  double wave_before = 0, total = 0;
+  uint32_t waves_count = 0;
+  for (int w = 0; w < kBuckets / 64; ++w) {
+    if (w == wave) wave_before = total;
+    if (w < wave) waves_count += s.counts[w];
+    total += s.sums[w];
+  }
+  // (the sum in front of a bucket is that up to the one before it, bit for bit)
+  const double inside = __shfl_up(upto, 1);
+  const double before = lane ? wave_before + inside : wave_before;
+  upto += wave_before, count_to += waves_count;
+  if (tid < kBuckets) s.before[tid] = before, s.count_before[tid] = count_to - count;
+  if (tid == 0) s.total = total;
+  __syncthreads();
+  choose_buckets(r, s, before, upto, count_to - count, count_to, frac);
+
+  // tokens of those buckets
+  for (int c = wave; c < parts; c += kPickThreads / 64) {
+    const float its = key_value((uint32_t)(heads[t * parts + c].top >> 32));
+    if (its == -__builtin_inff() || (infinite && its != largest)) continue;
+    const int top_bucket = bucket_of(its), shift = max(top_bucket, 1);
+    bool some = top_bucket < kBuckets && (s.flags[top_bucket >> 5] >> (top_bucket & 31) & 1);
+    for (int o = shift + lane; o < kBuckets && !infinite; o += 64)
+      if ((s.flags[o >> 5] >> (o & 31) & 1) && hists[(t * parts + c) * kBuckets + o - shift]) some = true;
+    if (!__any(some)) continue;
+    const int i0 = c * part_size, i1 = min(i0 + part_size, a.vocab);
+    for (int i = i0 + lane * 8; i < i1; i += 512) {
+      Raw8<DT> raw;
+      float x[8];
+      load_raw8<DT>(a.logits, t * a.ld + i, i1 - i, raw);
+      to_float8<DT>(raw, x);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (i + e >= i1 || !(x[e] > -__builtin_inff())) continue;
+        if (infinite && x[e] != largest) continue;
+        const int b = bucket_of(x[e]);
+        if (b >= kBuckets || !(s.flags[b >> 5] >> (b & 31) & 1)) continue;
+        const uint32_t n = atomicAdd(&s.n, 1u);
+        if (n < kList) s.list[n] = (unsigned long long)~order_key(x[e]) << 32 | (uint32_t)(i + e);
+      }
+    }
+  }
+  __syncthreads();
+  const int n = (int)s.n;
+  if (n > kList || n == 0) {
+    __syncthreads();
+    sample_digits<DT>(a, t, r, *(PickShared*)shared);
+    return;
+  }
+  sort_list(s, n);
+
+  // each thread has a run of the list
+  const int per = (n + kPickThreads - 1) / kPickThreads, x0 = min(tid * per, n), x1 = min(x0 + per, n);
+  constexpr int kPer = kList / kPickThreads;
+  double w[kPer], sum = 0;
+  int bucket[kPer];
+#pragma unroll
+  for (int q = 0; q < kPer; ++q) {
+    if (x0 + q < x1) {
+      const uint32_t k = ~(uint32_t)(s.list[x0 + q] >> 32);
+      w[q] = weight(r, k);
+      bucket[q] = bucket_of(key_value(k));
+      sum += w[q];
+    }
+  }
+  double run = sum;
+  for (int o = 1; o < 64; o <<= 1) {
+    const double u = __shfl_up(run, o);
+    if (lane >= o) run += u;
+  }
+  __syncthreads();
+  if (lane == 63) s.sums[wave] = run;
+  __syncthreads();
+  run -= sum;
+  for (int v = 0; v < wave; ++v) run += s.sums[v];
+  double at[kPer];                              // mass of the list in front of a token
+#pragma unroll
+  for (int q = 0; q < kPer; ++q) {
+    if (x0 + q < x1) {
+      at[q] = run;
+      run += w[q];
+      const int x = x0 + q;
+      int prev = -1;
+      if (x > 0) {
+        const uint32_t k = ~(uint32_t)(s.list[x - 1] >> 32);
+        prev = bucket_of(key_value(k));
+      }
+      if (prev != bucket[q]) s.seg_mass[bucket[q]] = at[q], s.seg_at[bucket[q]] = x;
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int q = 0; q < kPer; ++q)
+    if (x0 + q < x1) at[q] = s.before[bucket[q]] + (at[q] - s.seg_mass[bucket[q]]);
+  const auto rank = [&](int q) { return s.count_before[bucket[q]] + (uint32_t)(x0 + q) - s.seg_at[bucket[q]]; };
+  const auto largest_of = [](double p, double q) { return fmax(p, q); };
+
+  double kept = s.total;
+  const bool least = s.mlo >= fmin(s.khi, s.phi), other = s.mhi <= fmin(s.klo, s.plo);
+  if (s.k >= 0 && !other) {
+    double m = s.klo;
+#pragma unroll
+    for (int q = 0; q < kPer; ++q)
+      if (x0 + q < x1 && bucket[q] == s.k && rank(q) < r.top_k) m = fmax(m, at[q] + w[q]);
+    kept = block_fold(m, s.sums, largest_of);
+  }
+  if (r.top_p < 1.0 && !other) {
+    const double mass = r.top_p * kept;
+    double m = s.plo;
+#pragma unroll
+    for (int q = 0; q < kPer; ++q)
+      if (x0 + q < x1 && bucket[q] >= s.p0 && bucket[q] <= s.p1 && (at[q] < mass || rank(q) == 0)) m = fmax(m, at[q] + w[q]);
+    kept = block_fold(m, s.sums, largest_of);
+  }
+  if (s.m1 >= 0 && !least) {
+    double m = s.mlo;
+#pragma unroll
+    for (int q = 0; q < kPer; ++q)
+      if (x0 + q < x1 && bucket[q] >= s.m0 && bucket[q] <= s.m1 && (w[q] >= r.min_p || rank(q) == 0)) m = fmax(m, at[q] + w[q]);
+    kept = fmin(kept, block_fold(m, s.sums, largest_of));
+  }
+  const double drawn = r.u * kept;
+  double first = 1e9, last = -1;
+#pragma unroll
+  for (int q = 0; q < kPer; ++q)
+    if (x0 + q < x1 && bucket[q] >= s.u0 && bucket[q] <= s.u1) {
+      if (at[q] + w[q] > drawn) first = fmin(first, (double)(x0 + q));
+      else last = fmax(last, (double)(x0 + q));
+    }
+  first = block_fold(first, s.sums, [](double p, double q) { return fmin(p, q); });
+  last = block_fold(last, s.sums, largest_of);
+  const int x = (int)(first < 1e9 ? first : last);   // (none goes beyond only by the sums' rounding: the last one then)
+  if (x >= x0 && x < x1) {
+    const unsigned long long it = s.list[x];
+    a.tokens[t] = (int)(uint32_t)it;
+    if (a.probs) a.probs[t] = (float)(weight(r, ~(uint32_t)(it >> 32)) / kept);
+  }
+}
+
+constexpr int kPartLeast = kPartThreads * 8, kPartMost = kPartThreads * 16;
+static size_t sample_ws_bytes(int T, int vocab) {
+  const size_t parts = ((size_t)vocab + kPartLeast - 1) / kPartLeast;
+  return (size_t)T * parts * (sizeof(PartHead) + kBuckets * 8);
+}
+
+template <int DT>
+static int launch_sample(const SampleArgs& a, void* ws, hipStream_t s) {
+  // parts of 8192 tokens where that leaves compute units idle, else of 16384
+  const int part = (int64_t)a.T * ((a.vocab + kPartMost - 1) / kPartMost) < 512 ? kPartLeast : kPartMost;
+  const int parts = (a.vocab + part - 1) / part;
+  PartHead* heads = (PartHead*)ws;
+  unsigned long long* hists = (unsigned long long*)(heads + (size_t)a.T * parts);
+  static KernelSetup setup;
+  const int e = kernel_setup(setup, [] {
+    return hipFuncSetAttribute((const void*)sample_rows_kernel<DT>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(RowShared));
+  });
+  if (e) return e;
+  // (the grid's second dimension ends at 65535 rows)
+  for (int t0 = 0; t0 < a.T; t0 += 65535) {
+    SampleArgs b = a;
+    b.T = a.T - t0 < 65535 ? a.T - t0 : 65535;
+    b.logits = (const char*)a.logits + (size_t)t0 * a.ld * dtype_size(DT);
+    const auto from = [&](auto* p) { return p ? p + t0 : p; };
+    b.temperature = from(a.temperature), b.top_p = from(a.top_p), b.min_p = from(a.min_p), b.u = from(a.u), b.top_k = from(a.top_k);
+    b.tokens = from(a.tokens), b.probs = from(a.probs);
+    if (part == kPartLeast) sample_parts_kernel<DT, 8><<<dim3(parts, b.T), kPartThreads, 0, s>>>(b, heads, hists);
+    else sample_parts_kernel<DT, 16><<<dim3(parts, b.T), kPartThreads, 0, s>>>(b, heads, hists);
+    sample_rows_kernel<DT><<<b.T, kPickThreads, sizeof(RowShared), s>>>(b, heads, hists, parts, part);
+  }
+  return (int)hipGetLastError();
+}
+
+
+
 }  // namespace mdbf
 
 using namespace mdbf;
@@ -229,7 +639,7 @@ extern "C" {
 int mdbf_sample_workspace_bytes(int T, int vocab, size_t* bytes_out) {
   if (T < 1 || vocab < 1 || !bytes_out) return MDBF_EINVAL;
   if (vocab > kSampleMaxVocab) return MDBF_EUNSUPPORTED;
-  *bytes_out = 0;
+  *bytes_out = sample_ws_bytes(T, vocab);
   return MDBF_OK;
 }
 
@@ -247,10 +657,9 @@ int mdbf_sample(const mdbf_sample_t* settings, const void* logits_dev, int64_t l
   if (workspace_bytes < need) return MDBF_EWORKSPACE;
   const SampleArgs a = {logits_dev, settings->temperature_dev, settings->top_p_dev, settings->min_p_dev, u_dev, settings->top_k_dev,
                         tokens_dev, probs_dev, ld, T, vocab};
-  if (dtype == MDBF_F16) sample_kernel<MDBF_F16><<<T, kPickThreads, 0, (hipStream_t)stream>>>(a);
-  else if (dtype == MDBF_BF16) sample_kernel<MDBF_BF16><<<T, kPickThreads, 0, (hipStream_t)stream>>>(a);
-  else sample_kernel<MDBF_F32><<<T, kPickThreads, 0, (hipStream_t)stream>>>(a);
-  return hip_fail((int)hipGetLastError());
+  const hipStream_t q = (hipStream_t)stream;
+  return hip_fail(dtype == MDBF_F16 ? launch_sample<MDBF_F16>(a, workspace_dev, q)
+                  : dtype == MDBF_BF16 ? launch_sample<MDBF_BF16>(a, workspace_dev, q) : launch_sample<MDBF_F32>(a, workspace_dev, q));
 }
 
 }  // extern "C"

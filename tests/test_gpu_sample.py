@@ -1,0 +1,141 @@
+"""mdbf_sample against the definition in 64 bits: tokens equal, shares to the rounding of their type.  A token could differ only where the
+drawn number falls on an edge between two tokens to 1e-9 of the mass, which has a chance of 1e-4 over all rows here; rows are made from seeds."""
+import numpy as np
+import pytest
+
+from oracle import step_oracle as so
+
+pytestmark = pytest.mark.gpu
+TINY = 2.0 ** -24        # a share is a quotient of 64-bit sums, rounded once to fp32
+
+
+@pytest.fixture(scope="module")
+def gpu():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need a GPU")
+    from paper_2512_24545_amd import binding as mb
+    mb.lib()
+    return torch, mb
+
+
+def _logits(rng, T, V, spread=2.0, likely=20):
+    z = rng.standard_normal((T, V)) * spread
+    for row in z:
+        row[rng.integers(0, V, likely)] += 9 * rng.random(likely)
+    return z
+
+
+def _check(gpu, z, u, dtype="f32", pad=0, **settings):
+    torch, mb = gpu
+    T, V = z.shape
+    dt = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}[dtype]
+    wide = torch.full((T, V + pad), float("inf"), dtype=dt, device="cuda:0")
+    wide[:, :V] = torch.from_numpy(np.ascontiguousarray(z)).to(dt).to("cuda:0")
+    held = wide[:, :V]
+    on = {k: torch.from_numpy(np.array(np.broadcast_to(v, T))).to("cuda:0", torch.int32 if k == "top_k" else torch.float32)
+          for k, v in settings.items()}
+    ut = torch.from_numpy(np.ascontiguousarray(u, dtype=np.float32)).to("cuda:0")
+    tokens, probs = mb.mdbf_sample(held, ut, **on)
+    again = mb.mdbf_sample(held, ut, **on)
+    assert torch.equal(tokens, again[0]) and torch.equal(probs, again[1])
+    z64, u64 = held.double().cpu().numpy(), ut.double().cpu().numpy()
+    host = {k: v.double().cpu().numpy() for k, v in on.items()}
+    for t in range(T):
+        token, share = so.sample(z64[t], u64[t], **{k: v[t] for k, v in host.items()})
+        assert (int(tokens[t]), True) == (token, True), (t, int(tokens[t]), token, settings)
+        assert abs(float(probs[t]) - share) <= TINY * share + 1e-9 * share, (t, float(probs[t]), share)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("V", [1, 2, 7, 64, 1000, 8191, 8192, 8193, 32000, 70001])
+def test_plain_draws(gpu, V, dtype):
+    rng = np.random.default_rng(V)
+    _check(gpu, _logits(rng, 9, V), rng.random(9), dtype, pad=V % 3)
+
+
+@pytest.mark.parametrize("settings", [dict(top_k=1), dict(top_k=50), dict(top_k=5000), dict(top_p=0.9), dict(top_p=0.3), dict(top_p=0.999),
+                                      dict(min_p=0.02), dict(min_p=1.0), dict(top_k=40, top_p=0.8), dict(top_k=200, min_p=0.1),
+                                      dict(top_p=0.95, min_p=0.01), dict(top_k=30, top_p=0.9, min_p=0.05, temperature=0.7),
+                                      dict(temperature=1.5, top_p=0.98), dict(temperature=0.05), dict(temperature=30.0, top_k=1000)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_bounds(gpu, settings, dtype):
+    rng = np.random.default_rng(3)
+    for V in (777, 20000):
+        _check(gpu, _logits(rng, 16, V), rng.random(16), dtype, **settings)
+
+
+def test_each_row_has_its_own_settings(gpu):
+    rng = np.random.default_rng(4)
+    T = 200
+    _check(gpu, _logits(rng, T, 9000), rng.random(T), "bf16", temperature=rng.choice([0.0, 0.3, 1.0, 2.0], T), top_k=rng.choice([0, 1, 20, 4000], T),
+           top_p=rng.choice([0.1, 0.9, 1.0], T), min_p=rng.choice([0.0, 0.05], T))
+
+
+def test_more_rows_than_parts_are_cut_small_for(gpu):
+    rng = np.random.default_rng(5)
+    _check(gpu, _logits(rng, 300, 33000), rng.random(300), "f16", top_p=0.9)
+
+
+@pytest.mark.parametrize("V", [64, 9001, 40000])
+def test_equal_logits_go_by_index(gpu, V):
+    """All tokens alike: more equal ones than the list holds, and every bound falls among them."""
+    u = np.array([0.0, 0.25, 0.5, 0.75, 1 - 2.0 ** -24])
+    z = np.full((5, V), 1.25)
+    _check(gpu, z, u)
+    _check(gpu, z, u, top_p=0.5)
+    _check(gpu, z, u, top_k=V // 2, top_p=0.5)
+    _check(gpu, z, u, min_p=1.0)
+    z[:, V // 3:V // 2] = 2.25
+    _check(gpu, z, u, top_k=V // 4)
+    z[:, ::2] = -0.0
+    z[:, 1::2] = 0.0
+    _check(gpu, z, u)
+
+
+def test_flat_rows_that_overflow_the_list(gpu):
+    """Tokens in one bucket, but of different weights."""
+    rng = np.random.default_rng(6)
+    _check(gpu, rng.random((6, 50000)), rng.random(6), temperature=100.0)
+    _check(gpu, rng.random((6, 50000)), rng.random(6), temperature=100.0, top_k=30000, top_p=0.7, min_p=0.99)
+
+
+def test_bf16_ties_everywhere(gpu):
+    rng = np.random.default_rng(7)
+    z = np.round(rng.standard_normal((20, 30000)) * 2) / 2
+    for settings in (dict(), dict(top_p=0.9), dict(top_k=777), dict(min_p=0.3), dict(top_k=500, top_p=0.5, min_p=0.01)):
+        _check(gpu, z, rng.random(20), "bf16", **settings)
+
+
+def test_masks_infinities_and_nan(gpu):
+    rng = np.random.default_rng(8)
+    V = 20000
+    z = _logits(rng, 12, V)
+    z[0] = -np.inf
+    z[1] = np.nan
+    z[2] = -np.inf
+    z[2, 12345] = -3.0
+    z[3, rng.integers(0, V, V // 2)] = np.nan
+    z[4, [5, 17000]] = np.inf
+    z[5] = np.inf
+    z[6, 1:] = -np.inf
+    z[7] = -3.4e38
+    z[8, 8192:] = -np.inf                        # whole parts masked
+    z[9, :16384] = -np.inf
+    z[10] *= 1e30
+    z[11] *= 1e-30
+    u = rng.random(12)
+    for settings in (dict(), dict(top_p=0.9), dict(top_k=3), dict(min_p=0.5, temperature=0.5), dict(temperature=0.0)):
+        _check(gpu, z, u, **settings)
+    _check(gpu, z[:10], u[:10], "f16", top_p=0.8)
+
+
+def test_settings_at_their_ends(gpu):
+    rng = np.random.default_rng(9)
+    z = _logits(rng, 8, 5000)
+    u = np.array([0.0, 1.0, -1.0, 2.0, np.nan, 0.5, 2.0 ** -24, 1 - 2.0 ** -24])
+    inf, nan = np.inf, np.nan
+    for settings in (dict(), dict(top_p=np.array([0, -1, nan, 1, 2, 1e-9, 1 - 2.0 ** -24, 0.5])), dict(min_p=np.array([0, -1, nan, 1, 2, 1e-30, 1e-45, 1.0])),
+                     dict(top_k=np.array([0, -5, 1, 4999, 5000, 5001, 2 ** 31 - 1, 2])),
+                     dict(temperature=np.array([0, -1, nan, inf, 1e-45, 1e-30, 3e38, 1.0]))):
+        _check(gpu, z, u, **settings)
