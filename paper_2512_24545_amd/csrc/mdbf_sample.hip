@@ -301,52 +301,58 @@ __global__ __launch_bounds__(kPartThreads) void sample_parts_kernel(SampleArgs a
 }
 
 // What the second launch has in LDS.
+constexpr int kRuns = 4;                         // runs of neighbouring buckets that are looked at
+constexpr int kMaxParts = kSampleMaxVocab / (kPartThreads * 8);
 struct RowShared {
   unsigned long long list[kList];                // ~key, index: the order of the tokens
   double before[kBuckets], seg_mass[kBuckets];   // mass in front of a bucket, and of the list in front of a bucket's first
   uint32_t count_before[kBuckets], seg_at[kBuckets];
-  uint32_t flags[(kBuckets + 31) / 32];
+  unsigned long long flags[kBuckets / 64];
   double sums[kPickThreads / 64];
   uint32_t counts[kPickThreads / 64];
   unsigned long long tops[kPickThreads / 64];
+  unsigned long long part_extra[kMaxParts];      // of a part: its largest's bucket in the row (kBuckets: nothing there weighs), how many equal it, and
+  int32_t part_top[kMaxParts];                   // their fractions
+  uint32_t part_equal[kMaxParts], part_list[kMaxParts];
   double klo, khi, plo, phi, mlo, mhi, total;
   int k, p0, p1, m0, m1, u0, u1;
-  uint32_t n, all, found;
+  float lower[kRuns], upper[kRuns];
+  uint32_t n, parts, runs, dropped;
 };
 
-template <class Op>
-__device__ __forceinline__ double block_fold(double v, double* part, Op op) {
-  for (int o = 1; o < 64; o <<= 1) v = op(v, __shfl_xor(v, o));
+// what the wave wrote in LDS, or the workgroup, is there for all of it
+template <int THREADS>
+__device__ __forceinline__ void meet() {
+  if (THREADS > 64) {
+    __syncthreads();
+  } else {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// The value of the last (or first) thread for which `here` holds, where it rises with the threads; else `none`.
+template <int THREADS, bool FIRST>
+__device__ __forceinline__ double end_of(bool here, double v, double none, double* part) {
+  const unsigned long long b = __ballot(here);
+  const int who = !b ? 0 : FIRST ? __builtin_ctzll(b) : 63 - __builtin_clzll(b);
+  if (THREADS == 64) return b ? __shfl(v, who) : none;
   __syncthreads();
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+  if ((int)(threadIdx.x & 63) == who) part[threadIdx.x >> 6] = b ? v : none;
   __syncthreads();
   v = part[0];
-  for (int w = 1; w < kPickThreads / 64; ++w) v = op(v, part[w]);
+#pragma unroll
+  for (int w = 1; w < THREADS / 64; ++w) v = FIRST ? fmin(v, part[w]) : fmax(v, part[w]);
   return v;
 }
 
 // Which buckets have to be looked at: those of the bounds and of the drawn number, the latter ones' ends by the least and the most that the bounds
-// may leave.
-__device__ void choose_buckets(const RowSetting& r, RowShared& s, double before, double upto, uint32_t count_before, uint32_t count_to, double frac) {
+// may leave.  k, p0 .., m0 .., u0 .. are set to no bound before.
+__device__ __forceinline__ void choose_buckets(const RowSetting& r, RowShared& s, double before, double upto, uint32_t count_before, uint32_t count_to,
+                                               double frac) {
   const int o = threadIdx.x;
   const bool in = o < kBuckets;
-  const double total = s.total;
-  if (o == 0) {
-    s.k = -1, s.p0 = s.m0 = s.u0 = 0, s.p1 = s.m1 = s.u1 = -1;
-    s.klo = s.khi = s.plo = s.phi = s.mlo = s.mhi = total;
-  }
-  __syncthreads();
   if (in && r.top_k && count_before < r.top_k && count_to >= r.top_k) s.k = o, s.klo = before, s.khi = upto;
-  __syncthreads();
-  const double klo = s.klo, khi = s.khi;
-  __syncthreads();
-  if (r.top_p < 1.0) {
-    const double lo = r.top_p * klo * (1 - kSlack), hi = r.top_p * khi * (1 + kSlack);
-    if (o == 0) s.p1 = kBuckets - 1, s.plo = 0;
-    __syncthreads();
-    if (in && before < lo && upto >= lo) s.p0 = o, s.plo = before;
-    if (in && before <= hi && upto > hi) s.p1 = o, s.phi = upto;
-  }
   if (r.min_p > 0.0 && in) {
     const double last = -floor(frac + kPerOctave * log2(r.min_p));      // the bucket of that weight, or its neighbour, is `last` + 1
     const int m0 = (int)fmin(fmax(last, 0.0), (double)kBuckets), m1 = (int)fmin(fmax(last + 2, 0.0), (double)(kBuckets - 1));
@@ -356,11 +362,14 @@ __device__ void choose_buckets(const RowSetting& r, RowShared& s, double before,
     }
   }
   __syncthreads();
-  const double lo = fmin(klo, fmin(s.plo, s.mlo)), hi = fmin(khi, fmin(s.phi, s.mhi));
-  const double ulo = r.u * lo * (1 - kSlack), uhi = r.u * hi * (1 + kSlack);
+  const double klo = fmin(s.klo, s.total), khi = fmin(s.khi, s.total);
+  if (r.top_p < 1.0) {
+    const double lo = r.top_p * klo * (1 - kSlack), hi = r.top_p * khi * (1 + kSlack);
+    if (in && before < lo && upto >= lo) s.p0 = o, s.plo = before;
+    if (in && before <= hi && upto > hi) s.p1 = o, s.phi = upto;
+  }
   __syncthreads();
-  if (o == 0) s.u1 = kBuckets - 1;
-  __syncthreads();
+  const double ulo = r.u * fmin(klo, fmin(s.plo, s.mlo)) * (1 - kSlack), uhi = r.u * fmin(khi, fmin(s.phi, s.mhi)) * (1 + kSlack);
   if (in && before <= ulo && upto > ulo) s.u0 = o;
   if (in && before <= uhi && upto > uhi) s.u1 = o;
   __syncthreads();
@@ -368,25 +377,141 @@ __device__ void choose_buckets(const RowSetting& r, RowShared& s, double before,
   const bool least = s.mlo >= fmin(khi, s.phi), other = s.mhi <= fmin(klo, s.plo);
   const bool flag = in && ((!other && (o == s.k || (o >= s.p0 && o <= s.p1))) || (!least && o >= s.m0 && o <= s.m1) || (o >= s.u0 && o <= s.u1));
   const unsigned long long b = __ballot(flag);
-  if (in && (o & 63) == 0) s.flags[o >> 5] = (uint32_t)b, s.flags[(o >> 5) + 1] = (uint32_t)(b >> 32);
+  if (in && (o & 63) == 0) s.flags[o >> 6] = b;
   __syncthreads();
 }
+__device__ __forceinline__ bool flagged(const RowShared& s, int b) { return s.flags[b >> 6] >> (b & 63) & 1; }
 
-// The list in order: bitonic, in LDS.
-__device__ void sort_list(RowShared& s, int n) {
-  int size = 1;
+// The list in order, bitonic: a wave sorts and merges 64 neighbours in registers, what is further apart meets in LDS.
+__device__ __forceinline__ unsigned long long exchange(unsigned long long v, int x, int j, int k) {
+  const unsigned long long u = __shfl_xor(v, j);
+  return ((x & j) == 0) == ((x & k) == 0) ? (u < v ? u : v) : (u < v ? v : u);
+}
+template <int THREADS>
+__device__ __forceinline__ void sort_list(RowShared& s, int n) {
+  const int tid = threadIdx.x;
+  if (THREADS == 64) {                          // so few that each counts those in front of it
+    const unsigned long long v = tid < n ? s.list[tid] : ~0ull;
+    int place = 0;
+    for (int j = 0; j < n; ++j) place += __shfl(v, j) < v;
+    meet<64>();
+    if (v != ~0ull) s.list[place] = v;         // (those left out are alike)
+    meet<64>();
+    return;
+  }
+  int size = 64;
   while (size < n) size <<= 1;
-  for (int i = n + threadIdx.x; i < size; i += kPickThreads) s.list[i] = ~0ull;
-  __syncthreads();
-  for (int k = 2; k <= size; k <<= 1)
-    for (int j = k >> 1; j > 0; j >>= 1) {
-      for (int i = threadIdx.x; i < size / 2; i += kPickThreads) {
+  for (int x = tid; x < size; x += THREADS) {
+    unsigned long long v = x < n ? s.list[x] : ~0ull;
+#pragma unroll
+    for (int k = 2; k <= 64; k <<= 1)
+#pragma unroll
+      for (int j = k >> 1; j > 0; j >>= 1) v = exchange(v, x, j, k);
+    s.list[x] = v;
+  }
+  for (int k = 128; k <= size; k <<= 1) {
+    for (int j = k >> 1; j >= 64; j >>= 1) {
+      meet<THREADS>();
+      for (int i = tid; i < size / 2; i += THREADS) {
         const int x = ((i & ~(j - 1)) << 1) | (i & (j - 1)), y = x | j;
         const unsigned long long p = s.list[x], q = s.list[y];
         if ((p > q) == ((x & k) == 0)) s.list[x] = q, s.list[y] = p;
       }
-      __syncthreads();
     }
+    meet<THREADS>();
+    for (int x = tid; x < size; x += THREADS) {
+      unsigned long long v = s.list[x];
+#pragma unroll
+      for (int j = 32; j > 0; j >>= 1) v = exchange(v, x, j, k);
+      s.list[x] = v;
+    }
+  }
+  meet<THREADS>();
+}
+
+// The bounds and the draw on the list, `taken` entries of which n count, by THREADS threads with up to PER tokens each.
+template <int THREADS, int PER, class Bucket>
+__device__ __forceinline__ void pick(const SampleArgs& a, int64_t t, const RowSetting& r, RowShared& s, int taken, int n, const Bucket& bucket_of) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  sort_list<THREADS>(s, taken);
+  // each thread has a run of the list
+  const int per = (n + THREADS - 1) / THREADS, x0 = min(tid * per, n), x1 = min(x0 + per, n);
+  double w[PER], sum = 0;
+  int bucket[PER];
+#pragma unroll
+  for (int q = 0; q < PER; ++q) {
+    if (x0 + q < x1) {
+      const uint32_t k = ~(uint32_t)(s.list[x0 + q] >> 32);
+      w[q] = weight(r, k);
+      bucket[q] = bucket_of(key_value(k));
+      sum += w[q];
+    }
+  }
+  double run = sum;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const double u = __shfl_up(run, o);
+    if (lane >= o) run += u;
+  }
+  if (THREADS > 64) {
+    if (lane == 63) s.sums[wave] = run;
+    __syncthreads();
+  }
+  run -= sum;
+  if (THREADS > 64)
+    for (int v = 0; v < wave; ++v) run += s.sums[v];
+  double at[PER];                               // mass of the list in front of a token
+#pragma unroll
+  for (int q = 0; q < PER; ++q) {
+    if (x0 + q < x1) {
+      at[q] = run;
+      run += w[q];
+      const int x = x0 + q, prev = x > 0 ? bucket_of(key_value(~(uint32_t)(s.list[x - 1] >> 32))) : -1;
+      if (prev != bucket[q]) s.seg_mass[bucket[q]] = at[q], s.seg_at[bucket[q]] = x;
+    }
+  }
+  meet<THREADS>();
+#pragma unroll
+  for (int q = 0; q < PER; ++q)
+    if (x0 + q < x1) at[q] = s.before[bucket[q]] + (at[q] - s.seg_mass[bucket[q]]);
+  const auto rank = [&](int q) { return s.count_before[bucket[q]] + (uint32_t)(x0 + q) - s.seg_at[bucket[q]]; };
+  // what is kept is a first part of the order, and so is what each bound leaves: the least of their masses
+  double kept = s.total;
+  const bool least = s.mlo >= fmin(s.khi, fmin(s.phi, s.total)), other = s.mhi <= fmin(s.klo, fmin(s.plo, s.total));
+  // (of a thread's tokens the last one that a bound leaves; `m` is none of them)
+  const auto bound = [&](double m, auto holds) {
+    bool some = false;
+    double v = m;
+#pragma unroll
+    for (int q = 0; q < PER; ++q)
+      if (x0 + q < x1 && holds(q)) some = true, v = fmax(v, at[q] + w[q]);
+    return end_of<THREADS, false>(some, v, m, s.sums);
+  };
+  if (s.k >= 0 && !other) kept = bound(s.klo, [&](int q) { return bucket[q] == s.k && rank(q) < r.top_k; });
+  if (r.top_p < 1.0 && !other) {
+    const double mass = r.top_p * kept;
+    kept = bound(s.plo, [&](int q) { return bucket[q] >= s.p0 && bucket[q] <= s.p1 && (at[q] < mass || rank(q) == 0); });
+  }
+  if (s.m1 >= 0 && !least)
+    kept = fmin(kept, bound(s.mlo, [&](int q) { return bucket[q] >= s.m0 && bucket[q] <= s.m1 && (w[q] >= r.min_p || rank(q) == 0); }));
+  const double drawn = r.u * kept;
+  // the first that goes beyond it (or the last there is, if only the sums' rounding keeps that from it)
+  constexpr double kNone = 1e9;
+  double first = kNone, last = -1;
+#pragma unroll
+  for (int q = 0; q < PER; ++q)
+    if (x0 + q < x1 && bucket[q] >= s.u0 && bucket[q] <= s.u1) {
+      last = x0 + q;
+      if (at[q] + w[q] > drawn) first = fmin(first, x0 + q);
+    }
+  first = end_of<THREADS, true>(first < kNone, first, kNone, s.sums);
+  if (first == kNone) first = end_of<THREADS, false>(last >= 0, last, 0.0, s.sums);
+  const int x = (int)first;
+  if (x >= x0 && x < x1) {
+    const unsigned long long it = s.list[x];
+    a.tokens[t] = (int)(uint32_t)it;
+    if (a.probs) a.probs[t] = (float)(weight(r, ~(uint32_t)(it >> 32)) / kept);
+  }
 }
 
 template <int DT>
@@ -405,7 +530,11 @@ __global__ __launch_bounds__(kPickThreads) void sample_rows_kernel(SampleArgs a,
     if (u > top) top = u;
   }
   if (lane == 0) s.tops[wave] = top;
-  if (tid == 0) s.n = 0;
+  if (tid == 0) {
+    s.n = s.parts = s.dropped = s.runs = 0;
+    s.k = -1, s.p0 = s.m0 = s.u0 = 0, s.m1 = -1, s.u1 = kBuckets - 1;
+    s.klo = s.khi = s.phi = s.mlo = s.mhi = INFINITY;
+  }
   __syncthreads();
   for (int w = 0; w < kPickThreads / 64; ++w)
     if (s.tops[w] > top) top = s.tops[w];
@@ -424,27 +553,39 @@ __global__ __launch_bounds__(kPickThreads) void sample_rows_kernel(SampleArgs a,
 
   const auto bucket_of = [&](float x) { return x == largest ? 0 : 1 + (int)fmin(base - floor(degrees(r, x)), (double)kBuckets); };
 
-  // a thread's bucket, of all parts
+  for (int c = tid; c < parts; c += kPickThreads) {
+    const PartHead h = heads[t * parts + c];
+    const float its = key_value((uint32_t)(h.top >> 32));
+    const bool none = its == -__builtin_inff() || (infinite && its != largest);
+    const int b = none ? kBuckets : min(bucket_of(its), kBuckets);
+    const double d = degrees(r, its);
+    s.part_top[c] = b, s.part_equal[c] = (uint32_t)h.equal;
+    s.part_extra[c] = b == 0 || none ? 0 : (uint32_t)h.equal * (unsigned long long)(sixteenth(d - floor(d)) * (double)(1ull << kFracBits) + 0.5);
+  }
+  __syncthreads();
+
+  // a thread's bucket, of all parts (a part's begin with that of its largest, of the row's with bucket 1)
   uint32_t count = 0;
   unsigned long long extra = 0;
-  if (tid < kBuckets)
-    for (int c = 0; c < parts; ++c) {
-      const float its = key_value((uint32_t)(heads[t * parts + c].top >> 32));
-      if (its == -__builtin_inff() || (infinite && its != largest)) continue;
-      const int top_bucket = bucket_of(its);
-      if (tid == top_bucket) {
-        const uint32_t equal = (uint32_t)heads[t * parts + c].equal;
-        count += equal;
-        const double d = degrees(r, its);
-        if (tid) extra += equal * (unsigned long long)(sixteenth(d - floor(d)) * (double)(1ull << kFracBits) + 0.5);
+  if (tid < kBuckets) {
+    constexpr int U = 8;
+    const unsigned long long* row = hists + t * parts * kBuckets;
+    for (int c0 = 0; c0 < parts; c0 += U) {
+      unsigned long long h[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int c = c0 + u, shift = c < parts && !infinite ? max(s.part_top[c], 1) : kBuckets;
+        h[u] = tid >= shift ? row[(int64_t)c * kBuckets + tid - shift] : 0;
       }
-      // (its buckets begin with that of its largest, of the row's with bucket 1)
-      const int shift = max(top_bucket, 1);
-      if (infinite || tid < shift) continue;
-      const unsigned long long h = hists[(t * parts + c) * kBuckets + tid - shift];
-      count += (uint32_t)(h >> kCountBit);
-      extra += h & ((1ull << kCountBit) - 1);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int c = c0 + u;
+        count += (uint32_t)(h[u] >> kCountBit);
+        extra += h[u] & ((1ull << kCountBit) - 1);
+        if (c < parts && tid == s.part_top[c]) count += s.part_equal[c], extra += s.part_extra[c];
+      }
     }
+  }
   const double mass = tid == 0 ? (double)count
                                : ((double)count + (double)extra * (1.0 / (double)(1ull << kFracBits))) * exp2(-(tid - 1 + frac) / kPerOctave);
   uint32_t count_to = count;
@@ -468,130 +609,104 @@ __global__ __launch_bounds__(kPickThreads) void sample_rows_kernel(SampleArgs a,
   const double before = lane ? wave_before + inside : wave_before;
   upto += wave_before, count_to += waves_count;
   if (tid < kBuckets) s.before[tid] = before, s.count_before[tid] = count_to - count;
-  if (tid == 0) s.total = total;
+  if (tid == 0) s.total = total, s.p1 = r.top_p < 1.0 ? kBuckets - 1 : -1, s.plo = r.top_p < 1.0 ? 0.0 : INFINITY;
   __syncthreads();
   choose_buckets(r, s, before, upto, count_to - count, count_to, frac);
 
-  // tokens of those buckets
+  // parts that have tokens of those buckets
   for (int c = wave; c < parts; c += kPickThreads / 64) {
-    const float its = key_value((uint32_t)(heads[t * parts + c].top >> 32));
-    if (its == -__builtin_inff() || (infinite && its != largest)) continue;
-    const int top_bucket = bucket_of(its), shift = max(top_bucket, 1);
-    bool some = top_bucket < kBuckets && (s.flags[top_bucket >> 5] >> (top_bucket & 31) & 1);
-    for (int o = shift + lane; o < kBuckets && !infinite; o += 64)
-      if ((s.flags[o >> 5] >> (o & 31) & 1) && hists[(t * parts + c) * kBuckets + o - shift]) some = true;
-    if (!__any(some)) continue;
-    const int i0 = c * part_size, i1 = min(i0 + part_size, a.vocab);
-    for (int i = i0 + lane * 8; i < i1; i += 512) {
-      Raw8<DT> raw;
-      float x[8];
-      load_raw8<DT>(a.logits, t * a.ld + i, i1 - i, raw);
-      to_float8<DT>(raw, x);
+    const int top_bucket = s.part_top[c], shift = max(top_bucket, 1);
+    if (top_bucket >= kBuckets) continue;
+    bool some = flagged(s, top_bucket);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        if (i + e >= i1 || !(x[e] > -__builtin_inff())) continue;
-        if (infinite && x[e] != largest) continue;
-        const int b = bucket_of(x[e]);
-        if (b >= kBuckets || !(s.flags[b >> 5] >> (b & 31) & 1)) continue;
-        const uint32_t n = atomicAdd(&s.n, 1u);
-        if (n < kList) s.list[n] = (unsigned long long)~order_key(x[e]) << 32 | (uint32_t)(i + e);
+    for (int o = lane; o < kBuckets; o += 64)
+      if (flagged(s, o) && o >= shift && !infinite && hists[(t * parts + c) * kBuckets + o - shift]) some = true;
+    if (__any(some) && lane == 0) s.part_list[atomicAdd(&s.parts, 1u)] = c;
+  }
+  __syncthreads();
+  // Runs of such buckets as bounds of the logits, with room for rounding: tokens are taken by these, and those that are of other
+  // buckets after all left out afterwards.
+  if (tid < kBuckets && flagged(s, tid)) {
+    const bool from = tid == 0 || !flagged(s, tid - 1), to = tid == kBuckets - 1 || !flagged(s, tid + 1);
+    uint32_t run = 0;
+    for (int b = 0; b < kBuckets / 64; ++b) {            // runs that begin in front of this one, or with it
+      const unsigned long long f = s.flags[b], starts = f & ~(f << 1 | (b ? s.flags[b - 1] >> 63 : 0));
+      if (b * 64 <= tid) run += __popcll(tid - b * 64 >= 63 ? starts : starts & ((2ull << (tid - b * 64)) - 1));
+    }
+    const bool bounded = r.grid > 0 && !infinite;
+    if (run <= kRuns) {
+      if (from) {
+        const double x = (base - tid + 2) / r.grid;
+        s.upper[run - 1] = bounded && tid ? (float)(x + fabs(x) * 1e-6 + 1e-37) : INFINITY;
       }
+      if (to) {
+        const double x = (base - max(tid, 1) + 1) / r.grid;
+        s.lower[run - 1] = bounded ? (float)(x - fabs(x) * 1e-6 - 1e-37) : -3.4028234e38f;
+      }
+    }
+    if (to) atomicMax(&s.runs, run);
+  }
+  __syncthreads();
+  const int runs = (int)s.runs;                  // (never more than kRuns: those of top_k, top_p, min_p and the draw)
+  const float lo0 = s.lower[0], hi0 = s.upper[0], lo1 = runs > 1 ? s.lower[1] : INFINITY, hi1 = runs > 1 ? s.upper[1] : -INFINITY;
+  const int per_part = part_size / 512, pieces = (int)s.parts * per_part;
+  constexpr int U = DT == MDBF_F32 ? 2 : 4;
+  for (int p0 = wave; p0 < pieces; p0 += U * (kPickThreads / 64)) {
+    Raw8<DT> raw[U];
+    int at[U], there[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int p = p0 + u * (kPickThreads / 64);
+      at[u] = there[u] = 0;
+      if (p < pieces) {
+        at[u] = (int)s.part_list[p / per_part] * part_size + (p % per_part) * 512 + lane * 8;
+        there[u] = a.vocab - at[u];
+        if (there[u] > 0) load_raw8<DT>(a.logits, t * a.ld + at[u], there[u], raw[u]);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float x[8];
+      to_float8<DT>(raw[u], x);
+      uint32_t mask = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) mask |= (uint32_t)((x[e] >= lo0 && x[e] <= hi0) || (x[e] >= lo1 && x[e] <= hi1)) << e;
+      for (int q = 2; q < runs; ++q) {
+        const float lo = s.lower[q], hi = s.upper[q];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) mask |= (uint32_t)(x[e] >= lo && x[e] <= hi) << e;
+      }
+      mask &= there[u] >= 8 ? 255u : there[u] > 0 ? (1u << there[u]) - 1 : 0u;
+      if (!mask) continue;
+      uint32_t n = atomicAdd(&s.n, (uint32_t)__popc(mask));
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (mask >> e & 1) {
+          if (n < kList) s.list[n] = (unsigned long long)~order_key(x[e]) << 32 | (uint32_t)(at[u] + e);
+          ++n;
+        }
     }
   }
   __syncthreads();
-  const int n = (int)s.n;
-  if (n > kList || n == 0) {
+  const int taken = (int)s.n;
+  for (int x = tid; x < min(taken, kList); x += kPickThreads) {
+    const float v = key_value(~(uint32_t)(s.list[x] >> 32));
+    const int b = infinite && v != largest ? kBuckets : bucket_of(v);
+    if (b >= kBuckets || !flagged(s, b)) s.list[x] = ~0ull, atomicAdd(&s.dropped, 1u);   // (goes to the end)
+  }
+  __syncthreads();
+  const int n = taken - (int)s.dropped;
+  if (taken > kList || n == 0) {
     __syncthreads();
     sample_digits<DT>(a, t, r, *(PickShared*)shared);
     return;
   }
-  sort_list(s, n);
-
-  // each thread has a run of the list
-  const int per = (n + kPickThreads - 1) / kPickThreads, x0 = min(tid * per, n), x1 = min(x0 + per, n);
-  constexpr int kPer = kList / kPickThreads;
-  double w[kPer], sum = 0;
-  int bucket[kPer];
-#pragma unroll
-  for (int q = 0; q < kPer; ++q) {
-    if (x0 + q < x1) {
-      const uint32_t k = ~(uint32_t)(s.list[x0 + q] >> 32);
-      w[q] = weight(r, k);
-      bucket[q] = bucket_of(key_value(k));
-      sum += w[q];
-    }
-  }
-  double run = sum;
-  for (int o = 1; o < 64; o <<= 1) {
-    const double u = __shfl_up(run, o);
-    if (lane >= o) run += u;
-  }
-  __syncthreads();
-  if (lane == 63) s.sums[wave] = run;
-  __syncthreads();
-  run -= sum;
-  for (int v = 0; v < wave; ++v) run += s.sums[v];
-  double at[kPer];                              // mass of the list in front of a token
-#pragma unroll
-  for (int q = 0; q < kPer; ++q) {
-    if (x0 + q < x1) {
-      at[q] = run;
-      run += w[q];
-      const int x = x0 + q;
-      int prev = -1;
-      if (x > 0) {
-        const uint32_t k = ~(uint32_t)(s.list[x - 1] >> 32);
-        prev = bucket_of(key_value(k));
-      }
-      if (prev != bucket[q]) s.seg_mass[bucket[q]] = at[q], s.seg_at[bucket[q]] = x;
-    }
-  }
-  __syncthreads();
-#pragma unroll
-  for (int q = 0; q < kPer; ++q)
-    if (x0 + q < x1) at[q] = s.before[bucket[q]] + (at[q] - s.seg_mass[bucket[q]]);
-  const auto rank = [&](int q) { return s.count_before[bucket[q]] + (uint32_t)(x0 + q) - s.seg_at[bucket[q]]; };
-  const auto largest_of = [](double p, double q) { return fmax(p, q); };
-
-  double kept = s.total;
-  const bool least = s.mlo >= fmin(s.khi, s.phi), other = s.mhi <= fmin(s.klo, s.plo);
-  if (s.k >= 0 && !other) {
-    double m = s.klo;
-#pragma unroll
-    for (int q = 0; q < kPer; ++q)
-      if (x0 + q < x1 && bucket[q] == s.k && rank(q) < r.top_k) m = fmax(m, at[q] + w[q]);
-    kept = block_fold(m, s.sums, largest_of);
-  }
-  if (r.top_p < 1.0 && !other) {
-    const double mass = r.top_p * kept;
-    double m = s.plo;
-#pragma unroll
-    for (int q = 0; q < kPer; ++q)
-      if (x0 + q < x1 && bucket[q] >= s.p0 && bucket[q] <= s.p1 && (at[q] < mass || rank(q) == 0)) m = fmax(m, at[q] + w[q]);
-    kept = block_fold(m, s.sums, largest_of);
-  }
-  if (s.m1 >= 0 && !least) {
-    double m = s.mlo;
-#pragma unroll
-    for (int q = 0; q < kPer; ++q)
-      if (x0 + q < x1 && bucket[q] >= s.m0 && bucket[q] <= s.m1 && (w[q] >= r.min_p || rank(q) == 0)) m = fmax(m, at[q] + w[q]);
-    kept = fmin(kept, block_fold(m, s.sums, largest_of));
-  }
-  const double drawn = r.u * kept;
-  double first = 1e9, last = -1;
-#pragma unroll
-  for (int q = 0; q < kPer; ++q)
-    if (x0 + q < x1 && bucket[q] >= s.u0 && bucket[q] <= s.u1) {
-      if (at[q] + w[q] > drawn) first = fmin(first, (double)(x0 + q));
-      else last = fmax(last, (double)(x0 + q));
-    }
-  first = block_fold(first, s.sums, [](double p, double q) { return fmin(p, q); });
-  last = block_fold(last, s.sums, largest_of);
-  const int x = (int)(first < 1e9 ? first : last);   // (none goes beyond only by the sums' rounding: the last one then)
-  if (x >= x0 && x < x1) {
-    const unsigned long long it = s.list[x];
-    a.tokens[t] = (int)(uint32_t)it;
-    if (a.probs) a.probs[t] = (float)(weight(r, ~(uint32_t)(it >> 32)) / kept);
+  if (taken <= 64) {
+    if (wave == 0) pick<64, 1>(a, t, r, s, taken, n, bucket_of);
+  } else if (taken <= kPickThreads) {
+    pick<kPickThreads, 1>(a, t, r, s, taken, n, bucket_of);
+  } else {
+    pick<kPickThreads, kList / kPickThreads>(a, t, r, s, taken, n, bucket_of);
   }
 }
 
