@@ -194,64 +194,86 @@ __device__ __forceinline__ bool tile_of(const int32_t* tiles, int64_t t, int ada
   return true;
 }
 
-// V[split][place][rank] = sum over the split's channels of A[rank][c] X[row][c].  A wave has 16 rows; where a tile has fewer than 64 the other
-// waves take parts of the channels, and their sums meet in LDS.
+// V[split][place][rank] = sum over the split's channels of A[rank][c] X[row][c], 128 channels at a time.  A product's operand has a row per lane, and
+// sixteen rows are sixteen cache lines: so rows are loaded side by side, 256 bytes of each, and go through LDS (two buffers; the
+// sixteen pieces of a row lie exclusive-or its number, so that neither writes nor reads of sixteen lanes meet on a bank).  A wave has 16 rows
+// of X; where a tile has fewer than 64 the other waves take some of the four products along the channels, and their sums meet in
+// LDS.  6458 rows of 4096 channels, three projections of rank 16 (55 MB): 13.8 us, 32 with operands loaded as the products want them.
+constexpr int kInChannels = 128;
 template <int DT, int NS>
-__device__ __forceinline__ void in_tile(const InArgs& a, const InGroup& g, int adapter, int first, int count, int split, Acc4 (*part)[NS][64]) {
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, kg = lane >> 4;
+__device__ __forceinline__ void in_tile(const InArgs& a, const InGroup& g, int adapter, int first, int count, int split, U32x4 (*lds)[(4 + kInSlots) * 256]) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, kg = lane >> 4;
   const int subs = count <= 16 ? 1 : count <= 32 ? 2 : 4, sub = wave & (subs - 1), piece = wave / subs, pieces = 4 / subs;
-  const int steps = (g.n + 31) / 32, all = a.splits * pieces, at = split * pieces + piece;
-  const int s0 = (int)((int64_t)steps * at / all), s1 = (int)((int64_t)steps * (at + 1) / all);
+  const int stages = (g.n + kInChannels - 1) / kInChannels;
+  const int s0 = (int)((int64_t)stages * split / a.splits), s1 = (int)((int64_t)stages * (split + 1) / a.splits);
 
-  const int place = first + min(sub * 16 + i, count - 1);
-  const int row = cut(a.rows[place], a.T - 1);          // (a row that is none is left out at the end)
-  const int64_t x0 = (int64_t)row * g.ldx;
-  int64_t a0[NS];
+  // loading: a sixteenth of the threads per row, rows 16 apart
+  const int lr = tid >> 4, lc = tid & 15, slot = lr * 16 + (lc ^ lr);
+  int64_t x0[4], a0[NS];
   const void* A[NS];
 #pragma unroll
-  for (int s = 0; s < NS; ++s) {
-    const int p = g.proj[s], r = a.r[p];
-    A[s] = a.A[p];
-    a0[s] = ((int64_t)adapter * r + min(g.tile[s] * 16 + i, r - 1)) * g.n;
+  for (int q = 0; q < 4; ++q) {
+    const int row = q < subs ? cut(a.rows[first + min(q * 16 + lr, count - 1)], a.T - 1) : 0;    // (a row that is none is left out at the end)
+    x0[q] = (int64_t)row * g.ldx + lc * 8;
   }
+#pragma unroll
+  for (int q = 0; q < NS; ++q) {
+    const int p = g.proj[q], r = a.r[p];
+    A[q] = a.A[p];
+    a0[q] = ((int64_t)adapter * r + min(g.tile[q] * 16 + lr, r - 1)) * g.n + lc * 8;
+  }
+  Raw8<DT> rx[4], ra[NS];
+  const auto load = [&](int s) {
+    const int c = s * kInChannels, there = g.n - c - lc * 8;
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (q < subs) load_raw8<DT>(g.X, x0[q] + c, there, rx[q]);
+#pragma unroll
+    for (int q = 0; q < NS; ++q) load_raw8<DT>(A[q], a0[q] + c, there, ra[q]);
+  };
+  const auto store = [&](int b) {
+#pragma unroll
+    for (int q = 0; q < NS; ++q) lds[b][q * 256 + slot] = ra[q].w[0];
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (q < subs) lds[b][(NS + q) * 256 + slot] = rx[q].w[0];
+  };
   Acc4 acc[NS] = {};
-  const int full = min(s1, g.n / 32);
-  int s = s0;
-  constexpr int U = 4;
-  for (; s + U <= full; s += U) {
-    Raw8<DT> x[U], w[U][NS];
+  const auto products = [&](int b, int u) {
+    const int at = i * 16 + ((u * 4 + kg) ^ i);
+    const U32x4 x = lds[b][(NS + sub) * 256 + at];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int c = (s + u) * 32 + kg * 8;
-      load_raw8<DT>(g.X, x0 + c, 8, x[u]);
+    for (int q = 0; q < NS; ++q) acc[q] = product<DT>(x, lds[b][q * 256 + at], acc[q]);
+  };
+  if (s0 < s1) load(s0), store(0);
+  if (s0 + 1 < s1) load(s0 + 1);
+  __syncthreads();
+  for (int s = s0; s < s1; ++s) {
+    const int b = (s - s0) & 1;
+    if (subs == 4) {
 #pragma unroll
-      for (int q = 0; q < NS; ++q) load_raw8<DT>(A[q], a0[q] + c, 8, w[u][q]);
+      for (int u = 0; u < 4; ++u) products(b, u);
+    } else if (subs == 2) {
+      products(b, piece * 2);
+      products(b, piece * 2 + 1);
+    } else {
+      products(b, piece);
     }
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int q = 0; q < NS; ++q) acc[q] = product<DT>(x[u].w[0], w[u][q].w[0], acc[q]);
-  }
-  for (; s < s1; ++s) {
-    const int c = s * 32 + kg * 8;
-    Raw8<DT> x, w;
-    load_raw8<DT>(g.X, x0 + c, g.n - c, x);
-#pragma unroll
-    for (int q = 0; q < NS; ++q) {
-      load_raw8<DT>(A[q], a0[q] + c, g.n - c, w);
-      acc[q] = product<DT>(x.w[0], w.w[0], acc[q]);
-    }
+    if (s + 1 < s1) store(b ^ 1);
+    if (s + 2 < s1) load(s + 2);
+    __syncthreads();
   }
   if (pieces > 1) {
+    Acc4* part = (Acc4*)lds;
     if (piece) {
 #pragma unroll
-      for (int q = 0; q < NS; ++q) part[wave - subs][q][lane] = acc[q];
+      for (int q = 0; q < NS; ++q) part[((wave - subs) * NS + q) * 64 + lane] = acc[q];
     }
     __syncthreads();
     if (piece) return;
     for (int w = sub; w < 4 - subs; w += subs)
 #pragma unroll
-      for (int q = 0; q < NS; ++q) acc[q] += part[w][q][lane];
+      for (int q = 0; q < NS; ++q) acc[q] += part[(w * NS + q) * 64 + lane];
   }
   // lane: rank i of the tile, rows 4 kg ..
 #pragma unroll
@@ -266,76 +288,110 @@ __device__ __forceinline__ void in_tile(const InArgs& a, const InGroup& g, int a
 
 template <int DT>
 __global__ __launch_bounds__(256) void adapter_in_kernel(InArgs a) {
-  __shared__ Acc4 part[3][kInSlots][64];
+  __shared__ U32x4 lds[2][(4 + kInSlots) * 256];
   int adapter, first, count;
   if (!tile_of(a.tiles, blockIdx.x, a.adapters, a.T, adapter, first, count)) return;
   const InGroup& g = a.g[blockIdx.z];
-  if (g.slots == 1) in_tile<DT, 1>(a, g, adapter, first, count, blockIdx.y, (Acc4(*)[1][64])part);
-  else if (g.slots == 2) in_tile<DT, 2>(a, g, adapter, first, count, blockIdx.y, (Acc4(*)[2][64])part);
-  else if (g.slots == 3) in_tile<DT, 3>(a, g, adapter, first, count, blockIdx.y, (Acc4(*)[3][64])part);
-  else in_tile<DT, 4>(a, g, adapter, first, count, blockIdx.y, part);
+  if (g.slots == 1) in_tile<DT, 1>(a, g, adapter, first, count, blockIdx.y, lds);
+  else if (g.slots == 2) in_tile<DT, 2>(a, g, adapter, first, count, blockIdx.y, lds);
+  else if (g.slots == 3) in_tile<DT, 3>(a, g, adapter, first, count, blockIdx.y, lds);
+  else in_tile<DT, 4>(a, g, adapter, first, count, blockIdx.y, lds);
 }
 
-// Y[row][c] += scale sum over ranks of V[row][rank] B[c][rank].  V, a sum of the splits', is written as NL numbers of 16 bits that add up to it, one after
-// the other along the contraction in pieces of eight ranks, so that a rank of 16 with two of them is one product deep.  fp16 has not fp32's
-// exponents: there a row is brought to a largest of 1 first.  The columns of the products' tiles are laid out so that a lane ends with 16
-// neighbouring columns of one row.
-template <int DT, int YD, int NL>
-__global__ __launch_bounds__(256) void adapter_out_kernel(OutArgs a) {
-  extern __shared__ U32x4 limbs[];             // [sub][step][lane]
-  __shared__ uint32_t top[MDBF_ADAPTER_TILE];
-  __shared__ int32_t rows[MDBF_ADAPTER_TILE];
-  const OutProj& p = a.p[blockIdx.z];
-  int adapter, first, count;
-  if (p.yd != YD || (int64_t)blockIdx.y * p.chunk >= p.m) return;
-  if (!tile_of(a.tiles, blockIdx.x, a.adapters, a.T, adapter, first, count)) return;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, kg = lane >> 4;
-  const int eights = (p.r + 7) / 8, pieces = eights * NL, steps = (pieces + 3) / 4, subs = (count + 15) / 16;
+// How the numbers of 16 bits of V lie along the contraction: pieces of eight ranks, four to a product.  Up to two of them (rank 16) all numbers
+// of a rank follow each other, so that two of them fill one product; beyond, a product has one number of four pieces, and one operand of
+// B serves all of a rank's numbers.
+struct Pieces {
+  int eights, b_steps, limbs;                  // operands of B, and products per operand
+  bool packed;
+};
+template <int NL>
+__host__ __device__ inline Pieces pieces_of(int r) {
+  const int eights = (r + 7) / 8;
+  if (eights <= 2) return {eights, (eights * NL + 3) / 4, 1, true};
+  return {eights, (eights + 3) / 4, NL, false};
+}
 
-  if (tid < MDBF_ADAPTER_TILE) {
-    const int row = tid < count ? a.rows[first + tid] : -1;
-    rows[tid] = row < a.T ? row : -1;
-    top[tid] = 0;
-  }
-  // (V's columns behind a rank are zeros up to a multiple of 16)
-  const auto sum8 = [&](int t, int j, float (&v)[8]) {
+// Y[row][c] += scale sum over ranks of V[row][rank] B[c][rank].  V, a sum of the splits', is written as NL numbers of 16 bits that add up to it;
+// fp16 has not fp32's exponents: there a row is brought to a largest of 1 first.  The columns of the products' tiles are laid out so that a lane
+// ends with 16 neighbouring columns of one row.  A wave takes 64 columns and SUBS times 16 rows at a time (more would take the registers that
+// other waves need); what it needs of B and Y for the first ones is on its way while V is made.
+template <int DT, int YD, int NL, int SUBS>
+__device__ __forceinline__ void out_tile(const OutArgs& a, const OutProj& p, int adapter, int first, int count, U32x4* limbs, const int32_t* rows,
+                                         int32_t* exponents) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, kg = lane >> 4;
+  const Pieces f = pieces_of<NL>(p.r);
+  const int c_end = (int)min((int64_t)p.m, ((int64_t)blockIdx.y + 1) * p.chunk);
+
+  const auto load_b = [&](int cb, int s, Raw8<DT>(&w)[4]) {
+    const int piece = s * 4 + kg, j8 = (f.packed ? piece % f.eights : piece) * 8;
+    const bool there = f.packed ? piece < f.eights * NL : piece < f.eights;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = 0.0f;
-    for (int s = 0; s < a.splits; ++s) {
-      const float* src = a.V + ((int64_t)s * a.T + first + t) * a.width + p.column + j * 8;
-      const F32x4 x = *(const MDBF_GLOBAL F32x4*)src, y = *((const MDBF_GLOBAL F32x4*)src + 1);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] += x[e], v[4 + e] += y[e];
+    for (int j = 0; j < 4; ++j) {
+      // product row i of tile j is the column cb + (i / 4) * 16 + j * 4 + i % 4
+      const int c = min(cb + (i >> 2) * 16 + j * 4 + (i & 3), p.m - 1);
+      w[j] = {};
+      if (there) load_raw8<DT>(p.B, ((int64_t)adapter * p.m + c) * p.r + j8, p.r - j8, w[j]);
     }
   };
-  if (DT == MDBF_F16) {
-    __syncthreads();
-    for (int w = tid; w < count * eights; w += 256) {
-      const int t = w / eights;
-      float v[8];
-      sum8(t, w - t * eights, v);
+  const auto load_y = [&](int cb, int sub0, Raw8<YD>(&y)[SUBS][2]) {
+    const int c = cb + kg * 16;
+#pragma unroll
+    for (int sub = 0; sub < SUBS; ++sub) {
+      const int row = rows[(sub0 + sub) * 16 + i];
+      if (row >= 0 && c < p.m) {
+        const int64_t at = (int64_t)row * p.ldy + c;
+        load_raw8<YD>(p.Y, at, p.m - c, y[sub][0]);
+        if (c + 8 < p.m) load_raw8<YD>(p.Y, at + 8, p.m - c - 8, y[sub][1]);
+      }
+    }
+  };
+  int cb = (int)blockIdx.y * p.chunk + wave * kOutBlock;
+  Raw8<DT> w[4];
+  Raw8<YD> y[SUBS][2];
+  if (cb < c_end) load_b(cb, 0, w), load_y(cb, 0, y);
+  const int subs = (count + 16 * SUBS - 1) / (16 * SUBS) * SUBS;
+
+  // a row's pieces of eight ranks lie in a power of two of neighbouring lanes (V's columns behind a rank are zeros up to a multiple of 16)
+  const int shift = f.eights > 1 ? 32 - __builtin_clz(f.eights - 1) : 0;
+  for (int cell = tid; cell < subs << (4 + shift); cell += 256) {
+    const int t = cell >> shift, j = cell & ((1 << shift) - 1);
+    const bool in = t < count && j < f.eights;
+    float v[8] = {};
+    if (in) {
+      const float* src = a.V + (int64_t)(first + t) * a.width + p.column + j * 8;
+      const int64_t apart = (int64_t)a.T * a.width;
+      constexpr int U = 4;
+      for (int s0 = 0; s0 < a.splits; s0 += U) {
+        F32x4 x[U][2];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (s0 + u < a.splits) {
+            const MDBF_GLOBAL F32x4* q = (const MDBF_GLOBAL F32x4*)(src + (s0 + u) * apart);
+            x[u][0] = q[0], x[u][1] = q[1];
+          }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (s0 + u < a.splits) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] += x[u][0][e], v[4 + e] += x[u][1][e];
+          }
+      }
+    }
+    if (DT == MDBF_F16) {
       uint32_t m = 0;
 #pragma unroll
       for (int e = 0; e < 8; ++e) m = max(m, __builtin_bit_cast(uint32_t, v[e]) & 0x7fffffffu);
-      atomicMax(&top[t], m);
-    }
-    __syncthreads();
-  }
-  // the power of two that brings a row's largest into [1, 2); rows that are not finite stay
-  const auto exponent = [&](int t) { const int e = (int)(top[t] >> 23); return e == 255 || e == 0 ? 0 : e - 127; };
-  const int cells = subs * 16 * eights;
-  for (int w = tid; w < cells; w += 256) {
-    const int t = w / eights, j = w - t * eights;
-    float v[8] = {};
-    if (t < count) sum8(t, j, v);
-    if (DT == MDBF_F16) {
-      const int e = t < count ? exponent(t) : 0;
+      for (int o = 1; o < 1 << shift; o <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o));
+      // the power of two that brings a row's largest into [1, 2); rows that are not finite stay
+      const int b = (int)(m >> 23), e2 = b == 255 || b == 0 ? 0 : b - 127;
+      if (j == 0) exponents[t] = e2;
 #pragma unroll
-      for (int q = 0; q < 8; ++q) v[q] = __builtin_ldexpf(v[q], -e);
+      for (int e = 0; e < 8; ++e) v[e] = __builtin_ldexpf(v[e], -e2);
     }
+    if (j >= f.eights) continue;
 #pragma unroll
     for (int l = 0; l < NL; ++l) {
-      const int piece = l * eights + j;
       U32x4 out;
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
@@ -343,8 +399,8 @@ __global__ __launch_bounds__(256) void adapter_out_kernel(OutArgs a) {
         out[q] = h;
         float lo, hi;
         if (DT == MDBF_F16) {
-          const F16x2 f = __builtin_bit_cast(F16x2, h);
-          lo = (float)f[0], hi = (float)f[1];
+          const F16x2 z = __builtin_bit_cast(F16x2, h);
+          lo = (float)z[0], hi = (float)z[1];
         } else {
           lo = __builtin_bit_cast(float, h << 16), hi = __builtin_bit_cast(float, h & 0xffff0000u);
         }
@@ -352,56 +408,79 @@ __global__ __launch_bounds__(256) void adapter_out_kernel(OutArgs a) {
         v[2 * q] = __builtin_isfinite(lo) ? v[2 * q] - lo : 0.0f;
         v[2 * q + 1] = __builtin_isfinite(hi) ? v[2 * q + 1] - hi : 0.0f;
       }
-      limbs[((t >> 4) * steps + (piece >> 2)) * 64 + (piece & 3) * 16 + (t & 15)] = out;
+      const int piece = f.packed ? l * f.eights + j : j, step = f.packed ? piece >> 2 : (piece >> 2) * NL + l;
+      limbs[((t >> 4) * f.b_steps * f.limbs + step) * 64 + (piece & 3) * 16 + (t & 15)] = out;
     }
   }
-  for (int w = tid; w < subs * 16 * (steps * 4 - pieces); w += 256) {        // pieces behind the last
-    const int gap = steps * 4 - pieces, t = w / gap, piece = pieces + w - t * gap;
-    limbs[((t >> 4) * steps + (piece >> 2)) * 64 + (piece & 3) * 16 + (t & 15)] = U32x4{0, 0, 0, 0};
-  }
+  // pieces behind the last
+  const int filled = f.packed ? f.eights * NL : f.eights;
+  for (int t = tid; t < subs * 16; t += 256)
+    for (int piece = filled; piece < f.b_steps * 4; ++piece)
+      for (int l = 0; l < f.limbs; ++l)
+        limbs[((t >> 4) * f.b_steps * f.limbs + (piece >> 2) * f.limbs + l) * 64 + (piece & 3) * 16 + (t & 15)] = U32x4{0, 0, 0, 0};
   __syncthreads();
 
   const float scale = p.scale ? p.scale[adapter] : 1.0f;
-  const int c_end = min((int64_t)p.m, ((int64_t)blockIdx.y + 1) * p.chunk);
-  for (int cb = (int)blockIdx.y * p.chunk + wave * kOutBlock; cb < c_end; cb += 4 * kOutBlock) {
-    // product row i of tile j is the column cb + (i / 4) * 16 + j * 4 + i % 4
-    int64_t b0[4];
+  for (int sub0 = 0; cb < c_end;) {
+    const int c = cb + kg * 16;
+    Acc4 acc[SUBS][4] = {};
+    for (int s = 0; s < f.b_steps; ++s) {
+      Raw8<DT> b[4];
+      const bool more = s + 1 < f.b_steps;
+      if (more) load_b(cb, s + 1, b);
+      for (int l = 0; l < f.limbs; ++l)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) b0[j] = ((int64_t)adapter * p.m + min(cb + (i >> 2) * 16 + j * 4 + (i & 3), p.m - 1)) * p.r;
-    for (int sub = 0; sub < subs; ++sub) {
-      const int t = sub * 16 + i, row = rows[t], c = cb + kg * 16;
-      const bool there = t < count && row >= 0 && c < p.m;
-      Raw8<YD> y[2];
-      const int64_t at = (int64_t)max(row, 0) * p.ldy + c;
-      if (there) {
-        load_raw8<YD>(p.Y, at, p.m - c, y[0]);
-        if (c + 8 < p.m) load_raw8<YD>(p.Y, at + 8, p.m - c - 8, y[1]);
-      }
-      Acc4 acc[4] = {};
-      for (int s = 0; s < steps; ++s) {
-        const int piece = s * 4 + kg, j8 = (piece % eights) * 8;
-        const U32x4 v = limbs[(sub * steps + s) * 64 + lane];
+        for (int sub = 0; sub < SUBS; ++sub) {
+          const U32x4 v = limbs[(((sub0 + sub) * f.b_steps + s) * f.limbs + l) * 64 + lane];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          Raw8<DT> w = {};
-          if (piece < pieces) load_raw8<DT>(p.B, b0[j] + j8, p.r - j8, w);
-          acc[j] = product<DT>(w.w[0], v, acc[j]);
+          for (int j = 0; j < 4; ++j) acc[sub][j] = product<DT>(w[j].w[0], v, acc[sub][j]);
         }
-      }
-      if (!there) continue;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (more) w[j] = b[j];
+    }
+#pragma unroll
+    for (int sub = 0; sub < SUBS; ++sub) {
+      const int t = (sub0 + sub) * 16 + i, row = rows[t];
+      if (row < 0) continue;
       float factor = scale;
-      if (DT == MDBF_F16) factor = __builtin_ldexpf(factor, exponent(t));
+      if (DT == MDBF_F16) factor = __builtin_ldexpf(factor, exponents[t]);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         if (c + 8 * h >= p.m) break;
         float out[8];
-        to_float8<YD>(y[h], out);
+        to_float8<YD>(y[sub][h], out);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) out[e] = fmaf(factor, acc[2 * h + e / 4][e % 4], out[e]);
-        store_float8<YD, false>(p.Y, at + 8 * h, p.m - c - 8 * h, out);
+        for (int e = 0; e < 8; ++e) out[e] = fmaf(factor, acc[sub][2 * h + e / 4][e % 4], out[e]);
+        store_float8<YD, false>(p.Y, (int64_t)row * p.ldy + c + 8 * h, p.m - c - 8 * h, out);
       }
     }
+    const bool same = sub0 + SUBS < subs;      // more rows of these columns
+    sub0 = same ? sub0 + SUBS : 0;
+    if (!same) cb += 4 * kOutBlock;
+    if (cb < c_end) {
+      if (!same || f.b_steps > 1) load_b(cb, 0, w);
+      load_y(cb, sub0, y);
+    }
   }
+}
+
+template <int DT, int YD, int NL>
+__global__ __launch_bounds__(256, YD == MDBF_F32 ? 2 : 3) void adapter_out_kernel(OutArgs a) {
+  extern __shared__ U32x4 limbs[];             // [sub][operand of B][number][lane]
+  __shared__ int32_t rows[MDBF_ADAPTER_TILE], exponents[MDBF_ADAPTER_TILE];
+  const OutProj& p = a.p[blockIdx.z];
+  int adapter, first, count;
+  if (p.yd != YD || (int64_t)blockIdx.y * p.chunk >= p.m) return;
+  if (!tile_of(a.tiles, blockIdx.x, a.adapters, a.T, adapter, first, count)) return;
+  if (threadIdx.x < MDBF_ADAPTER_TILE) {
+    const int row = (int)threadIdx.x < count ? a.rows[first + threadIdx.x] : -1;
+    rows[threadIdx.x] = row < a.T ? row : -1;
+  }
+  __syncthreads();
+  if (count <= 16) out_tile<DT, YD, NL, 1>(a, p, adapter, first, count, limbs, rows, exponents);
+  else if (count <= 32) out_tile<DT, YD, NL, 2>(a, p, adapter, first, count, limbs, rows, exponents);
+  else out_tile<DT, YD, NL, 4>(a, p, adapter, first, count, limbs, rows, exponents);
 }
 
 // How a call is cut.
@@ -418,7 +497,7 @@ static AdapterShape adapter_shape(int count, const mdbf_adapter_t* list, int T, 
     slots += (list[i].r + 15) / 16;
     n = list[i].n > n ? list[i].n : n;
   }
-  // enough workgroups to fill the device twice, eight at most: the second launch reads every split's sums once per chunk of columns
+  // enough workgroups to fill the device twice, of 256 channels at least: the second launch reads every split's sums once per chunk of columns
   const int64_t groups = (slots + kInSlots - 1) / kInSlots;
   const int64_t want = 512 / (tile_room * groups);
   const int most = n / 256 < 16 ? n / 256 : 16;
@@ -440,17 +519,21 @@ static int check_adapters(int count, const mdbf_adapter_t* list, int dtype, int 
   return tile_room > (1ll << 30) ? MDBF_EUNSUPPORTED : MDBF_OK;
 }
 
+template <int NL>
+static size_t limb_bytes(int r) {
+  const Pieces f = pieces_of<NL>(r);
+  return (size_t)(MDBF_ADAPTER_TILE / 16) * f.b_steps * f.limbs * 1024;
+}
+
 template <int DT, int YD>
-static int launch_out(const OutArgs& o, int count, int64_t tile_room, int chunks, int eights, hipStream_t s) {
+static int launch_out(const OutArgs& o, int count, int64_t tile_room, int chunks, int rank, hipStream_t s) {
   constexpr int NL = DT == MDBF_BF16 && YD == MDBF_F32 ? 3 : 2;
-  const size_t lds = (size_t)(MDBF_ADAPTER_TILE / 16) * ((eights * NL + 3) / 4) * 1024;
   static KernelSetup setup;
   const int e = kernel_setup(setup, [] {
-    return hipFuncSetAttribute((const void*)adapter_out_kernel<DT, YD, NL>, hipFuncAttributeMaxDynamicSharedMemorySize,
-                               MDBF_ADAPTER_TILE / 16 * (kMaxRank / 8 * NL / 4) * 1024);
+    return hipFuncSetAttribute((const void*)adapter_out_kernel<DT, YD, NL>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)limb_bytes<NL>(kMaxRank));
   });
   if (e) return e;
-  adapter_out_kernel<DT, YD, NL><<<dim3((unsigned)tile_room, chunks, count), 256, lds, s>>>(o);
+  adapter_out_kernel<DT, YD, NL><<<dim3((unsigned)tile_room, chunks, count), 256, limb_bytes<NL>(rank), s>>>(o);
   return (int)hipGetLastError();
 }
 
@@ -462,7 +545,9 @@ static int launch_adapters(int count, const mdbf_adapter_t* list, int adapters, 
   OutArgs out = {};
   in.rows = out.rows = rows, in.tiles = out.tiles = tiles, in.V = V, out.V = V;
   in.adapters = out.adapters = adapters, in.T = out.T = T, in.width = out.width = sh.width, in.splits = out.splits = sh.splits;
-  int groups = 0, column = 0, yds = 0, eights[3] = {}, chunks[3] = {};
+  int64_t wide = 0;                            // workgroups per tile that take 512 columns each
+  for (int i = 0; i < count; ++i) wide += (list[i].m + 8 * kOutBlock - 1) / (8 * kOutBlock);
+  int groups = 0, column = 0, yds = 0, ranks[3] = {}, chunks[3] = {};
   for (int i = 0; i < count; ++i) {
     const mdbf_adapter_t& l = list[i];
     in.A[i] = l.A_dev, in.r[i] = l.r, in.column[i] = column;
@@ -475,19 +560,19 @@ static int launch_adapters(int count, const mdbf_adapter_t* list, int adapters, 
       g->proj[g->slots] = (uint8_t)i, g->tile[g->slots] = (uint8_t)t;
       ++g->slots;
     }
-    const int chunk = 4 * kOutBlock;
+    const int chunk = 4 * kOutBlock * (tile_room * wide >= 256 ? 2 : 1);
     out.p[i] = {l.B_dev, l.Y_dev, l.scale_dev, l.ldy, l.m, l.r, column, l.y_dtype, chunk};
     column += (l.r + 15) / 16 * 16;
     yds |= 1 << l.y_dtype;
-    const int c = (l.m + chunk - 1) / chunk, e = (l.r + 7) / 8;
+    const int c = (l.m + chunk - 1) / chunk;
     if (c > chunks[l.y_dtype]) chunks[l.y_dtype] = c;
-    if (e > eights[l.y_dtype]) eights[l.y_dtype] = e;
+    if (l.r > ranks[l.y_dtype]) ranks[l.y_dtype] = l.r;
   }
   adapter_in_kernel<DT><<<dim3((unsigned)tile_room, sh.splits, groups), 256, 0, s>>>(in);
   int e = (int)hipGetLastError();
-  if (!e && (yds & 1 << MDBF_F16)) e = launch_out<DT, MDBF_F16>(out, count, tile_room, chunks[MDBF_F16], eights[MDBF_F16], s);
-  if (!e && (yds & 1 << MDBF_BF16)) e = launch_out<DT, MDBF_BF16>(out, count, tile_room, chunks[MDBF_BF16], eights[MDBF_BF16], s);
-  if (!e && (yds & 1 << MDBF_F32)) e = launch_out<DT, MDBF_F32>(out, count, tile_room, chunks[MDBF_F32], eights[MDBF_F32], s);
+  if (!e && (yds & 1 << MDBF_F16)) e = launch_out<DT, MDBF_F16>(out, count, tile_room, chunks[MDBF_F16], ranks[MDBF_F16], s);
+  if (!e && (yds & 1 << MDBF_BF16)) e = launch_out<DT, MDBF_BF16>(out, count, tile_room, chunks[MDBF_BF16], ranks[MDBF_BF16], s);
+  if (!e && (yds & 1 << MDBF_F32)) e = launch_out<DT, MDBF_F32>(out, count, tile_room, chunks[MDBF_F32], ranks[MDBF_F32], s);
   return e;
 }
 
