@@ -1,0 +1,106 @@
+"""What the binding allocates for the operators around the projections on a named stream, and what it refuses before any call, without a GPU: with the
+stand-ins that record of test_binding_streams."""
+import pytest
+import torch
+
+import test_binding_streams as tb
+from paper_2512_24545_amd import binding as mb
+
+world = tb.world
+HOST = ("mdbf_adapter_tiles", "mdbf_adapters_workspace_bytes", "mdbf_sample_workspace_bytes")
+
+
+@pytest.fixture(autouse=True)
+def stand_ins(world, monkeypatch):
+    monkeypatch.setattr(tb.Library, "HOST", tb.Library.HOST + HOST)
+    monkeypatch.setattr(tb.Tensor, "get_device", lambda self: getattr(self, "index", 0), raising=False)
+    monkeypatch.setattr(tb.Tensor, "view", lambda self, *shape: tb.Tensor(shape, self.dtype, self.made_on), raising=False)
+    mb._torch_module.float8_e4m3fn = torch.float8_e4m3fn
+
+
+def T16(*shape):
+    return tb.Tensor(shape, torch.bfloat16)
+
+
+def f32(*shape):
+    return tb.Tensor(shape, torch.float32)
+
+
+def rows(T=5, requests=3, adapters=4):
+    return mb.AdapterRows(T, requests, adapters, rows=tb.ints(T), tiles=tb.ints(6, 4))
+
+
+def pool():
+    return mb.Adapters(T16(4, 8, 64), T16(4, 32, 8), f32(4))
+
+
+CALLS = {
+    "mdbf_add_norm": (lambda s: mb.mdbf_add_norm(T16(3, 64), T16(3, 64), f32(64), y_dtype="e4m3", stream=s), 3, 0),
+    "mdbf_adapter_rows": (lambda s: mb.mdbf_adapter_rows(tb.ints(4), tb.ints(3), 4, 5, stream=s), 1, 0),
+    "mdbf_adapters": (lambda s: mb.mdbf_adapters(rows(), [pool()], [T16(5, 64)], [T16(5, 32)], stream=s), 0, 1),
+    "mdbf_sample": (lambda s: mb.mdbf_sample(f32(3, 100), f32(3), stream=s), 2, 1),
+}
+
+
+@pytest.mark.parametrize("name", sorted(CALLS))
+def test_a_named_stream(world, name):
+    made, calls = world
+    call, results, workspaces = CALLS[name]
+    call(tb.SIDE)
+    assert calls == [(name, tb.SIDE.cuda_stream)] and len(made) == results + workspaces
+    assert all(t.made_on is tb.SIDE for t in made)
+    kept = [t for t in made if t.used_on]
+    assert len(kept) == results and all(t.used_on == [tb.CALLER] for t in kept)
+
+
+@pytest.mark.parametrize("name", sorted(CALLS))
+def test_the_current_stream(world, name):
+    made, calls = world
+    call, results, workspaces = CALLS[name]
+    call(None)
+    assert calls == [(name, tb.CALLER.cuda_stream)] and len(made) == results + workspaces
+    assert all(t.made_on is tb.CALLER and not t.used_on for t in made)
+
+
+def _elsewhere(t):
+    t.index = 1
+    return t
+
+
+REFUSED = {
+    "norm: another device": lambda: mb.mdbf_add_norm(_elsewhere(T16(3, 64))),
+    "norm: a weight of another device": lambda: mb.mdbf_add_norm(T16(3, 64), weight=_elsewhere(f32(64))),
+    "norm: residual of another shape": lambda: mb.mdbf_add_norm(T16(3, 64), T16(4, 64)),
+    "norm: residual_out without residual": lambda: mb.mdbf_add_norm(T16(3, 64), residual_out=T16(3, 64)),
+    "norm: residual_out of another type": lambda: mb.mdbf_add_norm(T16(3, 64), T16(3, 64), residual_out=f32(3, 64)),
+    "norm: scales without 8 bits": lambda: mb.mdbf_add_norm(T16(3, 64), scales=f32(3, 1)),
+    "norm: scales of another shape": lambda: mb.mdbf_add_norm(T16(3, 64), y_dtype="e4m3", scale_group=32, scales=tb.Tensor((3, 3), torch.uint8)),
+    "norm: a 16-bit weight": lambda: mb.mdbf_add_norm(T16(3, 64), weight=T16(64)),
+    "norm: out of another type than asked for": lambda: mb.mdbf_add_norm(T16(3, 64), y_dtype="f32", out=T16(3, 64)),
+    "rows: cu too short": lambda: mb.mdbf_adapter_rows(tb.ints(3), tb.ints(3), 4, 5),
+    "rows: 64-bit adapters": lambda: mb.mdbf_adapter_rows(tb.ints(4), tb.Tensor((3,), torch.int64), 4, 5),
+    "rows: tables of other sizes": lambda: mb.mdbf_adapter_rows(tb.ints(4), tb.ints(3), 4, 5, out=mb.AdapterRows(6, 3, 4)),
+    "rows: tables made by other means": lambda: mb.mdbf_adapter_rows(tb.ints(4), tb.ints(3), 4, 5, out=rows()),
+    "adapters: rows of other adapters": lambda: mb.mdbf_adapters(rows(adapters=5), [pool()], [T16(5, 64)], [T16(5, 32)]),
+    "adapters: X too narrow": lambda: mb.mdbf_adapters(rows(), [pool()], [T16(5, 63)], [T16(5, 32)]),
+    "adapters: X too short": lambda: mb.mdbf_adapters(rows(), [pool()], [T16(4, 64)], [T16(5, 32)]),
+    "adapters: Y too wide": lambda: mb.mdbf_adapters(rows(), [pool()], [T16(5, 64)], [T16(5, 33)]),
+    "adapters: X of another type": lambda: mb.mdbf_adapters(rows(), [pool()], [tb.Tensor((5, 64), torch.float16)], [T16(5, 32)]),
+    "adapters: fewer Ys": lambda: mb.mdbf_adapters(rows(), [pool()], [T16(5, 64)], []),
+    "adapters: none": lambda: mb.mdbf_adapters(rows(), [], [], []),
+    "adapters: another device": lambda: mb.mdbf_adapters(rows(), [pool()], [T16(5, 64)], [_elsewhere(T16(5, 32))]),
+    "adapters: factors that do not go together": lambda: mb.Adapters(T16(4, 8, 64), T16(4, 32, 9)),
+    "adapters: a 16-bit scale": lambda: mb.Adapters(T16(4, 8, 64), T16(4, 32, 8), T16(4)),
+    "sample: u of another length": lambda: mb.mdbf_sample(f32(3, 100), f32(4)),
+    "sample: top_k of another type": lambda: mb.mdbf_sample(f32(3, 100), f32(3), top_k=tb.Tensor((3,), torch.int64)),
+    "sample: a 64-bit temperature": lambda: mb.mdbf_sample(f32(3, 100), f32(3), temperature=tb.Tensor((3,), torch.float64)),
+    "sample: tokens of another type": lambda: mb.mdbf_sample(f32(3, 100), f32(3), tokens=tb.Tensor((3,), torch.int64)),
+    "sample: another device": lambda: mb.mdbf_sample(_elsewhere(f32(3, 100)), f32(3)),
+}
+
+
+@pytest.mark.parametrize("name", sorted(REFUSED))
+def test_refused(world, name):
+    with pytest.raises((AssertionError, mb.MdbfError)):
+        REFUSED[name]()
+    assert not world[1]
