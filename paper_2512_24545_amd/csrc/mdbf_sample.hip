@@ -34,14 +34,13 @@ struct RowSetting {
   uint32_t top, top_k;
   bool greedy;
 };
-__device__ __forceinline__ RowSetting row_setting(const SampleArgs& a, int64_t t, uint32_t top) {
+__device__ __forceinline__ RowSetting row_setting(const SampleArgs& a, int64_t t) {
   RowSetting r;
   const float temperature = a.temperature ? a.temperature[t] : 1.0f;
   r.greedy = !(temperature > 0.0f);
   r.per_degree = 1.0 / (double)temperature;
   r.grid = 16 * 1.44269504088896340736 / (double)temperature;   // sixteenths of a factor of two per unit of the logits
-  r.top = top;
-  r.largest = (double)key_value(top);
+  r.top = 0, r.largest = 0;                     // (the row's largest, when it is known)
   const int k = a.top_k ? a.top_k[t] : 0;
   r.top_k = k > 0 && k < a.vocab ? (uint32_t)k : 0;
   const float p = a.top_p ? a.top_p[t] : 1.0f, least = a.min_p ? a.min_p[t] : 0.0f, u = a.u[t];
@@ -207,20 +206,47 @@ __device__ void sample_digits(const SampleArgs& a, int64_t t, const RowSetting& 
 // of a sixteenth of a factor of two, floor(t), from the part's largest down, and sums there how many they are and their 2^(frac(t) / 16): one 64-bit whole
 // number a bucket, whose additions in LDS have no order.  The buckets of all parts of a row lie on one grid, so the second launch, a workgroup a
 // row, adds them up; prefix sums then tell in which bucket each bound and the drawn number lie.  Only the tokens of those few are looked
-// at by themselves: parts that have some are read again, their tokens put in order, and the bounds applied exactly.  Tokens that equal the part's
-// largest are counted apart, so that those that equal the row's largest, of weight 1, make up a bucket of an exact mass: where many are alike,
-// bounds fall on borders between them.
+// at by themselves, and the bounds applied exactly; the first launch leaves the tokens in the order of their buckets, so that these are a few runs of each
+// part's.  Tokens that equal the part's largest are counted apart, so that those that equal the row's largest, of weight 1, make up a bucket of an exact mass:
+// where many are alike, bounds fall on borders between them.
 constexpr int kBuckets = 768;                    // of a row: the largest, then 767 sixteenths, down to 2^-47 of it; less weighs nothing
 constexpr int kPerOctave = 16;
 constexpr int kFracBits = 39;                    // of 2^(frac / 16) - 1 < 0.0443: 16384 of them stay below 2^49, where the count begins
 constexpr int kCountBit = 49;
-constexpr int kList = 8192;                      // tokens that the second launch puts in order; rows that have more go by digits
+constexpr int kStored = 8192;                    // tokens of a part that the first launch leaves in order; what needs more reads the part again
+constexpr int kList = 8192;                      // tokens of a row that the second launch looks at; rows that have more go by digits
 constexpr int kPartThreads = 1024;
 constexpr double kSlack = 1e-9;                  // by which sums of buckets and of tokens may differ, and more
 
 struct PartHead {
   unsigned long long top;                        // key of the part's largest, ~its index: the largest with the lowest index is the largest number
-  unsigned long long equal;                      // tokens that equal it
+  uint32_t equal;                                // tokens that equal it
+  int32_t stored;                                // buckets whose tokens are left in order; -1: not even the ones that equal the largest
+};
+// A token as the first launch leaves it: its logit as it lies and its place in the part, resp. key and place.
+template <int DT>
+struct Left {
+  typedef uint32_t type;
+  __device__ static type make(uint32_t raw, uint32_t key, uint32_t at) { return raw << 16 | at; }
+  __device__ static uint32_t key(type v) {
+    if (DT == MDBF_F16) return order_key((float)__builtin_bit_cast(_Float16, (uint16_t)(v >> 16)));
+    return order_key(__builtin_bit_cast(float, v & 0xffff0000u));
+  }
+  __device__ static uint32_t at(type v) { return v & 0xffffu; }
+};
+template <>
+struct Left<MDBF_F32> {
+  typedef unsigned long long type;
+  __device__ static type make(uint32_t raw, uint32_t key, uint32_t at) { return (unsigned long long)key << 32 | at; }
+  __device__ static uint32_t key(type v) { return (uint32_t)(v >> 32); }
+  __device__ static uint32_t at(type v) { return (uint32_t)v; }
+};
+// What the first launch leaves, part by part.
+struct Parts {
+  PartHead* heads;
+  unsigned long long* hists;                     // kBuckets each
+  uint16_t* starts;                              // kBuckets: where each bucket's tokens begin in what is left, or its end
+  char* left;                                    // kStored tokens each
 };
 
 __device__ __forceinline__ double degrees(const RowSetting& r, float x) { return (double)x * r.grid; }
@@ -232,11 +258,37 @@ __device__ __forceinline__ double sixteenth(double x) {
   return x * fma(x, fma(x, fma(x, fma(x, fma(x, c6, c5), c4), c3), c2), c1);
 }
 
+// sums of the threads in front of this one, and of all, over a workgroup of 1024
+__device__ __forceinline__ uint32_t scan_counts(uint32_t v, uint32_t& total, uint32_t* waves) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  uint32_t to = v;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint32_t u = __shfl_up(to, o);
+    if (lane >= o) to += u;
+  }
+  __syncthreads();
+  if (lane == 63) waves[wave] = to;
+  __syncthreads();
+  uint32_t before = 0;
+  total = 0;
+#pragma unroll
+  for (int w = 0; w < 16; ++w) {
+    if (w == wave) before = total;
+    total += waves[w];
+  }
+  return before + to - v;
+}
+
 template <int DT, int EPT>
-__global__ __launch_bounds__(kPartThreads) void sample_parts_kernel(SampleArgs a, PartHead* heads, unsigned long long* hists) {
+__global__ __launch_bounds__(kPartThreads) void sample_parts_kernel(SampleArgs a, Parts parts) {
+  typedef typename Left<DT>::type Token;
+  extern __shared__ char staged[];
+  Token* order = (Token*)staged;
   __shared__ unsigned long long hist[kBuckets];
+  __shared__ uint32_t slot[kBuckets];
   __shared__ unsigned long long tops[kPartThreads / 64];
-  __shared__ uint32_t equal;
+  __shared__ uint32_t waves[kPartThreads / 64], equal, next_equal, fit, want, left;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t t = blockIdx.y, part = t * gridDim.x + blockIdx.x;
   const int i0 = blockIdx.x * (kPartThreads * EPT);
@@ -247,8 +299,9 @@ __global__ __launch_bounds__(kPartThreads) void sample_parts_kernel(SampleArgs a
     const int i = i0 + (p * kPartThreads + tid) * 8;
     if (i < a.vocab) load_raw8<DT>(a.logits, t * a.ld + i, a.vocab - i, raw[p]);
   }
+  RowSetting r = row_setting(a, t);
   for (int o = tid; o < kBuckets; o += kPartThreads) hist[o] = 0;
-  if (tid == 0) equal = 0;
+  if (tid == 0) equal = next_equal = fit = want = left = 0;
   float v[EPT], best = -__builtin_inff();
   int at = 0x7fffffff;
 #pragma unroll
@@ -274,82 +327,132 @@ __global__ __launch_bounds__(kPartThreads) void sample_parts_kernel(SampleArgs a
 #pragma unroll
   for (int w = 0; w < kPartThreads / 64; ++w)
     if (tops[w] > top) top = tops[w];
-  if (tid == 0) heads[part].top = top;
   const uint32_t key = (uint32_t)(top >> 32);
-  const RowSetting r = row_setting(a, t, key);
-  if (key <= kKeyNone || r.greedy) return;
+  if (key <= kKeyNone || r.greedy) {
+    if (tid == 0) parts.heads[part].top = top;
+    return;
+  }
   const float largest = key_value(key);
   const bool infinite = largest == __builtin_inff();    // then nothing else weighs
   const double base = floor(degrees(r, largest));
   uint32_t alike = 0;
+  int down[EPT];                                 // a token's bucket; -1: of the part's largest
 #pragma unroll
   for (int e = 0; e < EPT; ++e) {
     const bool same = v[e] == largest;
     alike += (uint32_t)__popcll(__ballot(same));
+    down[e] = same ? -1 : kBuckets;
     if (infinite || same) continue;
-    const double d = degrees(r, v[e]), f = floor(d), down = base - f;
-    if (down < kBuckets && v[e] > -__builtin_inff()) {
+    const double d = degrees(r, v[e]), f = floor(d), b = base - f;
+    if (b < kBuckets && v[e] > -__builtin_inff()) {
+      down[e] = (int)b;
       // (the sum with 2^52 has the whole number in its last bits)
       const double g = fma(sixteenth(d - f), (double)(1ull << kFracBits), 0x1p52);
-      atomicAdd(&hist[(int)down], __builtin_bit_cast(unsigned long long, g) - 0x4330000000000000ull + (1ull << kCountBit));
+      atomicAdd(&hist[down[e]], __builtin_bit_cast(unsigned long long, g) - 0x4330000000000000ull + (1ull << kCountBit));
     }
   }
-  if (lane == 0) atomicAdd(&equal, alike);
+  if (lane == 0 && alike) atomicAdd(&equal, alike);
   __syncthreads();
-  if (tid == 0) heads[part].equal = equal;
-  for (int o = tid; o < kBuckets; o += kPartThreads) hists[part * kBuckets + o] = hist[o];
+  // how far tokens are left in order: as many as there is room for, and no further than the row's own bounds can reach
+  const uint32_t n_equal = equal, count = tid < kBuckets ? (uint32_t)(hist[tid] >> kCountBit) : 0;
+  uint32_t all;
+  const uint32_t start = n_equal + scan_counts(count, all, waves);
+  if (tid < kBuckets) {
+    parts.hists[part * kBuckets + tid] = hist[tid];
+    slot[tid] = start;
+  }
+  // (top_p of what top_k leaves goes by the mass of tokens below min_p too)
+  const bool below = r.min_p == 0.0 || (r.top_k && r.top_p < 1.0) || tid < 4.0 - kPerOctave * log2(r.min_p);
+  const bool reach = tid < kBuckets && below && (!r.top_k || start < r.top_k), fits = reach && start + count <= kStored;
+  const unsigned long long reached = __ballot(reach), fitted = __ballot(fits);      // (both hold for the first buckets alone)
+  if (lane == 0 && reached) atomicAdd(&want, (uint32_t)__popcll(reached));
+  if (lane == 0 && fitted) atomicAdd(&fit, (uint32_t)__popcll(fitted));
+  if (fitted && lane == 63 - __builtin_clzll(fitted)) atomicMax(&left, start + count);
+  __syncthreads();
+  const bool room = n_equal <= kStored;
+  const int limit = room ? (int)fit : -1;
+  if (tid == 0) parts.heads[part] = {top, n_equal, !room ? -1 : fit == want ? kBuckets : (int)fit};
+  if (!room) return;
+  const uint32_t n_left = max(left, n_equal);
+  if (tid < kBuckets) parts.starts[part * kBuckets + tid] = (uint16_t)min(start, n_left);
+#pragma unroll
+  for (int e = 0; e < EPT; ++e) {
+    if (down[e] >= limit) continue;
+    const uint32_t place = atomicAdd(down[e] < 0 ? &next_equal : &slot[down[e]], 1u);
+    const uint32_t mine = ((e / 8) * kPartThreads + tid) * 8 + e % 8;
+    const uint32_t w = raw[e / 8].w[DT == MDBF_F32 ? (e % 8) / 4 : 0][DT == MDBF_F32 ? e % 4 : (e % 8) / 2];
+    order[place] = Left<DT>::make(DT == MDBF_F32 ? w : w >> (16 * (e & 1)) & 0xffffu, order_key(v[e]), mine);
+  }
+  __syncthreads();
+  const int bytes = (int)(n_left * sizeof(Token));
+  char* out = parts.left + part * (int64_t)(kStored * sizeof(Token));
+  for (int x = tid * 16; x < bytes; x += kPartThreads * 16) *(MDBF_GLOBAL U32x4*)(out + x) = *(const U32x4*)(staged + x);
 }
 
 // What the second launch has in LDS.
-constexpr int kRuns = 4;                         // runs of neighbouring buckets that are looked at
 constexpr int kMaxParts = kSampleMaxVocab / (kPartThreads * 8);
+constexpr int kBins = kPickThreads;
+constexpr int kRuns = 4;                         // runs of neighbouring buckets that are looked at
 struct RowShared {
   unsigned long long list[kList];                // ~key, index: the order of the tokens
-  double before[kBuckets], seg_mass[kBuckets];   // mass in front of a bucket, and of the list in front of a bucket's first
-  uint32_t count_before[kBuckets], seg_at[kBuckets];
-  unsigned long long flags[kBuckets / 64];
+  unsigned long long few[64];
+  double before[kBuckets];                       // mass and tokens in front of a bucket
+  uint32_t count_before[kBuckets];
+  uint16_t bin[kList];
+  unsigned long long bin_mass[kBins];
+  double bin_from[kBins];
+  uint32_t bin_count[kBins], bin_first[kBins];
   double sums[kPickThreads / 64];
   uint32_t counts[kPickThreads / 64];
   unsigned long long tops[kPickThreads / 64];
   unsigned long long part_extra[kMaxParts];      // of a part: its largest's bucket in the row (kBuckets: nothing there weighs), how many equal it, and
-  int32_t part_top[kMaxParts];                   // their fractions
+  int32_t part_top[kMaxParts];                   // their fractions; buckets whose tokens are in order
+  int32_t part_stored[kMaxParts];
   uint32_t part_equal[kMaxParts], part_list[kMaxParts];
   double klo, khi, plo, phi, mlo, mhi, total;
+  unsigned long long likely;
+  double value;
   int k, p0, p1, m0, m1, u0, u1;
-  float lower[kRuns], upper[kRuns];
-  uint32_t n, parts, runs, dropped;
+  int chosen[3];
+  uint32_t n, parts, n_few, key, ties;
 };
 
-// what the wave wrote in LDS, or the workgroup, is there for all of it
-template <int THREADS>
-__device__ __forceinline__ void meet() {
-  if (THREADS > 64) {
-    __syncthreads();
-  } else {
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
-    __builtin_amdgcn_wave_barrier();
-  }
-}
-
-// The value of the last (or first) thread for which `here` holds, where it rises with the threads; else `none`.
-template <int THREADS, bool FIRST>
-__device__ __forceinline__ double end_of(bool here, double v, double none, double* part) {
-  const unsigned long long b = __ballot(here);
-  const int who = !b ? 0 : FIRST ? __builtin_ctzll(b) : 63 - __builtin_clzll(b);
-  if (THREADS == 64) return b ? __shfl(v, who) : none;
-  __syncthreads();
-  if ((int)(threadIdx.x & 63) == who) part[threadIdx.x >> 6] = b ? v : none;
-  __syncthreads();
-  v = part[0];
+struct Runs {
+  int from[kRuns], to[kRuns];                    // disjoint, rising; empty ones at the end have from > to
+  int buckets;
+};
+// The union of up to four ranges.
+__device__ __forceinline__ Runs runs_of(const int (&lo)[kRuns], const int (&hi)[kRuns]) {
+  Runs r;
 #pragma unroll
-  for (int w = 1; w < THREADS / 64; ++w) v = FIRST ? fmin(v, part[w]) : fmax(v, part[w]);
-  return v;
+  for (int q = 0; q < kRuns; ++q) r.from[q] = hi[q] < lo[q] ? 1 << 20 : lo[q], r.to[q] = hi[q];
+  const auto order = [&](int x, int y) {
+    if (r.from[y] < r.from[x]) {
+      const int f = r.from[x], t = r.to[x];
+      r.from[x] = r.from[y], r.to[x] = r.to[y], r.from[y] = f, r.to[y] = t;
+    }
+  };
+  order(0, 1), order(2, 3), order(0, 2), order(1, 3), order(1, 2);
+  r.buckets = 0;
+#pragma unroll
+  for (int q = 0; q < kRuns; ++q) {
+#pragma unroll
+    for (int e = q + 1; e < kRuns; ++e)           // what touches it belongs to it
+      if (r.from[e] <= r.to[q] + 1 && r.from[q] < 1 << 20) r.to[q] = max(r.to[q], r.to[e]), r.from[e] = 1 << 20, r.to[e] = -1;
+    if (r.from[q] < 1 << 20) r.buckets += r.to[q] - r.from[q] + 1;
+  }
+  return r;
 }
 
 // Which buckets have to be looked at: those of the bounds and of the drawn number, the latter ones' ends by the least and the most that the bounds
-// may leave.  k, p0 .., m0 .., u0 .. are set to no bound before.
-__device__ __forceinline__ void choose_buckets(const RowSetting& r, RowShared& s, double before, double upto, uint32_t count_before, uint32_t count_to,
-                                               double frac) {
+// may leave.  k, p0 .., m0 .., u0 .. are set to no bound before.  `least`, `other`: min_p, resp. the other bounds, are sure to be undercut and
+// need none of their tokens.
+struct Choice {
+  bool least, other;
+  Runs runs;
+};
+__device__ __forceinline__ Choice choose_buckets(const RowSetting& r, RowShared& s, double before, double upto, uint32_t count_before, uint32_t count_to,
+                                                 double frac) {
   const int o = threadIdx.x;
   const bool in = o < kBuckets;
   if (in && r.top_k && count_before < r.top_k && count_to >= r.top_k) s.k = o, s.klo = before, s.khi = upto;
@@ -369,177 +472,245 @@ __device__ __forceinline__ void choose_buckets(const RowSetting& r, RowShared& s
     if (in && before <= hi && upto > hi) s.p1 = o, s.phi = upto;
   }
   __syncthreads();
-  const double ulo = r.u * fmin(klo, fmin(s.plo, s.mlo)) * (1 - kSlack), uhi = r.u * fmin(khi, fmin(s.phi, s.mhi)) * (1 + kSlack);
+  const double plo = s.plo, phi = s.phi, mlo = s.mlo, mhi = s.mhi;
+  const double ulo = r.u * fmin(klo, fmin(plo, mlo)) * (1 - kSlack), uhi = r.u * fmin(khi, fmin(phi, mhi)) * (1 + kSlack);
   if (in && before <= ulo && upto > ulo) s.u0 = o;
   if (in && before <= uhi && upto > uhi) s.u1 = o;
   __syncthreads();
-  // (a bound that another one is sure to undercut needs none of its tokens)
-  const bool least = s.mlo >= fmin(khi, s.phi), other = s.mhi <= fmin(klo, s.plo);
-  const bool flag = in && ((!other && (o == s.k || (o >= s.p0 && o <= s.p1))) || (!least && o >= s.m0 && o <= s.m1) || (o >= s.u0 && o <= s.u1));
-  const unsigned long long b = __ballot(flag);
-  if (in && (o & 63) == 0) s.flags[o >> 6] = b;
-  __syncthreads();
+  Choice c;
+  c.least = mlo >= fmin(khi, phi), c.other = mhi <= fmin(klo, plo);
+  const int lo[kRuns] = {s.k, s.p0, s.m0, s.u0}, hi[kRuns] = {c.other || s.k < 0 ? -2 : s.k, c.other ? -2 : s.p1, c.least ? -2 : s.m1, s.u1};
+  c.runs = runs_of(lo, hi);
+  return c;
 }
-__device__ __forceinline__ bool flagged(const RowShared& s, int b) { return s.flags[b >> 6] >> (b & 63) & 1; }
 
-// The list in order, bitonic: a wave sorts and merges 64 neighbours in registers, what is further apart meets in LDS.
-__device__ __forceinline__ unsigned long long exchange(unsigned long long v, int x, int j, int k) {
-  const unsigned long long u = __shfl_xor(v, j);
-  return ((x & j) == 0) == ((x & k) == 0) ? (u < v ? u : v) : (u < v ? v : u);
-}
-template <int THREADS>
-__device__ __forceinline__ void sort_list(RowShared& s, int n) {
-  const int tid = threadIdx.x;
-  if (THREADS == 64) {                          // so few that each counts those in front of it
-    const unsigned long long v = tid < n ? s.list[tid] : ~0ull;
-    int place = 0;
-    for (int j = 0; j < n; ++j) place += __shfl(v, j) < v;
-    meet<64>();
-    if (v != ~0ull) s.list[place] = v;         // (those left out are alike)
-    meet<64>();
-    return;
-  }
-  int size = 64;
-  while (size < n) size <<= 1;
-  for (int x = tid; x < size; x += THREADS) {
-    unsigned long long v = x < n ? s.list[x] : ~0ull;
+enum Bound { kByCount, kByMass, kByDraw };
+// Where in a bin of the list a bound lies: with kByCount and kByMass the mass of what it leaves, with kByDraw the token, which the
+// threads that find it write.  `target`: so many tokens, so much mass.  In bins of up to 64 tokens a wave puts them in order; others, in which
+// many are alike, go from one value to the next.
+template <int DT>
+__device__ double resolve(const SampleArgs& a, int64_t t, const RowSetting& r, RowShared& s, int n, int bin, double target, int what, double kept) {
+  const int tid = threadIdx.x, lane = tid & 63;
+  const uint32_t here = s.bin_count[bin];
+  double before = s.bin_from[bin];
+  uint32_t first = s.bin_first[bin];
+  __syncthreads();                               // (the last use of what follows is over)
+  if (tid == 0) s.n_few = 0, s.key = 0, s.ties = 0;
+  __syncthreads();
+  if (here <= 64) {
+    for (int x = tid; x < n; x += kPickThreads)
+      if (s.bin[x] == bin) s.few[atomicAdd(&s.n_few, 1u)] = s.list[x];
+    __syncthreads();
+    if (tid < 64) {
+      const int m = (int)here;
+      unsigned long long v = tid < m ? s.few[tid] : ~0ull;
+      int place = 0;
+      for (int j = 0; j < m; ++j) place += __shfl(v, j) < v;
+      if (tid < m) s.few[place] = v;
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+      __builtin_amdgcn_wave_barrier();
+      v = tid < m ? s.few[tid] : ~0ull;
+      const double w = tid < m ? weight(r, ~(uint32_t)(v >> 32)) : 0.0;
+      double to = w;
 #pragma unroll
-    for (int k = 2; k <= 64; k <<= 1)
-#pragma unroll
-      for (int j = k >> 1; j > 0; j >>= 1) v = exchange(v, x, j, k);
-    s.list[x] = v;
-  }
-  for (int k = 128; k <= size; k <<= 1) {
-    for (int j = k >> 1; j >= 64; j >>= 1) {
-      meet<THREADS>();
-      for (int i = tid; i < size / 2; i += THREADS) {
-        const int x = ((i & ~(j - 1)) << 1) | (i & (j - 1)), y = x | j;
-        const unsigned long long p = s.list[x], q = s.list[y];
-        if ((p > q) == ((x & k) == 0)) s.list[x] = q, s.list[y] = p;
+      for (int o = 1; o < 64; o <<= 1) {
+        const double u = __shfl_up(to, o);
+        if (lane >= o) to += u;
+      }
+      const double at = before + (to - w);
+      to += before;
+      const bool in = tid < m;
+      if (what == kByDraw) {
+        const unsigned long long b = __ballot(in && to > target);
+        const int x = b ? __builtin_ctzll(b) : m - 1;    // (none goes beyond it only by rounding)
+        if (tid == x) {
+          a.tokens[t] = (int)(uint32_t)v;
+          if (a.probs) a.probs[t] = (float)(w / kept);
+        }
+      } else {
+        const bool holds = what == kByCount ? (double)(first + lane) < target : at < target || first + lane == 0;
+        const unsigned long long b = __ballot(in && holds);
+        const double m1 = b ? __shfl(to, 63 - __builtin_clzll(b)) : before;
+        if (tid == 0) s.value = m1;
       }
     }
-    meet<THREADS>();
-    for (int x = tid; x < size; x += THREADS) {
-      unsigned long long v = s.list[x];
-#pragma unroll
-      for (int j = 32; j > 0; j >>= 1) v = exchange(v, x, j, k);
-      s.list[x] = v;
+    __syncthreads();
+    return s.value;
+  }
+  uint32_t last = 0xffffffffu, key = 0, ties = 0;
+  double w = 0;
+  for (uint32_t seen = 0; seen < here;) {
+    for (int x = tid; x < n; x += kPickThreads) {
+      const uint32_t k = ~(uint32_t)(s.list[x] >> 32);
+      if (s.bin[x] == bin && k < last) atomicMax(&s.key, k);
     }
-  }
-  meet<THREADS>();
-}
-
-// The bounds and the draw on the list, `taken` entries of which n count, by THREADS threads with up to PER tokens each.
-template <int THREADS, int PER, class Bucket>
-__device__ __forceinline__ void pick(const SampleArgs& a, int64_t t, const RowSetting& r, RowShared& s, int taken, int n, const Bucket& bucket_of) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  sort_list<THREADS>(s, taken);
-  // each thread has a run of the list
-  const int per = (n + THREADS - 1) / THREADS, x0 = min(tid * per, n), x1 = min(x0 + per, n);
-  double w[PER], sum = 0;
-  int bucket[PER];
-#pragma unroll
-  for (int q = 0; q < PER; ++q) {
-    if (x0 + q < x1) {
-      const uint32_t k = ~(uint32_t)(s.list[x0 + q] >> 32);
-      w[q] = weight(r, k);
-      bucket[q] = bucket_of(key_value(k));
-      sum += w[q];
-    }
-  }
-  double run = sum;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const double u = __shfl_up(run, o);
-    if (lane >= o) run += u;
-  }
-  if (THREADS > 64) {
-    if (lane == 63) s.sums[wave] = run;
+    __syncthreads();
+    key = s.key;
+    for (int x = tid; x < n; x += kPickThreads)
+      if (s.bin[x] == bin && ~(uint32_t)(s.list[x] >> 32) == key) atomicAdd(&s.ties, 1u);
+    __syncthreads();
+    ties = s.ties;
+    w = weight(r, key);
+    seen += ties;
+    const double to = before + (double)ties * w;
+    if (seen >= here || (what == kByCount ? (double)(first + ties) >= target : what == kByMass ? to >= target : to > target)) break;
+    before = to, first += ties, last = key;
+    __syncthreads();
+    if (tid == 0) s.key = 0, s.ties = 0;
     __syncthreads();
   }
-  run -= sum;
-  if (THREADS > 64)
-    for (int v = 0; v < wave; ++v) run += s.sums[v];
-  double at[PER];                               // mass of the list in front of a token
-#pragma unroll
-  for (int q = 0; q < PER; ++q) {
-    if (x0 + q < x1) {
-      at[q] = run;
-      run += w[q];
-      const int x = x0 + q, prev = x > 0 ? bucket_of(key_value(~(uint32_t)(s.list[x - 1] >> 32))) : -1;
-      if (prev != bucket[q]) s.seg_mass[bucket[q]] = at[q], s.seg_at[bucket[q]] = x;
-    }
+  if (what == kByCount) return before + fmin(target - (double)first, (double)ties) * w;
+  if (what == kByMass) {
+    const double j = w > 0 ? ceil((target - before) / w) : 0.0;
+    return before + fmin(fmax(j, first == 0 ? 1.0 : 0.0), (double)ties) * w;
   }
-  meet<THREADS>();
+  // the one with the right number among equal ones, by index: its thousand first, then itself
+  uint32_t tie = (uint32_t)fmin(fmax(w > 0 ? floor((target - before) / w) : 0.0, 0.0), (double)(ties - 1)), group = 0, total;
+  for (int level = 0; level < 2; ++level) {
+    __syncthreads();
+    s.bin_count[tid] = 0;
+    __syncthreads();
+    for (int x = tid; x < n; x += kPickThreads) {
+      const unsigned long long v = s.list[x];
+      const uint32_t i = (uint32_t)v;
+      if (~(uint32_t)(v >> 32) == key && s.bin[x] == bin && (level == 0 || i >> 10 == group)) atomicAdd(&s.bin_count[level ? i & 1023 : i >> 10], 1u);
+    }
+    __syncthreads();
+    const uint32_t c = s.bin_count[tid], from = scan_counts(c, total, s.counts);
+    if (c && from <= tie && tie < from + c) s.chosen[0] = tid, s.n_few = from;
+    __syncthreads();
+    if (level == 0) group = (uint32_t)s.chosen[0], tie -= s.n_few;
+  }
+  if (tid == 0) {
+    a.tokens[t] = (int)(group << 10 | (uint32_t)s.chosen[0]);
+    if (a.probs) a.probs[t] = (float)(w / kept);
+  }
+  return 0.0;
+}
+
+// The bounds and the draw on the list.  Its tokens are sorted into bins, as many to each of the buckets as there are threads for, whose prefix
+// sums tell the one in which a bound lies.
+template <int DT, class Bucket>
+__device__ __forceinline__ void pick(const SampleArgs& a, int64_t t, const RowSetting& r, RowShared& s, int n, const Choice& c, const Bucket& bucket_of) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int room = c.runs.buckets > 1 ? 32 - __builtin_clz(c.runs.buckets - 1) : 0, sub_bits = 10 - room;
+  if (tid < 3) s.chosen[tid] = -1;
+  if (tid == 0) s.likely = 0;
+  s.bin_count[tid] = 0, s.bin_mass[tid] = 0;
+  __syncthreads();
+  unsigned long long likely = 0;
+  for (int x = tid; x < n; x += kPickThreads) {
+    const uint32_t k = ~(uint32_t)(s.list[x] >> 32);
+    const float v = key_value(k);
+    const int b = bucket_of(v);
+    int at = b;
 #pragma unroll
-  for (int q = 0; q < PER; ++q)
-    if (x0 + q < x1) at[q] = s.before[bucket[q]] + (at[q] - s.seg_mass[bucket[q]]);
-  const auto rank = [&](int q) { return s.count_before[bucket[q]] + (uint32_t)(x0 + q) - s.seg_at[bucket[q]]; };
+    for (int q = kRuns - 1; q > 0; --q)          // buckets between the runs have no bins
+      if (b >= c.runs.from[q]) {
+        at = b - c.runs.from[q];
+#pragma unroll
+        for (int e = 0; e < q; ++e)
+          if (c.runs.from[e] <= c.runs.to[e]) at += c.runs.to[e] - c.runs.from[e] + 1;
+        break;
+      } else if (q == 1) {
+        at = b - c.runs.from[0];
+      }
+    const double d = degrees(r, v);
+    const int sub = b == 0 ? 0 : min((int)((1.0 - (d - floor(d))) * (1 << sub_bits)), (1 << sub_bits) - 1), bin = at << sub_bits | sub;
+    s.bin[x] = (uint16_t)bin;
+    const double w = weight(r, k);
+    const unsigned long long m = (unsigned long long)(w * 0x1p50 + 0.5);
+    atomicAdd(&s.bin_count[bin], 1u);
+    atomicAdd(&s.bin_mass[bin], m);
+    if (b >= s.m0 && b <= s.m1 && w >= r.min_p) likely += m;
+  }
+  if (likely) atomicAdd(&s.likely, likely);
+  __syncthreads();
+  const uint32_t count = s.bin_count[tid];
+  const double mass = (double)s.bin_mass[tid] * 0x1p-50;
+  uint32_t all;
+  const uint32_t first = scan_counts(count, all, s.counts);
+  double to = mass;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const double u = __shfl_up(to, o);
+    if (lane >= o) to += u;
+  }
+  if (lane == 63) s.sums[wave] = to;
+  __syncthreads();
+  double from = to - mass;
+#pragma unroll
+  for (int w = 0; w < kPickThreads / 64; ++w)
+    if (w < wave) from += s.sums[w];
+  s.bin_from[tid] = from, s.bin_first[tid] = first;
+  __syncthreads();
+  // the bin's bucket, and what is in front of the bin: of the bucket in the row, and of the bin in the bucket
+  int at = tid >> sub_bits, bucket = -1;
+#pragma unroll
+  for (int q = 0; q < kRuns; ++q) {
+    const int len = c.runs.to[q] - c.runs.from[q] + 1;
+    if (c.runs.from[q] > c.runs.to[q] || bucket >= 0) continue;
+    if (at < len) bucket = c.runs.from[q] + at;
+    at -= len;
+  }
+  const int head = tid >> sub_bits << sub_bits;
+  const double in_bucket = from - s.bin_from[head];
+  const uint32_t first_in = first - s.bin_first[head];
+  __syncthreads();
+  const double before = bucket < 0 ? 0.0 : s.before[bucket] + fmax(in_bucket, 0.0);
+  const uint32_t count_before = bucket < 0 ? 0 : s.count_before[bucket] + first_in;
+  s.bin_from[tid] = before, s.bin_first[tid] = count_before;
+
   // what is kept is a first part of the order, and so is what each bound leaves: the least of their masses
-  double kept = s.total;
-  const bool least = s.mlo >= fmin(s.khi, fmin(s.phi, s.total)), other = s.mhi <= fmin(s.klo, fmin(s.plo, s.total));
-  // (of a thread's tokens the last one that a bound leaves; `m` is none of them)
-  const auto bound = [&](double m, auto holds) {
-    bool some = false;
-    double v = m;
-#pragma unroll
-    for (int q = 0; q < PER; ++q)
-      if (x0 + q < x1 && holds(q)) some = true, v = fmax(v, at[q] + w[q]);
-    return end_of<THREADS, false>(some, v, m, s.sums);
+  const auto choose = [&](int which, bool holds) {
+    const unsigned long long b = __ballot(count && holds);
+    if (b && lane == 63 - __builtin_clzll(b)) atomicMax(&s.chosen[which], tid);
+    __syncthreads();
+    return s.chosen[which];
   };
-  if (s.k >= 0 && !other) kept = bound(s.klo, [&](int q) { return bucket[q] == s.k && rank(q) < r.top_k; });
-  if (r.top_p < 1.0 && !other) {
-    const double mass = r.top_p * kept;
-    kept = bound(s.plo, [&](int q) { return bucket[q] >= s.p0 && bucket[q] <= s.p1 && (at[q] < mass || rank(q) == 0); });
+  double kept = s.total;
+  if (s.k >= 0 && !c.other) {
+    const int bin = choose(0, bucket == s.k && count_before < r.top_k);
+    kept = bin < 0 ? s.klo : resolve<DT>(a, t, r, s, n, bin, (double)r.top_k, kByCount, 1.0);
   }
-  if (s.m1 >= 0 && !least)
-    kept = fmin(kept, bound(s.mlo, [&](int q) { return bucket[q] >= s.m0 && bucket[q] <= s.m1 && (w[q] >= r.min_p || rank(q) == 0); }));
+  if (r.top_p < 1.0 && !c.other) {
+    const double target = r.top_p * kept;
+    const int bin = choose(1, bucket >= s.p0 && bucket <= s.p1 && (before < target || count_before == 0));
+    kept = bin < 0 ? s.plo : resolve<DT>(a, t, r, s, n, bin, target, kByMass, 1.0);
+  }
+  if (s.m1 >= 0 && !c.least) kept = fmin(kept, r.min_p > 1.0 ? 1.0 : s.mlo + (double)s.likely * 0x1p-50);
   const double drawn = r.u * kept;
-  // the first that goes beyond it (or the last there is, if only the sums' rounding keeps that from it)
-  constexpr double kNone = 1e9;
-  double first = kNone, last = -1;
-#pragma unroll
-  for (int q = 0; q < PER; ++q)
-    if (x0 + q < x1 && bucket[q] >= s.u0 && bucket[q] <= s.u1) {
-      last = x0 + q;
-      if (at[q] + w[q] > drawn) first = fmin(first, x0 + q);
-    }
-  first = end_of<THREADS, true>(first < kNone, first, kNone, s.sums);
-  if (first == kNone) first = end_of<THREADS, false>(last >= 0, last, 0.0, s.sums);
-  const int x = (int)first;
-  if (x >= x0 && x < x1) {
-    const unsigned long long it = s.list[x];
-    a.tokens[t] = (int)(uint32_t)it;
-    if (a.probs) a.probs[t] = (float)(weight(r, ~(uint32_t)(it >> 32)) / kept);
-  }
+  const int bin = choose(2, bucket >= s.u0 && bucket <= s.u1 && (before <= drawn || count_before == s.count_before[s.u0]));
+  if (bin >= 0) resolve<DT>(a, t, r, s, n, bin, drawn, kByDraw, kept);
 }
 
 template <int DT>
-__global__ __launch_bounds__(kPickThreads) void sample_rows_kernel(SampleArgs a, const PartHead* heads, const unsigned long long* hists, int parts, int part_size) {
+__global__ __launch_bounds__(kPickThreads) void sample_rows_kernel(SampleArgs a, Parts left, int parts, int part_size) {
+  typedef typename Left<DT>::type Token;
   extern __shared__ char shared[];
   RowShared& s = *(RowShared*)shared;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t t = blockIdx.x;
-  unsigned long long top = 0;
-  for (int c = tid; c < parts; c += kPickThreads) {
-    const unsigned long long u = heads[t * parts + c].top;
-    if (u > top) top = u;
-  }
+  const int64_t t = blockIdx.x, row = t * parts;
+  PartHead head = {};
+  if (tid < parts) head = left.heads[row + tid];
+  RowSetting r = row_setting(a, t);
+  unsigned long long top = head.top;
+#pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
     const unsigned long long u = __shfl_xor(top, o);
     if (u > top) top = u;
   }
   if (lane == 0) s.tops[wave] = top;
   if (tid == 0) {
-    s.n = s.parts = s.dropped = s.runs = 0;
+    s.n = s.parts = 0;
     s.k = -1, s.p0 = s.m0 = s.u0 = 0, s.m1 = -1, s.u1 = kBuckets - 1;
     s.klo = s.khi = s.phi = s.mlo = s.mhi = INFINITY;
+    s.p1 = r.top_p < 1.0 ? kBuckets - 1 : -1, s.plo = r.top_p < 1.0 ? 0.0 : INFINITY;
   }
   __syncthreads();
-  for (int w = 0; w < kPickThreads / 64; ++w)
-    if (s.tops[w] > top) top = s.tops[w];
+  top = s.tops[0];
+  if (parts > 64 && s.tops[1] > top) top = s.tops[1];
   const uint32_t key = (uint32_t)(top >> 32);
-  const RowSetting r = row_setting(a, t, key);
   if (key <= kKeyNone || r.greedy) {
     if (tid == 0) {
       a.tokens[t] = key <= kKeyNone ? -1 : (int)~(uint32_t)top;
@@ -548,19 +719,18 @@ __global__ __launch_bounds__(kPickThreads) void sample_rows_kernel(SampleArgs a,
     return;
   }
   const float largest = key_value(key);
+  r.top = key, r.largest = (double)largest;
   const bool infinite = largest == __builtin_inff();
   const double most = infinite ? 0.0 : degrees(r, largest), base = floor(most), frac = most - base;
-
   const auto bucket_of = [&](float x) { return x == largest ? 0 : 1 + (int)fmin(base - floor(degrees(r, x)), (double)kBuckets); };
 
-  for (int c = tid; c < parts; c += kPickThreads) {
-    const PartHead h = heads[t * parts + c];
-    const float its = key_value((uint32_t)(h.top >> 32));
+  if (tid < parts) {
+    const float its = key_value((uint32_t)(head.top >> 32));
     const bool none = its == -__builtin_inff() || (infinite && its != largest);
     const int b = none ? kBuckets : min(bucket_of(its), kBuckets);
     const double d = degrees(r, its);
-    s.part_top[c] = b, s.part_equal[c] = (uint32_t)h.equal;
-    s.part_extra[c] = b == 0 || none ? 0 : (uint32_t)h.equal * (unsigned long long)(sixteenth(d - floor(d)) * (double)(1ull << kFracBits) + 0.5);
+    s.part_top[tid] = b, s.part_equal[tid] = none ? 0 : head.equal, s.part_stored[tid] = head.stored;
+    s.part_extra[tid] = b == 0 || none ? 0 : head.equal * (unsigned long long)(sixteenth(d - floor(d)) * (double)(1ull << kFracBits) + 0.5);
   }
   __syncthreads();
 
@@ -569,13 +739,13 @@ __global__ __launch_bounds__(kPickThreads) void sample_rows_kernel(SampleArgs a,
   unsigned long long extra = 0;
   if (tid < kBuckets) {
     constexpr int U = 8;
-    const unsigned long long* row = hists + t * parts * kBuckets;
+    const unsigned long long* hists = left.hists + row * kBuckets;
     for (int c0 = 0; c0 < parts; c0 += U) {
       unsigned long long h[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int c = c0 + u, shift = c < parts && !infinite ? max(s.part_top[c], 1) : kBuckets;
-        h[u] = tid >= shift ? row[(int64_t)c * kBuckets + tid - shift] : 0;
+        h[u] = tid >= shift ? hists[(int64_t)c * kBuckets + tid - shift] : 0;
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
@@ -590,6 +760,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_rows_kernel(SampleArgs a,
                                : ((double)count + (double)extra * (1.0 / (double)(1ull << kFracBits))) * exp2(-(tid - 1 + frac) / kPerOctave);
   uint32_t count_to = count;
   double upto = mass;
+#pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
     const uint32_t uc = __shfl_up(count_to, o);
     const double um = __shfl_up(upto, o);
@@ -599,6 +770,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_rows_kernel(SampleArgs a,
   __syncthreads();
   double wave_before = 0, total = 0;
   uint32_t waves_count = 0;
+#pragma unroll
   for (int w = 0; w < kBuckets / 64; ++w) {
     if (w == wave) wave_before = total;
     if (w < wave) waves_count += s.counts[w];
@@ -609,123 +781,109 @@ __global__ __launch_bounds__(kPickThreads) void sample_rows_kernel(SampleArgs a,
   const double before = lane ? wave_before + inside : wave_before;
   upto += wave_before, count_to += waves_count;
   if (tid < kBuckets) s.before[tid] = before, s.count_before[tid] = count_to - count;
-  if (tid == 0) s.total = total, s.p1 = r.top_p < 1.0 ? kBuckets - 1 : -1, s.plo = r.top_p < 1.0 ? 0.0 : INFINITY;
-  __syncthreads();
-  choose_buckets(r, s, before, upto, count_to - count, count_to, frac);
+  if (tid == 0) s.total = total;
+  const Choice c = choose_buckets(r, s, before, upto, count_to - count, count_to, frac);
 
-  // parts that have tokens of those buckets
-  for (int c = wave; c < parts; c += kPickThreads / 64) {
-    const int top_bucket = s.part_top[c], shift = max(top_bucket, 1);
+  // Tokens of those buckets: of each part runs of what the first launch has left in order.
+  for (int p = wave; p < parts; p += kPickThreads / 64) {
+    const int top_bucket = s.part_top[p], shift = max(top_bucket, 1), stored = s.part_stored[p], equal = (int)s.part_equal[p];
     if (top_bucket >= kBuckets) continue;
-    bool some = flagged(s, top_bucket);
+    const uint16_t* starts = left.starts + (row + p) * kBuckets;
+    const Token* tokens = (const Token*)left.left + (row + p) * kStored;
+    int begin[kRuns], end[kRuns];
+    bool again = false;
 #pragma unroll
-    for (int o = lane; o < kBuckets; o += 64)
-      if (flagged(s, o) && o >= shift && !infinite && hists[(t * parts + c) * kBuckets + o - shift]) some = true;
-    if (__any(some) && lane == 0) s.part_list[atomicAdd(&s.parts, 1u)] = c;
-  }
-  __syncthreads();
-  // Runs of such buckets as bounds of the logits, with room for rounding: tokens are taken by these, and those that are of other
-  // buckets after all left out afterwards.
-  if (tid < kBuckets && flagged(s, tid)) {
-    const bool from = tid == 0 || !flagged(s, tid - 1), to = tid == kBuckets - 1 || !flagged(s, tid + 1);
-    uint32_t run = 0;
-    for (int b = 0; b < kBuckets / 64; ++b) {            // runs that begin in front of this one, or with it
-      const unsigned long long f = s.flags[b], starts = f & ~(f << 1 | (b ? s.flags[b - 1] >> 63 : 0));
-      if (b * 64 <= tid) run += __popcll(tid - b * 64 >= 63 ? starts : starts & ((2ull << (tid - b * 64)) - 1));
-    }
-    const bool bounded = r.grid > 0 && !infinite;
-    if (run <= kRuns) {
-      if (from) {
-        const double x = (base - tid + 2) / r.grid;
-        s.upper[run - 1] = bounded && tid ? (float)(x + fabs(x) * 1e-6 + 1e-37) : INFINITY;
+    for (int q = 0; q < kRuns; ++q) {
+      const int from = c.runs.from[q], to = c.runs.to[q];
+      const bool ties = from <= top_bucket && top_bucket <= to;
+      const int o0 = max(from - shift, 0), o1 = infinite ? -1 : to - shift;
+      begin[q] = end[q] = 0;
+      if (from > to) continue;
+      if (o0 <= o1) {
+        begin[q] = starts[o0];
+        end[q] = starts[o1 + 1];                 // (o1 is the last bucket but one at most)
+        if (o1 >= stored) again = true;
       }
-      if (to) {
-        const double x = (base - max(tid, 1) + 1) / r.grid;
-        s.lower[run - 1] = bounded ? (float)(x - fabs(x) * 1e-6 - 1e-37) : -3.4028234e38f;
+      if (ties) {
+        if (o0 > o1) end[q] = equal;
+        begin[q] = 0;
+        if (stored < 0) again = true;
       }
     }
-    if (to) atomicMax(&s.runs, run);
+    if (again) {
+      if (lane == 0) s.part_list[atomicAdd(&s.parts, 1u)] = p;
+      continue;
+    }
+#pragma unroll
+    for (int q = 0; q < kRuns; ++q) {
+      const int m = end[q] - begin[q];
+      if (m <= 0) continue;
+      uint32_t place = 0;
+      if (lane == 0) place = atomicAdd(&s.n, (uint32_t)m);
+      place = __builtin_amdgcn_readfirstlane(place);
+      for (int x = lane; x < m && place + x < kList; x += 64) {
+        const Token v = tokens[begin[q] + x];
+        s.list[place + x] = (unsigned long long)~Left<DT>::key(v) << 32 | (uint32_t)(p * part_size + Left<DT>::at(v));
+      }
+    }
   }
   __syncthreads();
-  const int runs = (int)s.runs;                  // (never more than kRuns: those of top_k, top_p, min_p and the draw)
-  const float lo0 = s.lower[0], hi0 = s.upper[0], lo1 = runs > 1 ? s.lower[1] : INFINITY, hi1 = runs > 1 ? s.upper[1] : -INFINITY;
+  // Parts that had no room for all of them are read again.
   const int per_part = part_size / 512, pieces = (int)s.parts * per_part;
-  constexpr int U = DT == MDBF_F32 ? 2 : 4;
-  for (int p0 = wave; p0 < pieces; p0 += U * (kPickThreads / 64)) {
-    Raw8<DT> raw[U];
-    int at[U], there[U];
+  for (int p0 = wave; p0 < pieces; p0 += kPickThreads / 64) {
+    const int at = (int)s.part_list[p0 / per_part] * part_size + (p0 % per_part) * 512 + lane * 8, there = a.vocab - at;
+    if (there <= 0) continue;
+    Raw8<DT> raw;
+    float x[8];
+    load_raw8<DT>(a.logits, t * a.ld + at, there, raw);
+    to_float8<DT>(raw, x);
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int p = p0 + u * (kPickThreads / 64);
-      at[u] = there[u] = 0;
-      if (p < pieces) {
-        at[u] = (int)s.part_list[p / per_part] * part_size + (p % per_part) * 512 + lane * 8;
-        there[u] = a.vocab - at[u];
-        if (there[u] > 0) load_raw8<DT>(a.logits, t * a.ld + at[u], there[u], raw[u]);
-      }
-    }
+    for (int e = 0; e < 8; ++e) {
+      if (e >= there || !(x[e] > -__builtin_inff()) || (infinite && x[e] != largest)) continue;
+      const int b = bucket_of(x[e]);
+      bool take = false;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      float x[8];
-      to_float8<DT>(raw[u], x);
-      uint32_t mask = 0;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) mask |= (uint32_t)((x[e] >= lo0 && x[e] <= hi0) || (x[e] >= lo1 && x[e] <= hi1)) << e;
-      for (int q = 2; q < runs; ++q) {
-        const float lo = s.lower[q], hi = s.upper[q];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) mask |= (uint32_t)(x[e] >= lo && x[e] <= hi) << e;
-      }
-      mask &= there[u] >= 8 ? 255u : there[u] > 0 ? (1u << there[u]) - 1 : 0u;
-      if (!mask) continue;
-      uint32_t n = atomicAdd(&s.n, (uint32_t)__popc(mask));
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (mask >> e & 1) {
-          if (n < kList) s.list[n] = (unsigned long long)~order_key(x[e]) << 32 | (uint32_t)(at[u] + e);
-          ++n;
-        }
+      for (int q = 0; q < kRuns; ++q) take |= b >= c.runs.from[q] && b <= c.runs.to[q];
+      if (!take || b >= kBuckets) continue;
+      const uint32_t n = atomicAdd(&s.n, 1u);
+      if (n < kList) s.list[n] = (unsigned long long)~order_key(x[e]) << 32 | (uint32_t)(at + e);
     }
   }
   __syncthreads();
-  const int taken = (int)s.n;
-  for (int x = tid; x < min(taken, kList); x += kPickThreads) {
-    const float v = key_value(~(uint32_t)(s.list[x] >> 32));
-    const int b = infinite && v != largest ? kBuckets : bucket_of(v);
-    if (b >= kBuckets || !flagged(s, b)) s.list[x] = ~0ull, atomicAdd(&s.dropped, 1u);   // (goes to the end)
-  }
-  __syncthreads();
-  const int n = taken - (int)s.dropped;
-  if (taken > kList || n == 0) {
+  const int n = (int)s.n;
+  if (n > kList || n == 0) {
     __syncthreads();
     sample_digits<DT>(a, t, r, *(PickShared*)shared);
     return;
   }
-  if (taken <= 64) {
-    if (wave == 0) pick<64, 1>(a, t, r, s, taken, n, bucket_of);
-  } else if (taken <= kPickThreads) {
-    pick<kPickThreads, 1>(a, t, r, s, taken, n, bucket_of);
-  } else {
-    pick<kPickThreads, kList / kPickThreads>(a, t, r, s, taken, n, bucket_of);
-  }
+  pick<DT>(a, t, r, s, n, c, bucket_of);
 }
 
 constexpr int kPartLeast = kPartThreads * 8, kPartMost = kPartThreads * 16;
 static size_t sample_ws_bytes(int T, int vocab) {
   const size_t parts = ((size_t)vocab + kPartLeast - 1) / kPartLeast;
-  return (size_t)T * parts * (sizeof(PartHead) + kBuckets * 8);
+  return (size_t)T * parts * (sizeof(PartHead) + kBuckets * 10 + kStored * 8);
 }
 
 template <int DT>
 static int launch_sample(const SampleArgs& a, void* ws, hipStream_t s) {
-  // parts of 8192 tokens where that leaves compute units idle, else of 16384
-  const int part = (int64_t)a.T * ((a.vocab + kPartMost - 1) / kPartMost) < 512 ? kPartLeast : kPartMost;
+  // parts of 8192 tokens, as many as what is left in order has room for, where that leaves compute units idle or they are fp32; else of 16384
+  const int part = DT == MDBF_F32 || (int64_t)a.T * ((a.vocab + kPartMost - 1) / kPartMost) < 512 ? kPartLeast : kPartMost;
   const int parts = (a.vocab + part - 1) / part;
-  PartHead* heads = (PartHead*)ws;
-  unsigned long long* hists = (unsigned long long*)(heads + (size_t)a.T * parts);
+  const size_t all = (size_t)a.T * parts;
+  Parts left;
+  left.left = (char*)ws;
+  left.hists = (unsigned long long*)(left.left + all * kStored * sizeof(typename Left<DT>::type));
+  left.heads = (PartHead*)(left.hists + all * kBuckets);
+  left.starts = (uint16_t*)(left.heads + all);
+  constexpr int staged = kStored * (int)sizeof(typename Left<DT>::type);
   static KernelSetup setup;
   const int e = kernel_setup(setup, [] {
-    return hipFuncSetAttribute((const void*)sample_rows_kernel<DT>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(RowShared));
+    hipError_t e = hipFuncSetAttribute((const void*)sample_rows_kernel<DT>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(RowShared));
+    if (e == hipSuccess) e = hipFuncSetAttribute((const void*)sample_parts_kernel<DT, 8>, hipFuncAttributeMaxDynamicSharedMemorySize, staged);
+    if (e == hipSuccess && DT != MDBF_F32)
+      e = hipFuncSetAttribute((const void*)sample_parts_kernel<DT, DT == MDBF_F32 ? 8 : 16>, hipFuncAttributeMaxDynamicSharedMemorySize, staged);
+    return e;
   });
   if (e) return e;
   // (the grid's second dimension ends at 65535 rows)
@@ -736,14 +894,12 @@ static int launch_sample(const SampleArgs& a, void* ws, hipStream_t s) {
     const auto from = [&](auto* p) { return p ? p + t0 : p; };
     b.temperature = from(a.temperature), b.top_p = from(a.top_p), b.min_p = from(a.min_p), b.u = from(a.u), b.top_k = from(a.top_k);
     b.tokens = from(a.tokens), b.probs = from(a.probs);
-    if (part == kPartLeast) sample_parts_kernel<DT, 8><<<dim3(parts, b.T), kPartThreads, 0, s>>>(b, heads, hists);
-    else sample_parts_kernel<DT, 16><<<dim3(parts, b.T), kPartThreads, 0, s>>>(b, heads, hists);
-    sample_rows_kernel<DT><<<b.T, kPickThreads, sizeof(RowShared), s>>>(b, heads, hists, parts, part);
+    if (part == kPartLeast) sample_parts_kernel<DT, 8><<<dim3(parts, b.T), kPartThreads, staged, s>>>(b, left);
+    else sample_parts_kernel<DT, DT == MDBF_F32 ? 8 : 16><<<dim3(parts, b.T), kPartThreads, staged, s>>>(b, left);
+    sample_rows_kernel<DT><<<b.T, kPickThreads, sizeof(RowShared), s>>>(b, left, parts, part);
   }
   return (int)hipGetLastError();
 }
-
-
 
 }  // namespace mdbf
 
