@@ -281,7 +281,7 @@ __device__ __forceinline__ uint32_t scan_counts(uint32_t v, uint32_t& total, uin
 }
 
 template <int DT, int EPT>
-__global__ __launch_bounds__(kPartThreads) void sample_parts_kernel(SampleArgs a, Parts parts) {
+__global__ __launch_bounds__(kPartThreads, 8) void sample_parts_kernel(SampleArgs a, Parts parts) {
   typedef typename Left<DT>::type Token;
   extern __shared__ char staged[];
   Token* order = (Token*)staged;
@@ -624,24 +624,29 @@ __device__ __forceinline__ void pick(const SampleArgs& a, int64_t t, const RowSe
     atomicAdd(&s.bin_mass[bin], m);
     if (b >= s.m0 && b <= s.m1 && w >= r.min_p) likely += m;
   }
-  if (likely) atomicAdd(&s.likely, likely);
+  if (s.m1 >= 0 && !c.least) {
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) likely += __shfl_xor(likely, o);
+    if (lane == 0 && likely) atomicAdd(&s.likely, likely);
+  }
   __syncthreads();
   const uint32_t count = s.bin_count[tid];
   const double mass = (double)s.bin_mass[tid] * 0x1p-50;
-  uint32_t all;
-  const uint32_t first = scan_counts(count, all, s.counts);
+  uint32_t first = count;
   double to = mass;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
-    const double u = __shfl_up(to, o);
-    if (lane >= o) to += u;
+    const uint32_t uc = __shfl_up(first, o);
+    const double um = __shfl_up(to, o);
+    if (lane >= o) first += uc, to += um;
   }
-  if (lane == 63) s.sums[wave] = to;
+  if (lane == 63) s.sums[wave] = to, s.counts[wave] = first;
   __syncthreads();
   double from = to - mass;
+  first -= count;
 #pragma unroll
   for (int w = 0; w < kPickThreads / 64; ++w)
-    if (w < wave) from += s.sums[w];
+    if (w < wave) from += s.sums[w], first += s.counts[w];
   s.bin_from[tid] = from, s.bin_first[tid] = first;
   __syncthreads();
   // the bin's bucket, and what is in front of the bin: of the bucket in the row, and of the bin in the bucket
@@ -738,7 +743,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_rows_kernel(SampleArgs a,
   uint32_t count = 0;
   unsigned long long extra = 0;
   if (tid < kBuckets) {
-    constexpr int U = 8;
+    constexpr int U = 16;
     const unsigned long long* hists = left.hists + row * kBuckets;
     for (int c0 = 0; c0 < parts; c0 += U) {
       unsigned long long h[U];
