@@ -659,12 +659,21 @@ def _here(*tensors):
         assert t is None or t.get_device() == dev, "tensors of the current device are needed"
 
 
-def _rows_of(x, n=None):
-    """Row stride of a matrix whose rows' elements lie side by side."""
+def _rows_of(x, rows, cols):
+    """Row stride of a matrix (rows x cols) whose rows' elements lie side by side."""
     ld, one = x.stride()
-    rows, cols = x.shape
-    assert (one == 1 or cols == 1) and (n is None or cols == n), "a matrix with contiguous rows is needed"
+    assert one == 1 or cols == 1, "a matrix with contiguous rows is needed"
     return ld if ld >= cols or rows > 1 else cols
+
+
+def _matrix(like, shape, dtype, stream):
+    """A result of a call on `stream`, on the device of `like`."""
+    if stream is None:
+        return like.new_empty(shape, dtype=dtype)
+    return _result(lambda: like.new_empty(shape, dtype=dtype), stream)
+
+
+_Y_CODE = dict(DTYPE_CODE, e4m3=MDBF_E4M3)
 
 
 @functools.lru_cache(maxsize=256)
@@ -678,45 +687,56 @@ def mdbf_add_norm(x, residual=None, weight=None, eps=1e-6, y_dtype=None, scale_g
     (y, h, scales): h of the residual's type (None without residual), scales None but for e4m3; residual_out (may be the residual), out and
     scales are used where given."""
     torch = _torch()
-    T, n = x.shape
+    shape = x.shape
+    T, n = shape
     name = _DTYPE_NAME[x.dtype]
-    y_dtype = y_dtype or (name if out is None else "e4m3" if out.dtype == torch.float8_e4m3fn else _DTYPE_NAME[out.dtype])
-    eight = y_dtype == "e4m3"
     if out is None:
-        out = _result(lambda: torch.empty((T, n), dtype=_TORCH_DTYPE[y_dtype], device=x.device), stream)
+        y_dtype = y_dtype or name
+        out, ldy = _matrix(x, shape, _TORCH_DTYPE[y_dtype], stream), n
     else:
-        assert out.shape == (T, n) and out.dtype == _TORCH_DTYPE[y_dtype]
-    h_name, ldr, ldro = name, 0, 0
+        y_dtype = y_dtype or ("e4m3" if out.dtype == torch.float8_e4m3fn else _DTYPE_NAME[out.dtype])
+        assert out.shape == shape and out.dtype == _TORCH_DTYPE[y_dtype]
+        ldy = _rows_of(out, T, n)
+    h_name, ldr, ldro, lds, r_ptr, ro_ptr, s_ptr, w_ptr = name, 0, 0, 0, None, None, None, None
     if residual is not None:
-        assert residual.shape == (T, n)
-        h_name, ldr = _DTYPE_NAME[residual.dtype], _rows_of(residual)
+        assert residual.shape == shape
+        h_dtype = residual.dtype
+        h_name, ldr, r_ptr = _DTYPE_NAME[h_dtype], _rows_of(residual, T, n), residual.data_ptr()
         if residual_out is None:
-            residual_out = _result(lambda: torch.empty((T, n), dtype=residual.dtype, device=x.device), stream)
+            residual_out, ldro = _matrix(x, shape, h_dtype, stream), n
         else:
-            assert residual_out.shape == (T, n) and residual_out.dtype == residual.dtype
-        ldro = _rows_of(residual_out)
+            assert residual_out.shape == shape and residual_out.dtype == h_dtype
+            ldro = _rows_of(residual_out, T, n)
+        ro_ptr = residual_out.data_ptr()
     else:
         assert residual_out is None, "residual_out needs a residual"
-    lds = 0
-    if eight:
-        shape, dtype = ((T, -(-n // 32)), torch.uint8) if scale_group else ((T, 1), torch.float32)
+    if y_dtype == "e4m3":
+        columns, dtype = (-(-n // 32), torch.uint8) if scale_group else (1, torch.float32)
         if scales is None:
-            scales = _result(lambda: torch.empty(shape, dtype=dtype, device=x.device), stream)
+            scales = _matrix(x, (T, columns), dtype, stream)
         else:
-            assert scales.shape == shape and scales.dtype == dtype
-        lds = _rows_of(scales)
+            assert scales.shape == (T, columns) and scales.dtype == dtype
+        lds, s_ptr = _rows_of(scales, T, columns), scales.data_ptr()
     else:
         assert scales is None, "scales go with e4m3"
-    assert weight is None or _ints(weight, n, torch.float32), "the weight is n fp32"
+    if weight is not None:
+        assert _ints(weight, n, torch.float32), "the weight is n fp32"
+        w_ptr = weight.data_ptr()
     _here(x, residual, weight, residual_out, out, scales)
-    desc = _norm_desc(n, DTYPE_CODE[name], DTYPE_CODE[h_name], MDBF_E4M3 if eight else DTYPE_CODE[y_dtype], scale_group, eps)
-    status = (_lib or lib()).mdbf_add_norm(
-        desc, x.data_ptr(), _rows_of(x), None if residual is None else residual.data_ptr(), ldr, None if weight is None else weight.data_ptr(), T,
-        None if residual_out is None else residual_out.data_ptr(), ldro, out.data_ptr(), _rows_of(out), None if scales is None else scales.data_ptr(),
-        lds, _stream_ptr(stream))
+    desc = _norm_desc(n, DTYPE_CODE[name], DTYPE_CODE[h_name], _Y_CODE[y_dtype], scale_group, eps)
+    status = (_lib or lib()).mdbf_add_norm(desc, x.data_ptr(), _rows_of(x, T, n), r_ptr, ldr, w_ptr, T, ro_ptr, ldro, out.data_ptr(), ldy, s_ptr, lds,
+                                           _stream_ptr(stream))
     if status:
         _check(status, "mdbf_add_norm")
     return out, residual_out, scales
+
+
+@functools.lru_cache(maxsize=256)
+def _adapter_tiles(tokens, requests, adapters):
+    room = lib().mdbf_adapter_tiles(tokens, requests, adapters)
+    if room < 0:
+        _check(int(room), "mdbf_adapter_tiles")
+    return room
 
 
 class AdapterRows:
@@ -729,9 +749,7 @@ class AdapterRows:
         self.tokens, self.requests, self.adapters = tokens, requests, adapters
         self.rows, self.tiles, self.places = rows, tiles, None
         if rows is None or tiles is None:
-            room = (_lib or lib()).mdbf_adapter_tiles(tokens, requests, adapters)
-            if room < 0:
-                _check(int(room), "mdbf_adapter_tiles")
+            room = _adapter_tiles(tokens, requests, adapters)
             # (tiles first: their entries are read 16 bytes at a time)
             ints = _result(lambda: torch.empty(4 * room + tokens + requests, dtype=torch.int32, device=device), stream)
             self.tiles, self.rows, self.places = ints.split((4 * room, tokens, requests))
@@ -772,18 +790,21 @@ class Adapters:
         self.args = (A.data_ptr(), B.data_ptr(), None if scale is None else scale.data_ptr())
 
 
+_ADAPTER_LISTS = [AdapterDesc * count for count in range(MDBF_ADAPTER_MAX + 1)]
+
+
 def _adapter_list(rows, adapters, Xs, Ys):
     count, T = len(adapters), rows.tokens
-    assert 0 < count == len(Xs) == len(Ys)
-    arr = (AdapterDesc * count)()
+    assert 0 < count == len(Xs) == len(Ys) and count <= MDBF_ADAPTER_MAX
     dtype = adapters[0].A.dtype
-    for d, p, X, Y in zip(arr, adapters, Xs, Ys):
-        assert p.count == rows.adapters and p.A.dtype == X.dtype == dtype and X.shape == (T, p.n) and Y.shape == (T, p.m)
-        _here(X, Y, p.A, p.B, p.scale)
-        d.n, d.m, d.r, d.y_dtype = p.n, p.m, p.r, DTYPE_CODE[_DTYPE_NAME[Y.dtype]]
-        d.A_dev, d.B_dev, d.scale_dev = p.args
-        d.X_dev, d.ldx, d.Y_dev, d.ldy = X.data_ptr(), _rows_of(X), Y.data_ptr(), _rows_of(Y)
-    return arr, DTYPE_CODE[_DTYPE_NAME[dtype]]
+    tensors, descs = [rows.rows, rows.tiles], []
+    for p, X, Y in zip(adapters, Xs, Ys):
+        n, m = p.n, p.m
+        assert p.count == rows.adapters and p.A.dtype == X.dtype == dtype and X.shape == (T, n) and Y.shape == (T, m)
+        tensors += (X, Y, p.A, p.B, p.scale)
+        descs.append(AdapterDesc(n, m, p.r, DTYPE_CODE[_DTYPE_NAME[Y.dtype]], *p.args, X.data_ptr(), _rows_of(X, T, n), Y.data_ptr(), _rows_of(Y, T, m)))
+    _here(*tensors)
+    return _ADAPTER_LISTS[count](*descs), DTYPE_CODE[_DTYPE_NAME[dtype]]
 
 
 def mdbf_adapters_workspace(rows, adapters, Xs, Ys):
@@ -807,10 +828,11 @@ def mdbf_adapters(rows, adapters, Xs, Ys, workspace=None, stream=None):
     f16/bf16/f32.  Rows without an adapter stay as they are.  Returns Ys."""
     torch = _torch()
     arr, dtype = _adapter_list(rows, adapters, Xs, Ys)
-    _here(rows.rows, rows.tiles, workspace)
     if workspace is None:
         with _on(stream):
             workspace = torch.empty(_adapters_need(arr, dtype, rows), dtype=torch.uint8, device=Xs[0].device)
+    else:
+        _here(workspace)
     status = (_lib or lib()).mdbf_adapters(len(arr), arr, dtype, rows.adapters, rows.tokens, rows.rows.data_ptr(), rows.tiles.data_ptr(),
                                            rows.tiles.shape[0], workspace.data_ptr(), workspace.numel(), _stream_ptr(stream))
     if status:
@@ -853,7 +875,7 @@ def mdbf_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None,
     _here(logits, u, temperature, top_k, top_p, min_p, tokens, probs, workspace)
     desc = SampleDesc(*(None if s is None else s.data_ptr() for s in (temperature, top_k, top_p, min_p)))
     ws = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
-    status = (_lib or lib()).mdbf_sample(desc, logits.data_ptr(), _rows_of(logits), DTYPE_CODE[_DTYPE_NAME[logits.dtype]], T, vocab, u.data_ptr(),
+    status = (_lib or lib()).mdbf_sample(desc, logits.data_ptr(), _rows_of(logits, T, vocab), DTYPE_CODE[_DTYPE_NAME[logits.dtype]], T, vocab, u.data_ptr(),
                                          tokens.data_ptr(), probs.data_ptr(), *ws, _stream_ptr(stream))
     if status:
         _check(status, "mdbf_sample")

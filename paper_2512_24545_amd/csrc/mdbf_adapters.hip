@@ -5,8 +5,8 @@ namespace mdbf {
 
 // ---- rows by adapter ------------------------------------------------------------------------------------
 // A counting sort by one workgroup: tokens of each adapter (integer sums in LDS), a scan over the adapters for their first places and
-// tiles, then the requests in their order, 1024 at a time, each behind those of the same adapter in front of it.  The key
-// `adapters` stands for none and comes last.
+// tiles, then the requests in their order, 1024 at a time, each behind those of the same adapter in front of it: in its wave by a look at each
+// of the 64, then wave after wave.  The key `adapters` stands for none and comes last.
 constexpr int kRowThreads = 1024;
 constexpr int kRowMaxAdapters = 8192;     // three words each in LDS
 constexpr int kRowOneLaunch = 8192;       // rows, of up to kRowThreads requests, up to which the first launch writes them
@@ -41,11 +41,22 @@ __global__ __launch_bounds__(kRowThreads) void adapter_rows_kernel(RowArgs a) {
   __shared__ int32_t keys[kRowThreads], fresh[kRowThreads], first_row[kRowThreads + 1], first_place[kRowThreads];
   const int tid = threadIdx.x, N = a.adapters;
 
+  // a request's first row, rows and key
+  const auto request = [&](int i, int& from, int& f, int& k) {
+    const int asked = a.adapter[i];
+    from = cut(a.cu[i], a.T);
+    f = max(cut(a.cu[i + 1], a.T) - from, 0);
+    k = asked >= 0 && asked < N ? asked : N;
+  };
+  int from = 0, f = 0, k = N;
+  if (tid < a.requests) request(tid, from, f, k);
   for (int k = tid; k <= N; k += kRowThreads) count[k] = 0;
   __syncthreads();
-  for (int i = tid; i < a.requests; i += kRowThreads) {
-    const int f = cut(a.cu[i + 1], a.T) - cut(a.cu[i], a.T), k = a.adapter[i];
-    if (f > 0) atomicAdd(&count[k >= 0 && k < N ? k : N], (uint32_t)f);
+  if (f > 0) atomicAdd(&count[k], (uint32_t)f);
+  for (int i = tid + kRowThreads; i < a.requests; i += kRowThreads) {
+    int from_i, f_i, k_i;
+    request(i, from_i, f_i, k_i);
+    if (f_i > 0) atomicAdd(&count[k_i], (uint32_t)f_i);
   }
   __syncthreads();
 
@@ -83,25 +94,30 @@ __global__ __launch_bounds__(kRowThreads) void adapter_rows_kernel(RowArgs a) {
 
   for (int i0 = 0; i0 < a.requests; i0 += kRowThreads) {
     const int i = i0 + tid, n = min(a.requests - i0, kRowThreads);
-    __syncthreads();                       // the places of the requests before are in `place`, its readers are done
-    int from = 0, f = 0, k = N;
-    if (tid < n) {
-      from = cut(a.cu[i], a.T);
-      f = max(cut(a.cu[i + 1], a.T) - from, 0);
-      const int asked = a.adapter[i];
-      if (asked >= 0 && asked < N) k = asked;
-      keys[tid] = k, fresh[tid] = f, first_row[tid] = from;
+    if (i0) {                              // (the first ones' are in registers)
+      from = f = 0, k = N;
+      if (tid < n) request(i, from, f, k);
     }
-    __syncthreads();
+    keys[tid] = k, fresh[tid] = f, first_row[tid] = from;
     uint32_t mine = 0;
-    if (tid < n) {
-      mine = place[k];
-      for (int j = 0; j < tid; ++j) mine += keys[j] == k ? (uint32_t)fresh[j] : 0u;
-      a.places[i] = (int)mine;
-      first_place[tid] = (int)mine;
+    if ((tid & ~63) < n) {
+#pragma unroll
+      for (int j = 0; j < 63; ++j) {
+        const int kj = __builtin_amdgcn_readlane(k, j), fj = __builtin_amdgcn_readlane(f, j);
+        if (k == kj && (tid & 63) > j) mine += (uint32_t)fj;
+      }
     }
-    __syncthreads();
-    if (tid < n && f) atomicAdd(&place[k], (uint32_t)f);
+    __syncthreads();                       // (the tiles are out of `place`)
+    for (int w = 0; w * 64 < n; ++w) {
+      if (tid >> 6 == w && tid < n) {
+        mine += place[k];
+        a.places[i] = (int)mine;
+        first_place[tid] = (int)mine;
+      }
+      __syncthreads();
+      if (tid >> 6 == w && tid < n && f) atomicAdd(&place[k], (uint32_t)f);
+      __syncthreads();
+    }
   }
   if (!a.rows_here) return;
   // (up to kRowThreads requests, all of them in LDS)
