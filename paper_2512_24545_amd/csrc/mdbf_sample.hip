@@ -689,6 +689,59 @@ __device__ __forceinline__ void pick(const SampleArgs& a, int64_t t, const RowSe
   if (bin >= 0) resolve<DT>(a, t, r, s, n, bin, drawn, kByDraw, kept);
 }
 
+// The same on a list of up to 64 tokens, by one wave, which puts all of them in order.
+template <class Bucket>
+__device__ __forceinline__ void pick_few(const SampleArgs& a, int64_t t, const RowSetting& r, RowShared& s, int n, const Choice& c, const Bucket& bucket_of) {
+  const int lane = threadIdx.x;
+  const auto meet = [] {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+    __builtin_amdgcn_wave_barrier();
+  };
+  unsigned long long v = lane < n ? s.list[lane] : ~0ull;
+  int place = 0;
+  for (int j = 0; j < n; ++j) place += __shfl(v, j) < v;
+  if (lane < n) s.few[place] = v;
+  meet();
+  v = lane < n ? s.few[lane] : ~0ull;
+  const uint32_t key = ~(uint32_t)(v >> 32);
+  const bool in = lane < n;
+  const double w = in ? weight(r, key) : 0.0;
+  const int bucket = in ? bucket_of(key_value(key)) : kBuckets;
+  double to = w;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const double u = __shfl_up(to, o);
+    if (lane >= o) to += u;
+  }
+  // from a bucket's first token on, behind what is in front of the bucket in the row
+  const int neighbour = __shfl_up(bucket, 1);
+  const unsigned long long heads = __ballot(lane == 0 || bucket != neighbour);
+  const int head = 63 - __builtin_clzll(heads & (~0ull >> (63 - lane)));
+  const double at = in ? s.before[bucket] + (to - w - __shfl(to - w, head)) : 0.0;
+  const uint32_t rank = in ? s.count_before[bucket] + (uint32_t)(lane - head) : 0;
+  to = at + w;
+  const auto bound = [&](bool holds, double none) {
+    const unsigned long long b = __ballot(in && holds);
+    return b ? __shfl(to, 63 - __builtin_clzll(b)) : none;
+  };
+  double kept = s.total;
+  if (s.k >= 0 && !c.other) kept = bound(bucket == s.k && rank < r.top_k, s.klo);
+  if (r.top_p < 1.0 && !c.other) {
+    const double target = r.top_p * kept;
+    kept = bound(bucket >= s.p0 && bucket <= s.p1 && (at < target || rank == 0), s.plo);
+  }
+  if (s.m1 >= 0 && !c.least) kept = fmin(kept, bound(bucket >= s.m0 && bucket <= s.m1 && (w >= r.min_p || rank == 0), s.mlo));
+  const double drawn = r.u * kept;
+  const bool mine = in && bucket >= s.u0 && bucket <= s.u1;
+  const unsigned long long beyond = __ballot(mine && to > drawn), any = __ballot(mine);
+  // (none goes beyond it only by the sums' rounding: the last one then)
+  const int x = beyond ? __builtin_ctzll(beyond) : 63 - __builtin_clzll(any);
+  if (lane == x) {
+    a.tokens[t] = (int)(uint32_t)v;
+    if (a.probs) a.probs[t] = (float)(w / kept);
+  }
+}
+
 template <int DT>
 __global__ __launch_bounds__(kPickThreads) void sample_rows_kernel(SampleArgs a, Parts left, int parts, int part_size) {
   typedef typename Left<DT>::type Token;
@@ -861,7 +914,11 @@ __global__ __launch_bounds__(kPickThreads) void sample_rows_kernel(SampleArgs a,
     sample_digits<DT>(a, t, r, *(PickShared*)shared);
     return;
   }
-  pick<DT>(a, t, r, s, n, c, bucket_of);
+  if (n <= 64) {
+    if (wave == 0) pick_few(a, t, r, s, n, c, bucket_of);
+  } else {
+    pick<DT>(a, t, r, s, n, c, bucket_of);
+  }
 }
 
 constexpr int kPartLeast = kPartThreads * 8, kPartMost = kPartThreads * 16;
