@@ -211,51 +211,33 @@ __device__ void sample_digits(const SampleArgs& a, int64_t t, const RowSetting& 
 // where many are alike, bounds fall on borders between them.
 constexpr int kBuckets = 768;                    // of a row: the largest, then 767 sixteenths, down to 2^-47 of it; less weighs nothing
 constexpr int kPerOctave = 16;
-constexpr int kFracBits = 39;                    // of 2^(frac / 16) - 1 < 0.0443: 16384 of them stay below 2^49, where the count begins
+constexpr int kFracBits = 39;                    // of 2^(frac / 16) - 1 < 0.0443: a part's stay below 2^49, where the count begins
 constexpr int kCountBit = 49;
-constexpr int kStored = 8192;                    // tokens of a part that the first launch leaves in order; what needs more reads the part again
 constexpr int kList = 8192;                      // tokens of a row that the second launch looks at; rows that have more go by digits
-constexpr int kPartThreads = 1024;
+constexpr int kPartThreads = 512, kPart = 8192, kEach = kPart / kPartThreads;   // tokens of a part, of a thread
 constexpr double kSlack = 1e-9;                  // by which sums of buckets and of tokens may differ, and more
 
 struct PartHead {
-  unsigned long long top;                        // key of the part's largest, ~its index: the largest with the lowest index is the largest number
-  uint32_t equal;                                // tokens that equal it
-  int32_t stored;                                // buckets whose tokens are left in order; -1: not even the ones that equal the largest
-};
-// A token as the first launch leaves it: its logit as it lies and its place in the part, resp. key and place.
-template <int DT>
-struct Left {
-  typedef uint32_t type;
-  __device__ static type make(uint32_t raw, uint32_t key, uint32_t at) { return raw << 16 | at; }
-  __device__ static uint32_t key(type v) {
-    if (DT == MDBF_F16) return order_key((float)__builtin_bit_cast(_Float16, (uint16_t)(v >> 16)));
-    return order_key(__builtin_bit_cast(float, v & 0xffff0000u));
-  }
-  __device__ static uint32_t at(type v) { return v & 0xffffu; }
-};
-template <>
-struct Left<MDBF_F32> {
-  typedef unsigned long long type;
-  __device__ static type make(uint32_t raw, uint32_t key, uint32_t at) { return (unsigned long long)key << 32 | at; }
-  __device__ static uint32_t key(type v) { return (uint32_t)(v >> 32); }
-  __device__ static uint32_t at(type v) { return (uint32_t)v; }
+  unsigned long long top;                        // key of the part's largest, and, where that one is asked for, ~its index: of equal keys the lowest is largest
+  unsigned long long equal;                      // tokens that equal it
 };
 // What the first launch leaves, part by part.
 struct Parts {
   PartHead* heads;
   unsigned long long* hists;                     // kBuckets each
   uint16_t* starts;                              // kBuckets: where each bucket's tokens begin in what is left, or its end
-  char* left;                                    // kStored tokens each
+  uint16_t* left;                                // kPart: tokens in the order of their buckets, their places in the part
 };
 
 __device__ __forceinline__ double degrees(const RowSetting& r, float x) { return (double)x * r.grid; }
 
-// 2^(x / 16) - 1 for x in [0, 1): the exponential's series, to 6e-14
-__device__ __forceinline__ double sixteenth(double x) {
-  constexpr double q = 0.69314718055994530942 / kPerOctave;
-  constexpr double c1 = q, c2 = q * q / 2, c3 = q * q * q / 6, c4 = q * q * q * q / 24, c5 = q * q * q * q * q / 120, c6 = q * q * q * q * q * q / 720;
-  return x * fma(x, fma(x, fma(x, fma(x, fma(x, c6, c5), c4), c3), c2), c1);
+// What a token adds to its bucket: 1 in the count, and 2^(x / 16) - 1 in units of 2^-39 for x in [0, 1), the fraction of its t.  A polynomial through five
+// Chebyshev points, off by at most 2.6e-12; the sum with 2^52 and the count's bit has the whole number in its last bits.
+__device__ __forceinline__ unsigned long long bucket_word(double x) {
+  constexpr double unit = (double)(1ull << kFracBits);
+  const double g = fma(x, fma(x, fma(x, fma(x, 1.4997758288814042e-07 * unit, 1.3547982742839567e-05 * unit), 9.38385803440002e-04 * unit),
+                              0.04332169865857207 * unit), 2.528854437695519e-12 * unit + 0x1p52 + (double)(1ull << kCountBit));
+  return __builtin_bit_cast(unsigned long long, g) & 0xfffffffffffffull;
 }
 
 // sums of the threads in front of this one, and of all, over a workgroup of 1024
@@ -280,117 +262,120 @@ __device__ __forceinline__ uint32_t scan_counts(uint32_t v, uint32_t& total, uin
   return before + to - v;
 }
 
-template <int DT, int EPT>
-__global__ __launch_bounds__(kPartThreads, 8) void sample_parts_kernel(SampleArgs a, Parts parts) {
-  typedef typename Left<DT>::type Token;
-  extern __shared__ char staged[];
-  Token* order = (Token*)staged;
+template <int DT>
+__global__ __launch_bounds__(kPartThreads, 6) void sample_parts_kernel(SampleArgs a, Parts parts) {
+  __shared__ __align__(16) uint16_t order[kPart];
   __shared__ unsigned long long hist[kBuckets];
   __shared__ uint32_t slot[kBuckets];
-  __shared__ unsigned long long tops[kPartThreads / 64];
-  __shared__ uint32_t waves[kPartThreads / 64], equal, next_equal, fit, want, left;
+  __shared__ float tops[kPartThreads / 64];
+  __shared__ uint32_t waves[kPartThreads / 64], equal, next_equal, left, first;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t t = blockIdx.y, part = t * gridDim.x + blockIdx.x;
-  const int i0 = blockIdx.x * (kPartThreads * EPT);
+  const int i0 = blockIdx.x * kPart;
 
-  Raw8<DT> raw[EPT / 8];
+  Raw8<DT> raw[kEach / 8];
 #pragma unroll
-  for (int p = 0; p < EPT / 8; ++p) {
+  for (int p = 0; p < kEach / 8; ++p) {
     const int i = i0 + (p * kPartThreads + tid) * 8;
     if (i < a.vocab) load_raw8<DT>(a.logits, t * a.ld + i, a.vocab - i, raw[p]);
   }
-  RowSetting r = row_setting(a, t);
+  const RowSetting r = row_setting(a, t);
   for (int o = tid; o < kBuckets; o += kPartThreads) hist[o] = 0;
-  if (tid == 0) equal = next_equal = fit = want = left = 0;
-  float v[EPT], best = -__builtin_inff();
-  int at = 0x7fffffff;
+  if (tid == 0) equal = next_equal = left = 0, first = 0xffffffffu;
+  float v[kEach], best = -__builtin_inff();
 #pragma unroll
-  for (int p = 0; p < EPT / 8; ++p) {
-    const int i = i0 + (p * kPartThreads + tid) * 8;
+  for (int p = 0; p < kEach / 8; ++p) {
+    const int there = a.vocab - (i0 + (p * kPartThreads + tid) * 8);
     float x[8];
     to_float8<DT>(raw[p], x);
+    if (there < 8) {                             // (NaN, which nothing below counts)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float y = i + e < a.vocab && x[e] == x[e] ? x[e] : -__builtin_inff();
-      v[p * 8 + e] = y;
-      if (y > best) best = y, at = i + e;
+      for (int e = 0; e < 8; ++e)
+        if (e >= there) x[e] = __builtin_nanf("");
     }
-  }
-  unsigned long long top = (unsigned long long)order_key(best) << 32 | (uint32_t)~at;
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const unsigned long long u = __shfl_xor(top, o);
-    if (u > top) top = u;
+    for (int e = 0; e < 8; ++e) v[p * 8 + e] = x[e], best = fmaxf(best, x[e]);
   }
-  if (lane == 0) tops[wave] = top;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) best = fmaxf(best, __shfl_xor(best, o));
+  if (lane == 0) tops[wave] = best;
   __syncthreads();
+  float largest = tops[0];
 #pragma unroll
-  for (int w = 0; w < kPartThreads / 64; ++w)
-    if (tops[w] > top) top = tops[w];
-  const uint32_t key = (uint32_t)(top >> 32);
-  if (key <= kKeyNone || r.greedy) {
-    if (tid == 0) parts.heads[part].top = top;
+  for (int w = 1; w < kPartThreads / 64; ++w) largest = fmaxf(largest, tops[w]);
+  const auto place_of = [&](int e) { return (uint32_t)(((e / 8) * kPartThreads + tid) * 8 + e % 8); };
+  const uint32_t key = order_key(largest);
+  if (key <= kKeyNone || r.greedy) {             // then the first that equals it is all that is asked for
+    uint32_t at = 0xffffffffu;
+#pragma unroll
+    for (int e = kEach - 1; e >= 0; --e)
+      if (v[e] == largest) at = i0 + place_of(e);
+    atomicMin(&first, at);
+    __syncthreads();
+    if (tid == 0) parts.heads[part].top = (unsigned long long)key << 32 | ~first;
     return;
   }
-  const float largest = key_value(key);
   const bool infinite = largest == __builtin_inff();    // then nothing else weighs
   const double base = floor(degrees(r, largest));
   uint32_t alike = 0;
-  int down[EPT];                                 // a token's bucket; -1: of the part's largest
+  int down[kEach];                               // a token's bucket; -1: of the part's largest
 #pragma unroll
-  for (int e = 0; e < EPT; ++e) {
+  for (int e = 0; e < kEach; ++e) {
     const bool same = v[e] == largest;
     alike += (uint32_t)__popcll(__ballot(same));
     down[e] = same ? -1 : kBuckets;
-    if (infinite || same) continue;
     const double d = degrees(r, v[e]), f = floor(d), b = base - f;
-    if (b < kBuckets && v[e] > -__builtin_inff()) {
+    if (b < kBuckets && !same && !infinite) {           // (not of -inf, whose b is inf, and not of NaN)
       down[e] = (int)b;
-      // (the sum with 2^52 has the whole number in its last bits)
-      const double g = fma(sixteenth(d - f), (double)(1ull << kFracBits), 0x1p52);
-      atomicAdd(&hist[down[e]], __builtin_bit_cast(unsigned long long, g) - 0x4330000000000000ull + (1ull << kCountBit));
+      atomicAdd(&hist[down[e]], bucket_word(d - f));
     }
   }
   if (lane == 0 && alike) atomicAdd(&equal, alike);
   __syncthreads();
-  // how far tokens are left in order: as many as there is room for, and no further than the row's own bounds can reach
-  const uint32_t n_equal = equal, count = tid < kBuckets ? (uint32_t)(hist[tid] >> kCountBit) : 0;
-  uint32_t all;
-  const uint32_t start = n_equal + scan_counts(count, all, waves);
-  if (tid < kBuckets) {
-    parts.hists[part * kBuckets + tid] = hist[tid];
-    slot[tid] = start;
-  }
-  // (top_p of what top_k leaves goes by the mass of tokens below min_p too)
-  const bool below = r.min_p == 0.0 || (r.top_k && r.top_p < 1.0) || tid < 4.0 - kPerOctave * log2(r.min_p);
-  const bool reach = tid < kBuckets && below && (!r.top_k || start < r.top_k), fits = reach && start + count <= kStored;
-  const unsigned long long reached = __ballot(reach), fitted = __ballot(fits);      // (both hold for the first buckets alone)
-  if (lane == 0 && reached) atomicAdd(&want, (uint32_t)__popcll(reached));
-  if (lane == 0 && fitted) atomicAdd(&fit, (uint32_t)__popcll(fitted));
-  if (fitted && lane == 63 - __builtin_clzll(fitted)) atomicMax(&left, start + count);
-  __syncthreads();
-  const bool room = n_equal <= kStored;
-  const int limit = room ? (int)fit : -1;
-  if (tid == 0) parts.heads[part] = {top, n_equal, !room ? -1 : fit == want ? kBuckets : (int)fit};
-  if (!room) return;
-  const uint32_t n_left = max(left, n_equal);
-  if (tid < kBuckets) parts.starts[part * kBuckets + tid] = (uint16_t)min(start, n_left);
+  // Where each bucket's tokens begin, two buckets a thread, and how far they are left in order: no further than the row's own bounds can reach.
+  const uint32_t n_equal = equal;
+  const bool has = tid < kBuckets / 2;
+  const unsigned long long h0 = has ? hist[2 * tid] : 0, h1 = has ? hist[2 * tid + 1] : 0;
+  const uint32_t c0 = (uint32_t)(h0 >> kCountBit), c1 = (uint32_t)(h1 >> kCountBit);
+  uint32_t start = c0 + c1;
 #pragma unroll
-  for (int e = 0; e < EPT; ++e) {
-    if (down[e] >= limit) continue;
-    const uint32_t place = atomicAdd(down[e] < 0 ? &next_equal : &slot[down[e]], 1u);
-    const uint32_t mine = ((e / 8) * kPartThreads + tid) * 8 + e % 8;
-    const uint32_t w = raw[e / 8].w[DT == MDBF_F32 ? (e % 8) / 4 : 0][DT == MDBF_F32 ? e % 4 : (e % 8) / 2];
-    order[place] = Left<DT>::make(DT == MDBF_F32 ? w : w >> (16 * (e & 1)) & 0xffffu, order_key(v[e]), mine);
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint32_t u = __shfl_up(start, o);
+    if (lane >= o) start += u;
+  }
+  if (lane == 63) waves[wave] = start;
+  __syncthreads();
+  start += n_equal - (c0 + c1);
+#pragma unroll
+  for (int w = 0; w < kPartThreads / 64; ++w)
+    if (w < wave) start += waves[w];
+  // (top_p of what top_k leaves goes by the mass of tokens below min_p too)
+  const double deepest = r.min_p == 0.0 || (r.top_k && r.top_p < 1.0) ? kBuckets : 4.0 - kPerOctave * log2(r.min_p);
+  const bool reach0 = has && 2 * tid < deepest && (!r.top_k || start < r.top_k), reach1 = reach0 && 2 * tid + 1 < deepest && (!r.top_k || start + c0 < r.top_k);
+  const unsigned long long reached = __ballot(reach0);          // (holds for the first buckets alone)
+  if (reached && lane == 63 - __builtin_clzll(reached)) atomicMax(&left, start + c0 + (reach1 ? c1 : 0));
+  if (has) {
+    slot[2 * tid] = reach0 ? start : kPart, slot[2 * tid + 1] = reach1 ? start + c0 : kPart;
+    typedef unsigned long long Pair __attribute__((ext_vector_type(2)));
+    *((MDBF_GLOBAL Pair*)(parts.hists + part * kBuckets) + tid) = Pair{h0, h1};
   }
   __syncthreads();
-  const int bytes = (int)(n_left * sizeof(Token));
-  char* out = parts.left + part * (int64_t)(kStored * sizeof(Token));
-  for (int x = tid * 16; x < bytes; x += kPartThreads * 16) *(MDBF_GLOBAL U32x4*)(out + x) = *(const U32x4*)(staged + x);
+  const uint32_t n_left = max(left, n_equal);
+  if (has) ((MDBF_GLOBAL uint32_t*)(parts.starts + part * kBuckets))[tid] = min(start, n_left) | min(start + c0, n_left) << 16;
+  if (tid == 0) parts.heads[part] = {(unsigned long long)key << 32, n_equal};
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) {
+    if (down[e] >= kBuckets) continue;
+    const uint32_t place = atomicAdd(down[e] < 0 ? &next_equal : &slot[down[e]], 1u);
+    if (place < kPart) order[place] = (uint16_t)place_of(e);    // (slots that none reaches begin at kPart)
+  }
+  __syncthreads();
+  MDBF_GLOBAL U32x4* out = (MDBF_GLOBAL U32x4*)(parts.left + part * kPart);
+  for (uint32_t x = tid; x * 8 < n_left; x += kPartThreads) out[x] = ((const U32x4*)order)[x];
 }
 
 // What the second launch has in LDS.
-constexpr int kMaxParts = kSampleMaxVocab / (kPartThreads * 8);
+constexpr int kMaxParts = kSampleMaxVocab / kPart;
 constexpr int kBins = kPickThreads;
 constexpr int kRuns = 4;                         // runs of neighbouring buckets that are looked at
 struct RowShared {
@@ -406,15 +391,14 @@ struct RowShared {
   uint32_t counts[kPickThreads / 64];
   unsigned long long tops[kPickThreads / 64];
   unsigned long long part_extra[kMaxParts];      // of a part: its largest's bucket in the row (kBuckets: nothing there weighs), how many equal it, and
-  int32_t part_top[kMaxParts];                   // their fractions; buckets whose tokens are in order
-  int32_t part_stored[kMaxParts];
-  uint32_t part_equal[kMaxParts], part_list[kMaxParts];
+  int32_t part_top[kMaxParts];                   // their fractions
+  uint32_t part_equal[kMaxParts];
   double klo, khi, plo, phi, mlo, mhi, total;
   unsigned long long likely;
   double value;
   int k, p0, p1, m0, m1, u0, u1;
   int chosen[3];
-  uint32_t n, parts, n_few, key, ties;
+  uint32_t n, n_few, key, ties;
 };
 
 struct Runs {
@@ -743,8 +727,7 @@ __device__ __forceinline__ void pick_few(const SampleArgs& a, int64_t t, const R
 }
 
 template <int DT>
-__global__ __launch_bounds__(kPickThreads) void sample_rows_kernel(SampleArgs a, Parts left, int parts, int part_size) {
-  typedef typename Left<DT>::type Token;
+__global__ __launch_bounds__(kPickThreads) void sample_rows_kernel(SampleArgs a, Parts left, int parts) {
   extern __shared__ char shared[];
   RowShared& s = *(RowShared*)shared;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -760,7 +743,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_rows_kernel(SampleArgs a,
   }
   if (lane == 0) s.tops[wave] = top;
   if (tid == 0) {
-    s.n = s.parts = 0;
+    s.n = 0;
     s.k = -1, s.p0 = s.m0 = s.u0 = 0, s.m1 = -1, s.u1 = kBuckets - 1;
     s.klo = s.khi = s.phi = s.mlo = s.mhi = INFINITY;
     s.p1 = r.top_p < 1.0 ? kBuckets - 1 : -1, s.plo = r.top_p < 1.0 ? 0.0 : INFINITY;
@@ -787,8 +770,8 @@ __global__ __launch_bounds__(kPickThreads) void sample_rows_kernel(SampleArgs a,
     const bool none = its == -__builtin_inff() || (infinite && its != largest);
     const int b = none ? kBuckets : min(bucket_of(its), kBuckets);
     const double d = degrees(r, its);
-    s.part_top[tid] = b, s.part_equal[tid] = none ? 0 : head.equal, s.part_stored[tid] = head.stored;
-    s.part_extra[tid] = b == 0 || none ? 0 : head.equal * (unsigned long long)(sixteenth(d - floor(d)) * (double)(1ull << kFracBits) + 0.5);
+    s.part_top[tid] = b, s.part_equal[tid] = none ? 0 : (uint32_t)head.equal;
+    s.part_extra[tid] = b == 0 || none ? 0 : head.equal * (bucket_word(d - floor(d)) & ((1ull << kCountBit) - 1));
   }
   __syncthreads();
 
@@ -844,33 +827,21 @@ __global__ __launch_bounds__(kPickThreads) void sample_rows_kernel(SampleArgs a,
 
   // Tokens of those buckets: of each part runs of what the first launch has left in order.
   for (int p = wave; p < parts; p += kPickThreads / 64) {
-    const int top_bucket = s.part_top[p], shift = max(top_bucket, 1), stored = s.part_stored[p], equal = (int)s.part_equal[p];
+    const int top_bucket = s.part_top[p], shift = max(top_bucket, 1);
     if (top_bucket >= kBuckets) continue;
     const uint16_t* starts = left.starts + (row + p) * kBuckets;
-    const Token* tokens = (const Token*)left.left + (row + p) * kStored;
+    const uint16_t* tokens = left.left + (row + p) * kPart;
     int begin[kRuns], end[kRuns];
-    bool again = false;
 #pragma unroll
     for (int q = 0; q < kRuns; ++q) {
-      const int from = c.runs.from[q], to = c.runs.to[q];
-      const bool ties = from <= top_bucket && top_bucket <= to;
-      const int o0 = max(from - shift, 0), o1 = infinite ? -1 : to - shift;
+      const int from = c.runs.from[q], to = c.runs.to[q], o0 = max(from - shift, 0), o1 = infinite ? -1 : to - shift;
+      const bool with_top = from <= top_bucket && top_bucket <= to;
       begin[q] = end[q] = 0;
-      if (from > to) continue;
-      if (o0 <= o1) {
-        begin[q] = starts[o0];
-        end[q] = starts[o1 + 1];                 // (o1 is the last bucket but one at most)
-        if (o1 >= stored) again = true;
-      }
-      if (ties) {
-        if (o0 > o1) end[q] = equal;
+      if (o0 <= o1 && from <= to) begin[q] = starts[o0], end[q] = starts[o1 + 1];     // (o1 is the last bucket but one at most)
+      if (with_top) {
         begin[q] = 0;
-        if (stored < 0) again = true;
+        if (o0 > o1) end[q] = (int)s.part_equal[p];
       }
-    }
-    if (again) {
-      if (lane == 0) s.part_list[atomicAdd(&s.parts, 1u)] = p;
-      continue;
     }
 #pragma unroll
     for (int q = 0; q < kRuns; ++q) {
@@ -880,31 +851,9 @@ __global__ __launch_bounds__(kPickThreads) void sample_rows_kernel(SampleArgs a,
       if (lane == 0) place = atomicAdd(&s.n, (uint32_t)m);
       place = __builtin_amdgcn_readfirstlane(place);
       for (int x = lane; x < m && place + x < kList; x += 64) {
-        const Token v = tokens[begin[q] + x];
-        s.list[place + x] = (unsigned long long)~Left<DT>::key(v) << 32 | (uint32_t)(p * part_size + Left<DT>::at(v));
+        const int i = p * kPart + tokens[begin[q] + x];
+        s.list[place + x] = (unsigned long long)~order_key(load_as_float(a.logits, t * a.ld + i, DT)) << 32 | (uint32_t)i;
       }
-    }
-  }
-  __syncthreads();
-  // Parts that had no room for all of them are read again.
-  const int per_part = part_size / 512, pieces = (int)s.parts * per_part;
-  for (int p0 = wave; p0 < pieces; p0 += kPickThreads / 64) {
-    const int at = (int)s.part_list[p0 / per_part] * part_size + (p0 % per_part) * 512 + lane * 8, there = a.vocab - at;
-    if (there <= 0) continue;
-    Raw8<DT> raw;
-    float x[8];
-    load_raw8<DT>(a.logits, t * a.ld + at, there, raw);
-    to_float8<DT>(raw, x);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      if (e >= there || !(x[e] > -__builtin_inff()) || (infinite && x[e] != largest)) continue;
-      const int b = bucket_of(x[e]);
-      bool take = false;
-#pragma unroll
-      for (int q = 0; q < kRuns; ++q) take |= b >= c.runs.from[q] && b <= c.runs.to[q];
-      if (!take || b >= kBuckets) continue;
-      const uint32_t n = atomicAdd(&s.n, 1u);
-      if (n < kList) s.list[n] = (unsigned long long)~order_key(x[e]) << 32 | (uint32_t)(at + e);
     }
   }
   __syncthreads();
@@ -921,31 +870,23 @@ __global__ __launch_bounds__(kPickThreads) void sample_rows_kernel(SampleArgs a,
   }
 }
 
-constexpr int kPartLeast = kPartThreads * 8, kPartMost = kPartThreads * 16;
+static size_t sample_parts(int vocab) { return ((size_t)vocab + kPart - 1) / kPart; }
 static size_t sample_ws_bytes(int T, int vocab) {
-  const size_t parts = ((size_t)vocab + kPartLeast - 1) / kPartLeast;
-  return (size_t)T * parts * (sizeof(PartHead) + kBuckets * 10 + kStored * 8);
+  return (size_t)T * sample_parts(vocab) * (sizeof(PartHead) + kBuckets * (8 + 2) + kPart * 2);
 }
 
 template <int DT>
 static int launch_sample(const SampleArgs& a, void* ws, hipStream_t s) {
-  // parts of 8192 tokens, as many as what is left in order has room for, where that leaves compute units idle or they are fp32; else of 16384
-  const int part = DT == MDBF_F32 || (int64_t)a.T * ((a.vocab + kPartMost - 1) / kPartMost) < 512 ? kPartLeast : kPartMost;
-  const int parts = (a.vocab + part - 1) / part;
+  const int parts = (int)sample_parts(a.vocab);
   const size_t all = (size_t)a.T * parts;
   Parts left;
-  left.left = (char*)ws;
-  left.hists = (unsigned long long*)(left.left + all * kStored * sizeof(typename Left<DT>::type));
+  left.hists = (unsigned long long*)ws;
   left.heads = (PartHead*)(left.hists + all * kBuckets);
-  left.starts = (uint16_t*)(left.heads + all);
-  constexpr int staged = kStored * (int)sizeof(typename Left<DT>::type);
+  left.left = (uint16_t*)(left.heads + all);
+  left.starts = left.left + all * kPart;
   static KernelSetup setup;
   const int e = kernel_setup(setup, [] {
-    hipError_t e = hipFuncSetAttribute((const void*)sample_rows_kernel<DT>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(RowShared));
-    if (e == hipSuccess) e = hipFuncSetAttribute((const void*)sample_parts_kernel<DT, 8>, hipFuncAttributeMaxDynamicSharedMemorySize, staged);
-    if (e == hipSuccess && DT != MDBF_F32)
-      e = hipFuncSetAttribute((const void*)sample_parts_kernel<DT, DT == MDBF_F32 ? 8 : 16>, hipFuncAttributeMaxDynamicSharedMemorySize, staged);
-    return e;
+    return hipFuncSetAttribute((const void*)sample_rows_kernel<DT>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(RowShared));
   });
   if (e) return e;
   // (the grid's second dimension ends at 65535 rows)
@@ -956,9 +897,8 @@ static int launch_sample(const SampleArgs& a, void* ws, hipStream_t s) {
     const auto from = [&](auto* p) { return p ? p + t0 : p; };
     b.temperature = from(a.temperature), b.top_p = from(a.top_p), b.min_p = from(a.min_p), b.u = from(a.u), b.top_k = from(a.top_k);
     b.tokens = from(a.tokens), b.probs = from(a.probs);
-    if (part == kPartLeast) sample_parts_kernel<DT, 8><<<dim3(parts, b.T), kPartThreads, staged, s>>>(b, left);
-    else sample_parts_kernel<DT, DT == MDBF_F32 ? 8 : 16><<<dim3(parts, b.T), kPartThreads, staged, s>>>(b, left);
-    sample_rows_kernel<DT><<<b.T, kPickThreads, sizeof(RowShared), s>>>(b, left, parts, part);
+    sample_parts_kernel<DT><<<dim3(parts, b.T), kPartThreads, 0, s>>>(b, left);
+    sample_rows_kernel<DT><<<b.T, kPickThreads, sizeof(RowShared), s>>>(b, left, parts);
   }
   return (int)hipGetLastError();
 }
