@@ -3,6 +3,7 @@
     python3 -m paper_2512_24545_amd.workloads stack   --budget 1.5 --tokens 8 --passes 300 --warmup 100
     python3 -m paper_2512_24545_amd.workloads prefill --tokens 2048 --x-dtype f16 --passes 200 --warmup 300
     python3 -m paper_2512_24545_amd.workloads attention --requests 16 --cached 4000 --fresh 1 --kv-heads 8
+    python3 -m paper_2512_24545_amd.workloads step      --requests 16 --cached 4000 --fresh 1 --kv-heads 8 --adapters 8 --adapter-rank 16
 
 `stack`: the 32-layer decoder stack (224 independent products per pass: q, k, v, o, gate, up, down per
 layer, LLaMA-7B shapes at the given bit budget), `--tokens` activations per matrix, issued as one plan
@@ -10,7 +11,9 @@ through mdbf_forward_batch.  `prefill`: one 4096 x 4096, k = 2656, l = 16 layer 
 through mdbf_forward.  `attention`: the attention block of one decoder layer as a serving step runs it, `--fresh` new
 tokens for each of `--requests` requests behind `--cached` ones: q, k, v projections as one plan, places in the cache
 (mdbf_kv_slots), norm and rotation with keys and values into the 4-bit cache (mdbf_qk_norm_rope), attention over it
-(mdbf_kv_attention), output projection.  Layers are drawn on the device (random packed sign words, envelopes
+(mdbf_kv_attention), output projection.  `step`: the same between what stands around it, for requests that have low-rank adapters: the residual's
+addition and norm in front and behind (mdbf_add_norm), the adapters beside the four projections (mdbf_adapter_rows, mdbf_adapters), and for the
+last token of each request a compressed head and the choice of the next one (mdbf_sample).  Layers are drawn on the device (random packed sign words, envelopes
 |N(0,1)| * 0.02 + 1e-3 in fp16, activations N(0,1)).  With few passes and no warm-up this is the program to
 put under a profiler; bench.py remains the benchmark.
 """
@@ -133,6 +136,7 @@ class AttentionBlock:
     def step(self):
         p = mb.mdbf_kv_slots(self.cached, self.fresh, self.table, self.free, self.taken, self.cache.page_size, self.X.shape[0], out=self.places)
         self.plan.run()
+        self.projected()
         q, k, v = self.heads
         mb.mdbf_qk_norm_rope(q, k, self.rope, p.positions, q_weight=self.norm[0], k_weight=self.norm[1], q_out=self.turned,
                              cache=self.cache, v=v, slots=p.slots)
@@ -140,11 +144,57 @@ class AttentionBlock:
                              workspace=self.attention_workspace)
         return mb.mdbf_forward(self.o, self.out.flatten(1), y_dtype="f16", Y=self.Y, workspace=self.workspace)
 
+    def projected(self):
+        """What a program adds to q, k and v behind the projections."""
 
-def run_attention(torch, args):
-    g = torch.Generator(device="cuda:0")
-    g.manual_seed(6)
-    block = AttentionBlock(torch, g, args.requests, args.cached, args.fresh, args.kv_heads, args.budget)
+
+class ServingStep(AttentionBlock):
+    """The attention block between residual additions with norm, low-rank adapters beside its projections, and a head with the choice of each
+    request's next token behind it.  One request in nine has no adapter, one in eight takes the likeliest token."""
+    VOCAB = 32000
+
+    def __init__(self, torch, g, requests, cached, fresh, kv_heads, budget="1.5", adapters=8, rank=16, **kw):
+        super().__init__(torch, g, requests, cached, fresh, kv_heads, budget, **kw)
+        n, T, d = self.WIDTH, requests * fresh, kv_heads * self.HEAD_DIM
+        normal = lambda scale, *shape: torch.randn(shape, generator=g, device="cuda:0") * scale
+        self.stream, self.update = normal(2.0, T, n), normal(1.0, T, n).half()     # the residual stream, and what the layer in front adds to it
+        self.weights = [1 + normal(0.1, n) for _ in range(2)]
+        pool = lambda m: mb.Adapters(normal(n ** -0.5, adapters, rank, n).half(), normal(0.1 * rank ** -0.5, adapters, m, rank).half(), 0.5 + normal(0.1, adapters).abs())
+        self.pools, self.pool_o = [pool(n), pool(d), pool(d)], pool(n)
+        of = torch.randint(0, adapters, (requests,), generator=g, device="cuda:0", dtype=torch.int32)
+        self.adapter = torch.where(torch.arange(requests, device="cuda:0") % 9 == 8, -1, of)
+        self.rows = mb.AdapterRows(T, requests, adapters)
+        flat = self.out.flatten(1)
+        self.adapter_workspaces = [mb.mdbf_adapters_workspace(self.rows, self.pools, [self.X] * 3, self.qkv),
+                                   mb.mdbf_adapters_workspace(self.rows, [self.pool_o], [flat], [self.Y])]
+        self.between, self.behind = torch.zeros_like(self.stream), torch.zeros_like(self.stream)
+        self.normed = torch.zeros((T, n), dtype=torch.float16, device="cuda:0")
+        l = synth.stack_matrix_spec(budget, 0, 0)["l"]
+        self.head = _device_layer(torch, g, self.VOCAB, n, mb.mdbf_rank_for_budget(self.VOCAB, n, l, float(budget), 16, 32), l)
+        self.last = torch.arange(fresh - 1, T, fresh, device="cuda:0")
+        self.logits = torch.zeros((requests, self.VOCAB), dtype=torch.float32, device="cuda:0")
+        self.head_workspace = torch.empty(mb.mdbf_workspace_bytes(self.head.desc("f16", "f32"), requests), dtype=torch.uint8, device="cuda:0")
+        row = torch.arange(requests, device="cuda:0")
+        self.u = torch.rand((requests,), generator=g, device="cuda:0")
+        self.temperature = (0.6 + 0.1 * (row % 5)) * (row % 8 != 7)
+        self.top_k, self.top_p = torch.full_like(self.adapter, 50), torch.full_like(self.u, 0.9)
+        self.tokens, self.probs = torch.zeros_like(self.adapter), torch.zeros_like(self.u)
+        self.sample_workspace = mb.mdbf_sample_workspace(requests, self.VOCAB)
+
+    def projected(self):
+        mb.mdbf_adapter_rows(self.places.cu, self.adapter, self.rows.adapters, self.rows.tokens, out=self.rows)
+        mb.mdbf_adapters(self.rows, self.pools, [self.X] * 3, self.qkv, workspace=self.adapter_workspaces[0])
+
+    def step(self):
+        mb.mdbf_add_norm(self.update, self.stream, self.weights[0], out=self.X, residual_out=self.between)
+        super().step()
+        mb.mdbf_adapters(self.rows, [self.pool_o], [self.out.flatten(1)], [self.Y], workspace=self.adapter_workspaces[1])
+        mb.mdbf_add_norm(self.Y, self.between, self.weights[1], out=self.normed, residual_out=self.behind)
+        mb.mdbf_forward(self.head, self.normed[self.last], y_dtype="f32", Y=self.logits, workspace=self.head_workspace)
+        return mb.mdbf_sample(self.logits, self.u, self.temperature, self.top_k, self.top_p, tokens=self.tokens, probs=self.probs, workspace=self.sample_workspace)
+
+
+def _run_block(torch, args, block):
     block.step()
     torch.cuda.synchronize()
     assert block.places.status.item() == 0 and bool(block.Y.isfinite().all())
@@ -153,13 +203,26 @@ def run_attention(torch, args):
     with torch.cuda.graph(graph):
         block.step()
     graph_ms = _time(torch, graph.replay, args.warmup, args.passes)
-    return {"workload": "attention", "requests": args.requests, "cached": args.cached, "fresh": args.fresh, "kv_heads": args.kv_heads,
+    return {"workload": args.workload, "requests": args.requests, "cached": args.cached, "fresh": args.fresh, "kv_heads": args.kv_heads,
             "budget_bpw": args.budget, "cache_MB": block.cache.buffer.numel() / 1e6, "ms_per_step": ms, "ms_per_step_from_a_graph": graph_ms}
+
+
+def run_attention(torch, args):
+    g = torch.Generator(device="cuda:0")
+    g.manual_seed(6)
+    return _run_block(torch, args, AttentionBlock(torch, g, args.requests, args.cached, args.fresh, args.kv_heads, args.budget))
+
+
+def run_step(torch, args):
+    g = torch.Generator(device="cuda:0")
+    g.manual_seed(7)
+    block = ServingStep(torch, g, args.requests, args.cached, args.fresh, args.kv_heads, args.budget, args.adapters, args.adapter_rank)
+    return dict(_run_block(torch, args, block), adapters=args.adapters, adapter_rank=args.adapter_rank, vocab=block.VOCAB)
 
 
 def main(argv=None):
     ap = argparse.ArgumentParser(prog="python3 -m paper_2512_24545_amd.workloads")
-    ap.add_argument("workload", choices=["stack", "prefill", "attention"])
+    ap.add_argument("workload", choices=["stack", "prefill", "attention", "step"])
     ap.add_argument("--budget", default="1.5", choices=["1.0", "1.5", "2.0"])
     ap.add_argument("--tokens", type=int, default=None)
     ap.add_argument("--x-dtype", default="f16", choices=["f16", "bf16"])
@@ -167,6 +230,8 @@ def main(argv=None):
     ap.add_argument("--cached", type=int, default=4000)
     ap.add_argument("--fresh", type=int, default=1)
     ap.add_argument("--kv-heads", type=int, default=32, choices=[1, 2, 4, 8, 16, 32])
+    ap.add_argument("--adapters", type=int, default=8)
+    ap.add_argument("--adapter-rank", type=int, default=16)
     ap.add_argument("--passes", type=int, default=300)
     ap.add_argument("--warmup", type=int, default=100)
     args = ap.parse_args(argv)
@@ -176,7 +241,7 @@ def main(argv=None):
     mb.lib()
     if args.tokens is None:
         args.tokens = 8 if args.workload == "stack" else 2048
-    out = {"stack": run_stack, "prefill": run_prefill, "attention": run_attention}[args.workload](torch, args)
+    out = {"stack": run_stack, "prefill": run_prefill, "attention": run_attention, "step": run_step}[args.workload](torch, args)
     print(json.dumps(out), flush=True)
 
 
