@@ -450,7 +450,7 @@ int mdbf_adapter_rows(int T, int requests, int adapters, const int32_t* cu_dev, 
 
 /* One projection's adapters, and what they are applied to. */
 typedef struct {
-  int32_t n, m, r;         /* rank r 1 .. 256; adapters of lower ranks are filled up with zeros */
+  int32_t n, m, r;         /* n, m 1 .. 2^23; rank r 1 .. 256, adapters of lower ranks are filled up with zeros */
   int32_t y_dtype;
   const void* A_dev;       /* adapters x r x n, contiguous */
   const void* B_dev;       /* adapters x m x r, contiguous */
@@ -463,9 +463,10 @@ typedef struct {
 
 /* Y[t] += scale[a] B[a] (A[a] X[t]) for the rows t in the tiles, a the tile's adapter: the rows of requests without one stay as
  * they are.  `count` projections (1 .. MDBF_ADAPTER_MAX) of one step in one call, `dtype` that of all X, A and B (MDBF_F16 or MDBF_BF16); they may
- * share X, not Y.  Y overlaps nothing else that the call reads.  Sums are fp32; the inner values A X are rounded to three (fp32 Y) or two numbers of 16 bits that add up to
- * them to 2^-23 or 2^-16, in fp16 after a row's largest is brought to 1; Y is rounded once.  A row, a tile or an adapter outside of what T, tile_room and
- * `adapters` say is left out; a row must not be listed twice.  Repeated calls return the same bits; two launches. */
+ * share X, not Y.  Y overlaps nothing else that the call reads.  Sums are fp32.  The inner values A X are carried as 16-bit numbers that add up to them: two to
+ * 2^-16 of a value (bf16), three to 2^-23 (bf16, fp32 Y), two to 2^-22 of a row's largest (fp16, whatever its magnitude).  Y is rounded
+ * once.  A row, a tile or an adapter outside of what T, tile_room and `adapters` say is left out; a row must not be listed twice.  Repeated calls return
+ * the same bits; two launches, one more for each further type of Y.  The workspace holds the inner values. */
 #define MDBF_ADAPTER_MAX 8
 int mdbf_adapters_workspace_bytes(int count, const mdbf_adapter_t* list, int dtype, int adapters, int T, int64_t tile_room,
                                   size_t* bytes_out);
@@ -484,7 +485,7 @@ int mdbf_adapters(int count, const mdbf_adapter_t* list, int dtype, int adapters
  *   tokens         T int32; -1 in a row that holds nothing but -inf and NaN (NaN counts as -inf, whose weight is 0)
  *   probs          T fp32 or null: the token's weight over that of all kept ones; 0 with token -1
  * Among infinite logits each has the weight 1, and finite ones none.  Weights are fp64; those below 2^-47 of the largest count as none, and the sums that
- * bounds and draw go by are held to 5e-12 of themselves, in an order that is fixed or does not matter: repeated calls return the same bits.  Two launches.  The
+ * bounds and draw go by are held to 1e-11 of themselves, in an order that is fixed or does not matter: repeated calls return the same bits.  Two launches.  The
  * workspace's size (host arithmetic only, 25 KB per row and 8192 tokens) never shrinks with T and vocab (1 .. 2^20). */
 typedef struct {
   const float* temperature_dev;

@@ -159,6 +159,7 @@ __global__ __launch_bounds__(kRowChunk) void adapter_places_kernel(RowArgs a) {
 // a projection shares with the next one, X, is read once for up to four tiles of ranks.
 constexpr int kInSlots = 4;                    // tiles of 16 ranks per workgroup of the first launch
 constexpr int kMaxRank = 256;
+constexpr int kMaxWidth = 1 << 23;             // channels and columns: the second launch's grid ends at 65535 times 256 columns
 constexpr int kMaxGroups = MDBF_ADAPTER_MAX * kMaxRank / 16 / kInSlots;
 constexpr int kOutBlock = 64;                  // columns of Y that a wave takes at a time
 
@@ -530,7 +531,7 @@ static int check_adapters(int count, const mdbf_adapter_t* list, int dtype, int 
     const mdbf_adapter_t& l = list[i];
     if (l.n < 1 || l.m < 1 || l.r < 1) return MDBF_EINVAL;
     if (!row_dtype(l.y_dtype)) return MDBF_EDTYPE;
-    if (l.r > kMaxRank) return MDBF_EUNSUPPORTED;
+    if (l.r > kMaxRank || l.n > kMaxWidth || l.m > kMaxWidth) return MDBF_EUNSUPPORTED;
   }
   return tile_room > (1ll << 30) ? MDBF_EUNSUPPORTED : MDBF_OK;
 }

@@ -91,7 +91,7 @@ __device__ Place descend(const SampleArgs& a, int64_t t, const RowSetting& r, Pi
       const uint32_t k = key_at<DT>(a, t, i);
       if (shift < 24 && ((k ^ at.key) >> (shift + 8))) continue;
       atomicAdd(&s.count[(k >> shift) & 255], 1u);
-      const unsigned long long w = (unsigned long long)(weight(r, k) * kUnit);
+      const unsigned long long w = (unsigned long long)(weight(r, k) * kUnit + 0.5);
       if (w) atomicAdd(&s.mass[(k >> shift) & 255], w);
     }
     __syncthreads();
@@ -140,7 +140,7 @@ __device__ void sample_digits(const SampleArgs& a, int64_t t, const RowSetting& 
     unsigned long long total = 0, likely = 0;
     for (int i = tid; i < a.vocab; i += kPickThreads) {
       const double x = weight(r, key_at<DT>(a, t, i));
-      const unsigned long long w = (unsigned long long)(x * kUnit);
+      const unsigned long long w = (unsigned long long)(x * kUnit + 0.5);
       total += w;
       if (x >= r.min_p) likely += w;
     }

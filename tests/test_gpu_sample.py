@@ -139,3 +139,26 @@ def test_settings_at_their_ends(gpu):
                      dict(top_k=np.array([0, -5, 1, 4999, 5000, 5001, 2 ** 31 - 1, 2])),
                      dict(temperature=np.array([0, -1, nan, inf, 1e-45, 1e-30, 3e38, 1.0]))):
         _check(gpu, z, u, **settings)
+
+
+def test_more_rows_than_a_grid_has(gpu):
+    """65535 rows are a grid's second dimension."""
+    rng = np.random.default_rng(10)
+    T, V = 65600, 24
+    torch, mb = gpu
+    z = torch.from_numpy(rng.standard_normal((T, V)).astype(np.float32)).to("cuda:0")
+    u = torch.from_numpy(rng.random(T).astype(np.float32)).to("cuda:0")
+    on = dict(temperature=torch.from_numpy((0.5 + rng.random(T)).astype(np.float32)).to("cuda:0"), top_k=torch.randint(0, 9, (T,), device="cuda:0", dtype=torch.int32))
+    tokens, probs = mb.mdbf_sample(z, u, **on)
+    for t in list(range(0, T, 997)) + list(range(65530, 65540)) + [T - 1]:
+        token, share = so.sample(z[t].double().cpu().numpy(), float(u[t]), float(on["temperature"][t]), int(on["top_k"][t]))
+        assert int(tokens[t]) == token and abs(float(probs[t]) - share) <= (TINY + 1e-9) * share
+
+
+def test_many_light_tokens_behind_a_heavy_one(gpu):
+    """More tokens of one bucket than the list holds, each of a weight of 1e-5."""
+    rng = np.random.default_rng(11)
+    z = np.full((6, 50000), np.log(1e-5)) + 1e-3 * rng.random((6, 50000))
+    z[:, 31415] = 0.0
+    for settings in (dict(), dict(top_p=0.9), dict(top_k=30000)):
+        _check(gpu, z, 0.1 + 0.85 * rng.random(6), **settings)

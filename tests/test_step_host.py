@@ -119,7 +119,7 @@ def test_adapters_arguments():
         arr = (mb.AdapterDesc * max(len(list_), 1))(*list_) if list_ else None
         return L.mdbf_adapters(len(list_) if count is None else count, arr, dtype, adapters, T, rows, tiles, room, ws, size, None)
 
-    for kw, status in ((dict(n=0), -1), (dict(m=0), -1), (dict(r=0), -1), (dict(r=257), -5), (dict(y_dtype=3), -3), (dict(A_dev=None), -1), (dict(B_dev=None), -1),
+    for kw, status in ((dict(n=0), -1), (dict(m=0), -1), (dict(r=0), -1), (dict(r=257), -5), (dict(n=(1 << 23) + 1, ldx=1 << 24), -5), (dict(m=(1 << 23) + 1, ldy=1 << 24), -5), (dict(y_dtype=3), -3), (dict(A_dev=None), -1), (dict(B_dev=None), -1),
                        (dict(X_dev=None), -1), (dict(Y_dev=None), -1), (dict(ldx=99), -1), (dict(ldy=49), -1), (dict(A_dev=A + 8), -2), (dict(B_dev=A + 2), -2),
                        (dict(X_dev=A + 4), -2), (dict(Y_dev=A + 8), -2), (dict(scale_dev=A + 2), -2)):
         assert call(adapter(**kw)) == status, kw
