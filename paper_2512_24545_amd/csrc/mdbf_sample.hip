@@ -233,12 +233,20 @@ __device__ __forceinline__ double degrees(const RowSetting& r, float x) { return
 
 // What a token adds to its bucket: 1 in the count, and 2^(x / 16) - 1 in units of 2^-39 for x in [0, 1), the fraction of its t.  A polynomial through five
 // Chebyshev points, off by at most 2.6e-12; the sum with 2^52 and the count's bit has the whole number in its last bits.
-__device__ __forceinline__ unsigned long long bucket_word(double x) {
-  constexpr double unit = (double)(1ull << kFracBits);
-  const double g = fma(x, fma(x, fma(x, fma(x, 1.4997758288814042e-07 * unit, 1.3547982742839567e-05 * unit), 9.38385803440002e-04 * unit),
-                              0.04332169865857207 * unit), 2.528854437695519e-12 * unit + 0x1p52 + (double)(1ull << kCountBit));
-  return __builtin_bit_cast(unsigned long long, g) & 0xfffffffffffffull;
-}
+struct BucketWord {
+  double c0, c1, c2, c3, c4;
+  __device__ __forceinline__ BucketWord() {
+    constexpr double unit = (double)(1ull << kFracBits);
+    c4 = 1.4997758288814042e-07 * unit, c3 = 1.3547982742839567e-05 * unit, c2 = 9.38385803440002e-04 * unit, c1 = 0.04332169865857207 * unit;
+    c0 = 2.528854437695519e-12 * unit + 0x1p52 + (double)(1ull << kCountBit);
+    // (as values that the compiler does not know they stay in scalar registers; it would copy constants into a sum's register every time)
+    asm("" : "+s"(c0), "+s"(c1), "+s"(c2), "+s"(c3), "+s"(c4));
+  }
+  __device__ __forceinline__ unsigned long long operator()(double x) const {
+    const double g = fma(x, fma(x, fma(x, fma(x, c4, c3), c2), c1), c0);
+    return __builtin_bit_cast(unsigned long long, g) & 0xfffffffffffffull;
+  }
+};
 
 // sums of the threads in front of this one, and of all, over a workgroup of 1024
 __device__ __forceinline__ uint32_t scan_counts(uint32_t v, uint32_t& total, uint32_t* waves) {
@@ -317,6 +325,7 @@ __global__ __launch_bounds__(kPartThreads, 6) void sample_parts_kernel(SampleArg
   }
   const bool infinite = largest == __builtin_inff();    // then nothing else weighs
   const double base = floor(degrees(r, largest));
+  const BucketWord bucket_word;
   uint32_t alike = 0;
   int down[kEach];                               // a token's bucket; -1: of the part's largest
 #pragma unroll
@@ -771,7 +780,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_rows_kernel(SampleArgs a,
     const int b = none ? kBuckets : min(bucket_of(its), kBuckets);
     const double d = degrees(r, its);
     s.part_top[tid] = b, s.part_equal[tid] = none ? 0 : (uint32_t)head.equal;
-    s.part_extra[tid] = b == 0 || none ? 0 : head.equal * (bucket_word(d - floor(d)) & ((1ull << kCountBit) - 1));
+    s.part_extra[tid] = b == 0 || none ? 0 : head.equal * (BucketWord()(d - floor(d)) & ((1ull << kCountBit) - 1));
   }
   __syncthreads();
 
