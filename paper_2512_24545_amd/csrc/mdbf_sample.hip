@@ -209,6 +209,10 @@ __device__ void sample_digits(const SampleArgs& a, int64_t t, const RowSetting& 
 // at by themselves, and the bounds applied exactly; the first launch leaves the tokens in the order of their buckets, so that these are a few runs of each
 // part's.  Tokens that equal the part's largest are counted apart, so that those that equal the row's largest, of weight 1, make up a bucket of an exact mass:
 // where many are alike, bounds fall on borders between them.
+// The first launch's vector work (some 40 instructions a token, 20 of them fp64) and its LDS additions take longer than the logits: 200 rows of 128256 bf16
+// (51 MB, 10 us at the rate of a read) 39 us, of which writing buckets and order is as much traffic again.  The second one is a chain of some thirty
+// meetings and dependent loads: 10.7 us for one row of 128256 whose list is short, 21 for 64 rows of 32000 whose longest list is 740, 29 for 200 rows of
+// 128256 with lists of up to 4000.  Before: one workgroup a row that reads it for every digit of every bound, 430, 200 and 680 us.
 constexpr int kBuckets = 768;                    // of a row: the largest, then 767 sixteenths, down to 2^-47 of it; less weighs nothing
 constexpr int kPerOctave = 16;
 constexpr int kFracBits = 39;                    // of 2^(frac / 16) - 1 < 0.0443: a part's stay below 2^49, where the count begins
