@@ -10,6 +10,7 @@ import contextlib
 import ctypes as C
 import functools
 import os
+import struct
 
 import numpy as np
 
@@ -151,8 +152,8 @@ def lib():
     L.mdbf_adapter_tiles.restype = i64
     L.mdbf_adapter_tiles.argtypes = [C.c_int, C.c_int, C.c_int]
     L.mdbf_adapter_rows.argtypes = [C.c_int, C.c_int, C.c_int, vp, vp, vp, vp, i64, vp, vp]
-    L.mdbf_adapters_workspace_bytes.argtypes = [C.c_int, C.POINTER(AdapterDesc), C.c_int, C.c_int, C.c_int, i64, C.POINTER(sz)]
-    L.mdbf_adapters.argtypes = [C.c_int, C.POINTER(AdapterDesc), C.c_int, C.c_int, C.c_int, vp, vp, i64, vp, sz, vp]
+    L.mdbf_adapters_workspace_bytes.argtypes = [C.c_int, vp, C.c_int, C.c_int, C.c_int, i64, C.POINTER(sz)]
+    L.mdbf_adapters.argtypes = [C.c_int, vp, C.c_int, C.c_int, C.c_int, vp, vp, i64, vp, sz, vp]
     L.mdbf_sample_workspace_bytes.argtypes = [C.c_int, C.c_int, C.POINTER(sz)]
     L.mdbf_sample.argtypes = [C.POINTER(SampleDesc), vp, i64, C.c_int, C.c_int, C.c_int, vp, vp, vp, vp, sz, vp]
     L.mdbf_strerror.restype = C.c_char_p
@@ -787,10 +788,11 @@ class Adapters:
         _torch()
         assert scale is None or _ints(scale, self.count, _torch_module.float32)
         self.A, self.B, self.scale = A, B, scale
-        self.args = (A.data_ptr(), B.data_ptr(), None if scale is None else scale.data_ptr())
+        self.args = (A.data_ptr(), B.data_ptr(), 0 if scale is None else scale.data_ptr())
 
 
-_ADAPTER_LISTS = [AdapterDesc * count for count in range(MDBF_ADAPTER_MAX + 1)]
+_pack_adapter = struct.Struct("4i7q").pack       # an AdapterDesc's bytes, in a third of the time that making one takes
+assert struct.calcsize("4i7q") == C.sizeof(AdapterDesc)
 
 
 def _adapter_list(rows, adapters, Xs, Ys):
@@ -802,21 +804,21 @@ def _adapter_list(rows, adapters, Xs, Ys):
         n, m = p.n, p.m
         assert p.count == rows.adapters and p.A.dtype == X.dtype == dtype and X.shape == (T, n) and Y.shape == (T, m)
         tensors += (X, Y, p.A, p.B, p.scale)
-        descs.append(AdapterDesc(n, m, p.r, DTYPE_CODE[_DTYPE_NAME[Y.dtype]], *p.args, X.data_ptr(), _rows_of(X, T, n), Y.data_ptr(), _rows_of(Y, T, m)))
+        descs.append(_pack_adapter(n, m, p.r, DTYPE_CODE[_DTYPE_NAME[Y.dtype]], *p.args, X.data_ptr(), _rows_of(X, T, n), Y.data_ptr(), _rows_of(Y, T, m)))
     _here(*tensors)
-    return _ADAPTER_LISTS[count](*descs), DTYPE_CODE[_DTYPE_NAME[dtype]]
+    return b"".join(descs), count, DTYPE_CODE[_DTYPE_NAME[dtype]]
 
 
 def mdbf_adapters_workspace(rows, adapters, Xs, Ys):
     """The workspace (uint8 CUDA tensor) of an mdbf_adapters call with these arguments."""
     torch = _torch()
-    arr, dtype = _adapter_list(rows, adapters, Xs, Ys)
-    return torch.empty(_adapters_need(arr, dtype, rows), dtype=torch.uint8, device=Xs[0].device)
+    arr, count, dtype = _adapter_list(rows, adapters, Xs, Ys)
+    return torch.empty(_adapters_need(arr, count, dtype, rows), dtype=torch.uint8, device=Xs[0].device)
 
 
-def _adapters_need(arr, dtype, rows):
+def _adapters_need(arr, count, dtype, rows):
     need = C.c_size_t(0)
-    status = (_lib or lib()).mdbf_adapters_workspace_bytes(len(arr), arr, dtype, rows.adapters, rows.tokens, rows.tiles.shape[0], C.byref(need))
+    status = (_lib or lib()).mdbf_adapters_workspace_bytes(count, arr, dtype, rows.adapters, rows.tokens, rows.tiles.shape[0], C.byref(need))
     if status:
         _check(status, "mdbf_adapters_workspace_bytes")
     return need.value
@@ -827,13 +829,13 @@ def mdbf_adapters(rows, adapters, Xs, Ys, workspace=None, stream=None):
     projections have written Ys.  rows: an AdapterRows; adapters: an Adapters per projection; Xs (T, n) of the adapters' type, Ys (T, m)
     f16/bf16/f32.  Rows without an adapter stay as they are.  Returns Ys."""
     torch = _torch()
-    arr, dtype = _adapter_list(rows, adapters, Xs, Ys)
+    arr, count, dtype = _adapter_list(rows, adapters, Xs, Ys)
     if workspace is None:
         with _on(stream):
-            workspace = torch.empty(_adapters_need(arr, dtype, rows), dtype=torch.uint8, device=Xs[0].device)
+            workspace = torch.empty(_adapters_need(arr, count, dtype, rows), dtype=torch.uint8, device=Xs[0].device)
     else:
         _here(workspace)
-    status = (_lib or lib()).mdbf_adapters(len(arr), arr, dtype, rows.adapters, rows.tokens, rows.rows.data_ptr(), rows.tiles.data_ptr(),
+    status = (_lib or lib()).mdbf_adapters(count, arr, dtype, rows.adapters, rows.tokens, rows.rows.data_ptr(), rows.tiles.data_ptr(),
                                            rows.tiles.shape[0], workspace.data_ptr(), workspace.numel(), _stream_ptr(stream))
     if status:
         _check(status, "mdbf_adapters")
