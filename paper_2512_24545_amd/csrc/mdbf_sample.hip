@@ -129,55 +129,53 @@ __device__ Place descend(const SampleArgs& a, int64_t t, const RowSetting& r, Pi
     at.ties = s.count[s.digit];
   }
   return at;
-}// A row that nothing else serves: read again for every digit.
+}
+
+// A row that nothing else serves: read again for every digit.
 template <int DT>
 __device__ void sample_digits(const SampleArgs& a, int64_t t, const RowSetting& r, PickShared& s) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  uint32_t key = r.top, tie = 0;
-  double prob = 1.0;
-  {
-    // what is kept is a first part of the order, and so is what each bound leaves: the least of their masses
-    unsigned long long total = 0, likely = 0;
-    for (int i = tid; i < a.vocab; i += kPickThreads) {
-      const double x = weight(r, key_at<DT>(a, t, i));
-      const unsigned long long w = (unsigned long long)(x * kUnit + 0.5);
-      total += w;
-      if (x >= r.min_p) likely += w;
-    }
-    for (int q = 0; q < 2; ++q) {
-      unsigned long long v = q ? likely : total;
-      for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o);
-      __syncthreads();
-      if (lane == 0) s.sum[wave] = v;
-      __syncthreads();
-      v = 0;
-      for (int w = 0; w < kPickThreads / 64; ++w) v += s.sum[w];
-      (q ? likely : total) = v;
-    }
-    double kept = (double)total;
-    if (r.top_k) {
-      const Place p = descend<DT>(a, t, r, s, r.top_k, 0.0, false);
-      kept = (double)p.mass_before + (double)(r.top_k - p.before) * (weight(r, p.key) * kUnit);
-    }
-    double least = kept;
-    if (r.top_p < 1.0) {
-      const double mass = r.top_p * kept;
-      const Place p = descend<DT>(a, t, r, s, 0, mass, false);
-      const double w = weight(r, p.key) * kUnit, b = (double)p.mass_before;
-      double j = w > 0 ? ceil((mass - b) / w) : 1.0;
-      j = fmin(fmax(j, 1.0), (double)p.ties);
-      least = fmin(least, b + j * w);
-    }
-    if (r.min_p > 0.0) least = fmin(least, fmax((double)likely, kUnit));
-    kept = least;
-    const double mass = r.u * kept;
-    const Place p = descend<DT>(a, t, r, s, 0, mass, true);
-    const double w = weight(r, p.key) * kUnit, b = (double)p.mass_before;
-    key = p.key;
-    const double j = w > 0 ? floor((mass - b) / w) : 0.0;
-    tie = (uint32_t)fmin(fmax(j, 0.0), (double)(p.ties - 1));
-    prob = w / kept;
+  // what is kept is a first part of the order, and so is what each bound leaves: the least of their masses
+  unsigned long long total = 0, likely = 0;
+  for (int i = tid; i < a.vocab; i += kPickThreads) {
+    const double x = weight(r, key_at<DT>(a, t, i));
+    const unsigned long long w = (unsigned long long)(x * kUnit + 0.5);
+    total += w;
+    if (x >= r.min_p) likely += w;
   }
+  for (int q = 0; q < 2; ++q) {
+    unsigned long long v = q ? likely : total;
+    for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o);
+    __syncthreads();
+    if (lane == 0) s.sum[wave] = v;
+    __syncthreads();
+    v = 0;
+    for (int w = 0; w < kPickThreads / 64; ++w) v += s.sum[w];
+    (q ? likely : total) = v;
+  }
+  double kept = (double)total;
+  if (r.top_k) {
+    const Place p = descend<DT>(a, t, r, s, r.top_k, 0.0, false);
+    kept = (double)p.mass_before + (double)(r.top_k - p.before) * (weight(r, p.key) * kUnit);
+  }
+  double least = kept;
+  if (r.top_p < 1.0) {
+    const double mass = r.top_p * kept;
+    const Place p = descend<DT>(a, t, r, s, 0, mass, false);
+    const double w = weight(r, p.key) * kUnit, b = (double)p.mass_before;
+    double j = w > 0 ? ceil((mass - b) / w) : 1.0;
+    j = fmin(fmax(j, 1.0), (double)p.ties);
+    least = fmin(least, b + j * w);
+  }
+  if (r.min_p > 0.0) least = fmin(least, fmax((double)likely, kUnit));
+  kept = least;
+  const double mass = r.u * kept;
+  const Place p = descend<DT>(a, t, r, s, 0, mass, true);
+  const double w = weight(r, p.key) * kUnit, b = (double)p.mass_before;
+  const uint32_t key = p.key;
+  const double j = w > 0 ? floor((mass - b) / w) : 0.0;
+  const uint32_t tie = (uint32_t)fmin(fmax(j, 0.0), (double)(p.ties - 1));
+  const double prob = w / kept;
   // the index of that one among equal logits
   uint32_t before = 0;
   for (int i0 = 0; i0 < a.vocab; i0 += kPickThreads) {
@@ -219,7 +217,7 @@ constexpr int kFracBits = 39;                    // of 2^(frac / 16) - 1 < 0.044
 constexpr int kCountBit = 49;
 constexpr int kList = 8192;                      // tokens of a row that the second launch looks at; rows that have more go by digits
 constexpr int kPartThreads = 512, kPart = 8192, kEach = kPart / kPartThreads;   // tokens of a part, of a thread
-constexpr double kSlack = 1e-9;                  // by which sums of buckets and of tokens may differ, and more
+constexpr double kSlack = 1e-7;                  // more than sums of buckets and of tokens differ by, with logits of up to 1e9 temperatures
 
 struct PartHead {
   unsigned long long top;                        // key of the part's largest, and, where that one is asked for, ~its index: of equal keys the lowest is largest
