@@ -522,6 +522,9 @@ static AdapterShape adapter_shape(int count, const mdbf_adapter_t* list, int T, 
   const int64_t want = 512 / (tile_room * groups);
   const int most = n / 256 < 16 ? n / 256 : 16;
   sh.splits = (int)(want < most ? want : most);
+  // (and of the more rows a tile has, the more that is)
+  const int64_t rows = T / tile_room > 1 ? T / tile_room : 1, few = 256 / rows > 4 ? 256 / rows : 4;
+  if (sh.splits > few) sh.splits = (int)few;
   if (sh.splits < 1) sh.splits = 1;
   sh.bytes = (size_t)sh.splits * T * sh.width * 4;
   return sh;
@@ -580,7 +583,7 @@ static int launch_adapters(int count, const mdbf_adapter_t* list, int adapters, 
       g->proj[g->slots] = (uint8_t)i, g->tile[g->slots] = (uint8_t)t;
       ++g->slots;
     }
-    const int chunk = 4 * kOutBlock * (tile_room * wide >= 256 ? 2 : 1);
+    const int chunk = 4 * kOutBlock * (tile_room * wide >= 512 ? 2 : 1);
     out.p[i] = {l.B_dev, l.Y_dev, l.scale_dev, l.ldy, l.m, l.r, column, l.y_dtype, chunk};
     column += (l.r + 15) / 16 * 16;
     yds |= 1 << l.y_dtype;
