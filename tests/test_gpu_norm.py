@@ -157,3 +157,21 @@ def test_rows_beyond_two_to_the_31_elements(gpu):
     X.copy_(torch.from_numpy(rng.standard_normal((3, 1024)).astype(np.float32)).to("cuda:0").to(torch.bfloat16))
     Y, _, _ = mb.mdbf_add_norm(X)
     _close(Y, so.add_norm(X.double().cpu().numpy(), None, None, float(np.float32(1e-6)))[0], "bf16")
+
+
+def test_views_of_every_kind(gpu):
+    """One row or one channel of something larger, rows that are not side by side: results are the same, and rows of their own."""
+    torch, mb = gpu
+    rng = np.random.default_rng(4)
+    store = _rows(torch, rng, 12, 600, "f32", 0)
+    for x in (store[3:4, 100:228], store[::3, :128], store[:, 4:5], store[5:6, 8:9], store[2:3], store[:, :0 + 1]):
+        if x.data_ptr() % 16:
+            x = torch.nn.functional.pad(x, (0, 7))[:, :x.shape[1]]
+        y, h, _ = mb.mdbf_add_norm(x, x)
+        want, sums = so.add_norm(x.double().cpu().numpy(), x.double().cpu().numpy(), None, float(np.float32(1e-6)))
+        _close(y, want, "f32")
+        assert torch.equal(h, x + x) and y.shape == h.shape == x.shape
+    with pytest.raises(AssertionError):
+        mb.mdbf_add_norm(store.T)
+    with pytest.raises(mb.MdbfError):
+        mb.mdbf_add_norm(store[:1].expand(12, 600))

@@ -14,8 +14,10 @@ HOST = ("mdbf_adapter_tiles", "mdbf_adapters_workspace_bytes", "mdbf_sample_work
 def stand_ins(world, monkeypatch):
     monkeypatch.setattr(tb.Library, "HOST", tb.Library.HOST + HOST)
     monkeypatch.setattr(tb.Tensor, "get_device", lambda self: getattr(self, "index", 0), raising=False)
-    monkeypatch.setattr(tb.Tensor, "view", lambda self, *shape: tb.Tensor(shape, self.dtype, self.made_on), raising=False)
+    monkeypatch.setattr(tb.Tensor, "as_strided", lambda self, shape, strides: tb.Tensor(shape, self.dtype, self.made_on), raising=False)
+    monkeypatch.setattr(tb.Tensor, "split_with_sizes", tb.Tensor.split, raising=False)
     monkeypatch.setattr(tb.Tensor, "new_empty", lambda self, shape, dtype: mb._torch_module.empty(tuple(shape), dtype=dtype), raising=False)
+    mb._torch_module.empty_like = lambda like, dtype=None: mb._torch_module.empty(tuple(like.shape), dtype=dtype)
     mb._torch_module.float8_e4m3fn = torch.float8_e4m3fn
 
 
