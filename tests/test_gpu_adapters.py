@@ -223,3 +223,13 @@ def test_pools_beyond_two_to_the_31_elements(gpu):
     x = X.double().cpu().numpy()
     want = so.adapters(x, of_small, A64, B64, None)
     assert (np.abs(Y.double().cpu().numpy() - want) <= _bound(x, of_small, A64, B64, np.ones(3), np.zeros_like(want), want, "bf16", "f32")).all()
+
+
+def test_wide_projections(gpu):
+    """More channels and columns than any chunk, split and row of tiles."""
+    _check(gpu, 4, 2, 3, [(70001, 70003, 4)], "bf16", ["f32"], seed=9)
+    _check(gpu, 70, 1, 1, [(40000, 16, 33), (40000, 30000, 16)], "f16", ["f16", "f16"], seed=10)
+
+
+def test_a_step_of_one_row_and_many_adapters(gpu):
+    _check(gpu, 1, 500, 1, [(256, 256, 16), (256, 8, 64)], "bf16", ["bf16", "bf16"], seed=11)

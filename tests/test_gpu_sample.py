@@ -162,3 +162,25 @@ def test_many_light_tokens_behind_a_heavy_one(gpu):
     z[:, 31415] = 0.0
     for settings in (dict(), dict(top_p=0.9), dict(top_k=30000)):
         _check(gpu, z, 0.1 + 0.85 * rng.random(6), **settings)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+def test_the_largest_vocabulary(gpu, dtype):
+    """2^20 tokens, 128 parts: one near the end alone, thousands alike, and everything."""
+    rng = np.random.default_rng(12)
+    z = _logits(rng, 4, 1 << 20)
+    z[1, :] = -np.inf
+    z[1, (1 << 20) - 1] = -5.0
+    z[2, ::300] = 12.0
+    for settings in (dict(), dict(top_p=0.95, min_p=1e-4), dict(top_k=100000)):
+        _check(gpu, z, rng.random(4), dtype, **settings)
+
+
+def test_logits_at_every_scale(gpu):
+    """Offsets and spreads from far below to far above 1: weights go by differences, over a temperature of that scale."""
+    rng = np.random.default_rng(13)
+    for scale in (1e-6, 1e-3, 1e3, 1e6):
+        for offset in (0.0, 1.0, -300.0):
+            z = (_logits(rng, 3, 6000) + offset) * scale
+            _check(gpu, z, rng.random(3), temperature=scale)
+            _check(gpu, z, rng.random(3), temperature=scale, top_p=0.9, top_k=1000)
