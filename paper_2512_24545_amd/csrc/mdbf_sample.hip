@@ -208,7 +208,7 @@ __device__ void sample_digits(const SampleArgs& a, int64_t t, const RowSetting& 
 // part's.  Tokens that equal the part's largest are counted apart, so that those that equal the row's largest, of weight 1, make up a bucket of an exact mass:
 // where many are alike, bounds fall on borders between them.
 // The first launch's vector work (some 40 instructions a token, 20 of them fp64) and its LDS additions take longer than the logits: 200 rows of 128256 bf16
-// (51 MB, 10 us at the rate of a read) 39 us, of which writing buckets and order is as much traffic again.  The second one is a chain of some thirty
+// (51 MB, 10 us at the rate of a read) 37.5 us, of which writing buckets and order is as much traffic again.  The second one is a chain of some thirty
 // meetings and dependent loads: 10.7 us for one row of 128256 whose list is short, 21 for 64 rows of 32000 whose longest list is 740, 29 for 200 rows of
 // 128256 with lists of up to 4000.  Before: one workgroup a row that reads it for every digit of every bound, 430, 200 and 680 us.
 constexpr int kBuckets = 768;                    // of a row: the largest, then 767 sixteenths, down to 2^-47 of it; less weighs nothing
@@ -276,9 +276,9 @@ template <int DT>
 __global__ __launch_bounds__(kPartThreads, 6) void sample_parts_kernel(SampleArgs a, Parts parts) {
   __shared__ __align__(16) uint16_t order[kPart];
   __shared__ unsigned long long hist[kBuckets];
-  __shared__ uint32_t slot[kBuckets];
+  __shared__ uint32_t slot[kBuckets + 2];        // the next place in the order of those that equal the largest, then of each bucket's
   __shared__ float tops[kPartThreads / 64];
-  __shared__ uint32_t waves[kPartThreads / 64], equal, next_equal, left, first;
+  __shared__ uint32_t waves[kPartThreads / 64], equal, left, first;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t t = blockIdx.y, part = t * gridDim.x + blockIdx.x;
   const int i0 = blockIdx.x * kPart;
@@ -291,7 +291,7 @@ __global__ __launch_bounds__(kPartThreads, 6) void sample_parts_kernel(SampleArg
   }
   const RowSetting r = row_setting(a, t);
   for (int o = tid; o < kBuckets; o += kPartThreads) hist[o] = 0;
-  if (tid == 0) equal = next_equal = left = 0, first = 0xffffffffu;
+  if (tid == 0) equal = left = slot[0] = 0, first = 0xffffffffu;
   float v[kEach], best = -__builtin_inff();
 #pragma unroll
   for (int p = 0; p < kEach / 8; ++p) {
@@ -329,16 +329,17 @@ __global__ __launch_bounds__(kPartThreads, 6) void sample_parts_kernel(SampleArg
   const double base = floor(degrees(r, largest));
   const BucketWord bucket_word;
   uint32_t alike = 0;
-  int down[kEach];                               // a token's bucket; -1: of the part's largest
+  int down[kEach];                               // a token's slot: 0 of the largest, 1 + its bucket; beyond the last: none
 #pragma unroll
   for (int e = 0; e < kEach; ++e) {
     const bool same = v[e] == largest;
     alike += (uint32_t)__popcll(__ballot(same));
-    down[e] = same ? -1 : kBuckets;
+    down[e] = same ? 0 : kBuckets + 1;
     const double d = degrees(r, v[e]), f = floor(d), b = base - f;
     if (b < kBuckets && !same && !infinite) {           // (not of -inf, whose b is inf, and not of NaN)
-      down[e] = (int)b;
-      atomicAdd(&hist[down[e]], bucket_word(d - f));
+      const int o = (int)b;
+      down[e] = o + 1;
+      atomicAdd(&hist[o], bucket_word(d - f));
     }
   }
   if (lane == 0 && alike) atomicAdd(&equal, alike);
@@ -366,7 +367,7 @@ __global__ __launch_bounds__(kPartThreads, 6) void sample_parts_kernel(SampleArg
   const unsigned long long reached = __ballot(reach0);          // (holds for the first buckets alone)
   if (reached && lane == 63 - __builtin_clzll(reached)) atomicMax(&left, start + c0 + (reach1 ? c1 : 0));
   if (has) {
-    slot[2 * tid] = reach0 ? start : kPart, slot[2 * tid + 1] = reach1 ? start + c0 : kPart;
+    slot[2 * tid + 1] = reach0 ? start : kPart, slot[2 * tid + 2] = reach1 ? start + c0 : kPart;
     typedef unsigned long long Pair __attribute__((ext_vector_type(2)));
     *((MDBF_GLOBAL Pair*)(parts.hists + part * kBuckets) + tid) = Pair{h0, h1};
   }
@@ -374,12 +375,15 @@ __global__ __launch_bounds__(kPartThreads, 6) void sample_parts_kernel(SampleArg
   const uint32_t n_left = max(left, n_equal);
   if (has) ((MDBF_GLOBAL uint32_t*)(parts.starts + part * kBuckets))[tid] = min(start, n_left) | min(start + c0, n_left) << 16;
   if (tid == 0) parts.heads[part] = {(unsigned long long)key << 32, n_equal};
+  uint32_t place[kEach];                         // (asked for together, so that their trips overlap: one after another 39 us instead of 37.5 above)
 #pragma unroll
   for (int e = 0; e < kEach; ++e) {
-    if (down[e] >= kBuckets) continue;
-    const uint32_t place = atomicAdd(down[e] < 0 ? &next_equal : &slot[down[e]], 1u);
-    if (place < kPart) order[place] = (uint16_t)place_of(e);    // (slots that none reaches begin at kPart)
+    place[e] = kPart;
+    if (down[e] <= kBuckets) place[e] = atomicAdd(&slot[down[e]], 1u);
   }
+#pragma unroll
+  for (int e = 0; e < kEach; ++e)
+    if (place[e] < kPart) order[place[e]] = (uint16_t)place_of(e);    // (slots that none reaches begin at kPart)
   __syncthreads();
   MDBF_GLOBAL U32x4* out = (MDBF_GLOBAL U32x4*)(parts.left + part * kPart);
   for (uint32_t x = tid; x * 8 < n_left; x += kPartThreads) out[x] = ((const U32x4*)order)[x];
