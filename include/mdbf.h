@@ -439,8 +439,8 @@ int mdbf_add_norm(const mdbf_norm_t* desc, const void* x_dev, int64_t ldx, const
  *   tiles  (tile_room x 4) (adapter, place of its first row in rows, rows of the tile, 0): an adapter's rows in tiles of
  *                          MDBF_ADAPTER_TILE, its last one shorter, in the order of rows; (-1, 0, 0, 0) behind the last
  *   places (requests)      the place of each request's first row in rows; requests without an adapter come behind the others
- * For mdbf_adapters rows and tiles may be made by other means.  cu must not fall and lies in 0 .. T; where it does not, nothing outside of the
- * tables is written, but they are of no use.  At most 8192 adapters.  One launch, two for long steps.
+ * For mdbf_adapters rows and tiles may be made by other means.  cu must not fall and lies in 0 .. T (rows in front of cu[0] and from cu[requests] on
+ * are no request's and have no adapter); where it does not, nothing outside of the tables is written, but they are of no use.  At most 8192 adapters.  One launch, two for long steps.
  * tile_room: at least mdbf_adapter_tiles(T, requests, adapters), as many as there can be (host only; a negative mdbf_status for
  * bad arguments). */
 #define MDBF_ADAPTER_TILE 64

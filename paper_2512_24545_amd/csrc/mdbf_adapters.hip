@@ -22,6 +22,10 @@ struct RowArgs {
 
 __device__ __forceinline__ int cut(int v, int most) { return min(max(v, 0), most); }
 
+// The place of a row that is no request's (lo: the last request that begins at it or before, -1: none).  The requests' rows, from `first` to `end`, take the
+// places from 0 on: rows in front of them come right behind those, and rows behind them keep theirs, so that each place has one row.
+__device__ __forceinline__ uint32_t place_of_no_request(int t, int lo, int first, int end) { return lo < 0 ? (uint32_t)end - (uint32_t)first + (uint32_t)t : (uint32_t)t; }
+
 // inclusive sums over the workgroup's threads
 __device__ __forceinline__ void row_scan(uint32_t& a, uint32_t& b, uint32_t (*waves)[2]) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -131,8 +135,8 @@ __global__ __launch_bounds__(kRowThreads) void adapter_rows_kernel(RowArgs a) {
       else hi = mid;
     }
     const bool in = lo >= 0 && t - first_row[lo] < fresh[lo];
-    const uint32_t at = in ? (uint32_t)first_place[lo] + (uint32_t)(t - first_row[lo]) : (uint32_t)t;
-    // (rows behind the last request keep their places: there the tables end)
+    const uint32_t at = in ? (uint32_t)first_place[lo] + (uint32_t)(t - first_row[lo])
+                           : place_of_no_request(t, lo, first_row[0], first_row[a.requests - 1] + fresh[a.requests - 1]);
     if (at < (uint32_t)a.T) a.rows[at] = in && keys[lo] < N ? t : -1;
   }
 }
@@ -150,7 +154,8 @@ __global__ __launch_bounds__(kRowChunk) void adapter_places_kernel(RowArgs a) {
   const int from = lo < 0 ? 0 : cut(a.cu[lo], a.T);
   const bool in = lo >= 0 && t < cut(a.cu[lo + 1], a.T);
   const int k = in ? a.adapter[lo] : -1;
-  const uint32_t at = in ? (uint32_t)a.places[lo] + (uint32_t)(t - from) : (uint32_t)t;
+  const uint32_t at = in ? (uint32_t)a.places[lo] + (uint32_t)(t - from)
+                         : place_of_no_request(t, lo, cut(a.cu[0], a.T), cut(a.cu[a.requests], a.T));
   if (at < (uint32_t)a.T) a.rows[at] = k >= 0 && k < a.adapters ? t : -1;
 }
 

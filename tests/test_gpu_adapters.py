@@ -233,3 +233,19 @@ def test_wide_projections(gpu):
 
 def test_a_step_of_one_row_and_many_adapters(gpu):
     _check(gpu, 1, 500, 1, [(256, 256, 16), (256, 8, 64)], "bf16", ["bf16", "bf16"], seed=11)
+
+
+@pytest.mark.parametrize("requests,adapters,fresh,first", [(1, 1, 2, 2), (5, 3, 4, 1), (64, 32, 1, 64), (37, 9, 40, 1000), (1024, 100, 3, 77), (1500, 400, 1, 5),
+                                                           (500, 100, 300, 9000), (3, 2, 9000, 12345)])
+def test_a_step_whose_first_rows_are_no_requests(gpu, requests, adapters, fresh, first):
+    """cu begins behind 0, as that of a part of a step's requests does: in one launch and in two."""
+    torch, mb = gpu
+    rng = np.random.default_rng(requests + first)
+    for behind in (0, 7):
+        cu, of = _step(rng, requests, adapters, fresh)
+        cu = cu + first
+        T = int(cu[-1]) + behind
+        got = mb.mdbf_adapter_rows(_ints(torch, cu), _ints(torch, of), adapters, T)
+        rows, tiles, places = so.adapter_tables(cu.tolist(), of.tolist(), adapters, T, got.tiles.shape[0])
+        assert np.array_equal(got.rows.cpu().numpy(), rows)
+        assert np.array_equal(got.tiles.cpu().numpy(), tiles) and np.array_equal(got.places.cpu().numpy(), places)
