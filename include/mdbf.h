@@ -484,7 +484,7 @@ int mdbf_adapters(int count, const mdbf_adapter_t* list, int dtype, int adapters
  *   min_p          T fp32 or null; NaN: no bound
  *   tokens         T int32; -1 in a row that holds nothing but -inf and NaN (NaN counts as -inf, whose weight is 0)
  *   probs          T fp32 or null: the token's weight over that of all kept ones; 0 with token -1
- * Among infinite logits each has the weight 1, and finite ones none.  Weights are fp64; those below 2^-47 of the largest count as none, and the sums that
+ * Among infinite logits each has the weight 1, and finite ones none.  Weights are fp64; those below 2^-47 of the largest may count as none, and the sums that
  * bounds and draw go by are held to 1e-11 of themselves, in an order that is fixed or does not matter: repeated calls return the same bits.  Two launches.  The
  * workspace's size (host arithmetic only, 25 KB per row and 8192 tokens) never shrinks with T and vocab (1 .. 2^20). */
 typedef struct {

@@ -62,116 +62,131 @@ __device__ __forceinline__ uint32_t key_at(const SampleArgs& a, int64_t t, int i
 }
 
 constexpr int kPickThreads = 1024;
-constexpr double kUnit = 0x1p43;                // weights as whole numbers: their sums do not go by the order of the additions
+
+// Masses as whole numbers, whose sums do not go by the order of the additions: units of 2^-43, and what is left of a weight in units of 2^-65.
+// (2^20 weights of 1 are 2^63 of the ones, their rests at most 2^42 of the others: there a count fits above them.)  A weight is off by 2^-66, so many
+// equal ones, whose errors are the same and add up, by 2^-46 together; one word of 2^-43 alone would be off by 6e-8.
+constexpr int kRestBits = 22, kTallyBit = 43;
+struct Mass {
+  unsigned long long units, rests;
+  __device__ __forceinline__ Mass() : units(0), rests(0) {}
+  __device__ __forceinline__ Mass(unsigned long long u, unsigned long long r) : units(u + (r >> kRestBits)), rests(r & ((1ull << kRestBits) - 1)) {}
+  __device__ __forceinline__ explicit Mass(double w) {
+    const double x = w * 0x1p43;
+    units = (unsigned long long)x;
+    rests = (unsigned long long)((x - (double)units) * (double)(1 << kRestBits) + 0.5);
+  }
+  __device__ __forceinline__ Mass operator+(const Mass& m) const { return Mass(units + m.units, rests + m.rests); }
+  __device__ __forceinline__ double value() const { return ((double)units + (double)rests * (1.0 / (1 << kRestBits))) * 0x1p-43; }
+};
 
 struct PickShared {
-  uint32_t count[256];
-  unsigned long long mass[256];
-  unsigned long long sum[kPickThreads / 64];
+  unsigned long long units[256], rests[256];     // (the rests' words: how many tokens, above kTallyBit)
+  unsigned long long sum[2][kPickThreads / 64];
   uint32_t found[kPickThreads / 64];
   uint32_t digit, count_before;
-  unsigned long long mass_before;
+  Mass before;
 };
+__device__ __forceinline__ uint32_t tokens_of(unsigned long long word) { return (uint32_t)(word >> kTallyBit); }
+__device__ __forceinline__ Mass mass_of(unsigned long long units, unsigned long long word) { return Mass(units, word & ((1ull << kTallyBit) - 1)); }
 
 // The place in the order of keys at which the number of tokens reaches `count`, or else their mass reaches `mass` (or goes beyond it).  Four
 // digits of eight bits, the largest first.
 struct Place {
   uint32_t key, ties, before;                   // of equal keys there are `ties`; tokens and mass in front of them
-  unsigned long long mass_before;
+  Mass mass_before;
 };
-template <int DT>
-__device__ Place descend(const SampleArgs& a, int64_t t, const RowSetting& r, PickShared& s, uint32_t count, double mass, bool beyond) {
+template <int DT, class Weight>
+__device__ Place descend(const SampleArgs& a, int64_t t, const Weight& weight_of, PickShared& s, uint32_t count, double mass, bool beyond) {
   const int tid = threadIdx.x, lane = tid & 63;
-  Place at = {0, 0, 0, 0};
+  Place at = {0, 0, 0, {}};
   for (int shift = 24; shift >= 0; shift -= 8) {
     __syncthreads();
-    if (tid < 256) s.count[tid] = 0, s.mass[tid] = 0;
+    if (tid < 256) s.units[tid] = 0, s.rests[tid] = 0;
     __syncthreads();
     for (int i = tid; i < a.vocab; i += kPickThreads) {
       const uint32_t k = key_at<DT>(a, t, i);
       if (shift < 24 && ((k ^ at.key) >> (shift + 8))) continue;
-      atomicAdd(&s.count[(k >> shift) & 255], 1u);
-      const unsigned long long w = (unsigned long long)(weight(r, k) * kUnit + 0.5);
-      if (w) atomicAdd(&s.mass[(k >> shift) & 255], w);
+      const Mass m(weight_of(k));
+      atomicAdd(&s.rests[(k >> shift) & 255], 1ull << kTallyBit | m.rests);
+      if (m.units) atomicAdd(&s.units[(k >> shift) & 255], m.units);
     }
     __syncthreads();
     if (tid < 64) {
-      uint32_t c = 0;
-      unsigned long long m = 0;
-      for (int q = 0; q < 4; ++q) c += s.count[255 - lane * 4 - q], m += s.mass[255 - lane * 4 - q];
-      uint32_t c_to = c;
-      unsigned long long m_to = m;
+      unsigned long long units = 0, word = 0;
+      for (int q = 0; q < 4; ++q) units += s.units[255 - lane * 4 - q], word += s.rests[255 - lane * 4 - q];
+      const uint32_t c = tokens_of(word);
+      unsigned long long units_to = units, word_to = word;
       for (int o = 1; o < 64; o <<= 1) {
-        const uint32_t uc = __shfl_up(c_to, o);
-        const unsigned long long um = __shfl_up(m_to, o);
-        if (lane >= o) c_to += uc, m_to += um;
+        const unsigned long long uu = __shfl_up(units_to, o), uw = __shfl_up(word_to, o);
+        if (lane >= o) units_to += uu, word_to += uw;
       }
-      c_to += at.before, m_to += at.mass_before;
-      const bool here = c && (count ? c_to >= count : beyond ? (double)m_to > mass : (double)m_to >= mass);
-      const unsigned long long hit = __ballot(here), any = __ballot(c != 0);
+      const auto reached = [&](uint32_t c, const Mass& m) { return count ? c >= count : beyond ? m.value() > mass : m.value() >= mass; };
+      const unsigned long long hit = __ballot(c && reached(at.before + tokens_of(word_to), at.mass_before + mass_of(units_to, word_to))), any = __ballot(c != 0);
       const int who = hit ? __builtin_ctzll(hit) : 63 - __builtin_clzll(any);
       if (lane == who) {
-        uint32_t cb = c_to - c;
-        unsigned long long mb = m_to - m;
+        uint32_t cb = at.before + tokens_of(word_to) - c;
+        Mass mb = at.mass_before + mass_of(units_to - units, word_to - word);
         for (int q = 0; q < 4; ++q) {
-          const uint32_t b = 255 - lane * 4 - q, cc = s.count[b];
+          const uint32_t b = 255 - lane * 4 - q, cc = tokens_of(s.rests[b]);
           if (!cc) continue;
-          s.digit = b, s.count_before = cb, s.mass_before = mb;
-          const double m2 = (double)(mb + s.mass[b]);
-          if (count ? cb + cc >= count : beyond ? m2 > mass : m2 >= mass) break;
-          cb += cc, mb += s.mass[b];
+          s.digit = b, s.count_before = cb, s.before = mb;
+          cb += cc, mb = mb + mass_of(s.units[b], s.rests[b]);
+          if (reached(cb, mb)) break;
         }
       }
     }
     __syncthreads();
     at.key |= s.digit << shift;
-    at.before = s.count_before, at.mass_before = s.mass_before;
-    at.ties = s.count[s.digit];
+    at.before = s.count_before, at.mass_before = s.before;
+    at.ties = tokens_of(s.rests[s.digit]);
   }
   return at;
 }
 
-// A row that nothing else serves: read again for every digit.
-template <int DT>
-__device__ void sample_digits(const SampleArgs& a, int64_t t, const RowSetting& r, PickShared& s) {
+// A row that nothing else serves: read again for every digit.  `weighs`: whether a logit lies in the buckets, as below: the same tokens weigh nothing on both ways.  128256
+// logits, us: 450 flat ones, 1050 with top_k and top_p too, 1030 equal ones (whose LDS additions all meet).
+template <int DT, class Weighs>
+__device__ void sample_digits(const SampleArgs& a, int64_t t, const RowSetting& r, PickShared& s, const Weighs& weighs) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const auto weight_of = [&](uint32_t key) { return weighs(key_value(key)) ? weight(r, key) : 0.0; };
   // what is kept is a first part of the order, and so is what each bound leaves: the least of their masses
-  unsigned long long total = 0, likely = 0;
+  Mass total, likely;
   for (int i = tid; i < a.vocab; i += kPickThreads) {
-    const double x = weight(r, key_at<DT>(a, t, i));
-    const unsigned long long w = (unsigned long long)(x * kUnit + 0.5);
-    total += w;
-    if (x >= r.min_p) likely += w;
+    const double x = weight_of(key_at<DT>(a, t, i));
+    const Mass w(x);
+    total = total + w;
+    if (x >= r.min_p) likely = likely + w;
   }
   for (int q = 0; q < 2; ++q) {
-    unsigned long long v = q ? likely : total;
-    for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o);
+    Mass v = q ? likely : total;
+    for (int o = 1; o < 64; o <<= 1) v = v + Mass(__shfl_xor(v.units, o), __shfl_xor(v.rests, o));
     __syncthreads();
-    if (lane == 0) s.sum[wave] = v;
+    if (lane == 0) s.sum[0][wave] = v.units, s.sum[1][wave] = v.rests;
     __syncthreads();
-    v = 0;
-    for (int w = 0; w < kPickThreads / 64; ++w) v += s.sum[w];
+    v = Mass();
+    for (int w = 0; w < kPickThreads / 64; ++w) v = v + Mass(s.sum[0][w], s.sum[1][w]);
     (q ? likely : total) = v;
   }
-  double kept = (double)total;
+  double kept = total.value();
   if (r.top_k) {
-    const Place p = descend<DT>(a, t, r, s, r.top_k, 0.0, false);
-    kept = (double)p.mass_before + (double)(r.top_k - p.before) * (weight(r, p.key) * kUnit);
+    const Place p = descend<DT>(a, t, weight_of, s, r.top_k, 0.0, false);
+    kept = p.mass_before.value() + (double)(r.top_k - p.before) * weight_of(p.key);
   }
   double least = kept;
   if (r.top_p < 1.0) {
     const double mass = r.top_p * kept;
-    const Place p = descend<DT>(a, t, r, s, 0, mass, false);
-    const double w = weight(r, p.key) * kUnit, b = (double)p.mass_before;
+    const Place p = descend<DT>(a, t, weight_of, s, 0, mass, false);
+    const double w = weight_of(p.key), b = p.mass_before.value();
     double j = w > 0 ? ceil((mass - b) / w) : 1.0;
     j = fmin(fmax(j, 1.0), (double)p.ties);
     least = fmin(least, b + j * w);
   }
-  if (r.min_p > 0.0) least = fmin(least, fmax((double)likely, kUnit));
+  if (r.min_p > 0.0) least = fmin(least, fmax(likely.value(), 1.0));
   kept = least;
   const double mass = r.u * kept;
-  const Place p = descend<DT>(a, t, r, s, 0, mass, true);
-  const double w = weight(r, p.key) * kUnit, b = (double)p.mass_before;
+  const Place p = descend<DT>(a, t, weight_of, s, 0, mass, true);
+  const double w = weight_of(p.key), b = p.mass_before.value();
   const uint32_t key = p.key;
   const double j = w > 0 ? floor((mass - b) / w) : 0.0;
   const uint32_t tie = (uint32_t)fmin(fmax(j, 0.0), (double)(p.ties - 1));
@@ -875,7 +890,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_rows_kernel(SampleArgs a,
   const int n = (int)s.n;
   if (n > kList || n == 0) {
     __syncthreads();
-    sample_digits<DT>(a, t, r, *(PickShared*)shared);
+    sample_digits<DT>(a, t, r, *(PickShared*)shared, [&](float x) { return bucket_of(x) < kBuckets; });
     return;
   }
   if (n <= 64) {

@@ -184,3 +184,44 @@ def test_logits_at_every_scale(gpu):
             z = (_logits(rng, 3, 6000) + offset) * scale
             _check(gpu, z, rng.random(3), temperature=scale)
             _check(gpu, z, rng.random(3), temperature=scale, top_p=0.9, top_k=1000)
+
+
+@pytest.mark.parametrize("V", [9000, 128256, 1 << 20])
+@pytest.mark.parametrize("logit", [-9.0, -18.0, -21.0])
+def test_thousands_of_equal_light_tokens(gpu, V, logit):
+    """One token of weight 1, the others alike and light: rounding of a weight is the same for all of them and adds up.  Sums held to 1e-11 of
+    themselves move a place among the light ones by up to 1e-11 (1 / weight + V), 0.013 tokens; u and top_p are numbers whose place is no
+    nearer than a tenth of a token to an edge, in 64 significant bits."""
+    torch, mb = gpu
+    rng = np.random.default_rng(V)
+    heavy, w = V // 3, np.exp(np.longdouble(logit))
+    z = torch.full((1, V), logit, device="cuda:0")
+    z[0, heavy] = 0.0
+
+    def numbers(kept, count):
+        """fp32 numbers at which kept weights of 1 + (kept - 1) w are cut among the light ones, and the place of each cut."""
+        total = 1 + (kept - 1) * w
+        u = ((1 + (kept - 1) * w * rng.random(50 * count)) / total).astype(np.float32)
+        place = (u.astype(np.longdouble) * total - 1) / w
+        part = place - np.floor(place)
+        good = (part > 0.1) & (part < 0.9) & (place > 0) & (u <= 1 - 2.0 ** -24)
+        return u[good][:count], np.floor(place[good][:count]).astype(np.int64)
+
+    def check(kept, **on):
+        u, place = numbers(kept, 24)
+        if len(u) == 0:                                             # (light ones that weigh less together than a step of u)
+            return
+        tokens, probs = mb.mdbf_sample(z.expand(len(u), V).contiguous(), torch.from_numpy(u).to("cuda:0"),
+                                       **{k: torch.full((len(u),), v, dtype=torch.int32 if k == "top_k" else torch.float32, device="cuda:0") for k, v in on.items()})
+        assert np.array_equal(tokens.cpu().numpy(), np.where(place < heavy, place, place + 1)), (on, kept)
+        share = float(w / (1 + (kept - 1) * w))
+        assert (np.abs(probs.double().cpu().numpy() - share) <= (TINY + 1e-11) * share).all()
+
+    check(V)
+    check(V // 2, top_k=V // 2)
+    p, place = numbers(V, 3)
+    for p, place in zip(p, place):
+        check(int(place) + 2, top_p=float(p))                      # the one that the bound falls into is kept
+    p, place = numbers(V // 2, 3)
+    for p, place in zip(p, place):
+        check(int(place) + 2, top_p=float(p), top_k=V // 2)
