@@ -228,11 +228,11 @@ __device__ void sample_digits(const SampleArgs& a, int64_t t, const RowSetting& 
 // 128256 with lists of up to 4000.  Before: one workgroup a row that reads it for every digit of every bound, 430, 200 and 680 us.
 constexpr int kBuckets = 768;                    // of a row: the largest, then 767 sixteenths, down to 2^-47 of it; less weighs nothing
 constexpr int kPerOctave = 16;
-constexpr int kFracBits = 39;                    // of 2^(frac / 16) - 1 < 0.0443: a part's stay below 2^49, where the count begins
+constexpr int kFracBits = 39;                    // of 2^(frac / 16) - 1 + kBias < 0.0443: a part's stay below 2^49, where the count begins
 constexpr int kCountBit = 49;
 constexpr int kList = 8192;                      // tokens of a row that the second launch looks at; rows that have more go by digits
 constexpr int kPartThreads = 512, kPart = 8192, kEach = kPart / kPartThreads;   // tokens of a part, of a thread
-constexpr double kSlack = 1e-7;                  // more than sums of buckets and of tokens differ by, with logits of up to 1e9 temperatures
+constexpr double kSlack = 1e-7;                  // far more than sums of buckets and of tokens differ by
 
 struct PartHead {
   unsigned long long top;                        // key of the part's largest, and, where that one is asked for, ~its index: of equal keys the lowest is largest
@@ -246,16 +246,21 @@ struct Parts {
   uint16_t* left;                                // kPart: tokens in the order of their buckets, their places in the part
 };
 
+// t, rounded: its floor, the bucket, goes with the order of the logits, in every part alike.
 __device__ __forceinline__ double degrees(const RowSetting& r, float x) { return (double)x * r.grid; }
+// t - floor without t's rounding, which at ten million temperatures from zero would be 1e-9 of a weight: a little below 0 or above 1 where t was rounded over
+// a whole number.  (Distinct logits of 24 bits share buckets up to t = 2^34, so by at most 2^-20 of t.)
+__device__ __forceinline__ double fraction(const RowSetting& r, float x, double floor) { return fma((double)x, r.grid, -floor); }
+constexpr double kBias = 0x1p-16;                // a token adds this more, so that its whole number is none below 0
 
-// What a token adds to its bucket: 1 in the count, and 2^(x / 16) - 1 in units of 2^-39 for x in [0, 1), the fraction of its t.  A polynomial through five
+// What a token adds to its bucket: 1 in the count, and 2^(x / 16) - 1 + kBias in units of 2^-39 for x in [0, 1], the fraction of its t.  A polynomial through five
 // Chebyshev points, off by at most 2.6e-12; the sum with 2^52 and the count's bit has the whole number in its last bits.
 struct BucketWord {
   double c0, c1, c2, c3, c4;
   __device__ __forceinline__ BucketWord() {
     constexpr double unit = (double)(1ull << kFracBits);
     c4 = 1.4997758288814042e-07 * unit, c3 = 1.3547982742839567e-05 * unit, c2 = 9.38385803440002e-04 * unit, c1 = 0.04332169865857207 * unit;
-    c0 = 2.528854437695519e-12 * unit + 0x1p52 + (double)(1ull << kCountBit);
+    c0 = (2.528854437695519e-12 + kBias) * unit + 0x1p52 + (double)(1ull << kCountBit);
     // (as values that the compiler does not know they stay in scalar registers; it would copy constants into a sum's register every time)
     asm("" : "+s"(c0), "+s"(c1), "+s"(c2), "+s"(c3), "+s"(c4));
   }
@@ -354,7 +359,7 @@ __global__ __launch_bounds__(kPartThreads, 6) void sample_parts_kernel(SampleArg
     if (b < kBuckets && !same && !infinite) {           // (not of -inf, whose b is inf, and not of NaN)
       const int o = (int)b;
       down[e] = o + 1;
-      atomicAdd(&hist[o], bucket_word(d - f));
+      atomicAdd(&hist[o], bucket_word(fraction(r, v[e], f)));
     }
   }
   if (lane == 0 && alike) atomicAdd(&equal, alike);
@@ -792,16 +797,17 @@ __global__ __launch_bounds__(kPickThreads) void sample_rows_kernel(SampleArgs a,
   const float largest = key_value(key);
   r.top = key, r.largest = (double)largest;
   const bool infinite = largest == __builtin_inff();
-  const double most = infinite ? 0.0 : degrees(r, largest), base = floor(most), frac = most - base;
+  const double base = infinite ? 0.0 : floor(degrees(r, largest));
+  // (beyond 2^53 it is no fraction, and nothing but the largest weighs)
+  const double frac = infinite ? 0.0 : fmin(fmax(fraction(r, largest, base), -kBias), 1 + kBias);
   const auto bucket_of = [&](float x) { return x == largest ? 0 : 1 + (int)fmin(base - floor(degrees(r, x)), (double)kBuckets); };
 
   if (tid < parts) {
     const float its = key_value((uint32_t)(head.top >> 32));
     const bool none = its == -__builtin_inff() || (infinite && its != largest);
     const int b = none ? kBuckets : min(bucket_of(its), kBuckets);
-    const double d = degrees(r, its);
     s.part_top[tid] = b, s.part_equal[tid] = none ? 0 : (uint32_t)head.equal;
-    s.part_extra[tid] = b == 0 || none ? 0 : head.equal * (BucketWord()(d - floor(d)) & ((1ull << kCountBit) - 1));
+    s.part_extra[tid] = b == 0 || b >= kBuckets ? 0 : head.equal * (BucketWord()(fraction(r, its, floor(degrees(r, its)))) & ((1ull << kCountBit) - 1));
   }
   __syncthreads();
 
@@ -828,7 +834,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_rows_kernel(SampleArgs a,
     }
   }
   const double mass = tid == 0 ? (double)count
-                               : ((double)count + (double)extra * (1.0 / (double)(1ull << kFracBits))) * exp2(-(tid - 1 + frac) / kPerOctave);
+                               : ((double)count * (1 - kBias) + (double)extra * (1.0 / (double)(1ull << kFracBits))) * exp2(-(tid - 1 + frac) / kPerOctave);
   uint32_t count_to = count;
   double upto = mass;
 #pragma unroll

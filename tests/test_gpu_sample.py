@@ -225,3 +225,33 @@ def test_thousands_of_equal_light_tokens(gpu, V, logit):
     p, place = numbers(V // 2, 3)
     for p, place in zip(p, place):
         check(int(place) + 2, top_p=float(p), top_k=V // 2)
+
+
+@pytest.mark.parametrize("temperature", [0.0888, 0.0815])
+def test_logits_of_millions_of_temperatures(gpu, temperature):
+    """Logits that differ by a last bit, ten million temperatures from zero: 500000 tokens in front of the few that are looked at and 540000 behind
+    them, all summed by buckets.  u are the numbers whose place is 3e-5 to 1.5e-4 tokens from an edge, on either side; sums held to 1e-11
+    of themselves move a place by 1e-11 V = 1.1e-5."""
+    torch, mb = gpu
+    rng = np.random.default_rng(14)
+    T32, V, few = np.float32(temperature), 1 << 20, 6000
+    level = np.float32(2.0 ** 20) - np.float32(2.0 ** -4) * np.arange(1, 8, dtype=np.float32)    # the next numbers below 2^20
+    counts = [1, 0, 0, 0, 500000, few, V - few - 500001]
+    z = np.repeat(level, counts)
+    order = rng.permutation(V)
+    row = np.empty(V, dtype=np.float32)
+    row[order] = z
+    w = np.exp((level.astype(np.longdouble) - level[0]) / np.longdouble(T32))
+    before = 1 + counts[4] * w[4]
+    total = before + few * w[5] + counts[6] * w[6]
+    u = np.unique(rng.uniform(float(before / total), float((before + few * w[5]) / total), 400000).astype(np.float32))
+    place = (u.astype(np.longdouble) * total - before) / w[5]
+    part = place - np.floor(place)
+    edge = np.minimum(part, 1 - part)
+    pick = (edge > 3e-5) & (edge < 1.5e-4) & (place > 0) & (place < few)
+    u, place = u[pick], np.floor(place[pick]).astype(np.int64)
+    assert len(u) >= 4
+    held = torch.from_numpy(row).to("cuda:0").expand(len(u), V).contiguous()
+    tokens, _ = mb.mdbf_sample(held, torch.from_numpy(u).to("cuda:0"), torch.full((len(u),), float(T32), device="cuda:0"))
+    want = np.sort(np.flatnonzero(row == level[5]))[place]
+    assert np.array_equal(tokens.cpu().numpy(), want)
