@@ -255,3 +255,13 @@ def test_logits_of_millions_of_temperatures(gpu, temperature):
     tokens, _ = mb.mdbf_sample(held, torch.from_numpy(u).to("cuda:0"), torch.full((len(u),), float(T32), device="cuda:0"))
     want = np.sort(np.flatnonzero(row == level[5]))[place]
     assert np.array_equal(tokens.cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("V", [10, 40, 300, 5000, 20000])
+def test_different_logits_of_equal_weight(gpu, V):
+    """An infinite temperature: every sum is a whole number, and so are the places of bounds and draws, on edges too."""
+    rng = np.random.default_rng(V + 1)
+    z = rng.standard_normal((8, V))
+    u = np.array([0.0, 0.5, 0.25, 0.75, 0.125, 1 - 2.0 ** -24, 0.875, 0.375])
+    for settings in (dict(), dict(top_p=0.5), dict(top_p=0.25, top_k=V // 2), dict(top_p=0.75, min_p=1.0)):
+        _check(gpu, z, u, temperature=np.inf, **settings)
