@@ -265,3 +265,18 @@ def test_different_logits_of_equal_weight(gpu, V):
     u = np.array([0.0, 0.5, 0.25, 0.75, 0.125, 1 - 2.0 ** -24, 0.875, 0.375])
     for settings in (dict(), dict(top_p=0.5), dict(top_p=0.25, top_k=V // 2), dict(top_p=0.75, min_p=1.0)):
         _check(gpu, z, u, temperature=np.inf, **settings)
+
+
+@pytest.mark.parametrize("temperature", [np.inf, 1e6, 3e4])
+@pytest.mark.parametrize("V", [300, 3000, 8000])
+def test_thousands_of_different_logits_of_nearly_one_weight(gpu, V, temperature):
+    """All of them in one bin of a bucket, or in a few: the bounds and the draw are found among their digits.  (A place is 1e-9 V tokens from where the
+    64-bit sums have it, so 1e-5 of the draws could differ.)"""
+    rng = np.random.default_rng(V)
+    z = rng.standard_normal((6, V))
+    z[3] = np.abs(z[3])
+    z[4, ::7] = -np.inf
+    z[5, :V // 2] = z[5, 0]
+    for settings in (dict(), dict(top_k=V // 3), dict(top_k=5), dict(top_p=0.37), dict(top_p=0.9, top_k=V // 2), dict(min_p=1 - 1e-6), dict(min_p=1.0), dict(top_p=0.5, min_p=0.99999)):
+        _check(gpu, z, rng.random(6), temperature=temperature, **settings)
+        _check(gpu, z, rng.random(6), "bf16", temperature=temperature, **settings)
