@@ -141,6 +141,13 @@ __global__ __launch_bounds__(WAVES > 4 ? WAVES * 64 : 256) void norm_kernel(Norm
     if (scale == 0.0f) scale = 1.0f;
     if (bad) scale = __builtin_nanf("");
     if (lane == 0) ((MDBF_GLOBAL float*)a.scales)[t * a.lds] = scale;
+    if (scale < 0x1p-126f) {                // of few bits: y may be more than 464 of it, for which the conversion has NaN instead of 448
+      const float most = 448.0f * scale;
+#pragma unroll
+      for (int v = 0; v < VPT; ++v)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[v][i] = fminf(fmaxf(h[v][i], -most), most);
+    }
 #pragma unroll
     for (int v = 0; v < VPT; ++v) {
       const int c = (v * LANES + lane) * 8;

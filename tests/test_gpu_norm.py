@@ -175,3 +175,22 @@ def test_views_of_every_kind(gpu):
         mb.mdbf_add_norm(store.T)
     with pytest.raises(mb.MdbfError):
         mb.mdbf_add_norm(store[:1].expand(12, 600))
+
+
+def test_scales_that_round_to_a_coarse_number(gpu):
+    """Rows whose largest over 448 has few bits: what passes 448 scales is 448, as the nearest such number, and no NaN."""
+    torch, mb = gpu
+    step = 2.0 ** -149
+    tops = [100, 223, 225, 300, 448, 500, 600, 671, 673, 900, 1100, 5000, 100000]
+    n = 96
+    rng = np.random.default_rng(5)
+    y = np.array([[t * step * (-1) ** i * (1 - i / n) for i in range(n)] for t in tops])
+    # (a row of ones and its mean: y is the weight, a row of weights per call)
+    for t, row in zip(tops, y):
+        w = torch.from_numpy(row.astype(np.float32)).to("cuda:0")
+        q, _, s = mb.mdbf_add_norm(torch.ones((3, n), device="cuda:0"), weight=w, eps=0.0, y_dtype="e4m3")
+        scale = np.float32(t * step) / np.float32(448)
+        scale = np.float32(1) if scale == 0 else scale
+        assert (s.cpu().numpy() == scale).all()
+        want = so.e4m3(w.double().cpu().numpy() / float(scale))
+        assert np.array_equal(q.float().cpu().numpy(), np.broadcast_to(want, (3, n))), t
