@@ -427,7 +427,8 @@ typedef struct {
  *                    smallest power of two (from 2^-126 on) that leaves the largest magnitude at most 448; 255 and NaN codes for a block with a NaN or an infinity
  * in it.
  * Rows are ldx, ldr, ldro, ldy elements apart (any, at least n).  Outputs may be the inputs themselves where strides and
- * types agree, and otherwise overlap nothing.  One launch. */
+ * types agree, and otherwise overlap nothing.  One launch; of millions of rows, one for each 2^31
+ * threads. */
 int mdbf_add_norm(const mdbf_norm_t* desc, const void* x_dev, int64_t ldx, const void* residual_dev, int64_t ldr,
                   const float* weight_dev, int T, void* residual_out_dev, int64_t ldro, void* y_dev, int64_t ldy,
                   void* scales_dev, int64_t lds, void* stream);

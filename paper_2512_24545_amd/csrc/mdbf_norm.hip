@@ -12,7 +12,7 @@ struct NormArgs {
   const void *x, *res;
   const float* weight;
   void *res_out, *y, *scales;
-  int64_t ldx, ldr, ldro, ldy, lds;
+  int64_t ldx, ldr, ldro, ldy, lds, t0;           // t0: the launch's first row
   int32_t T, n, yd, group;
   float eps;
 };
@@ -77,7 +77,7 @@ __global__ __launch_bounds__(WAVES > 4 ? WAVES * 64 : 256) void norm_kernel(Norm
   __shared__ double sums[WAVES];
   __shared__ uint32_t tops[WAVES];
   const int lane = threadIdx.x & (LANES - 1);
-  const int64_t t = (int64_t)blockIdx.x * ROWS + (ROWS > 1 ? threadIdx.x / LANES : 0);
+  const int64_t t = a.t0 + (int64_t)blockIdx.x * ROWS + (ROWS > 1 ? threadIdx.x / LANES : 0);
   if (t >= a.T) return;                     // (rows of one wave only: no barrier follows there)
 
   Raw8<XD> rx[VPT];
@@ -186,11 +186,16 @@ __global__ __launch_bounds__(WAVES > 4 ? WAVES * 64 : 256) void norm_kernel(Norm
 }
 
 template <int XD, int HD, int WAVES, int VPT>
-static void launch_norm_w(const NormArgs& a, bool stream, hipStream_t s) {
+static void launch_norm_w(const NormArgs& all, bool stream, hipStream_t s) {
   constexpr int ROWS = WAVES >= 4 ? 1 : 4 / WAVES;
-  const dim3 grid((unsigned)((a.T + (int64_t)ROWS - 1) / ROWS)), block(WAVES * 64 * ROWS);
-  if (stream) norm_kernel<XD, HD, WAVES, VPT, true><<<grid, block, 0, s>>>(a);
-  else norm_kernel<XD, HD, WAVES, VPT, false><<<grid, block, 0, s>>>(a);
+  const int64_t groups = (all.T + (int64_t)ROWS - 1) / ROWS, most = (1ll << 31) / (WAVES * 64 * ROWS);
+  for (int64_t g0 = 0; g0 < groups; g0 += most) {   // (a launch has less than 2^32 threads: beyond, their number wraps without an error)
+    NormArgs a = all;
+    a.t0 = g0 * ROWS;
+    const dim3 grid((unsigned)(groups - g0 < most ? groups - g0 : most)), block(WAVES * 64 * ROWS);
+    if (stream) norm_kernel<XD, HD, WAVES, VPT, true><<<grid, block, 0, s>>>(a);
+    else norm_kernel<XD, HD, WAVES, VPT, false><<<grid, block, 0, s>>>(a);
+  }
 }
 
 template <int XD, int HD>
@@ -231,7 +236,7 @@ int mdbf_add_norm(const mdbf_norm_t* desc, const void* x_dev, int64_t ldx, const
   const void* ptrs[] = {x_dev, residual_dev, weight_dev, residual_out_dev, y_dev, scales_dev};
   for (const void* p : ptrs)
     if (!ptr_aligned(p, 16)) return MDBF_EALIGN;
-  const NormArgs a = {x_dev, residual_dev, weight_dev, residual_out_dev, y_dev, scales_dev, ldx, ldr, ldro, ldy, lds,
+  const NormArgs a = {x_dev, residual_dev, weight_dev, residual_out_dev, y_dev, scales_dev, ldx, ldr, ldro, ldy, lds, 0,
                       T, n, desc->y_dtype, desc->scale_group, desc->eps};
   const int64_t written = (int64_t)T * n * ((eight ? 1 : dtype_size(desc->y_dtype)) + (residual_out_dev ? dtype_size(desc->h_dtype) : 0));
   const bool nt = written > kNormStreamBytes;

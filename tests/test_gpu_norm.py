@@ -194,3 +194,25 @@ def test_scales_that_round_to_a_coarse_number(gpu):
         assert (s.cpu().numpy() == scale).all()
         want = so.e4m3(w.double().cpu().numpy() / float(scale))
         assert np.array_equal(q.float().cpu().numpy(), np.broadcast_to(want, (3, n))), t
+
+
+def test_more_rows_than_a_launch_has(gpu):
+    """A launch ends at 2^32 threads: 2^26 rows of a wave each."""
+    torch, mb = gpu
+    T = 2 ** 26 + 5
+    X = torch.randn(T, device="cuda:0").bfloat16().view(T, 1)
+    X[X == 0] = 1
+    Y, _, _ = mb.mdbf_add_norm(X, eps=0.0)
+    assert torch.equal(Y, X.sign())
+
+
+def test_more_rows_of_a_workgroup_each_than_a_launch_has(gpu):
+    """2^23 rows of four waves: around the border between launches, and at the end."""
+    torch, mb = gpu
+    T, n = 2 ** 23 + 3, 520
+    X = torch.empty((T, n), dtype=torch.bfloat16, device="cuda:0").normal_()
+    Y, _, S = mb.mdbf_add_norm(X, y_dtype="e4m3")
+    for rows in (slice(0, 5), slice(2 ** 23 - 3, T)):
+        again, _, scales = mb.mdbf_add_norm(X[rows], y_dtype="e4m3")
+        assert torch.equal(Y[rows].view(torch.uint8), again.view(torch.uint8)) and torch.equal(S[rows], scales)
+    assert (S > 0).all() and (S < 1).all()
