@@ -168,6 +168,7 @@ __global__ __launch_bounds__(kRowChunk) void adapter_places_kernel(RowArgs a) {
 constexpr int kInSlots = 4;                    // tiles of 16 ranks per workgroup of the first launch
 constexpr int kMaxRank = 256;
 constexpr int kMaxWidth = 1 << 23;             // channels and columns: the second launch's grid ends at 65535 times 256 columns
+constexpr int64_t kMaxTiles = (1 << 24) - 1;    // a launch has less than 2^32 threads: beyond, their number wraps without an error
 constexpr int kMaxGroups = MDBF_ADAPTER_MAX * kMaxRank / 16 / kInSlots;
 constexpr int kOutBlock = 64;                  // columns of Y that a wave takes at a time
 
@@ -544,7 +545,7 @@ static int check_adapters(int count, const mdbf_adapter_t* list, int dtype, int 
     if (!row_dtype(l.y_dtype)) return MDBF_EDTYPE;
     if (l.r > kMaxRank || l.n > kMaxWidth || l.m > kMaxWidth) return MDBF_EUNSUPPORTED;
   }
-  return tile_room > (1ll << 30) ? MDBF_EUNSUPPORTED : MDBF_OK;
+  return tile_room > kMaxTiles ? MDBF_EUNSUPPORTED : MDBF_OK;
 }
 
 template <int NL>

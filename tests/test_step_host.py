@@ -162,3 +162,12 @@ def test_new_types_are_refused_where_they_were():
     assert L.mdbf_workspace_bytes(C.byref(d), 1, C.byref(out)) == -3
     rope = mb.RopeDesc(4, 2, 128, 0, 0, 1, 3, 0, 1e-6)
     assert L.mdbf_qk_norm_rope(rope, A, 512, A, 256, None, None, None, None, 1, A, 512, A, 256, None, None, 0, None, 0, None, None) == -3
+
+
+def test_more_tiles_than_a_launch_has():
+    """2^24 tiles would be 2^32 threads, which a launch does not have."""
+    L, out = mb.lib(), C.c_size_t(0)
+    arr = (mb.AdapterDesc * 1)(adapter())
+    for room, status in ((1 << 24, -5), (1 << 31, -5), ((1 << 24) - 1, -4)):
+        assert L.mdbf_adapters(1, arr, 1, 4, 10, A, A, room, A, 0, None) == status
+        assert L.mdbf_adapters_workspace_bytes(1, arr, 1, 4, 10, room, C.byref(out)) == (0 if status == -4 else status)
