@@ -777,16 +777,28 @@ def mdbf_adapter_rows(cu, adapter, adapters, tokens, out=None, stream=None):
 
 
 class Adapters:
-    """The low-rank adapters of one projection (m x n): A (adapters, r, n), B (adapters, m, r), f16 or bf16, and scale (adapters fp32, or None)."""
+    """The low-rank adapters of one projection (m x n): A (adapters, r, n), B (adapters, m, r), f16 or bf16, and scale (adapters fp32, or None).  Other
+    tensors are another Adapters; where one of these gets other memory (set_, data), it is checked again and used from there."""
 
     def __init__(self, A, B, scale=None):
+        _torch()
         self.count, self.r, self.n = A.shape
         self.m = B.shape[1]
-        assert B.shape == (self.count, self.m, self.r) and A.dtype == B.dtype and A.is_contiguous() and B.is_contiguous()
-        _torch()
-        assert scale is None or _ints(scale, self.count, _torch_module.float32)
-        self.A, self.B, self.scale = A, B, scale
-        self.args = (A.data_ptr(), B.data_ptr(), 0 if scale is None else scale.data_ptr())
+        self.dtype = A.dtype
+        self.tensors, self.checked = (A, B, scale), None
+        self.args()
+
+    A, B, scale = (property(lambda self, i=i: self.tensors[i]) for i in range(3))
+
+    def args(self):
+        """Addresses of the three."""
+        A, B, scale = self.tensors
+        at = A.data_ptr(), B.data_ptr(), 0 if scale is None else scale.data_ptr()
+        if at != self.checked:
+            assert A.shape == (self.count, self.r, self.n) and B.shape == (self.count, self.m, self.r) and A.is_contiguous() and B.is_contiguous()
+            assert A.dtype == B.dtype == self.dtype and (scale is None or _ints(scale, self.count, _torch_module.float32))
+            self.checked = at
+        return at
 
 
 _pack_adapter = struct.Struct("4i7q").pack       # an AdapterDesc's bytes, in a third of the time that making one takes
@@ -796,13 +808,18 @@ assert struct.calcsize("4i7q") == C.sizeof(AdapterDesc)
 def _adapter_list(rows, adapters, Xs, Ys):
     count, T = len(adapters), rows.tokens
     assert 0 < count == len(Xs) == len(Ys) and count <= MDBF_ADAPTER_MAX
-    dtype = adapters[0].A.dtype
-    tensors, descs = [rows.rows, rows.tiles], []
+    dtype = adapters[0].dtype
+    tensors, descs, last, last_n = [rows.rows, rows.tiles], [], None, 0
     for p, X, Y in zip(adapters, Xs, Ys):
         n, m = p.n, p.m
-        assert p.count == rows.adapters and p.A.dtype == X.dtype == dtype and X.shape == (T, n) and Y.shape == (T, m)
-        tensors += (X, Y, p.A, p.B, p.scale)
-        descs.append(_pack_adapter(n, m, p.r, DTYPE_CODE[_DTYPE_NAME[Y.dtype]], *p.args, X.data_ptr(), _rows_of(X, T, n), Y.data_ptr(), _rows_of(Y, T, m)))
+        if X is not last or n != last_n:         # (projections most often share it)
+            assert X.dtype == dtype and X.shape == (T, n)
+            tensors.append(X)
+            x_args, last, last_n = (X.data_ptr(), _rows_of(X, T, n)), X, n
+        assert p.count == rows.adapters and p.dtype == dtype and Y.shape == (T, m)
+        tensors.append(Y)
+        tensors += p.tensors
+        descs.append(_pack_adapter(n, m, p.r, DTYPE_CODE[_DTYPE_NAME[Y.dtype]], *p.args(), *x_args, Y.data_ptr(), _rows_of(Y, T, m)))
     _here(*tensors)
     return b"".join(descs), count, DTYPE_CODE[_DTYPE_NAME[dtype]]
 

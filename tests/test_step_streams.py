@@ -107,3 +107,36 @@ def test_refused(world, name):
     with pytest.raises((AssertionError, mb.MdbfError)):
         REFUSED[name]()
     assert not world[1]
+
+
+class Moved(tb.Tensor):
+    """A tensor whose memory can be swapped, as set_ and data do."""
+    at = 4096
+
+    def data_ptr(self):
+        return self.at
+
+
+def test_adapters_that_get_other_memory(world, monkeypatch):
+    """A call reads where its adapters lie then, and checks them again if that changed; they are not replaced behind its back."""
+    A, B, scale = Moved((4, 8, 64), torch.bfloat16), Moved((4, 32, 8), torch.bfloat16), Moved((4,), torch.float32)
+    p, sent = mb.Adapters(A, B, scale), []
+    record = mb._lib
+    monkeypatch.setattr(type(record), "mdbf_adapters", lambda self, count, arr, *rest: sent.append(mb.struct.unpack("4i7q", arr)[4:7]) or 0, raising=False)
+    call = lambda: mb.mdbf_adapters(rows(), [p], [T16(5, 64)], [T16(5, 32)])             # noqa: E731
+    call()
+    A.at, B.at, scale.at = 1 << 20, 2 << 20, 3 << 20
+    call()
+    assert sent == [(4096, 4096, 4096), (1 << 20, 2 << 20, 3 << 20)]
+    for t, attribute, other in ((A, "shape", (3, 8, 64)), (B, "shape", (4, 31, 8)), (B, "dtype", torch.float16), (scale, "dtype", torch.bfloat16)):
+        kept = getattr(t, attribute)
+        setattr(t, attribute, other)
+        t.at += 16
+        with pytest.raises(AssertionError):
+            call()
+        setattr(t, attribute, kept)
+        call()
+    for name in ("A", "B", "scale"):
+        with pytest.raises(AttributeError):
+            setattr(p, name, B)
+    assert (p.A, p.B, p.scale) == (A, B, scale) and len(sent) == 6
