@@ -464,9 +464,17 @@ class KVCache:
         if buffer is None:
             torch = _torch()
             buffer = torch.zeros(pages * self.page_bytes, dtype=torch.uint8, device=device)
-        self.buffer = buffer
         assert buffer.is_cuda and buffer.is_contiguous() and buffer.element_size() == 1
-        self.args = (buffer.data_ptr(), buffer.numel())
+        self.pool = buffer
+
+    @property
+    def buffer(self):
+        return self.pool
+
+    @property
+    def args(self):
+        """Where the pool lies now, and its bytes (the library refuses fewer than the pages are)."""
+        return self.pool.data_ptr(), self.pool.numel()
 
 
 class KVSlots:

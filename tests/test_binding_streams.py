@@ -150,3 +150,23 @@ def test_the_current_stream(world, name):
     assert calls == [(name, CALLER.cuda_stream)]
     assert len(made) == results + WORKSPACES.get(name, 0)
     assert all(t.made_on is CALLER and not t.used_on for t in made)
+
+
+def test_a_pool_that_gets_other_memory(world, monkeypatch):
+    """Calls read where the cache's pool lies then (its storage may be swapped); another pool is another KVCache."""
+    class Moved(Tensor):
+        at = 4096
+
+        def data_ptr(self):
+            return self.at
+
+    pool, sent = Moved((40 * 2 * 64 * 136,), torch.uint8), []
+    monkeypatch.setattr(Library, "mdbf_kv_append", lambda self, desc, at, size, *rest: sent.append((at, size)) or 0, raising=False)
+    c = mb.KVCache(40, 2, 128, 64, "bf16", buffer=pool)
+    slots = Tensor((5,), torch.int64)
+    mb.mdbf_kv_append(c, heads(5, 2), heads(5, 2), slots)
+    pool.at, pool.shape = 1 << 20, (64,)
+    mb.mdbf_kv_append(c, heads(5, 2), heads(5, 2), slots)
+    assert sent == [(4096, 40 * 2 * 64 * 136), (1 << 20, 64)] and c.buffer is pool
+    with pytest.raises(AttributeError):
+        c.buffer = pool
