@@ -749,13 +749,14 @@ def _adapter_tiles(tokens, requests, adapters):
 class AdapterRows:
     """A step's rows in the order of their adapters: rows (tokens), tiles (room x 4) and places (requests), int32 (include/mdbf.h has their
     contents).  Made once for these sizes, it can be handed to every step's mdbf_adapter_rows; rows and tiles may also be
-    given."""
+    given, both of them."""
 
     def __init__(self, tokens, requests, adapters, device="cuda:0", stream=None, rows=None, tiles=None):
         torch = _torch()
+        assert (rows is None) == (tiles is None), "rows and tiles go together"
         self.tokens, self.requests, self.adapters = tokens, requests, adapters
         self.rows, self.tiles, self.places = rows, tiles, None
-        if rows is None or tiles is None:
+        if rows is None:
             room = _adapter_tiles(tokens, requests, adapters)
             # (tiles first: their entries are read 16 bytes at a time)
             ints = _result(lambda: torch.empty(4 * room + tokens + requests, dtype=torch.int32, device=device), stream)

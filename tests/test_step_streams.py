@@ -140,3 +140,11 @@ def test_adapters_that_get_other_memory(world, monkeypatch):
         with pytest.raises(AttributeError):
             setattr(p, name, B)
     assert (p.A, p.B, p.scale) == (A, B, scale) and len(sent) == 6
+
+
+@pytest.mark.parametrize("given", ["rows", "tiles"])
+def test_half_of_the_tables(world, given):
+    """Rows without tiles, or tiles without rows, are no tables, and are not dropped either."""
+    with pytest.raises(AssertionError):
+        mb.AdapterRows(5, 3, 4, **{given: tb.ints(5) if given == "rows" else tb.ints(6, 4)})
+    assert not world[0]
