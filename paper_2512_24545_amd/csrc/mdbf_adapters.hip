@@ -512,7 +512,7 @@ __global__ __launch_bounds__(256, YD == MDBF_F32 ? 2 : 3) void adapter_out_kerne
 // How a call is cut.
 struct AdapterShape {
   int width, splits;
-  size_t bytes;
+  size_t split_bytes;                          // V of one split
 };
 static AdapterShape adapter_shape(int count, const mdbf_adapter_t* list, int T, int64_t tile_room) {
   AdapterShape sh = {0, 1, 0};
@@ -532,7 +532,7 @@ static AdapterShape adapter_shape(int count, const mdbf_adapter_t* list, int T, 
   const int64_t rows = T / tile_room > 1 ? T / tile_room : 1, few = 256 / rows > 4 ? 256 / rows : 4;
   if (sh.splits > few) sh.splits = (int)few;
   if (sh.splits < 1) sh.splits = 1;
-  sh.bytes = (size_t)sh.splits * T * sh.width * 4;
+  sh.split_bytes = (size_t)T * sh.width * 4;
   return sh;
 }
 
@@ -568,8 +568,10 @@ static int launch_out(const OutArgs& o, int count, int64_t tile_room, int chunks
 
 template <int DT>
 static int launch_adapters(int count, const mdbf_adapter_t* list, int adapters, int T, const int32_t* rows, const int32_t* tiles, int64_t tile_room,
-                           float* V, hipStream_t s) {
-  const AdapterShape sh = adapter_shape(count, list, T, tile_room);
+                           float* V, size_t workspace_bytes, hipStream_t s) {
+  AdapterShape sh = adapter_shape(count, list, T, tile_room);
+  // (fewer rows may be cut into more splits than the workspace of a larger step has room for)
+  if (workspace_bytes / sh.split_bytes < (size_t)sh.splits) sh.splits = (int)(workspace_bytes / sh.split_bytes);
   InArgs in = {};
   OutArgs out = {};
   in.rows = out.rows = rows, in.tiles = out.tiles = tiles, in.V = V, out.V = V;
@@ -645,7 +647,8 @@ int mdbf_adapters_workspace_bytes(int count, const mdbf_adapter_t* list, int dty
   if (!bytes_out) return MDBF_EINVAL;
   const int st = check_adapters(count, list, dtype, adapters, T, tile_room);
   if (st) return st;
-  *bytes_out = adapter_shape(count, list, T, tile_room).bytes;
+  const AdapterShape sh = adapter_shape(count, list, T, tile_room);
+  *bytes_out = sh.splits * sh.split_bytes;
   return MDBF_OK;
 }
 
@@ -665,11 +668,11 @@ int mdbf_adapters(int count, const mdbf_adapter_t* list, int dtype, int adapters
     for (int j = 0; j < i; ++j)
       if (list[j].Y_dev == l.Y_dev) return MDBF_EINVAL;
   }
-  if (workspace_bytes < adapter_shape(count, list, T, tile_room).bytes) return MDBF_EWORKSPACE;
+  if (workspace_bytes < adapter_shape(count, list, T, tile_room).split_bytes) return MDBF_EWORKSPACE;
   float* V = (float*)workspace_dev;
   return hip_fail(dtype == MDBF_F16
-                      ? launch_adapters<MDBF_F16>(count, list, adapters, T, rows_dev, tiles_dev, tile_room, V, (hipStream_t)stream)
-                      : launch_adapters<MDBF_BF16>(count, list, adapters, T, rows_dev, tiles_dev, tile_room, V, (hipStream_t)stream));
+                      ? launch_adapters<MDBF_F16>(count, list, adapters, T, rows_dev, tiles_dev, tile_room, V, workspace_bytes, (hipStream_t)stream)
+                      : launch_adapters<MDBF_BF16>(count, list, adapters, T, rows_dev, tiles_dev, tile_room, V, workspace_bytes, (hipStream_t)stream));
 }
 
 }  // extern "C"

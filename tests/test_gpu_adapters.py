@@ -249,3 +249,33 @@ def test_a_step_whose_first_rows_are_no_requests(gpu, requests, adapters, fresh,
         rows, tiles, places = so.adapter_tables(cu.tolist(), of.tolist(), adapters, T, got.tiles.shape[0])
         assert np.array_equal(got.rows.cpu().numpy(), rows)
         assert np.array_equal(got.tiles.cpu().numpy(), tiles) and np.array_equal(got.places.cpu().numpy(), places)
+
+
+def test_a_workspace_of_a_larger_step(gpu):
+    """A program's one workspace, of its largest step, serves every smaller one, though few rows are cut into more parts."""
+    torch, mb = gpu
+    rng = np.random.default_rng(15)
+    n, m, r = 4096, 72, 16
+    up = lambda *shape: torch.from_numpy(rng.standard_normal(shape).astype(np.float32)).to("cuda:0").bfloat16()   # noqa: E731
+    pool = mb.Adapters(up(2, r, n) * n ** -0.5, up(2, m, r))
+    steps = {}
+    for T in (600, 200, 66, 9, 1):
+        rows = mb.mdbf_adapter_rows(_ints(torch, [0, T]), _ints(torch, [1]), 2, T)
+        X, Y = up(T, n), torch.zeros((T, m), dtype=torch.float32, device="cuda:0")
+        steps[T] = rows, X, Y, mb.mdbf_adapters_workspace(rows, [pool], [X], [Y])
+    sizes = {T: s[3].numel() for T, s in steps.items()}
+    assert sizes[200] > sizes[600] // 3                              # (per row: more)
+    for most in (600, 200, 66):
+        for T in (t for t in steps if t <= most):
+            rows, X, Y, _ = steps[T]
+            store = torch.full((sizes[most] + 64,), 77, dtype=torch.uint8, device="cuda:0")
+            x, a, b = (v.double().cpu().numpy() for v in (X, pool.A, pool.B))
+            of = np.full(T, 1)
+            want = so.adapters(x, of, a, b, None)
+            for workspace in (store[:sizes[most]], store[:T * 16 * 4]):    # and the least that there is: one part
+                Y.zero_()
+                mb.mdbf_adapters(rows, [pool], [X], [Y], workspace=workspace)
+                assert (np.abs(Y.double().cpu().numpy() - want) <= _bound(x, of, a, b, np.ones(2), np.zeros_like(want), want, "bf16", "f32")).all()
+            assert (store[sizes[most]:] == 77).all()
+            with pytest.raises(mb.MdbfError, match="EWORKSPACE"):
+                mb.mdbf_adapters(rows, [pool], [X], [Y], workspace=store[:T * 16 * 4 - 16])
