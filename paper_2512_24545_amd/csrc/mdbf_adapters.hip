@@ -340,8 +340,8 @@ __host__ __device__ inline Pieces pieces_of(int r) {
 
 // Y[row][c] += scale sum over ranks of V[row][rank] B[c][rank].  V, a sum of the splits', is written as NL numbers of 16 bits that add up to it;
 // fp16 has not fp32's exponents: there a row is brought to a largest of 1 first.  The columns of the products' tiles are laid out so that a lane
-// ends with 16 neighbouring columns of one row.  A wave takes 64 columns and SUBS times 16 rows at a time (more would take the registers that
-// other waves need); what it needs of B and Y for the first ones is on its way while V is made.
+// ends with 16 neighbouring columns of one row.  A wave takes 64 columns and all of the tile's rows, SUBS times 16, at a time; what it needs of B and Y for
+// the first ones is on its way while V is made.
 template <int DT, int YD, int NL, int SUBS>
 __device__ __forceinline__ void out_tile(const OutArgs& a, const OutProj& p, int adapter, int first, int count, U32x4* limbs, const int32_t* rows,
                                          int32_t* exponents) {
@@ -360,11 +360,11 @@ __device__ __forceinline__ void out_tile(const OutArgs& a, const OutProj& p, int
       if (there) load_raw8<DT>(p.B, ((int64_t)adapter * p.m + c) * p.r + j8, p.r - j8, w[j]);
     }
   };
-  const auto load_y = [&](int cb, int sub0, Raw8<YD>(&y)[SUBS][2]) {
+  const auto load_y = [&](int cb, Raw8<YD>(&y)[SUBS][2]) {
     const int c = cb + kg * 16;
 #pragma unroll
     for (int sub = 0; sub < SUBS; ++sub) {
-      const int row = rows[(sub0 + sub) * 16 + i];
+      const int row = rows[sub * 16 + i];
       if (row >= 0 && c < p.m) {
         const int64_t at = (int64_t)row * p.ldy + c;
         load_raw8<YD>(p.Y, at, p.m - c, y[sub][0]);
@@ -375,12 +375,11 @@ __device__ __forceinline__ void out_tile(const OutArgs& a, const OutProj& p, int
   int cb = (int)blockIdx.y * p.chunk + wave * kOutBlock;
   Raw8<DT> w[4];
   Raw8<YD> y[SUBS][2];
-  if (cb < c_end) load_b(cb, 0, w), load_y(cb, 0, y);
-  const int subs = (count + 16 * SUBS - 1) / (16 * SUBS) * SUBS;
+  if (cb < c_end) load_b(cb, 0, w), load_y(cb, y);
 
   // a row's pieces of eight ranks lie in a power of two of neighbouring lanes (V's columns behind a rank are zeros up to a multiple of 16)
   const int shift = f.eights > 1 ? 32 - __builtin_clz(f.eights - 1) : 0;
-  for (int cell = tid; cell < subs << (4 + shift); cell += 256) {
+  for (int cell = tid; cell < SUBS << (4 + shift); cell += 256) {
     const int t = cell >> shift, j = cell & ((1 << shift) - 1);
     const bool in = t < count && j < f.eights;
     float v[8] = {};
@@ -440,14 +439,14 @@ __device__ __forceinline__ void out_tile(const OutArgs& a, const OutProj& p, int
   }
   // pieces behind the last
   const int filled = f.packed ? f.eights * NL : f.eights;
-  for (int t = tid; t < subs * 16; t += 256)
+  for (int t = tid; t < SUBS * 16; t += 256)
     for (int piece = filled; piece < f.b_steps * 4; ++piece)
       for (int l = 0; l < f.limbs; ++l)
         limbs[((t >> 4) * f.b_steps * f.limbs + (piece >> 2) * f.limbs + l) * 64 + (piece & 3) * 16 + (t & 15)] = U32x4{0, 0, 0, 0};
   __syncthreads();
 
   const float scale = p.scale ? p.scale[adapter] : 1.0f;
-  for (int sub0 = 0; cb < c_end;) {
+  while (cb < c_end) {
     const int c = cb + kg * 16;
     Acc4 acc[SUBS][4] = {};
     for (int s = 0; s < f.b_steps; ++s) {
@@ -457,7 +456,7 @@ __device__ __forceinline__ void out_tile(const OutArgs& a, const OutProj& p, int
       for (int l = 0; l < f.limbs; ++l)
 #pragma unroll
         for (int sub = 0; sub < SUBS; ++sub) {
-          const U32x4 v = limbs[(((sub0 + sub) * f.b_steps + s) * f.limbs + l) * 64 + lane];
+          const U32x4 v = limbs[((sub * f.b_steps + s) * f.limbs + l) * 64 + lane];
 #pragma unroll
           for (int j = 0; j < 4; ++j) acc[sub][j] = product<DT>(w[j].w[0], v, acc[sub][j]);
         }
@@ -467,7 +466,7 @@ __device__ __forceinline__ void out_tile(const OutArgs& a, const OutProj& p, int
     }
 #pragma unroll
     for (int sub = 0; sub < SUBS; ++sub) {
-      const int t = (sub0 + sub) * 16 + i, row = rows[t];
+      const int t = sub * 16 + i, row = rows[t];
       if (row < 0) continue;
       float factor = scale;
       if (DT == MDBF_F16) factor = __builtin_ldexpf(factor, exponents[t]);
@@ -481,13 +480,8 @@ __device__ __forceinline__ void out_tile(const OutArgs& a, const OutProj& p, int
         store_float8<YD, false>(p.Y, (int64_t)row * p.ldy + c + 8 * h, p.m - c - 8 * h, out);
       }
     }
-    const bool same = sub0 + SUBS < subs;      // more rows of these columns
-    sub0 = same ? sub0 + SUBS : 0;
-    if (!same) cb += 4 * kOutBlock;
-    if (cb < c_end) {
-      if (!same || f.b_steps > 1) load_b(cb, 0, w);
-      load_y(cb, sub0, y);
-    }
+    cb += 4 * kOutBlock;
+    if (cb < c_end) load_b(cb, 0, w), load_y(cb, y);
   }
 }
 
