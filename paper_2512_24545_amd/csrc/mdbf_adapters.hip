@@ -339,7 +339,8 @@ __host__ __device__ inline Pieces pieces_of(int r) {
 }
 
 // Y[row][c] += scale sum over ranks of V[row][rank] B[c][rank].  V, a sum of the splits', is written as NL numbers of 16 bits that add up to it;
-// fp16 has not fp32's exponents: there a row is brought to a largest of 1 first.  The columns of the products' tiles are laid out so that a lane
+// fp16 has not fp32's exponents: there a row is brought to a largest of 2^14 to 2^15 first, so that the numbers of ranks far below the largest are there too, down to
+// 2^-24 (2^-39 of the largest; with a largest of 1 they ended at 2^-24 of it).  The columns of the products' tiles are laid out so that a lane
 // ends with 16 neighbouring columns of one row.  A wave takes 64 columns and all of the tile's rows, SUBS times 16, at a time; what it needs of B and Y for
 // the first ones is on its way while V is made.
 template <int DT, int YD, int NL, int SUBS>
@@ -408,8 +409,8 @@ __device__ __forceinline__ void out_tile(const OutArgs& a, const OutProj& p, int
 #pragma unroll
       for (int e = 0; e < 8; ++e) m = max(m, __builtin_bit_cast(uint32_t, v[e]) & 0x7fffffffu);
       for (int o = 1; o < 1 << shift; o <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o));
-      // the power of two that brings a row's largest into [1, 2); rows that are not finite stay
-      const int b = (int)(m >> 23), e2 = b == 255 || b == 0 ? 0 : b - 127;
+      // the power of two that brings a row's largest into [2^14, 2^15); rows that are not finite stay
+      const int b = (int)(m >> 23), e2 = b == 255 || b == 0 ? 0 : b - 127 - 14;
       if (j == 0) exponents[t] = e2;
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = __builtin_ldexpf(v[e], -e2);

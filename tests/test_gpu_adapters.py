@@ -279,3 +279,33 @@ def test_a_workspace_of_a_larger_step(gpu):
             assert (store[sizes[most]:] == 77).all()
             with pytest.raises(mb.MdbfError, match="EWORKSPACE"):
                 mb.mdbf_adapters(rows, [pool], [X], [Y], workspace=store[:T * 16 * 4 - 16])
+
+
+@pytest.mark.parametrize("x_dtype,y_dtype", [("f16", "f16"), ("f16", "f32"), ("bf16", "bf16"), ("bf16", "f32"), ("bf16", "f16")])
+@pytest.mark.parametrize("r,below", [(8, 18), (16, 18), (40, 18), (16, 24)])
+def test_ranks_far_below_a_rows_largest(gpu, r, below, x_dtype, y_dtype):
+    """Columns of B that read only ranks 2^-below of the row's largest inner value.  Inner values are carried to 2^-22 of themselves (bf16 with 16-bit results: 2^-16) or (fp16) 2^-38 of the row's
+    largest; with the sums' own n steps that leaves results to half a step of their type and some 2^-15."""
+    torch, mb = gpu
+    rng = np.random.default_rng(r)
+    T, n, m = 40, 64, 70
+    dt = _dt(torch, x_dtype)
+    up = lambda a: torch.from_numpy(a.astype(np.float32)).to("cuda:0").to(dt)                 # noqa: E731
+    a = rng.standard_normal((1, r, n))
+    a[0, 0] *= 2.0 ** 12
+    a[0, 1:] *= 2.0 ** (12 - below)
+    b = rng.standard_normal((1, m, r)) * 64
+    b[0, :-1, 0] = 0                                                # (the last column reads the largest one)
+    A, B, X = up(a), up(b), up(rng.standard_normal((T, n)))
+    Y = torch.zeros((T, m), dtype=_dt(torch, y_dtype), device="cuda:0")
+    rows = mb.mdbf_adapter_rows(_ints(torch, [0, T]), _ints(torch, [0]), 1, T)
+    mb.mdbf_adapters(rows, [mb.Adapters(A, B)], [X], [Y])
+    x, a, b = (v.double().cpu().numpy() for v in (X, A[0], B[0]))
+    inner, size = x @ a.T, np.abs(x) @ np.abs(a).T
+    off = (n + 8) * 2.0 ** -24 * size + (2.0 ** -16 if x_dtype == "bf16" and y_dtype != "f32" else 2.0 ** -22) * np.abs(inner) + (2.0 ** -38 * np.abs(inner).max(1, keepdims=True) if x_dtype == "f16" else 0)
+    want = inner @ b.T
+    bound = (off + 2 * (r + 8) * 2.0 ** -24 * np.abs(inner)) @ np.abs(b).T * (1 + 2.0 ** -7) + HALF[y_dtype] * np.abs(want) + TINY[y_dtype]
+    got = Y.double().cpu().numpy()
+    assert np.isfinite(got[:, :-1]).all() and (np.abs(got - want) <= bound)[:, :-1].all()
+    if y_dtype != "f16":                                            # (the last column is beyond fp16)
+        assert (np.abs(got - want) <= bound)[:, -1].all()
