@@ -469,15 +469,17 @@ __device__ __forceinline__ void out_tile(const OutArgs& a, const OutProj& p, int
     for (int sub = 0; sub < SUBS; ++sub) {
       const int t = sub * 16 + i, row = rows[t];
       if (row < 0) continue;
-      float factor = scale;
-      if (DT == MDBF_F16) factor = __builtin_ldexpf(factor, exponents[t]);
+      const int e2 = DT == MDBF_F16 ? exponents[t] : 0;    // (into the sum, which stays far from fp32's ends; a scale may be near them)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         if (c + 8 * h >= p.m) break;
         float out[8];
         to_float8<YD>(y[sub][h], out);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) out[e] = fmaf(factor, acc[sub][2 * h + e / 4][e % 4], out[e]);
+        for (int e = 0; e < 8; ++e) {
+          const float sum = acc[sub][2 * h + e / 4][e % 4];
+          out[e] = fmaf(scale, DT == MDBF_F16 ? __builtin_ldexpf(sum, e2) : sum, out[e]);
+        }
         store_float8<YD, false>(p.Y, (int64_t)row * p.ldy + c + 8 * h, p.m - c - 8 * h, out);
       }
     }

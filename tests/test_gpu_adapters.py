@@ -309,3 +309,25 @@ def test_ranks_far_below_a_rows_largest(gpu, r, below, x_dtype, y_dtype):
     assert np.isfinite(got[:, :-1]).all() and (np.abs(got - want) <= bound)[:, :-1].all()
     if y_dtype != "f16":                                            # (the last column is beyond fp16)
         assert (np.abs(got - want) <= bound)[:, -1].all()
+
+
+@pytest.mark.parametrize("x_dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("scale", [1e-37, 1e-30, 1e30])
+def test_scales_near_the_ends_of_fp32(gpu, x_dtype, scale):
+    """Small inner values with large columns of B, and the other way round: the products stay numbers of full precision."""
+    torch, mb = gpu
+    rng = np.random.default_rng(16)
+    T, n, m, r = 9, 40, 24, 8
+    dt = _dt(torch, x_dtype)
+    up = lambda a: torch.from_numpy(a.astype(np.float32)).to("cuda:0").to(dt)                 # noqa: E731
+    small, large = 2.0 ** -12, 2.0 ** 12
+    a, b, x = (small, large, small) if scale < 1 else (large, small, 64.0)
+    A, B, X = (up(rng.standard_normal(shape) * f) for shape, f in (((1, r, n), a), ((1, m, r), b), ((T, n), x)))
+    Y = torch.zeros((T, m), dtype=torch.float32, device="cuda:0")
+    rows = mb.mdbf_adapter_rows(_ints(torch, [0, T]), _ints(torch, [0]), 1, T)
+    scales = torch.full((1,), scale, device="cuda:0")
+    mb.mdbf_adapters(rows, [mb.Adapters(A, B, scales)], [X], [Y])
+    x, a, b, s = (v.double().cpu().numpy() for v in (X, A, B, scales))
+    want = so.adapters(x, [0] * T, a, b, s)
+    bound = _bound(x, [0] * T, a, b, s, np.zeros_like(want), want, x_dtype, "f32")
+    assert np.abs(want).max() < 2.0 ** 127 and (np.abs(Y.double().cpu().numpy() - want) <= bound).all()
