@@ -407,10 +407,13 @@ __device__ __forceinline__ void out_tile(const OutArgs& a, const OutProj& p, int
     if (DT == MDBF_F16) {
       uint32_t m = 0;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) m = max(m, __builtin_bit_cast(uint32_t, v[e]) & 0x7fffffffu);
+      for (int e = 0; e < 8; ++e) {            // (an infinity, which an adapter may hold, is one at any power of two)
+        const uint32_t b = __builtin_bit_cast(uint32_t, v[e]) & 0x7fffffffu;
+        m = max(m, b < 0x7f800000u ? b : 0u);
+      }
       for (int o = 1; o < 1 << shift; o <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o));
-      // the power of two that brings a row's largest into [2^14, 2^15); rows that are not finite stay
-      const int b = (int)(m >> 23), e2 = b == 255 || b == 0 ? 0 : b - 127 - 14;
+      // the power of two that brings a row's largest finite value into [2^14, 2^15)
+      const int b = (int)(m >> 23), e2 = b == 0 ? 0 : b - 127 - 14;
       if (j == 0) exponents[t] = e2;
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = __builtin_ldexpf(v[e], -e2);

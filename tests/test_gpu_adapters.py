@@ -331,3 +331,19 @@ def test_scales_near_the_ends_of_fp32(gpu, x_dtype, scale):
     want = so.adapters(x, [0] * T, a, b, s)
     bound = _bound(x, [0] * T, a, b, s, np.zeros_like(want), want, x_dtype, "f32")
     assert np.abs(want).max() < 2.0 ** 127 and (np.abs(Y.double().cpu().numpy() - want) <= bound).all()
+
+
+def test_an_infinite_inner_value_beside_large_ones(gpu):
+    """fp16: an infinity leaves the other inner values of its row within fp16's range, so that the sum is that infinity and no NaN."""
+    torch, mb = gpu
+    T, n, m, r = 20, 64, 40, 16
+    A = torch.full((1, r, n), 60000.0, dtype=torch.float16, device="cuda:0")
+    A[0, 3, 5] = float("inf")
+    B = -torch.ones((1, m, r), dtype=torch.float16, device="cuda:0")
+    B[0, :, 3] = 1.0
+    X = torch.ones((T, n), dtype=torch.float16, device="cuda:0")
+    X[::2] = -1.0
+    Y = torch.zeros((T, m), dtype=torch.float32, device="cuda:0")
+    rows = mb.mdbf_adapter_rows(_ints(torch, [0, T]), _ints(torch, [0]), 1, T)
+    mb.mdbf_adapters(rows, [mb.Adapters(A, B)], [X], [Y])
+    assert (Y[1::2] == float("inf")).all() and (Y[::2] == float("-inf")).all()
