@@ -464,10 +464,9 @@ typedef struct {
 
 /* Y[t] += scale[a] B[a] (A[a] X[t]) for the rows t in the tiles, a the tile's adapter: the rows of requests without one stay as
  * they are.  `count` projections (1 .. MDBF_ADAPTER_MAX) of one step in one call, `dtype` that of all X, A and B (MDBF_F16 or MDBF_BF16); they may
- * share X, not Y.  Y overlaps nothing else that the call reads.  Sums are fp32.  The inner values A X are carried as 16-bit numbers that add up to them: two to
- * 2^-16 of a value (bf16), three to 2^-23 (bf16, fp32 Y), two to 2^-22 of a
- * value or 2^-38 of a row's largest (fp16).  Y is rounded
- * once.  A row, a tile or an adapter outside of what T, tile_room and `adapters` say is left out; a row must not be listed twice.  tile_room up to 2^24 - 1.
+ * share X, not Y.  Y overlaps nothing else that the call reads.  Sums are fp32.  The inner values A X are fp32 too, and carried as 16-bit numbers that add up to
+ * them: three of bf16, all of a value's bits; two of fp16, off by up to 2^-23 of a value or 2^-38 of the row's largest.  (An infinity in B makes NaN.)  Y is
+ * rounded once.  A row, a tile or an adapter outside of what T, tile_room and `adapters` say is left out; a row must not be listed twice.  tile_room up to 2^24 - 1.
  * The workspace holds the inner values, summed in up to 16 parts of the channels: mdbf_adapters_workspace_bytes has room for as many as are fastest, which
  * need not grow with T.  Where there is room for fewer a call makes fewer, one at least (4 bytes for each row and each rank, ranks rounded up to 16), so the
  * workspace of a largest step serves all smaller ones.  Repeated calls with a workspace of one size return the same bits.  Two launches, one more for each

@@ -324,9 +324,13 @@ __global__ __launch_bounds__(256) void adapter_in_kernel(InArgs a) {
   else in_tile<DT, 4>(a, g, adapter, first, count, blockIdx.y, lds);
 }
 
-// How the numbers of 16 bits of V lie along the contraction: pieces of eight ranks, four to a product.  Up to two of them (rank 16) all numbers
-// of a rank follow each other, so that two of them fill one product; beyond, a product has one number of four pieces, and one operand of
-// B serves all of a rank's numbers.
+// V goes into the second product as numbers of 16 bits that add up to it: three of bf16, which have all of its bits, or two of fp16, off by 2^-23 of
+// a value at most (what is left behind the first one's 11 bits are multiples of 2^-23 of up to 2^-11, and the second one's step is 2^-22 there).
+template <int DT>
+constexpr int kNumbers = DT == MDBF_BF16 ? 3 : 2;
+// How they lie along the contraction: pieces of eight ranks, four to a product.  Up to two of them (rank 16) the numbers follow each other, the
+// first one's pieces, the second one's, and so on over as many products as that takes; beyond, a product has four pieces of one number.  Either way one
+// operand of B serves all numbers.  (q, k and v of 6458 rows of prompts, 58.9 us as with two numbers a value; 61.7 with an operand of B for the third ones.)
 struct Pieces {
   int eights, b_steps, limbs;                  // operands of B, and products per operand
   bool packed;
@@ -334,25 +338,25 @@ struct Pieces {
 template <int NL>
 __host__ __device__ inline Pieces pieces_of(int r) {
   const int eights = (r + 7) / 8;
-  if (eights <= 2) return {eights, (eights * NL + 3) / 4, 1, true};
+  if (eights <= 2) return {eights, 1, (eights * NL + 3) / 4, true};
   return {eights, (eights + 3) / 4, NL, false};
 }
 
-// Y[row][c] += scale sum over ranks of V[row][rank] B[c][rank].  V, a sum of the splits', is written as NL numbers of 16 bits that add up to it;
-// fp16 has not fp32's exponents: there a row is brought to a largest of 2^14 to 2^15 first, so that the numbers of ranks far below the largest are there too, down to
+// Y[row][c] += scale sum over ranks of V[row][rank] B[c][rank].  fp16 has not fp32's exponents: there a row is brought to a largest of 2^14 to 2^15 first, so that the numbers of ranks far below the largest are there too, down to
 // 2^-24 (2^-39 of the largest; with a largest of 1 they ended at 2^-24 of it).  The columns of the products' tiles are laid out so that a lane
 // ends with 16 neighbouring columns of one row.  A wave takes 64 columns and all of the tile's rows, SUBS times 16, at a time; what it needs of B and Y for
 // the first ones is on its way while V is made.
-template <int DT, int YD, int NL, int SUBS>
+template <int DT, int YD, int SUBS>
 __device__ __forceinline__ void out_tile(const OutArgs& a, const OutProj& p, int adapter, int first, int count, U32x4* limbs, const int32_t* rows,
                                          int32_t* exponents) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, kg = lane >> 4;
+  constexpr int NL = kNumbers<DT>;
   const Pieces f = pieces_of<NL>(p.r);
   const int c_end = (int)min((int64_t)p.m, ((int64_t)blockIdx.y + 1) * p.chunk);
 
   const auto load_b = [&](int cb, int s, Raw8<DT>(&w)[4]) {
     const int piece = s * 4 + kg, j8 = (f.packed ? piece % f.eights : piece) * 8;
-    const bool there = f.packed ? piece < f.eights * NL : piece < f.eights;
+    const bool there = f.packed || piece < f.eights;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       // product row i of tile j is the column cb + (i / 4) * 16 + j * 4 + i % 4
@@ -377,6 +381,13 @@ __device__ __forceinline__ void out_tile(const OutArgs& a, const OutProj& p, int
   Raw8<DT> w[4];
   Raw8<YD> y[SUBS][2];
   if (cb < c_end) load_b(cb, 0, w), load_y(cb, y);
+
+  // pieces behind the last (here, while B and Y are on their way)
+  const int steps = f.packed ? f.limbs : f.b_steps, numbers = f.packed ? 1 : NL;
+  for (int t = tid; t < SUBS * 16; t += 256)
+    for (int piece = f.packed ? f.eights * NL : f.eights; piece < steps * 4; ++piece)
+      for (int l = 0; l < numbers; ++l)
+        limbs[((t >> 4) * steps * numbers + (piece >> 2) * numbers + l) * 64 + (piece & 3) * 16 + (t & 15)] = U32x4{0, 0, 0, 0};
 
   // a row's pieces of eight ranks lie in a power of two of neighbouring lanes (V's columns behind a rank are zeros up to a multiple of 16)
   const int shift = f.eights > 1 ? 32 - __builtin_clz(f.eights - 1) : 0;
@@ -441,12 +452,6 @@ __device__ __forceinline__ void out_tile(const OutArgs& a, const OutProj& p, int
       limbs[((t >> 4) * f.b_steps * f.limbs + step) * 64 + (piece & 3) * 16 + (t & 15)] = out;
     }
   }
-  // pieces behind the last
-  const int filled = f.packed ? f.eights * NL : f.eights;
-  for (int t = tid; t < SUBS * 16; t += 256)
-    for (int piece = filled; piece < f.b_steps * 4; ++piece)
-      for (int l = 0; l < f.limbs; ++l)
-        limbs[((t >> 4) * f.b_steps * f.limbs + (piece >> 2) * f.limbs + l) * 64 + (piece & 3) * 16 + (t & 15)] = U32x4{0, 0, 0, 0};
   __syncthreads();
 
   const float scale = p.scale ? p.scale[adapter] : 1.0f;
@@ -457,6 +462,7 @@ __device__ __forceinline__ void out_tile(const OutArgs& a, const OutProj& p, int
       Raw8<DT> b[4];
       const bool more = s + 1 < f.b_steps;
       if (more) load_b(cb, s + 1, b);
+#pragma unroll NL
       for (int l = 0; l < f.limbs; ++l)
 #pragma unroll
         for (int sub = 0; sub < SUBS; ++sub) {
@@ -491,7 +497,7 @@ __device__ __forceinline__ void out_tile(const OutArgs& a, const OutProj& p, int
   }
 }
 
-template <int DT, int YD, int NL>
+template <int DT, int YD>
 __global__ __launch_bounds__(256, YD == MDBF_F32 ? 2 : 3) void adapter_out_kernel(OutArgs a) {
   extern __shared__ U32x4 limbs[];             // [sub][operand of B][number][lane]
   __shared__ int32_t rows[MDBF_ADAPTER_TILE], exponents[MDBF_ADAPTER_TILE];
@@ -504,9 +510,9 @@ __global__ __launch_bounds__(256, YD == MDBF_F32 ? 2 : 3) void adapter_out_kerne
     rows[threadIdx.x] = row < a.T ? row : -1;
   }
   __syncthreads();
-  if (count <= 16) out_tile<DT, YD, NL, 1>(a, p, adapter, first, count, limbs, rows, exponents);
-  else if (count <= 32) out_tile<DT, YD, NL, 2>(a, p, adapter, first, count, limbs, rows, exponents);
-  else out_tile<DT, YD, NL, 4>(a, p, adapter, first, count, limbs, rows, exponents);
+  if (count <= 16) out_tile<DT, YD, 1>(a, p, adapter, first, count, limbs, rows, exponents);
+  else if (count <= 32) out_tile<DT, YD, 2>(a, p, adapter, first, count, limbs, rows, exponents);
+  else out_tile<DT, YD, 4>(a, p, adapter, first, count, limbs, rows, exponents);
 }
 
 // How a call is cut.
@@ -556,13 +562,13 @@ static size_t limb_bytes(int r) {
 
 template <int DT, int YD>
 static int launch_out(const OutArgs& o, int count, int64_t tile_room, int chunks, int rank, hipStream_t s) {
-  constexpr int NL = DT == MDBF_BF16 && YD == MDBF_F32 ? 3 : 2;
+  constexpr int NL = kNumbers<DT>;
   static KernelSetup setup;
   const int e = kernel_setup(setup, [] {
-    return hipFuncSetAttribute((const void*)adapter_out_kernel<DT, YD, NL>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)limb_bytes<NL>(kMaxRank));
+    return hipFuncSetAttribute((const void*)adapter_out_kernel<DT, YD>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)limb_bytes<NL>(kMaxRank));
   });
   if (e) return e;
-  adapter_out_kernel<DT, YD, NL><<<dim3((unsigned)tile_room, chunks, count), 256, limb_bytes<NL>(rank), s>>>(o);
+  adapter_out_kernel<DT, YD><<<dim3((unsigned)tile_room, chunks, count), 256, limb_bytes<NL>(rank), s>>>(o);
   return (int)hipGetLastError();
 }
 

@@ -284,7 +284,7 @@ def test_a_workspace_of_a_larger_step(gpu):
 @pytest.mark.parametrize("x_dtype,y_dtype", [("f16", "f16"), ("f16", "f32"), ("bf16", "bf16"), ("bf16", "f32"), ("bf16", "f16")])
 @pytest.mark.parametrize("r,below", [(8, 18), (16, 18), (40, 18), (16, 24)])
 def test_ranks_far_below_a_rows_largest(gpu, r, below, x_dtype, y_dtype):
-    """Columns of B that read only ranks 2^-below of the row's largest inner value.  Inner values are carried to 2^-22 of themselves (bf16 with 16-bit results: 2^-16) or (fp16) 2^-38 of the row's
+    """Columns of B that read only ranks 2^-below of the row's largest inner value.  Inner values are carried to 2^-23 of themselves or (fp16) 2^-38 of the row's
     largest; with the sums' own n steps that leaves results to half a step of their type and some 2^-15."""
     torch, mb = gpu
     rng = np.random.default_rng(r)
@@ -302,7 +302,7 @@ def test_ranks_far_below_a_rows_largest(gpu, r, below, x_dtype, y_dtype):
     mb.mdbf_adapters(rows, [mb.Adapters(A, B)], [X], [Y])
     x, a, b = (v.double().cpu().numpy() for v in (X, A[0], B[0]))
     inner, size = x @ a.T, np.abs(x) @ np.abs(a).T
-    off = (n + 8) * 2.0 ** -24 * size + (2.0 ** -16 if x_dtype == "bf16" and y_dtype != "f32" else 2.0 ** -22) * np.abs(inner) + (2.0 ** -38 * np.abs(inner).max(1, keepdims=True) if x_dtype == "f16" else 0)
+    off = (n + 8) * 2.0 ** -24 * size + 2.0 ** -23 * np.abs(inner) + (2.0 ** -38 * np.abs(inner).max(1, keepdims=True) if x_dtype == "f16" else 0)
     want = inner @ b.T
     bound = (off + 2 * (r + 8) * 2.0 ** -24 * np.abs(inner)) @ np.abs(b).T * (1 + 2.0 ** -7) + HALF[y_dtype] * np.abs(want) + TINY[y_dtype]
     got = Y.double().cpu().numpy()
@@ -347,3 +347,34 @@ def test_an_infinite_inner_value_beside_large_ones(gpu):
     rows = mb.mdbf_adapter_rows(_ints(torch, [0, T]), _ints(torch, [0]), 1, T)
     mb.mdbf_adapters(rows, [mb.Adapters(A, B)], [X], [Y])
     assert (Y[1::2] == float("inf")).all() and (Y[::2] == float("-inf")).all()
+
+
+@pytest.mark.parametrize("x_dtype,y_dtype", [("f16", "f16"), ("f16", "f32"), ("bf16", "bf16"), ("bf16", "f32"), ("bf16", "f16")])
+@pytest.mark.parametrize("r", [2, 8, 16, 24, 64])
+def test_inner_values_that_cancel(gpu, r, x_dtype, y_dtype):
+    """Whole numbers of 23 bits whose differences are small ones: every sum is exact in 32 bits, and so are the results."""
+    torch, mb = gpu
+    rng = np.random.default_rng(r)
+    T, n, m = 50, 96, 33
+    dt = _dt(torch, x_dtype)
+    top = 2048 if x_dtype == "f16" else 256                          # whole numbers that the type holds
+    x = rng.integers(1, 100, (T, n))
+    x[:, n - 1] = rng.integers(1, 12, T)                             # what is left of a pair of ranks
+    a = rng.integers(1, top, (1, r, n)) * (2048 // top)
+    a[0, :, n - 1] = 0
+    a[0, 1::2] = a[0, ::2][:, :n]
+    a[0, 1::2, n - 1] = 1
+    a[0, ::2, 0] = a[0, 1::2, 0]
+    inner = x @ a[0].T
+    assert inner.max() < 2 ** 23 and inner.max() > 2 ** 20
+    sign = rng.integers(0, 2, (m, r // 2)) * 2 - 1
+    b = np.zeros((1, m, r))
+    b[0, :, ::2], b[0, :, 1::2] = sign, -sign
+    up = lambda v: torch.from_numpy(v.astype(np.float32)).to("cuda:0").to(dt)                 # noqa: E731
+    A, B, X = up(a), up(b), up(x)
+    assert np.array_equal(A.double().cpu().numpy(), a) and np.array_equal(X.double().cpu().numpy(), x)
+    Y = torch.zeros((T, m), dtype=_dt(torch, y_dtype), device="cuda:0")
+    rows = mb.mdbf_adapter_rows(_ints(torch, [0, T]), _ints(torch, [0]), 1, T)
+    mb.mdbf_adapters(rows, [mb.Adapters(A, B)], [X], [Y])
+    want = inner @ b[0].T
+    assert np.abs(want).max() <= 12 * r // 2 and np.array_equal(Y.double().cpu().numpy(), torch.from_numpy(want).to(_dt(torch, y_dtype)).double().numpy())
