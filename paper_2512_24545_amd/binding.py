@@ -834,7 +834,7 @@ def _adapter_list(rows, adapters, Xs, Ys):
 
 
 def mdbf_adapters_workspace(rows, adapters, Xs, Ys):
-    """The workspace (uint8 CUDA tensor) of an mdbf_adapters call with these arguments."""
+    """The workspace (uint8 CUDA tensor) of an mdbf_adapters call with these arguments; it serves calls of fewer rows too."""
     torch = _torch()
     arr, count, dtype = _adapter_list(rows, adapters, Xs, Ys)
     return torch.empty(_adapters_need(arr, count, dtype, rows), dtype=torch.uint8, device=Xs[0].device)
@@ -874,10 +874,9 @@ def _sample_need(T, vocab):
 
 
 def mdbf_sample_workspace(T, vocab, device="cuda:0"):
-    """The workspace (uint8 CUDA tensor, or None where none is needed) of mdbf_sample calls of up to these sizes."""
+    """The workspace (uint8 CUDA tensor) of mdbf_sample calls of up to these sizes."""
     torch = _torch()
-    n = _sample_need(T, vocab)
-    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
+    return torch.empty(_sample_need(T, vocab), dtype=torch.uint8, device=device)
 
 
 def mdbf_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, tokens=None, probs=None, workspace=None, stream=None):
@@ -900,9 +899,8 @@ def mdbf_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None,
             workspace = mdbf_sample_workspace(T, vocab, logits.device)
     _here(logits, u, temperature, top_k, top_p, min_p, tokens, probs, workspace)
     desc = SampleDesc(*(None if s is None else s.data_ptr() for s in (temperature, top_k, top_p, min_p)))
-    ws = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
     status = (_lib or lib()).mdbf_sample(desc, logits.data_ptr(), _rows_of(logits, T, vocab), DTYPE_CODE[_DTYPE_NAME[logits.dtype]], T, vocab, u.data_ptr(),
-                                         tokens.data_ptr(), probs.data_ptr(), *ws, _stream_ptr(stream))
+                                         tokens.data_ptr(), probs.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream_ptr(stream))
     if status:
         _check(status, "mdbf_sample")
     return tokens, probs

@@ -163,8 +163,8 @@ __global__ __launch_bounds__(kRowChunk) void adapter_places_kernel(RowArgs a) {
 // Two launches: V = A X by tiles of rows, ranks and parts of the channels, then Y += scale B V by tiles of rows and columns of
 // Y.  Both on 16x16x32 products.  What has to be moved is X, the adapters in use and Y, twice: a tile of rows shares its adapter, and what
 // a projection shares with the next one, X, is read once for up to four tiles of ranks.  Measured, us of the two launches: q, k and v of 4096 for
-// 64 requests on 28 adapters of rank 16 (24 MB) 6.6 + 8.5, latency; two projections of 11008 for 256 requests on 4 adapters of rank 64 (37 MB) 9.4 + 19,
-// where the second launch adds up the first one's eight splits in every workgroup; q, k and v of 6458 rows of prompts (332 MB) 15 + 60, HBM.
+// 64 requests on 28 adapters of rank 16 (24 MB) 6.6 + 9.1, latency; two projections of 11008 for 256 requests on 4 adapters of rank 64 (37 MB) 9.4 + 19,
+// where the second launch adds up the first one's eight splits in every workgroup; q, k and v of 6458 rows of prompts (332 MB) 14.5 + 59, HBM.
 constexpr int kInSlots = 4;                    // tiles of 16 ranks per workgroup of the first launch
 constexpr int kMaxRank = 256;
 constexpr int kMaxWidth = 1 << 23;             // channels and columns: the second launch's grid ends at 65535 times 256 columns

@@ -6,7 +6,10 @@
 namespace mdbf {
 
 constexpr int kNormMaxChannels = 65536;
-constexpr int64_t kNormStreamBytes = 32ll << 20;   // results beyond this are stored past the caches
+// Results beyond this are stored past the caches: 8192 rows of 4096 bf16 channels with the new stream (134 MB) 39.0 us instead of 41.1, 16384 75.5 instead of
+// 94.3, with a read of y behind them 52.3 and 52.0, 99.6 and 112.6; of 256 rows (4 MB) 4.2 and 4.3, 7.0 and 7.0.  (Between 8 and 32 MB it would gain
+// too, 16 MB 5.1 us instead of 7.3: the border is that of the attention block's results.)
+constexpr int64_t kNormStreamBytes = 32ll << 20;
 
 struct NormArgs {
   const void *x, *res;
@@ -66,9 +69,10 @@ __device__ __forceinline__ void store_codes8(void* base, int64_t at, int count, 
 }
 
 // h = x + residual, y = h / sqrt(mean h^2 + eps) * w: rows are read once and stay in registers, eight channels a lane and piece, WAVES waves
-// a row (workgroups of four waves where a row takes one).  The squares are exact in fp64 and so in effect is their sum, whatever its
+// a row (workgroups of four waves where a row takes one).  (Beyond 16384 channels sixteen waves have eight pieces and 128 registers each: with a residual 24
+// to 51 of them lie in scratch memory.)  The squares are exact in fp64 and so in effect is their sum, whatever its
 // order: what is rounded to 8 bits afterwards, and the scales, do not go by the shape of the launch; beside the loads that costs nothing.
-// Bound by HBM where it is large: 8192 rows of 4096 bf16 channels with residual into e4m3 with a scale byte per 32 (236 MB) 43.8 us, 5.4
+// Bound by HBM where it is large: 8192 rows of 4096 bf16 channels with residual into e4m3 with a scale byte per 32 (236 MB) 37.8 us, 6.2
 // TB/s, more than a copy's 4.9 because more is read than written; 64 rows are the latency of a launch, its loads and one meeting of the
 // waves, 4.2 us.  HD: the stream's type, -1 without residual.
 template <int XD, int HD, int WAVES, int VPT, bool STREAM>
@@ -198,6 +202,11 @@ static void launch_norm_w(const NormArgs& all, bool stream, hipStream_t s) {
   }
 }
 
+// Waves and pieces by the width: few rows want many waves, whose loads are on their way together, and many rows few, whose meetings cost less; one choice
+// serves both within some per cent.  us of 64 rows, and of 16 million channels in all (bf16, with residual):
+//   512   1 x 1 2.9, 21.0; 4 x 1 2.8, 27.5                       11008   16 x 2 4.5, 23.3; 8 x 4 4.8, 22.7; 4 x 8 6.4, 24.9
+//   2048  4 x 1 3.0, 21.3; 1 x 4 4.7, 19.6; 8 x 1 3.0, 21.3      16384   16 x 2 5.3, 22.1; 8 x 4 5.6, 21.8; 4 x 8 7.6, 21.2
+//   4096  4 x 2 3.7, 21.1; 8 x 1 3.3, 21.6; 16 x 1 3.4, 24.3     32768   16 x 8 8.0, 23.9; 16 x 4 7.6, 24.6; 65536   16 x 8 13.8, 22.8
 template <int XD, int HD>
 static void launch_norm_h(const NormArgs& a, bool stream, hipStream_t s) {
   if (a.n <= 512) launch_norm_w<XD, HD, 1, 1>(a, stream, s);
