@@ -790,24 +790,25 @@ class Adapters:
     tensors are another Adapters; where one of these gets other memory (set_, data), it is checked again and used from there."""
 
     def __init__(self, A, B, scale=None):
-        _torch()
         self.count, self.r, self.n = A.shape
-        self.m = B.shape[1]
-        self.dtype = A.dtype
-        self.tensors, self.checked = (A, B, scale), None
-        self.args()
+        self.m, self.dtype = B.shape[1], A.dtype
+        self.tensors = A, B, scale
+        self.check(A, B, scale)
 
     A, B, scale = (property(lambda self, i=i: self.tensors[i]) for i in range(3))
 
-    def args(self):
-        """Addresses of the three."""
+    def check(self, A, B, scale):
+        assert B.shape == (self.count, self.m, self.r) and B.dtype == self.dtype and A.is_contiguous() and B.is_contiguous()
+        if scale is None:
+            self.checked = A.data_ptr(), B.data_ptr(), 0
+        else:
+            assert _ints(scale, self.count, _torch().float32)
+            self.checked = A.data_ptr(), B.data_ptr(), scale.data_ptr()
+
+    def check_again(self):
         A, B, scale = self.tensors
-        at = A.data_ptr(), B.data_ptr(), 0 if scale is None else scale.data_ptr()
-        if at != self.checked:
-            assert A.shape == (self.count, self.r, self.n) and B.shape == (self.count, self.m, self.r) and A.is_contiguous() and B.is_contiguous()
-            assert A.dtype == B.dtype == self.dtype and (scale is None or _ints(scale, self.count, _torch_module.float32))
-            self.checked = at
-        return at
+        assert A.shape == (self.count, self.r, self.n) and A.dtype == self.dtype
+        self.check(A, B, scale)
 
 
 _pack_adapter = struct.Struct("4i7q").pack       # an AdapterDesc's bytes, in a third of the time that making one takes
@@ -826,9 +827,12 @@ def _adapter_list(rows, adapters, Xs, Ys):
             tensors.append(X)
             x_args, last, last_n = (X.data_ptr(), _rows_of(X, T, n)), X, n
         assert p.count == rows.adapters and p.dtype == dtype and Y.shape == (T, m)
-        tensors.append(Y)
-        tensors += p.tensors
-        descs.append(_pack_adapter(n, m, p.r, DTYPE_CODE[_DTYPE_NAME[Y.dtype]], *p.args(), *x_args, Y.data_ptr(), _rows_of(Y, T, m)))
+        A, B, scale = p.tensors
+        tensors += (Y, A, B, scale)
+        at = A.data_ptr(), B.data_ptr(), 0 if scale is None else scale.data_ptr()
+        if at != p.checked:
+            p.check_again()
+        descs.append(_pack_adapter(n, m, p.r, DTYPE_CODE[_DTYPE_NAME[Y.dtype]], *at, *x_args, Y.data_ptr(), _rows_of(Y, T, m)))
     _here(*tensors)
     return b"".join(descs), count, DTYPE_CODE[_DTYPE_NAME[dtype]]
 
