@@ -225,8 +225,8 @@ __device__ void sample_digits(const SampleArgs& a, int64_t t, const RowSetting& 
 // part's.  Tokens that equal the part's largest are counted apart, so that those that equal the row's largest, of weight 1, make up a bucket of an exact mass:
 // where many are alike, bounds fall on borders between them.
 // The first launch's vector work (some 40 instructions a token, 20 of them fp64) and its LDS additions take longer than the logits: 200 rows of 128256 bf16
-// (51 MB, 10 us at the rate of a read) 37.5 us, of which writing buckets and order is as much traffic again.  The second one is a chain of some thirty
-// meetings and dependent loads: 10.7 us for one row of 128256 whose list is short, 21 for 64 rows of 32000 whose longest list is 740, 29 for 200 rows of
+// (51 MB, 10 us at the rate of a read) 37.9 us, of which writing buckets and order is as much traffic again.  The second one is a chain of some thirty
+// meetings and dependent loads: 11 us for one row of 128256 whose list is short, 21 for 64 rows of 32000 whose longest list is 740, 29 for 200 rows of
 // 128256 with lists of up to 4000.  Before: one workgroup a row that reads it for every digit of every bound, 430, 200 and 680 us.
 constexpr int kBuckets = 768;                    // of a row: the largest, then 767 sixteenths, down to 2^-47 of it; less weighs nothing
 constexpr int kPerOctave = 16;
@@ -398,7 +398,7 @@ __global__ __launch_bounds__(kPartThreads, 6) void sample_parts_kernel(SampleArg
   const uint32_t n_left = max(left, n_equal);
   if (has) ((MDBF_GLOBAL uint32_t*)(parts.starts + part * kBuckets))[tid] = min(start, n_left) | min(start + c0, n_left) << 16;
   if (tid == 0) parts.heads[part] = {(unsigned long long)key << 32, n_equal};
-  uint32_t place[kEach];                         // (asked for together, so that their trips overlap: one after another 39 us instead of 37.5 above)
+  uint32_t place[kEach];                         // (asked for together, so that their trips overlap: one after another 39 us instead of 37.5)
 #pragma unroll
   for (int e = 0; e < kEach; ++e) {
     place[e] = kPart;
