@@ -777,6 +777,7 @@ def mdbf_adapter_rows(cu, adapter, adapters, tokens, out=None, stream=None):
         o = AdapterRows(tokens, n, adapters, adapter.device, stream)
     else:
         assert (o.tokens, o.requests, o.adapters) == (tokens, n, adapters) and o.places is not None
+        assert _ints(o.rows, tokens) and _ints(o.places, n) and _ints(o.tiles, 4 * o.tiles.shape[0])
     _here(cu, adapter, o.rows)
     status = (_lib or lib()).mdbf_adapter_rows(tokens, n, adapters, cu.data_ptr(), adapter.data_ptr(), o.rows.data_ptr(), o.tiles.data_ptr(),
                                                o.tiles.shape[0], o.places.data_ptr(), _stream_ptr(stream))

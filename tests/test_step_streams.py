@@ -148,3 +148,14 @@ def test_half_of_the_tables(world, given):
     with pytest.raises(AssertionError):
         mb.AdapterRows(5, 3, 4, **{given: tb.ints(5) if given == "rows" else tb.ints(6, 4)})
     assert not world[0]
+
+
+@pytest.mark.parametrize("name,table", [("rows", (4,)), ("rows", (5, 2)), ("places", (2,)), ("tiles", (6, 3))])
+def test_tables_whose_parts_were_replaced(world, name, table):
+    """The parts of an AdapterRows that is handed to a call have the sizes that the kernel writes."""
+    out = mb.AdapterRows(5, 3, 4)
+    mb.mdbf_adapter_rows(tb.ints(4), tb.ints(3), 4, 5, out=out)
+    setattr(out, name, tb.ints(*table))
+    with pytest.raises(AssertionError):
+        mb.mdbf_adapter_rows(tb.ints(4), tb.ints(3), 4, 5, out=out)
+    assert len(world[1]) == 1
